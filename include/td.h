@@ -415,6 +415,198 @@ typedef struct {
 } td_model;
 int td_model_bytes(const td_model *m, uint64_t *cv, uint64_t *tcv, double *tcv_dock);
 
+/* ---- Operators a model runs on a served batch -------------------------------------------------
+ * A get hands a worker state token ids, per-token columns and cu_seqlens; the inference states owe
+ * the dock log-probabilities and entropies computed from logits, and the actor update turns the
+ * batch into a loss and its gradient (Fig. 2).  These calls are the steps between the batch and the
+ * model: the embedding rows of its token ids, the log-probability and entropy of its tokens
+ * under the model's logits, the clipped policy loss, and the gradients of all three.
+ *
+ * They follow the conventions at the top of this file: caller-owned device memory, work enqueued
+ * on `stream` only, no synchronisation, no allocation, nothing kept between calls but what a
+ * workspace comment says.  The argument structs are host memory, read during the call; `device`
+ * is the CUDA device that the pointers belong to (the caller's current device is restored).
+ * Sizes that a get decides on the device are read there: where a call takes a td_batch, the number
+ * of samples comes from the get's result block, so the host need not know it and the call can
+ * stand in a CUDA graph behind the get.  A token id outside [0, vocab) never causes an access
+ * outside the operands: a negative id marks a position without a token; an id >= vocab is treated
+ * the same and TD_ERR_OOB_INDEX is OR-ed into *status (device, may be NULL; never cleared here).
+ * Every sum is in 32 bits or more and in a fixed order: the same call on the same data gives the
+ * same bits. */
+enum { TD_F16 = 3 };                       /* operands of the operators; a column cannot have it */
+
+/* The row structure of a served batch. */
+typedef struct {
+    uint32_t max_samples, reserved;
+    const int32_t *cu_prompt, *cu_response;   /* device [max_samples + 1], as a get writes them */
+    const td_result *result;                  /* device: result->n_samples samples (at most
+                                                 max_samples); NULL: exactly max_samples */
+} td_batch;
+
+enum { TD_ROWS_TOKEN = 0, TD_ROWS_STREAM = 1 };                    /* td_logprob_args.rows */
+
+/* Log-probability and entropy of tokens under rows of logits x, at temperature tau:
+ *   z_v = (x_v - max x) / tau,  S = sum_v e^(z_v),  logprob = z_y - ln S,
+ *   entropy = ln S - (sum_v e^(z_v) z_v) / S        (a term with e^(z_v) = 0 is 0).
+ * rows = TD_ROWS_TOKEN: logits row t belongs to targets[t]; tokens t < n_tokens, and with a batch
+ *   t < cu_response[n_samples].
+ * rows = TD_ROWS_STREAM: logits are laid out as the fused token stream (td_get_out.seq), targets
+ *   as the packed response column; response token j of sample i is predicted by stream row
+ *   cu_prompt[i + 1] + cu_response[i] + j - 1, the position before it (the first token of a
+ *   sample without a prompt has none).  Needs batch with both cu arrays.
+ * Outputs are in token order, i.e. packed as td_put_back takes them.  A token without a target or
+ * without a row gets 0 everywhere.  A row whose logits are all -inf has no distribution: logprob
+ * -inf, entropy 0, norm {-inf, 0}.  NaN or +inf in a row makes its outputs NaN.  Outputs of
+ * tokens past the batch's end are not written. */
+typedef struct {
+    const void *logits;                    /* device [n_rows][logits_stride] of dtype */
+    int64_t  logits_stride;                /* elements from row to row, >= 0; rows need no alignment */
+    int32_t  dtype;                        /* TD_F32 | TD_BF16 | TD_F16 */
+    uint32_t vocab, n_rows, n_tokens;      /* n_rows, n_tokens < 2^31; TD_ROWS_TOKEN: n_tokens <= n_rows */
+    int32_t  rows;
+    float    temperature;                  /* > 0, finite */
+    int32_t  device;
+    const int32_t *targets;                /* device [n_tokens] */
+    const td_batch *batch;                 /* host struct, or NULL (TD_ROWS_TOKEN only) */
+    float *logprob;                        /* device [n_tokens]                      required */
+    float *norm;                           /* device [n_tokens][2]: {max x, ln S}, for the gradient; or NULL */
+    float *entropy;                        /* device [n_tokens], or NULL */
+    void  *entropy_bf16;                   /* the same rounded to a TD_BF16 column, or NULL */
+    uint32_t *status;
+} td_logprob_args;
+int td_token_logprob(const td_logprob_args *args, void *stream);
+
+/* Gradient of the above with respect to the logits: with g, h the gradients of a loss with respect
+ * to a token's logprob and entropy and p_v = e^(z_v) / S,
+ *   grad_v = (g * ([v = y] - p_v) - h * p_v * (ln p_v + entropy)) / tau.
+ * Every one of the n_rows rows is written: rows no token belongs to, rows of tokens without
+ * a target, and rows whose g and h are both 0 get zeros (their logits are not read); a row whose
+ * logits were all -inf gets zeros.  grad_logits may be the logits buffer itself (same pointer, same
+ * stride). */
+typedef struct {
+    const void *logits;
+    int64_t  logits_stride;
+    int32_t  dtype;
+    uint32_t vocab, n_rows, n_tokens;
+    int32_t  rows;
+    float    temperature;
+    int32_t  device;
+    const int32_t *targets;
+    const td_batch *batch;
+    const float *norm;                     /* device [n_tokens][2], from td_token_logprob  required */
+    const float *entropy;                  /* device [n_tokens]; required with grad_entropy */
+    const float *grad_logprob;             /* device [n_tokens], or NULL (zeros)            */
+    const float *grad_entropy;             /* device [n_tokens], or NULL (zeros); one of the two is required */
+    void    *grad_logits;                  /* device [n_rows][grad_stride] of dtype  required */
+    int64_t  grad_stride;                  /* >= vocab */
+    uint32_t *status;
+} td_logprob_grad_args;
+int td_token_logprob_grad(const td_logprob_grad_args *args, void *stream);
+
+/* Clipped policy loss with a KL term, and its gradient, over the response tokens of a batch.
+ * Per counted token, with A the advantage and every log ratio limited to [-30, 30] (its gradient is
+ * 0 where the limit acts):
+ *   ratio = e^(logprob - old_logprob)                      (old_logprob == NULL: 1, with gradient)
+ *   pg    = max(-A ratio, -A clip(ratio, 1 - clip_low, 1 + clip_high));
+ *           dual_clip > 0 and A < 0: at most -A dual_clip
+ *   d     = ref_logprob - logprob
+ *   kl    = -d | d^2 / 2 | e^d - 1 - d                     (TD_KL_K1 | K2 | K3)
+ *   loss  = sum over counted tokens of weight * (pg + kl_coef kl - entropy_coef entropy)
+ * A token is counted if it lies in a sample's response and its mask byte is not 0; what the
+ * other positions of the inputs hold is never used.  weight:
+ *   TD_MEAN_TOKENS   1 / norm,               norm = 0: the number of counted tokens
+ *   TD_MEAN_SAMPLES  1 / (norm * counted tokens of the sample),  norm = 0: the number of samples
+ * (norm > 0 lets micro-batches of one update share a denominator, or divides by a fixed length.)
+ * Layout of the per-token arrays: row_width = 0: packed, sample i at cu_response[i]; else padded,
+ * sample i at i * row_width (a longer response is cut there), max_samples rows.  Gradients are
+ * written at every one of n_tokens positions, 0 where no counted token is, and carry grad_scale.
+ * With no counted token at all the loss is 0. */
+enum { TD_KL_K1 = 1, TD_KL_K2 = 2, TD_KL_K3 = 3 };
+enum { TD_MEAN_TOKENS = 0, TD_MEAN_SAMPLES = 1 };
+enum {                                     /* td_policy_args.stats */
+    TD_POLICY_LOSS = 0,                    /* the loss                                               */
+    TD_POLICY_PG = 1, TD_POLICY_KL = 2, TD_POLICY_ENTROPY = 3,  /* weighted sums of pg, kl, entropy  */
+    TD_POLICY_CLIPPED = 4,                 /* share of counted tokens whose pg is held by a clip      */
+    TD_POLICY_OLD_KL = 5,                  /* mean of old_logprob - logprob over counted tokens       */
+    TD_POLICY_RATIO = 6,                   /* mean ratio over counted tokens                         */
+    TD_POLICY_TOKENS = 7,                  /* counted tokens                                         */
+    TD_POLICY_STATS = 8
+};
+typedef struct {
+    const td_batch *batch;                 /* cu_response required, cu_prompt unused */
+    uint64_t n_tokens;                     /* positions of the per-token arrays; packed: < 2^31, tokens past it are
+                                              not counted; padded: max_samples * row_width */
+    uint64_t row_width;
+    int32_t  column_dtype;                 /* of old_logprob and ref_logprob: TD_F32 | TD_BF16 */
+    int32_t  kl_kind, reduction, device;
+    float    clip_low, clip_high;          /* >= 0, clip_low <= 1 */
+    float    dual_clip;                    /* 0: off, else > 1 */
+    float    kl_coef, entropy_coef, norm, grad_scale;
+    uint32_t reserved;
+    const float *logprob;                  /* device [n_tokens] */
+    const void  *old_logprob;              /* or NULL */
+    const void  *ref_logprob;              /* or NULL: no kl term */
+    const float *entropy;                  /* or NULL: no entropy term */
+    const uint8_t *mask;                   /* or NULL: every response token counts */
+    const float *advantages;               /* device [max_samples] */
+    float *grad_logprob;                   /* device [n_tokens]            required */
+    float *grad_entropy;                   /* device [n_tokens], or NULL (then entropy's term has no gradient) */
+    float *stats;                          /* device [TD_POLICY_STATS]     required */
+    void  *workspace;                      /* device, 256-byte aligned, zero-filled once after allocation, private
+                                              to this call while it is in flight */
+    uint64_t workspace_bytes;              /* >= td_policy_loss_workspace_bytes(max_samples) */
+} td_policy_args;
+size_t td_policy_loss_workspace_bytes(uint32_t max_samples);
+int td_policy_loss(const td_policy_args *args, void *stream);
+
+enum { TD_TOKENS_PROMPT = 1, TD_TOKENS_RESPONSE = 2, TD_TOKENS_SEQ = 3 };   /* which tokens of a batch `ids` holds */
+
+/* Embedding rows: out[t] = scale * table[ids[t]], computed in float and rounded once; zeros for a
+ * position without a token and, with a batch, for the positions past its tokens (prompt ids,
+ * response ids, or the fused stream: `tokens`). */
+typedef struct {
+    const int32_t *ids;                    /* device [n_tokens] */
+    uint32_t n_tokens, vocab, dim;         /* n_tokens < 2^31 */
+    int32_t  dtype;                        /* of table and out: TD_F32 | TD_BF16 | TD_F16 */
+    const void *table;                     /* device [vocab][table_stride] */
+    int64_t  table_stride;                 /* elements; strides >= dim */
+    void    *out;                          /* device [n_tokens][out_stride] */
+    int64_t  out_stride;
+    float    scale;
+    int32_t  tokens, device;
+    uint32_t reserved;
+    const td_batch *batch;                 /* or NULL: all n_tokens */
+    uint32_t *status;
+} td_embed_args;
+int td_embed(const td_embed_args *args, void *stream);
+
+/* Gradient of the above with respect to the table: row v gets scale * (sum of grad_out[t] over
+ * the positions with ids[t] = v), summed in float in ascending order of position by blocks of the
+ * sorted positions, so that the result does not depend on timing.
+ *   accumulate = 0: every row of grad_table is written, 0 where no token is;
+ *   accumulate = 1: the sum is added to the rows that occur (in float, rounded once), others keep
+ *                   their contents and are not touched. */
+typedef struct {
+    const int32_t *ids;
+    uint32_t n_tokens, vocab, dim;
+    int32_t  dtype;                        /* of grad_out */
+    const void *grad_out;                  /* device [n_tokens][out_stride] */
+    int64_t  out_stride;
+    int32_t  grad_dtype;                   /* of grad_table: TD_F32 or dtype */
+    int32_t  accumulate;
+    void    *grad_table;                   /* device [vocab][table_stride] */
+    int64_t  table_stride;
+    float    scale;
+    int32_t  tokens, device;
+    uint32_t reserved;
+    const td_batch *batch;
+    void    *workspace;                    /* device, 256-byte aligned, any contents, private to this call while in flight */
+    uint64_t workspace_bytes;              /* >= td_embed_grad_workspace_bytes(n_tokens, vocab, dim) */
+    uint32_t *status;
+} td_embed_grad_args;
+size_t td_embed_grad_workspace_bytes(uint32_t n_tokens, uint32_t vocab, uint32_t dim);
+int td_embed_grad(const td_embed_grad_args *args, void *stream);
+
 const char *td_strerror(int code);
 
 #ifdef __cplusplus

@@ -13,7 +13,7 @@ from typing import Dict, List, Optional, Sequence, Tuple
 
 from . import build as _build
 
-I32, F32, BF16 = 0, 1, 2
+I32, F32, BF16, F16 = 0, 1, 2, 3       # F16: operands of the operators, not columns
 SCALAR, PROMPT, RESPONSE = 0, 1, 2
 PACKED, PADDED = 0, 1
 OUT_LEFT_PAD_PROMPT = 1            # td_get_out.flags
@@ -23,6 +23,13 @@ ERR_OOB_INDEX, ERR_DUP_PUT, ERR_LEN_MISMATCH, ERR_ARENA_FULL = 1, 2, 4, 8
 ERR_OUT_TRUNCATED, ERR_LOOKBACK_TIMEOUT, ERR_BAD_LENGTH, ERR_COPY_TIMEOUT = 16, 32, 64, 128
 (BAD_STORED_WITHOUT_ROW, BAD_ROW_PLACEMENT, BAD_ROW_OVERLAP, BAD_STATUS_BITS, BAD_SERVED_UNCLAIMED,
  BAD_SERVED_NOT_READY, BAD_COUNTERS) = 1, 2, 4, 8, 16, 32, 64          # td_debug_validate
+
+ROWS_TOKEN, ROWS_STREAM = 0, 1                       # layout of logits rows
+KL_K1, KL_K2, KL_K3 = 1, 2, 3
+MEAN_TOKENS, MEAN_SAMPLES = 0, 1
+(POLICY_LOSS, POLICY_PG, POLICY_KL, POLICY_ENTROPY, POLICY_CLIPPED, POLICY_OLD_KL, POLICY_RATIO, POLICY_TOKENS,
+ POLICY_STATS) = range(9)
+TOKENS_PROMPT, TOKENS_RESPONSE, TOKENS_SEQ = 1, 2, 3  # which tokens of a batch an id array holds
 
 DTYPE_TAG = {"i32": I32, "f32": F32, "bf16": BF16}
 CLASS_TAG = {"scalar": SCALAR, "prompt": PROMPT, "response": RESPONSE}
@@ -35,7 +42,9 @@ EXPORTS = ["td_query_workspace", "td_create", "td_destroy", "td_put", "td_get",
            "td_put_host_stage_bytes", "td_put_host", "td_get_host", "td_put_many",
            "td_plan_bytes", "td_plan_create", "td_plan_destroy", "td_get_many", "td_get_static",
            "td_model_bytes", "td_put_back", "td_put_back_many", "td_put_many_host", "td_get_many_host", "td_get_many_host_stage_bytes", "td_debug_validate",
-           "td_debug_lookback"]
+           "td_debug_lookback",
+           "td_token_logprob", "td_token_logprob_grad", "td_policy_loss_workspace_bytes", "td_policy_loss",
+           "td_embed", "td_embed_grad_workspace_bytes", "td_embed_grad"]
 
 
 class TdModel(C.Structure):
@@ -107,6 +116,54 @@ class TdStats(C.Structure):
                 ("n_truncated", C.c_uint64), ("n_bad_length", C.c_uint64),
                 ("n_claim_conflicts", C.c_uint64), ("n_lookback_timeouts", C.c_uint64),
                 ("error_word", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class TdBatch(C.Structure):
+    _fields_ = [("max_samples", C.c_uint32), ("reserved", C.c_uint32), ("cu_prompt", C.c_void_p),
+                ("cu_response", C.c_void_p), ("result", C.c_void_p)]
+
+
+_LOGITS_FIELDS = [("logits", C.c_void_p), ("logits_stride", C.c_int64), ("dtype", C.c_int32), ("vocab", C.c_uint32),
+                  ("n_rows", C.c_uint32), ("n_tokens", C.c_uint32), ("rows", C.c_int32), ("temperature", C.c_float),
+                  ("device", C.c_int32), ("targets", C.c_void_p), ("batch", C.POINTER(TdBatch))]
+
+
+class TdLogprobArgs(C.Structure):
+    _fields_ = _LOGITS_FIELDS + [("logprob", C.c_void_p), ("norm", C.c_void_p), ("entropy", C.c_void_p),
+                                 ("entropy_bf16", C.c_void_p), ("status", C.c_void_p)]
+
+
+class TdLogprobGradArgs(C.Structure):
+    _fields_ = _LOGITS_FIELDS + [("norm", C.c_void_p), ("entropy", C.c_void_p), ("grad_logprob", C.c_void_p),
+                                 ("grad_entropy", C.c_void_p), ("grad_logits", C.c_void_p),
+                                 ("grad_stride", C.c_int64), ("status", C.c_void_p)]
+
+
+class TdPolicyArgs(C.Structure):
+    _fields_ = [("batch", C.POINTER(TdBatch)), ("n_tokens", C.c_uint64), ("row_width", C.c_uint64),
+                ("column_dtype", C.c_int32), ("kl_kind", C.c_int32), ("reduction", C.c_int32), ("device", C.c_int32),
+                ("clip_low", C.c_float), ("clip_high", C.c_float), ("dual_clip", C.c_float), ("kl_coef", C.c_float),
+                ("entropy_coef", C.c_float), ("norm", C.c_float), ("grad_scale", C.c_float), ("reserved", C.c_uint32),
+                ("logprob", C.c_void_p), ("old_logprob", C.c_void_p), ("ref_logprob", C.c_void_p),
+                ("entropy", C.c_void_p), ("mask", C.c_void_p), ("advantages", C.c_void_p),
+                ("grad_logprob", C.c_void_p), ("grad_entropy", C.c_void_p), ("stats", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class TdEmbedArgs(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("n_tokens", C.c_uint32), ("vocab", C.c_uint32), ("dim", C.c_uint32),
+                ("dtype", C.c_int32), ("table", C.c_void_p), ("table_stride", C.c_int64), ("out", C.c_void_p),
+                ("out_stride", C.c_int64), ("scale", C.c_float), ("tokens", C.c_int32), ("device", C.c_int32),
+                ("reserved", C.c_uint32), ("batch", C.POINTER(TdBatch)), ("status", C.c_void_p)]
+
+
+class TdEmbedGradArgs(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("n_tokens", C.c_uint32), ("vocab", C.c_uint32), ("dim", C.c_uint32),
+                ("dtype", C.c_int32), ("grad_out", C.c_void_p), ("out_stride", C.c_int64), ("grad_dtype", C.c_int32),
+                ("accumulate", C.c_int32), ("grad_table", C.c_void_p), ("table_stride", C.c_int64),
+                ("scale", C.c_float), ("tokens", C.c_int32), ("device", C.c_int32), ("reserved", C.c_uint32),
+                ("batch", C.POINTER(TdBatch)), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+                ("status", C.c_void_p)]
 
 
 class TdError(RuntimeError):
@@ -195,6 +252,14 @@ def lib():
         L.td_get_static.argtypes = [vp, u32, u32, C.POINTER(TdGetOut), vp]
         L.td_model_bytes.restype = C.c_int
         L.td_model_bytes.argtypes = [C.POINTER(TdModel), C.POINTER(u64), C.POINTER(u64), C.POINTER(C.c_double)]
+        for name, args in (("td_token_logprob", TdLogprobArgs), ("td_token_logprob_grad", TdLogprobGradArgs),
+                           ("td_policy_loss", TdPolicyArgs), ("td_embed", TdEmbedArgs), ("td_embed_grad", TdEmbedGradArgs)):
+            getattr(L, name).restype = C.c_int
+            getattr(L, name).argtypes = [C.POINTER(args), vp]
+        L.td_policy_loss_workspace_bytes.restype = C.c_size_t
+        L.td_policy_loss_workspace_bytes.argtypes = [u32]
+        L.td_embed_grad_workspace_bytes.restype = C.c_size_t
+        L.td_embed_grad_workspace_bytes.argtypes = [u32, u32, u32]
         _lib = L
     return _lib
 
@@ -569,3 +634,264 @@ class Dock:
 
     def launch_count(self) -> int:
         return lib().td_launch_count(self.handle)
+
+
+# -- operators a model runs on a served batch ------------------------------------
+_TAG: Dict = {}               # torch dtype -> TD_* tag
+_KINDS: Dict = {}             # element kind of a vector -> torch dtypes
+
+
+def _torch_types():
+    import torch
+    _KINDS.update(i32=(torch.int32,), f32=(torch.float32,), bf16=(torch.bfloat16,), u8=(torch.uint8,),
+                  mask=(torch.bool, torch.uint8))
+    _TAG.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+
+
+def _tag(t, what: str, allowed) -> int:
+    if not _TAG:
+        _torch_types()
+    tag = _TAG.get(t.dtype)
+    if tag not in allowed:
+        raise ValueError(f"{what}: {t.dtype} is not supported here")
+    return tag
+
+
+def _vector(t, n: int, what: str, kind: str, device: int) -> Optional[int]:
+    """Address of a contiguous device tensor of at least n elements of the kind, None for None."""
+    if t is None:
+        return None
+    if not _KINDS:
+        _torch_types()
+    if t.dtype not in _KINDS[kind] or t.numel() < n or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{what}: needs a contiguous {kind} tensor of at least {n} elements on cuda:{device}, "
+                         f"got {t.dtype} {tuple(t.shape)} strides {tuple(t.stride())} on {t.device}")
+    return t.data_ptr()
+
+
+def _matrix(t, what: str, allowed, device: int):
+    """(address, row stride, dtype tag) of a device matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.get_device() != device or (t.stride(1) != 1 and t.size(1) > 1):
+        raise ValueError(f"{what}: needs a matrix with contiguous rows on cuda:{device}, got {tuple(t.shape)} "
+                         f"strides {tuple(t.stride())} on {t.device}")
+    # torch may give a matrix of one row, or of none, any row stride
+    return t.data_ptr(), t.stride(0) if t.size(0) > 1 else t.size(1), _tag(t, what, allowed)
+
+
+def _device_of(t, what: str) -> int:
+    d = t.get_device()
+    if d < 0:
+        raise ValueError(f"{what}: needs a CUDA tensor")
+    return d
+
+
+def _op_stream(stream, device: int) -> int:
+    if stream is None:
+        import torch
+        return torch.cuda.current_stream(device).cuda_stream
+    return _stream_ptr(stream)
+
+
+_FLOATS = (F32, BF16, F16)
+
+
+class Batch:
+    """The row structure of a batch: cu_seqlens as a get writes them, and where its number of
+    samples is decided on the device, the get's result block."""
+
+    def __init__(self, cu_prompt=None, cu_response=None, result=None):
+        some = cu_response if cu_response is not None else cu_prompt
+        if some is None:
+            raise ValueError("a batch needs cu_prompt or cu_response")
+        self.device = _device_of(some, "cu_response")
+        n = some.numel() - 1
+        if n < 0:
+            raise ValueError("cu arrays have one entry more than samples")
+        self.cu_prompt, self.cu_response, self.result = cu_prompt, cu_response, result       # kept alive
+        self.max_samples = n
+        self.struct = TdBatch(n, 0, _vector(cu_prompt, n + 1, "cu_prompt", "i32", self.device),
+                              _vector(cu_response, n + 1, "cu_response", "i32", self.device),
+                              _vector(result, C.sizeof(TdResult), "result", "u8", self.device))
+        self.pointer = C.pointer(self.struct)
+
+    @classmethod
+    def of(cls, bufs: GetBuffers) -> "Batch":
+        """The batch last served into `bufs` when the stream gets there; its size stays on the device."""
+        return cls(bufs.cu_prompt, bufs.cu_response, bufs.result)
+
+
+def _batch_pointer(batch: Optional[Batch], device: int):
+    if batch is None:
+        return None
+    if batch.device != device:
+        raise ValueError(f"batch: on cuda:{batch.device}, the operands are on cuda:{device}")
+    return batch.pointer
+
+
+class LogprobBuffers:
+    """Outputs of token_logprob for up to n_tokens tokens, in token order: logprob, norm (row maximum
+    and log-sum, what the gradient needs), entropy, entropy_bf16 (a column's type), status."""
+
+    def __init__(self, n_tokens: int, device: int = 0, entropy: bool = False, entropy_bf16: bool = False):
+        import torch
+        dev = torch.device("cuda", device)
+        f32 = torch.float32
+        self.n_tokens, self.device = n_tokens, device
+        self.logprob = torch.zeros(n_tokens, dtype=f32, device=dev)
+        self.norm = torch.zeros(n_tokens, 2, dtype=f32, device=dev)
+        self.entropy = torch.zeros(n_tokens, dtype=f32, device=dev) if entropy else None
+        self.entropy_bf16 = torch.zeros(n_tokens, dtype=torch.bfloat16, device=dev) if entropy_bf16 else None
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self.args = TdLogprobArgs()
+        self.args.device = device
+        self.args.logprob, self.args.norm = self.logprob.data_ptr(), self.norm.data_ptr()
+        self.args.entropy = self.entropy.data_ptr() if entropy else None
+        self.args.entropy_bf16 = self.entropy_bf16.data_ptr() if entropy_bf16 else None
+        self.args.status = self.status.data_ptr()
+
+
+def token_logprob(out: LogprobBuffers, logits, targets, temperature: float = 1.0, batch: Optional[Batch] = None,
+                  rows: int = ROWS_TOKEN, stream=None) -> LogprobBuffers:
+    """Log-probability (and entropy) of `targets` (int32) under the rows of `logits` (float32, bfloat16
+    or float16, rows contiguous, any row stride) at a temperature.  rows = ROWS_STREAM: logits
+    follow the batch's fused token stream, targets its packed response column."""
+    a, device, n = out.args, out.device, targets.numel()
+    if n > out.n_tokens:
+        raise ValueError(f"targets: {n} tokens, the buffers hold {out.n_tokens}")
+    a.targets = _vector(targets, 0, "targets", "i32", device)
+    a.logits, a.logits_stride, a.dtype = _matrix(logits, "logits", _FLOATS, device)
+    a.n_rows, a.vocab = logits.shape
+    a.n_tokens, a.rows, a.temperature = n, rows, temperature
+    a.batch = _batch_pointer(batch, device)
+    _check("td_token_logprob", lib().td_token_logprob(a, _op_stream(stream, device)))
+    return out
+
+
+def token_logprob_grad(grad_logits, logits, targets, norm, grad_logprob=None, entropy=None, grad_entropy=None,
+                       temperature: float = 1.0, batch: Optional[Batch] = None, rows: int = ROWS_TOKEN, status=None,
+                       stream=None):
+    """Gradient of token_logprob with respect to the logits, written to every row of grad_logits
+    (which may be `logits`), from the gradients with respect to logprob and entropy and what the
+    forward call left in norm and entropy."""
+    device, n = _device_of(grad_logits, "grad_logits"), targets.numel()
+    x, stride, tag = _matrix(logits, "logits", _FLOATS, device)
+    g, gstride, gtag = _matrix(grad_logits, "grad_logits", _FLOATS, device)
+    if tag != gtag or grad_logits.shape != logits.shape:
+        raise ValueError("grad_logits: needs the shape and type of logits")
+    a = TdLogprobGradArgs(x, stride, tag, logits.shape[1], logits.shape[0], n, rows, temperature, device,
+                          _vector(targets, 0, "targets", "i32", device), _batch_pointer(batch, device),
+                          _vector(norm, 2 * n, "norm", "f32", device),
+                          _vector(entropy, n, "entropy", "f32", device),
+                          _vector(grad_logprob, n, "grad_logprob", "f32", device),
+                          _vector(grad_entropy, n, "grad_entropy", "f32", device), g, gstride,
+                          _vector(status, 1, "status", "i32", device))
+    _check("td_token_logprob_grad", lib().td_token_logprob_grad(a, _op_stream(stream, device)))
+    return grad_logits
+
+
+class PolicyLossConfig:
+    """Coefficients of policy_loss (td_policy_args has the formulas)."""
+
+    def __init__(self, clip_low: float = 0.2, clip_high: float = 0.2, dual_clip: float = 0.0, kl_coef: float = 0.0,
+                 kl_kind: int = KL_K3, entropy_coef: float = 0.0, reduction: int = MEAN_TOKENS, norm: float = 0.0,
+                 grad_scale: float = 1.0):
+        self.clip_low, self.clip_high, self.dual_clip = clip_low, clip_high, dual_clip
+        self.kl_coef, self.kl_kind, self.entropy_coef = kl_coef, kl_kind, entropy_coef
+        self.reduction, self.norm, self.grad_scale = reduction, norm, grad_scale
+
+
+class PolicyLossBuffers:
+    """Outputs and workspace of policy_loss for up to n_tokens positions and max_samples samples:
+    grad_logprob, grad_entropy (entropy=True), stats with its views terms (loss, pg, kl, entropy),
+    rates (clipped, old kl, ratio) and tokens."""
+
+    def __init__(self, n_tokens: int, max_samples: int, device: int = 0, entropy: bool = False):
+        import torch
+        dev = torch.device("cuda", device)
+        self.n_tokens, self.max_samples, self.device = n_tokens, max_samples, device
+        self.grad_logprob = torch.zeros(n_tokens, dtype=torch.float32, device=dev)
+        self.grad_entropy = torch.zeros(n_tokens, dtype=torch.float32, device=dev) if entropy else None
+        self.stats = torch.zeros(POLICY_STATS, dtype=torch.float32, device=dev)
+        self.terms, self.rates, self.tokens = self.stats[:4], self.stats[4:7], self.stats[7:]
+        nbytes = lib().td_policy_loss_workspace_bytes(max_samples)
+        self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=dev)
+        a = self.args = TdPolicyArgs()
+        a.device = device
+        a.grad_logprob = self.grad_logprob.data_ptr()
+        a.grad_entropy = self.grad_entropy.data_ptr() if entropy else None
+        a.stats, a.workspace, a.workspace_bytes = self.stats.data_ptr(), self.workspace.data_ptr(), nbytes
+
+
+def policy_loss(out: PolicyLossBuffers, batch: Batch, logprob, advantages, old_logprob=None, ref_logprob=None,
+                entropy=None, mask=None, config: Optional[PolicyLossConfig] = None, row_width: int = 0,
+                stream=None) -> PolicyLossBuffers:
+    """Clipped policy loss with a KL term and its gradients over the response tokens of a batch.
+    Per-token tensors are packed (row_width = 0: sample i at cu_response[i]) or padded (sample i at
+    i * row_width); old_logprob and ref_logprob are float32 or bfloat16 columns; mask is bool or
+    uint8; advantages are per sample."""
+    a, device, n = out.args, out.device, logprob.numel()
+    if n > out.n_tokens or batch.max_samples > out.max_samples:
+        raise ValueError(f"{n} positions of {batch.max_samples} samples, the buffers hold {out.n_tokens} of {out.max_samples}")
+    if config is None:
+        config = PolicyLossConfig()
+    a.clip_low, a.clip_high, a.dual_clip = config.clip_low, config.clip_high, config.dual_clip
+    a.kl_coef, a.kl_kind, a.entropy_coef = config.kl_coef, config.kl_kind, config.entropy_coef
+    a.reduction, a.norm, a.grad_scale = config.reduction, config.norm, config.grad_scale
+    a.batch = _batch_pointer(batch, device)
+    a.n_tokens, a.row_width = n, row_width
+    a.logprob = _vector(logprob, n, "logprob", "f32", device)
+    column = "f32"
+    some = old_logprob if old_logprob is not None else ref_logprob
+    a.column_dtype = F32
+    if some is not None and _tag(some, "old_logprob / ref_logprob", (F32, BF16)) == BF16:
+        a.column_dtype, column = BF16, "bf16"
+    a.old_logprob = _vector(old_logprob, n, "old_logprob", column, device)
+    a.ref_logprob = _vector(ref_logprob, n, "ref_logprob", column, device)
+    a.entropy = _vector(entropy, n, "entropy", "f32", device)
+    a.mask = _vector(mask, n, "mask", "mask", device)
+    a.advantages = _vector(advantages, batch.max_samples, "advantages", "f32", device)
+    _check("td_policy_loss", lib().td_policy_loss(a, _op_stream(stream, device)))
+    return out
+
+
+def embed(out, ids, table, scale: float = 1.0, batch: Optional[Batch] = None, tokens: int = TOKENS_SEQ, status=None,
+          stream=None):
+    """out[t] = scale * table[ids[t]] (ids int32; out and table float32, bfloat16 or float16); zeros
+    where ids[t] is no token and, with a batch, behind its tokens."""
+    device, n = _device_of(out, "out"), ids.numel()
+    o, ostride, otag = _matrix(out, "out", _FLOATS, device)
+    t, tstride, tag = _matrix(table, "table", _FLOATS, device)
+    if tag != otag or out.shape[0] != n or out.shape[1] != table.shape[1]:
+        raise ValueError(f"out: needs shape ({n}, {table.shape[1]}) and type {table.dtype}")
+    a = TdEmbedArgs(_vector(ids, 0, "ids", "i32", device), n, table.shape[0], table.shape[1], tag, t, tstride, o,
+                    ostride, scale, tokens, device, 0, _batch_pointer(batch, device),
+                    _vector(status, 1, "status", "i32", device))
+    _check("td_embed", lib().td_embed(a, _op_stream(stream, device)))
+    return out
+
+
+class EmbedGradWorkspace:
+    """Workspace of embed_grad for up to n_tokens positions and rows of dim columns."""
+
+    def __init__(self, n_tokens: int, vocab: int, dim: int, device: int = 0):
+        import torch
+        self.nbytes = lib().td_embed_grad_workspace_bytes(n_tokens, vocab, dim)
+        self.memory = torch.empty(self.nbytes, dtype=torch.uint8, device=torch.device("cuda", device))
+
+
+def embed_grad(grad_table, ids, grad_out, workspace: EmbedGradWorkspace, scale: float = 1.0, accumulate: bool = False,
+               batch: Optional[Batch] = None, tokens: int = TOKENS_SEQ, status=None, stream=None):
+    """Gradient of embed with respect to the table: row v gets scale * the sum of grad_out over the
+    positions of id v.  accumulate: added to the rows that occur; otherwise every row is written.
+    grad_table is float32 or of grad_out's type."""
+    device, n = _device_of(grad_table, "grad_table"), ids.numel()
+    g, gstride, gtag = _matrix(grad_table, "grad_table", _FLOATS, device)
+    o, ostride, tag = _matrix(grad_out, "grad_out", _FLOATS, device)
+    if grad_out.shape[0] != n or grad_out.shape[1] != grad_table.shape[1]:
+        raise ValueError(f"grad_out: needs shape ({n}, {grad_table.shape[1]})")
+    a = TdEmbedGradArgs(_vector(ids, 0, "ids", "i32", device), n, grad_table.shape[0], grad_table.shape[1], tag, o,
+                        ostride, gtag, 1 if accumulate else 0, g, gstride, scale, tokens, device, 0,
+                        _batch_pointer(batch, device), workspace.memory.data_ptr(), workspace.nbytes,
+                        _vector(status, 1, "status", "i32", device))
+    _check("td_embed_grad", lib().td_embed_grad(a, _op_stream(stream, device)))
+    return grad_table

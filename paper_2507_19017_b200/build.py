@@ -1,4 +1,4 @@
-"""Builds the C-ABI library (csrc/td.cu -> libtd.so, beside this file) with nvcc for sm_100a."""
+"""Builds the C-ABI library (csrc/*.cu -> libtd.so, beside this file) with nvcc for sm_100a."""
 from __future__ import annotations
 
 import os
@@ -9,8 +9,9 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libtd.so")
-SOURCES = ["td.cu"]
-HEADERS = ["td_device.cuh", "td_alloc.cuh", "td_put.cuh", "td_get.cuh"]
+SOURCES = ["td.cu", "td_ops.cu"]
+HEADERS = ["td_common.cuh", "td_device.cuh", "td_alloc.cuh", "td_put.cuh", "td_get.cuh", 
+           "td_range.h", "td_ops.cuh", "td_logprob.cuh", "td_policy.cuh", "td_embed.cuh"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

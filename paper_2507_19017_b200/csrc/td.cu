@@ -12,23 +12,9 @@
 #include "td_device.cuh"
 #include "td_get.cuh"
 #include "td_put.cuh"
+#include "td_range.h"
 
 using namespace td;
-
-// Named ranges around the public calls for timeline tools (NVTX; compiled in with -DTD_NVTX, the
-// header-only nvtx3 that ships with the toolkit; otherwise the macro is empty).
-#ifdef TD_NVTX
-#include <nvtx3/nvToolsExt.h>
-namespace {
-struct TdRange {
-    explicit TdRange(const char *name) { nvtxRangePushA(name); }
-    ~TdRange() { nvtxRangePop(); }
-};
-}  // namespace
-#define TD_RANGE(name) TdRange td_range_guard(name)
-#else
-#define TD_RANGE(name) do { } while (0)
-#endif
 
 struct td_dock {
     DockView dv;

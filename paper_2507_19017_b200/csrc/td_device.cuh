@@ -5,13 +5,13 @@
 #include <stdint.h>
 
 #include "../../include/td.h"
+#include "td_common.cuh"
 
 namespace td {
 
 constexpr int kMaxColumns = 32;
 constexpr int kPutCounterSlots = 64;         // streams that can put into a dock with chunks handed out by a counter
 constexpr uint32_t kRowAlign = 8;            // rows start on multiples of 8 elements (>= 16 bytes)
-constexpr uint32_t kFullMask = 0xffffffffu;
 // Internal bit of the dock's error word, never reported: a put since the last reset came with a
 // cu array that is not a non-decreasing sequence inside [0, data_elems].  Row positions in such
 // an array cannot be searched, so the scatter then takes its rows one by one.
@@ -114,15 +114,6 @@ __device__ __forceinline__ unsigned long long ld_acquire_u64(const unsigned long
 __device__ __forceinline__ void st_release_u64(unsigned long long *p, unsigned long long v) {
     asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(p), "l"(v) : "memory");
 }
-
-// Programmatic dependent launch: the kernels of one call are chained so that the next one is
-// launched, and runs its prologue, while the previous one is still finishing.  A kernel calls
-// griddep_wait() before it touches anything the kernel before it in the stream wrote (the wait
-// returns when that kernel has completed and its writes are visible; without the launch
-// attribute it returns at once), and griddep_launch_dependents() as soon as the next kernel
-// may be brought on.
-__device__ __forceinline__ void griddep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void griddep_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 __device__ __forceinline__ void flag_error(const DockView &dv, uint32_t bit, int counter, uint32_t count = 1) {
     atomicOr(dv.errword, bit);

@@ -1,0 +1,385 @@
+// Host side of the operators on a served batch (include/td.h): argument checks and launches.
+// Nothing is allocated and nothing synchronises.
+#include <atomic>
+#include <cmath>
+#include <utility>
+
+#include "td_embed.cuh"
+#include "td_logprob.cuh"
+#include "td_policy.cuh"
+#include "td_range.h"
+
+using namespace td;
+
+namespace {
+
+constexpr uint64_t kMaxGrid = 0x7fffffffull;
+constexpr uint32_t kIndexLimit = 1u << 31;
+
+inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+inline uint32_t size_of(int32_t dtype) { return dtype == TD_F32 ? 4u : 2u; }
+inline bool float_type(int32_t dtype) { return dtype == TD_F32 || dtype == TD_BF16 || dtype == TD_F16; }
+inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// The call's device made current, and the caller's put back.
+class DeviceGuard {
+public:
+    explicit DeviceGuard(int device) {
+        ok_ = cudaGetDevice(&before_) == cudaSuccess;
+        if (ok_ && before_ != device) {
+            ok_ = cudaSetDevice(device) == cudaSuccess;
+            changed_ = ok_;
+        }
+    }
+    ~DeviceGuard() { if (changed_) cudaSetDevice(before_); }
+    DeviceGuard(const DeviceGuard &) = delete;
+    DeviceGuard &operator=(const DeviceGuard &) = delete;
+    bool ok() const { return ok_; }
+private:
+    int before_ = 0;
+    bool ok_ = false, changed_ = false;
+};
+
+// Launch that may be brought on while the kernel ahead of it in the stream drains; every kernel here
+// waits for that one before it touches memory.  cluster: blocks per cluster.
+template <typename... KArgs, typename... Args>
+cudaError_t launch(void (*kernel)(KArgs...), uint64_t grid, uint32_t block, cudaStream_t st, uint32_t cluster, Args &&...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((uint32_t)grid);
+    cfg.blockDim = dim3(block);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cluster > 1) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = cluster;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
+    return cudaLaunchKernelEx(&cfg, kernel, KArgs(std::forward<Args>(args))...);
+}
+
+BatchView view_of(const td_batch *b) {
+    if (!b) return BatchView{nullptr, nullptr, nullptr, 0u};
+    return BatchView{b->cu_prompt, b->cu_response, b->result, b->max_samples};
+}
+bool batch_ok(const td_batch *b, bool need_prompt, bool need_response) {
+    return b->max_samples < kIndexLimit && aligned(b->cu_prompt, 4) && aligned(b->cu_response, 4) && aligned(b->result, 8) &&
+           (b->cu_prompt || !need_prompt) && (b->cu_response || !need_response);
+}
+
+// What the two log-probability calls share.
+template <typename A>
+int check_logprob(const A *a) {
+    if (!a || !float_type(a->dtype) || a->vocab == 0 || a->vocab >= kIndexLimit) return TD_EINVAL;
+    if (a->n_rows >= kIndexLimit || a->n_tokens >= kIndexLimit || a->logits_stride < 0) return TD_EINVAL;
+    if (!(a->temperature > 0.0f) || !std::isfinite(a->temperature) || !std::isfinite(1.4426951f / a->temperature)) return TD_EINVAL;
+    if (a->rows != TD_ROWS_TOKEN && a->rows != TD_ROWS_STREAM) return TD_EINVAL;
+    if (a->rows == TD_ROWS_TOKEN && a->n_tokens > a->n_rows) return TD_EINVAL;
+    if (a->rows == TD_ROWS_STREAM && !a->batch) return TD_EINVAL;
+    if (a->batch && !batch_ok(a->batch, a->rows == TD_ROWS_STREAM, true)) return TD_EINVAL;
+    if ((a->n_rows && !a->logits) || (a->n_tokens && !a->targets)) return TD_EINVAL;
+    if (!aligned(a->logits, size_of(a->dtype)) || !aligned(a->targets, 4) || !aligned(a->status, 4)) return TD_EINVAL;
+    return TD_OK;
+}
+template <typename A>
+LogprobArgs logprob_args(const A *a) {
+    LogprobArgs k{};
+    k.logits = a->logits;
+    k.stride = a->logits_stride;
+    k.vocab = a->vocab;
+    k.n_rows = a->n_rows;
+    k.n_tokens = a->n_tokens;
+    k.stream_rows = a->rows == TD_ROWS_STREAM;
+    k.inv_tau = (float)(1.0 / (double)a->temperature);
+    k.scale2 = (float)(1.4426950408889634 / (double)a->temperature);
+    k.batch = view_of(a->batch);
+    k.targets = a->targets;
+    k.status = a->status;
+    return k;
+}
+
+template <typename T>
+cudaError_t run_logprob(const LogprobArgs &k, cudaStream_t st) {
+    // Blocks of a cluster per row: enough to fill the machine when there are few rows, while every
+    // thread still has a vector of the row.
+    const uint32_t nvec = k.vocab / Elem<T>::kVec;
+    uint32_t parts = 1;
+    while (parts < 8 && (uint64_t)k.n_tokens * parts * 2 <= 296 && nvec >= parts * 2 * kLogprobThreads) parts *= 2;
+    auto *kernel = k.entropy || k.entropy_bf16 ? token_logprob_kernel<T, true> : token_logprob_kernel<T, false>;
+    return launch(kernel, (uint64_t)k.n_tokens * parts, kLogprobThreads, st, parts, k);
+}
+template <typename T>
+cudaError_t run_logprob_grad(const LogprobArgs &k, cudaStream_t st) {
+    return launch(token_logprob_grad_kernel<T>, (uint64_t)k.n_rows * k.chunks, kGradThreads, st, 1u, k);
+}
+
+uint32_t policy_blocks(uint64_t n_tokens) {
+    const uint64_t want = (n_tokens + 4 * kPolicyThreads - 1) / (4 * kPolicyThreads);
+    return (uint32_t)(want < 1 ? 1 : want < kPolicyMaxBlocks ? want : kPolicyMaxBlocks);
+}
+
+struct EmbedGradLayout {
+    size_t keys[2], pos[2], counts, partial, total;
+    uint32_t n_tiles, n_chunks, rows_per_chunk;
+};
+EmbedGradLayout embed_layout(uint32_t n_tokens, uint32_t dim) {
+    EmbedGradLayout L{};
+    L.rows_per_chunk = n_tokens <= (1u << 17) ? 32u : 128u;
+    L.n_tiles = (n_tokens + kSortTile - 1) / kSortTile;
+    L.n_chunks = (n_tokens + L.rows_per_chunk - 1) / L.rows_per_chunk;
+    size_t p = 0;
+    auto take = [&](size_t bytes) { const size_t at = p; p = round_up(p + bytes, 256); return at; };
+    for (int k = 0; k < 2; ++k) { L.keys[k] = take((size_t)n_tokens * 4); L.pos[k] = take((size_t)n_tokens * 4); }
+    L.counts = take((size_t)L.n_tiles * kSortBins * 4);
+    L.partial = take(2 * (size_t)L.n_chunks * dim * 4);
+    L.total = p ? p : 256;
+    return L;
+}
+
+template <typename T, typename G>
+cudaError_t run_embed_grad(EmbedArgs k, const EmbedGradLayout &L, uint8_t *ws, bool wide_in, bool wide_out, cudaStream_t st) {
+    cudaError_t rc;
+    if (k.n_tokens) {
+        int bits = 0;
+        while (bits < 32 && (k.vocab >> bits) != 0) ++bits;  // the keys are 0 .. vocab
+        const int passes = (bits + kSortBits - 1) / kSortBits;
+        for (int p = 0; p < passes; ++p) {
+            SortPass s{};
+            s.shift = (uint32_t)(p * kSortBits);
+            s.first = p == 0;
+            s.n_tiles = L.n_tiles;
+            s.counts = reinterpret_cast<uint32_t *>(ws + L.counts);
+            s.keys_in = reinterpret_cast<uint32_t *>(ws + L.keys[(p + 1) & 1]);
+            s.pos_in = reinterpret_cast<uint32_t *>(ws + L.pos[(p + 1) & 1]);
+            s.keys_out = reinterpret_cast<uint32_t *>(ws + L.keys[p & 1]);
+            s.pos_out = reinterpret_cast<uint32_t *>(ws + L.pos[p & 1]);
+            if ((rc = launch(sort_count_kernel, L.n_tiles, kSortThreads, st, 1u, k, s)) != cudaSuccess) return rc;
+            if ((rc = launch(sort_place_kernel, L.n_tiles, kSortThreads, st, 1u, k, s)) != cudaSuccess) return rc;
+            k.keys = s.keys_out;
+            k.pos = s.pos_out;
+        }
+    }
+    if (!k.accumulate && (rc = launch(embed_zero_kernel<G>, (k.vocab + 31ull) / 32, kSumThreads, st, 1u, k, wide_out)) != cudaSuccess) return rc;
+    if (!k.n_tokens) return cudaSuccess;
+    const uint32_t slices = (k.dim + kSumWarpCols - 1) / kSumWarpCols;
+    const uint64_t grid = ((uint64_t)k.n_chunks * slices + kSumThreads / 32 - 1) / (kSumThreads / 32);
+    if ((rc = launch(embed_sum_kernel<T, G>, grid, kSumThreads, st, 1u, k, slices, wide_in, wide_out)) != cudaSuccess) return rc;
+    return launch(embed_join_kernel<G>, grid, kSumThreads, st, 1u, k, slices, wide_out);
+}
+
+}  // namespace
+
+extern "C" {
+
+int td_token_logprob(const td_logprob_args *a, void *stream) {
+    TD_RANGE("td_token_logprob");
+    const int chk = check_logprob(a);
+    if (chk != TD_OK) return chk;
+    if (a->n_tokens == 0) return TD_OK;
+    if (!a->logprob || !aligned(a->logprob, 4) || !aligned(a->norm, 4) || !aligned(a->entropy, 4) || !aligned(a->entropy_bf16, 2))
+        return TD_EINVAL;
+    DeviceGuard dev(a->device);
+    if (!dev.ok()) return TD_ECUDA;
+    LogprobArgs k = logprob_args(a);
+    k.logprob = a->logprob;
+    k.norm = a->norm;
+    k.entropy = a->entropy;
+    k.entropy_bf16 = static_cast<__nv_bfloat16 *>(a->entropy_bf16);
+    cudaStream_t st = (cudaStream_t)stream;
+    const cudaError_t rc = a->dtype == TD_F32 ? run_logprob<float>(k, st)
+                         : a->dtype == TD_BF16 ? run_logprob<__nv_bfloat16>(k, st) : run_logprob<__half>(k, st);
+    return rc == cudaSuccess ? TD_OK : TD_ECUDA;
+}
+
+int td_token_logprob_grad(const td_logprob_grad_args *a, void *stream) {
+    TD_RANGE("td_token_logprob_grad");
+    const int chk = check_logprob(a);
+    if (chk != TD_OK) return chk;
+    if (a->n_rows == 0) return TD_OK;
+    if (!a->grad_logits || !aligned(a->grad_logits, size_of(a->dtype)) || a->grad_stride < (int64_t)a->vocab) return TD_EINVAL;
+    if (a->grad_logits == a->logits && a->grad_stride != a->logits_stride) return TD_EINVAL;
+    if (a->n_tokens && (!a->norm || (!a->grad_logprob && !a->grad_entropy) || (a->grad_entropy && !a->entropy))) return TD_EINVAL;
+    if (!aligned(a->norm, 4) || !aligned(a->entropy, 4) || !aligned(a->grad_logprob, 4) || !aligned(a->grad_entropy, 4)) return TD_EINVAL;
+    LogprobArgs k = logprob_args(a);
+    k.norm_in = a->norm;
+    k.entropy_in = a->entropy;
+    k.grad_logprob = a->grad_logprob;
+    k.grad_entropy = a->grad_entropy;
+    k.grad = a->grad_logits;
+    k.grad_stride = a->grad_stride;
+    const uint32_t per_vec = 16u / size_of(a->dtype);
+    const uint32_t nvec = (a->vocab + per_vec - 1) / per_vec;
+    k.chunks = (nvec + kGradVectors - 1) / kGradVectors;
+    if ((uint64_t)a->n_rows * k.chunks > kMaxGrid) return TD_EINVAL;
+    DeviceGuard dev(a->device);
+    if (!dev.ok()) return TD_ECUDA;
+    cudaStream_t st = (cudaStream_t)stream;
+    const cudaError_t rc = a->dtype == TD_F32 ? run_logprob_grad<float>(k, st)
+                         : a->dtype == TD_BF16 ? run_logprob_grad<__nv_bfloat16>(k, st) : run_logprob_grad<__half>(k, st);
+    return rc == cudaSuccess ? TD_OK : TD_ECUDA;
+}
+
+size_t td_policy_loss_workspace_bytes(uint32_t max_samples) {
+    return round_up(256 + (size_t)kPolicyMaxBlocks * kPolicySums * 8 + (size_t)max_samples * 4, 256);
+}
+
+int td_policy_loss(const td_policy_args *a, void *stream) {
+    TD_RANGE("td_policy_loss");
+    if (!a || !a->batch || !batch_ok(a->batch, false, true)) return TD_EINVAL;
+    if (a->row_width) {
+        if (a->row_width >= kIndexLimit || a->n_tokens != (uint64_t)a->batch->max_samples * a->row_width) return TD_EINVAL;
+    } else if (a->n_tokens >= kIndexLimit) return TD_EINVAL;
+    if (a->column_dtype != TD_F32 && a->column_dtype != TD_BF16) return TD_EINVAL;
+    if (a->ref_logprob && (a->kl_kind < TD_KL_K1 || a->kl_kind > TD_KL_K3)) return TD_EINVAL;
+    if (a->reduction != TD_MEAN_TOKENS && a->reduction != TD_MEAN_SAMPLES) return TD_EINVAL;
+    if (!(a->clip_low >= 0.0f) || !(a->clip_low <= 1.0f) || !(a->clip_high >= 0.0f)) return TD_EINVAL;
+    if (!(a->dual_clip == 0.0f || a->dual_clip > 1.0f) || !(a->norm >= 0.0f)) return TD_EINVAL;
+    if (!std::isfinite(a->kl_coef) || !std::isfinite(a->entropy_coef) || !std::isfinite(a->norm) || !std::isfinite(a->grad_scale)) return TD_EINVAL;
+    if (!a->stats || !aligned(a->stats, 4)) return TD_EINVAL;
+    if (a->n_tokens && (!a->logprob || !a->advantages || !a->grad_logprob)) return TD_EINVAL;
+    const size_t cs = size_of(a->column_dtype);
+    if (!aligned(a->logprob, 4) || !aligned(a->old_logprob, cs) || !aligned(a->ref_logprob, cs) || !aligned(a->entropy, 4) ||
+        !aligned(a->advantages, 4) || !aligned(a->grad_logprob, 4) || !aligned(a->grad_entropy, 4)) return TD_EINVAL;
+    if (!a->workspace || !aligned(a->workspace, 256) || a->workspace_bytes < td_policy_loss_workspace_bytes(a->batch->max_samples))
+        return TD_EWORKSPACE;
+    DeviceGuard dev(a->device);
+    if (!dev.ok()) return TD_ECUDA;
+
+    PolicyArgs k{};
+    k.batch = view_of(a->batch);
+    k.n_tokens = a->n_tokens;
+    k.row_width = a->row_width;
+    k.bf16_columns = a->column_dtype == TD_BF16;
+    k.kl_kind = a->kl_kind;
+    k.mean_samples = a->reduction == TD_MEAN_SAMPLES;
+    k.lo = 1.0f - a->clip_low;
+    k.hi = 1.0f + a->clip_high;
+    k.dual_clip = a->dual_clip;
+    k.kl_coef = a->ref_logprob ? a->kl_coef : 0.0f;
+    k.entropy_coef = a->entropy ? a->entropy_coef : 0.0f;
+    k.norm = a->norm;
+    k.grad_scale = a->grad_scale;
+    k.logprob = a->logprob;
+    k.old_logprob = a->old_logprob;
+    k.ref_logprob = a->ref_logprob;
+    k.entropy = a->entropy;
+    k.mask = a->mask;
+    k.advantages = a->advantages;
+    k.grad_logprob = a->grad_logprob;
+    k.grad_entropy = a->grad_entropy;
+    k.stats = a->stats;
+    uint8_t *ws = static_cast<uint8_t *>(a->workspace);
+    k.ticket = reinterpret_cast<uint32_t *>(ws);
+    k.partials = reinterpret_cast<double *>(ws + 256);
+    k.counts = reinterpret_cast<int32_t *>(ws + 256 + (size_t)kPolicyMaxBlocks * kPolicySums * 8);
+    k.need_counts = k.mean_samples ? a->mask != nullptr : a->norm == 0.0f && (a->mask || a->row_width);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (k.need_counts && a->batch->max_samples) {
+        const uint32_t per = kPolicyThreads / 32;
+        if (launch(policy_count_kernel, (a->batch->max_samples + per - 1) / per, kPolicyThreads, st, 1u, k) != cudaSuccess) return TD_ECUDA;
+    }
+    // four positions per access where every array allows it
+    const bool wide = aligned(k.logprob, 16) && aligned(k.old_logprob, 4 * cs) && aligned(k.ref_logprob, 4 * cs) &&
+                      aligned(k.entropy, 16) && aligned(k.mask, 4) && aligned(k.grad_logprob, 16) && aligned(k.grad_entropy, 16);
+    const cudaError_t rc = launch(wide ? policy_loss_kernel<4> : policy_loss_kernel<1>, policy_blocks(a->n_tokens), kPolicyThreads, st, 1u, k);
+    return rc == cudaSuccess ? TD_OK : TD_ECUDA;
+}
+
+int td_embed(const td_embed_args *a, void *stream) {
+    TD_RANGE("td_embed");
+    if (!a || !float_type(a->dtype) || a->vocab == 0 || a->vocab >= kIndexLimit || a->dim == 0 || a->dim >= kIndexLimit) return TD_EINVAL;
+    if (a->n_tokens >= kIndexLimit || a->table_stride < (int64_t)a->dim || a->out_stride < (int64_t)a->dim) return TD_EINVAL;
+    if (a->batch && (a->tokens < TD_TOKENS_PROMPT || a->tokens > TD_TOKENS_SEQ ||
+                     !batch_ok(a->batch, a->tokens & TD_TOKENS_PROMPT, a->tokens & TD_TOKENS_RESPONSE))) return TD_EINVAL;
+    if (a->n_tokens == 0) return TD_OK;
+    const uint32_t es = size_of(a->dtype);
+    if (!a->ids || !a->table || !a->out || !aligned(a->ids, 4) || !aligned(a->table, es) || !aligned(a->out, es) || !aligned(a->status, 4))
+        return TD_EINVAL;
+    const uint32_t per_piece = kEmbedVectors * (16u / es);
+    const uint32_t pieces = (a->dim + per_piece - 1) / per_piece;
+    const uint64_t grid = ((uint64_t)a->n_tokens * pieces + kEmbedThreads / 32 - 1) / (kEmbedThreads / 32);
+    if (grid > kMaxGrid) return TD_EINVAL;
+    DeviceGuard dev(a->device);
+    if (!dev.ok()) return TD_ECUDA;
+    EmbedArgs k{};
+    k.ids = a->ids;
+    k.n_tokens = a->n_tokens;
+    k.vocab = a->vocab;
+    k.dim = a->dim;
+    k.tokens = (uint32_t)a->tokens;
+    k.scale = a->scale;
+    k.batch = view_of(a->batch);
+    k.status = a->status;
+    k.table = a->table;
+    k.out = a->out;
+    k.table_stride = a->table_stride;
+    k.out_stride = a->out_stride;
+    // rows of both sides start on 16-byte boundaries
+    const bool wide = aligned(a->table, 16) && aligned(a->out, 16) && a->table_stride * es % 16 == 0 && a->out_stride * es % 16 == 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    auto go = [&](auto *wide_kernel, auto *narrow_kernel) { return launch(wide ? wide_kernel : narrow_kernel, grid, kEmbedThreads, st, 1u, k, pieces); };
+    const cudaError_t rc = a->dtype == TD_F32 ? go(embed_kernel<float, true>, embed_kernel<float, false>)
+                         : a->dtype == TD_BF16 ? go(embed_kernel<__nv_bfloat16, true>, embed_kernel<__nv_bfloat16, false>)
+                                               : go(embed_kernel<__half, true>, embed_kernel<__half, false>);
+    return rc == cudaSuccess ? TD_OK : TD_ECUDA;
+}
+
+size_t td_embed_grad_workspace_bytes(uint32_t n_tokens, uint32_t vocab, uint32_t dim) {
+    (void)vocab;
+    return n_tokens < kIndexLimit && dim < kIndexLimit ? embed_layout(n_tokens, dim).total : 0;
+}
+
+int td_embed_grad(const td_embed_grad_args *a, void *stream) {
+    TD_RANGE("td_embed_grad");
+    if (!a || !float_type(a->dtype) || a->vocab == 0 || a->vocab >= kIndexLimit || a->dim == 0 || a->dim >= kIndexLimit) return TD_EINVAL;
+    if (a->grad_dtype != TD_F32 && a->grad_dtype != a->dtype) return TD_EINVAL;
+    if (a->n_tokens >= kIndexLimit || a->table_stride < (int64_t)a->dim || a->out_stride < 0) return TD_EINVAL;
+    if (a->accumulate != 0 && a->accumulate != 1) return TD_EINVAL;
+    if (a->batch && (a->tokens < TD_TOKENS_PROMPT || a->tokens > TD_TOKENS_SEQ ||
+                     !batch_ok(a->batch, a->tokens & TD_TOKENS_PROMPT, a->tokens & TD_TOKENS_RESPONSE))) return TD_EINVAL;
+    const uint32_t es = size_of(a->dtype), gs = size_of(a->grad_dtype);
+    if (!a->grad_table || !aligned(a->grad_table, gs) || !aligned(a->status, 4)) return TD_EINVAL;
+    if (a->n_tokens && (!a->ids || !a->grad_out || !aligned(a->ids, 4) || !aligned(a->grad_out, es))) return TD_EINVAL;
+    const EmbedGradLayout L = embed_layout(a->n_tokens, a->dim);
+    if (!a->workspace || !aligned(a->workspace, 256) || a->workspace_bytes < L.total) return TD_EWORKSPACE;
+    const uint64_t slices = (a->dim + kSumWarpCols - 1) / kSumWarpCols;
+    if (((uint64_t)L.n_chunks * slices) / (kSumThreads / 32) >= kMaxGrid) return TD_EINVAL;
+    DeviceGuard dev(a->device);
+    if (!dev.ok()) return TD_ECUDA;
+    EmbedArgs k{};
+    k.ids = a->ids;
+    k.n_tokens = a->n_tokens;
+    k.vocab = a->vocab;
+    k.dim = a->dim;
+    k.tokens = (uint32_t)a->tokens;
+    k.scale = a->scale;
+    k.batch = view_of(a->batch);
+    k.status = a->status;
+    k.grad_out = a->grad_out;
+    k.out_stride = a->out_stride;
+    k.grad_table = a->grad_table;
+    k.table_stride = a->table_stride;
+    k.accumulate = (uint32_t)a->accumulate;
+    k.rows_per_chunk = L.rows_per_chunk;
+    k.n_chunks = L.n_chunks;
+    uint8_t *ws = static_cast<uint8_t *>(a->workspace);
+    k.partial = reinterpret_cast<float *>(ws + L.partial);
+    const bool wide_in = aligned(a->grad_out, 16) && a->out_stride * es % 16 == 0;
+    const bool wide_out = aligned(a->grad_table, 16) && a->table_stride * gs % 16 == 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t rc;
+    if (a->dtype == TD_F32) rc = run_embed_grad<float, float>(k, L, ws, wide_in, wide_out, st);
+    else if (a->dtype == TD_BF16)
+        rc = a->grad_dtype == TD_F32 ? run_embed_grad<__nv_bfloat16, float>(k, L, ws, wide_in, wide_out, st)
+                                     : run_embed_grad<__nv_bfloat16, __nv_bfloat16>(k, L, ws, wide_in, wide_out, st);
+    else
+        rc = a->grad_dtype == TD_F32 ? run_embed_grad<__half, float>(k, L, ws, wide_in, wide_out, st)
+                                     : run_embed_grad<__half, __half>(k, L, ws, wide_in, wide_out, st);
+    return rc == cudaSuccess ? TD_OK : TD_ECUDA;
+}
+
+}  // extern "C"
