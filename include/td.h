@@ -535,7 +535,7 @@ enum {                                     /* td_policy_args.stats */
 typedef struct {
     const td_batch *batch;                 /* cu_response required, cu_prompt unused */
     uint64_t n_tokens;                     /* positions of the per-token arrays; packed: < 2^31, tokens past it are
-                                              not counted; padded: max_samples * row_width */
+                                              not counted; padded: max_samples * row_width, < 2^40 */
     uint64_t row_width;
     int32_t  column_dtype;                 /* of old_logprob and ref_logprob: TD_F32 | TD_BF16 */
     int32_t  kl_kind, reduction, device;

@@ -669,13 +669,15 @@ def _vector(t, n: int, what: str, kind: str, device: int) -> Optional[int]:
     return t.data_ptr()
 
 
-def _matrix(t, what: str, allowed, device: int):
-    """(address, row stride, dtype tag) of a device matrix whose rows are contiguous."""
-    if t.dim() != 2 or t.get_device() != device or (t.stride(1) != 1 and t.size(1) > 1):
-        raise ValueError(f"{what}: needs a matrix with contiguous rows on cuda:{device}, got {tuple(t.shape)} "
-                         f"strides {tuple(t.stride())} on {t.device}")
+def _matrix(t, what: str, device: int):
+    """(address, row stride, dtype tag, rows, columns) of a device matrix of floats whose rows are contiguous."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or t.get_device() != device or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{what}: needs a matrix with contiguous rows on cuda:{device}, got {tuple(shape)} "
+                         f"strides {stride} on {t.device}")
+    rows, cols = shape
     # torch may give a matrix of one row, or of none, any row stride
-    return t.data_ptr(), t.stride(0) if t.size(0) > 1 else t.size(1), _tag(t, what, allowed)
+    return t.data_ptr(), stride[0] if rows > 1 else cols, _tag(t, what, _FLOATS), rows, cols
 
 
 def _device_of(t, what: str) -> int:
@@ -687,11 +689,17 @@ def _device_of(t, what: str) -> int:
 
 def _op_stream(stream, device: int) -> int:
     if stream is None:
-        import torch
-        return torch.cuda.current_stream(device).cuda_stream
+        global _current_stream
+        if _current_stream is None:
+            import torch
+            torch.cuda.init()
+            # the handle alone; torch.cuda.current_stream() builds a Stream object around it, at 1.3 us a call
+            _current_stream = torch._C._cuda_getCurrentRawStream
+        return _current_stream(device)
     return _stream_ptr(stream)
 
 
+_current_stream = None
 _FLOATS = (F32, BF16, F16)
 
 
@@ -759,8 +767,7 @@ def token_logprob(out: LogprobBuffers, logits, targets, temperature: float = 1.0
     if n > out.n_tokens:
         raise ValueError(f"targets: {n} tokens, the buffers hold {out.n_tokens}")
     a.targets = _vector(targets, 0, "targets", "i32", device)
-    a.logits, a.logits_stride, a.dtype = _matrix(logits, "logits", _FLOATS, device)
-    a.n_rows, a.vocab = logits.shape
+    a.logits, a.logits_stride, a.dtype, a.n_rows, a.vocab = _matrix(logits, "logits", device)
     a.n_tokens, a.rows, a.temperature = n, rows, temperature
     a.batch = _batch_pointer(batch, device)
     _check("td_token_logprob", lib().td_token_logprob(a, _op_stream(stream, device)))
@@ -774,11 +781,11 @@ def token_logprob_grad(grad_logits, logits, targets, norm, grad_logprob=None, en
     (which may be `logits`), from the gradients with respect to logprob and entropy and what the
     forward call left in norm and entropy."""
     device, n = _device_of(grad_logits, "grad_logits"), targets.numel()
-    x, stride, tag = _matrix(logits, "logits", _FLOATS, device)
-    g, gstride, gtag = _matrix(grad_logits, "grad_logits", _FLOATS, device)
-    if tag != gtag or grad_logits.shape != logits.shape:
+    x, stride, tag, n_rows, vocab = _matrix(logits, "logits", device)
+    g, gstride, gtag, grad_rows, grad_vocab = _matrix(grad_logits, "grad_logits", device)
+    if tag != gtag or grad_rows != n_rows or grad_vocab != vocab:
         raise ValueError("grad_logits: needs the shape and type of logits")
-    a = TdLogprobGradArgs(x, stride, tag, logits.shape[1], logits.shape[0], n, rows, temperature, device,
+    a = TdLogprobGradArgs(x, stride, tag, vocab, n_rows, n, rows, temperature, device,
                           _vector(targets, 0, "targets", "i32", device), _batch_pointer(batch, device),
                           _vector(norm, 2 * n, "norm", "f32", device),
                           _vector(entropy, n, "entropy", "f32", device),
@@ -859,11 +866,11 @@ def embed(out, ids, table, scale: float = 1.0, batch: Optional[Batch] = None, to
     """out[t] = scale * table[ids[t]] (ids int32; out and table float32, bfloat16 or float16); zeros
     where ids[t] is no token and, with a batch, behind its tokens."""
     device, n = _device_of(out, "out"), ids.numel()
-    o, ostride, otag = _matrix(out, "out", _FLOATS, device)
-    t, tstride, tag = _matrix(table, "table", _FLOATS, device)
-    if tag != otag or out.shape[0] != n or out.shape[1] != table.shape[1]:
-        raise ValueError(f"out: needs shape ({n}, {table.shape[1]}) and type {table.dtype}")
-    a = TdEmbedArgs(_vector(ids, 0, "ids", "i32", device), n, table.shape[0], table.shape[1], tag, t, tstride, o,
+    o, ostride, otag, out_rows, out_dim = _matrix(out, "out", device)
+    t, tstride, tag, vocab, dim = _matrix(table, "table", device)
+    if tag != otag or out_rows != n or out_dim != dim:
+        raise ValueError(f"out: needs shape ({n}, {dim}) and type {table.dtype}")
+    a = TdEmbedArgs(_vector(ids, 0, "ids", "i32", device), n, vocab, dim, tag, t, tstride, o,
                     ostride, scale, tokens, device, 0, _batch_pointer(batch, device),
                     _vector(status, 1, "status", "i32", device))
     _check("td_embed", lib().td_embed(a, _op_stream(stream, device)))
@@ -885,11 +892,11 @@ def embed_grad(grad_table, ids, grad_out, workspace: EmbedGradWorkspace, scale: 
     positions of id v.  accumulate: added to the rows that occur; otherwise every row is written.
     grad_table is float32 or of grad_out's type."""
     device, n = _device_of(grad_table, "grad_table"), ids.numel()
-    g, gstride, gtag = _matrix(grad_table, "grad_table", _FLOATS, device)
-    o, ostride, tag = _matrix(grad_out, "grad_out", _FLOATS, device)
-    if grad_out.shape[0] != n or grad_out.shape[1] != grad_table.shape[1]:
-        raise ValueError(f"grad_out: needs shape ({n}, {grad_table.shape[1]})")
-    a = TdEmbedGradArgs(_vector(ids, 0, "ids", "i32", device), n, grad_table.shape[0], grad_table.shape[1], tag, o,
+    g, gstride, gtag, vocab, dim = _matrix(grad_table, "grad_table", device)
+    o, ostride, tag, out_rows, out_dim = _matrix(grad_out, "grad_out", device)
+    if out_rows != n or out_dim != dim:
+        raise ValueError(f"grad_out: needs shape ({n}, {dim})")
+    a = TdEmbedGradArgs(_vector(ids, 0, "ids", "i32", device), n, vocab, dim, tag, o,
                         ostride, gtag, 1 if accumulate else 0, g, gstride, scale, tokens, device, 0,
                         _batch_pointer(batch, device), workspace.memory.data_ptr(), workspace.nbytes,
                         _vector(status, 1, "status", "i32", device))

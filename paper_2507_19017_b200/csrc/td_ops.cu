@@ -43,10 +43,12 @@ private:
 // Launch that may be brought on while the kernel ahead of it in the stream drains; every kernel here
 // waits for that one before it touches memory.  cluster: blocks per cluster.
 template <typename... KArgs, typename... Args>
-cudaError_t launch(void (*kernel)(KArgs...), uint64_t grid, uint32_t block, cudaStream_t st, uint32_t cluster, Args &&...args) {
+cudaError_t launch_smem(void (*kernel)(KArgs...), uint64_t grid, uint32_t block, size_t smem, cudaStream_t st, uint32_t cluster,
+                        Args &&...args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((uint32_t)grid);
     cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -61,6 +63,12 @@ cudaError_t launch(void (*kernel)(KArgs...), uint64_t grid, uint32_t block, cuda
     }
     return cudaLaunchKernelEx(&cfg, kernel, KArgs(std::forward<Args>(args))...);
 }
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch(void (*kernel)(KArgs...), uint64_t grid, uint32_t block, cudaStream_t st, uint32_t cluster, Args &&...args) {
+    return launch_smem(kernel, grid, block, 0, st, cluster, std::forward<Args>(args)...);
+}
+
 
 BatchView view_of(const td_batch *b) {
     if (!b) return BatchView{nullptr, nullptr, nullptr, 0u};
@@ -120,6 +128,26 @@ cudaError_t run_logprob_grad(const LogprobArgs &k, cudaStream_t st) {
 uint32_t policy_blocks(uint64_t n_tokens) {
     const uint64_t want = (n_tokens + 4 * kPolicyThreads - 1) / (4 * kPolicyThreads);
     return (uint32_t)(want < 1 ? 1 : want < kPolicyMaxBlocks ? want : kPolicyMaxBlocks);
+}
+
+// The instance for a call: positions per access, the KL term's form, mask and entropy or none.
+template <int kVec, int kKl, bool kMask, bool kEnt>
+cudaError_t run_policy(const PolicyArgs &k, cudaStream_t st) {
+    constexpr size_t smem = kPolicyStages * PolicyStage<kVec, kKl, kMask, kEnt>::kBytes;
+    if (smem > 40 * 1024) {                                  // with the fixed arrays, beyond the 48 KB a launch gets unasked
+        const cudaError_t rc = cudaFuncSetAttribute(policy_loss_kernel<kVec, kKl, kMask, kEnt>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (rc != cudaSuccess) return rc;
+    }
+    return launch_smem(policy_loss_kernel<kVec, kKl, kMask, kEnt>, policy_blocks(k.n_tokens), kPolicyThreads, smem, st, 1u, k);
+}
+template <int kVec, int kKl>
+cudaError_t run_policy(const PolicyArgs &k, cudaStream_t st) {
+    if (k.mask) return k.entropy ? run_policy<kVec, kKl, true, true>(k, st) : run_policy<kVec, kKl, true, false>(k, st);
+    return k.entropy ? run_policy<kVec, kKl, false, true>(k, st) : run_policy<kVec, kKl, false, false>(k, st);
+}
+template <int kVec>
+cudaError_t run_policy(const PolicyArgs &k, int kl, cudaStream_t st) {
+    return kl == kNoKl ? run_policy<kVec, kNoKl>(k, st) : kl == kKlExp ? run_policy<kVec, kKlExp>(k, st) : run_policy<kVec, kKlPoly>(k, st);
 }
 
 struct EmbedGradLayout {
@@ -231,7 +259,7 @@ int td_policy_loss(const td_policy_args *a, void *stream) {
     TD_RANGE("td_policy_loss");
     if (!a || !a->batch || !batch_ok(a->batch, false, true)) return TD_EINVAL;
     if (a->row_width) {
-        if (a->row_width >= kIndexLimit || a->n_tokens != (uint64_t)a->batch->max_samples * a->row_width) return TD_EINVAL;
+        if (a->row_width >= kIndexLimit || a->n_tokens != (uint64_t)a->batch->max_samples * a->row_width || a->n_tokens >= 1ull << 40) return TD_EINVAL;
     } else if (a->n_tokens >= kIndexLimit) return TD_EINVAL;
     if (a->column_dtype != TD_F32 && a->column_dtype != TD_BF16) return TD_EINVAL;
     if (a->ref_logprob && (a->kl_kind < TD_KL_K1 || a->kl_kind > TD_KL_K3)) return TD_EINVAL;
@@ -254,11 +282,12 @@ int td_policy_loss(const td_policy_args *a, void *stream) {
     k.n_tokens = a->n_tokens;
     k.row_width = a->row_width;
     k.bf16_columns = a->column_dtype == TD_BF16;
-    k.kl_kind = a->kl_kind;
+    k.kl_c1 = a->kl_kind == TD_KL_K1 ? -1.0f : 0.0f;
+    k.kl_c2 = a->kl_kind == TD_KL_K2 ? 0.5f : 0.0f;
     k.mean_samples = a->reduction == TD_MEAN_SAMPLES;
     k.lo = 1.0f - a->clip_low;
     k.hi = 1.0f + a->clip_high;
-    k.dual_clip = a->dual_clip;
+    k.dual_clip = a->dual_clip > 0.0f ? a->dual_clip : INFINITY;
     k.kl_coef = a->ref_logprob ? a->kl_coef : 0.0f;
     k.entropy_coef = a->entropy ? a->entropy_coef : 0.0f;
     k.norm = a->norm;
@@ -285,7 +314,8 @@ int td_policy_loss(const td_policy_args *a, void *stream) {
     // four positions per access where every array allows it
     const bool wide = aligned(k.logprob, 16) && aligned(k.old_logprob, 4 * cs) && aligned(k.ref_logprob, 4 * cs) &&
                       aligned(k.entropy, 16) && aligned(k.mask, 4) && aligned(k.grad_logprob, 16) && aligned(k.grad_entropy, 16);
-    const cudaError_t rc = launch(wide ? policy_loss_kernel<4> : policy_loss_kernel<1>, policy_blocks(a->n_tokens), kPolicyThreads, st, 1u, k);
+    const int kl = !a->ref_logprob ? kNoKl : a->kl_kind == TD_KL_K3 ? kKlExp : kKlPoly;
+    const cudaError_t rc = wide ? run_policy<4>(k, kl, st) : run_policy<1>(k, kl, st);
     return rc == cudaSuccess ? TD_OK : TD_ECUDA;
 }
 

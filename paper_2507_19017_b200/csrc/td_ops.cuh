@@ -67,7 +67,12 @@ __device__ __forceinline__ float exp2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-// max(x, lo) that keeps a NaN
+// max(x, lo) and min(x, hi) that keep a NaN
+__device__ __forceinline__ float min_nan(float x, float hi) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(hi));
+    return r;
+}
 __device__ __forceinline__ float max_nan(float x, float lo) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(lo));
