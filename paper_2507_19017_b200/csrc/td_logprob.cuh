@@ -40,76 +40,150 @@ __device__ __forceinline__ int32_t target_of(const LogprobArgs &a, uint32_t t) {
     return y;
 }
 
-// Running maximum m, S = sum 2^t and W = sum 2^t t with t = (x - m) * scale2, over the scores seen
-// so far.  m starts at the lowest finite float, so that -inf scores give 2^-inf = 0 without a test.
+// Sums over the scores seen so far, relative to a reference: S = sum 2^t and W = sum 2^t t.  How t comes from a
+// score x (c = scale2) and when the reference moves depends on the pass:
+//   quick: t = x c - ref, one packed multiply-add per two scores; ref is the rounded product of a score
+//          and c, moved up when a score passes it by more than 2^kSlack, so that it seldom moves.  -inf is
+//          raised to the type's kLow first (entropy only), which keeps 0 * t finite; the reference begins half
+//          way down to it.
+//   safe:  t = (x - ref) c, not below kFarBelow; ref is the running maximum, from the lowest finite float up.
+// The quick pass is right unless the row's maximum times c is beyond 1e30, or within 1000 of kLow / 2 times c: rows
+// masked by the lowest finite value, of infinities, at extreme temperatures.  Those go
+// through the safe pass.
 struct Running {
-    float m, s, w;
+    float ref, s, w;
 };
+constexpr float kSlack = 4.0f;
 
-// Moves the reference from r.m up to m.
-__device__ __forceinline__ void lift(Running &r, float m, float scale2) {
-    const float d = fmaxf((r.m - m) * scale2, kFarBelow);
+// Moves the reference up; unit: what a difference of references is worth in t (1 quick, c safe).
+__device__ __forceinline__ void lift(Running &r, float ref, float unit) {
+    const float d = fmaxf((r.ref - ref) * unit, kFarBelow);
     const float f = exp2_approx(d);
     r.w = f * fmaf(d, r.s, r.w);
     r.s *= f;
-    r.m = m;
+    r.ref = ref;
 }
-
-__device__ __forceinline__ void join(Running &r, Running o, float scale2) {
-    const float m = fmaxf(r.m, o.m);
-    lift(r, m, scale2);
-    lift(o, m, scale2);
+__device__ __forceinline__ void join(Running &r, Running o, float unit) {
+    const float ref = fmaxf(r.ref, o.ref);
+    lift(r, ref, unit);
+    lift(o, ref, unit);
     r.s += o.s;
     r.w += o.w;
 }
 
-template <typename T, int U, bool kEntropy>
-__device__ __forceinline__ void take(Running &r, f32x2 &s2, f32x2 &w2, const uint4 (&v)[U], float scale2) {
-    const float cm = Elem<T>::vmax(v);
-    if (cm > r.m) {                                          // the pairs' sums hang on the old reference
+// A thread's share of a pass: the reference, the sums as pairs, the maximum.
+struct Share {
+    float ref, top;
+    f32x2 s, w;
+    __device__ __forceinline__ Running total() const {
         float a, b, c, d;
-        unpack2(s2, a, b);
-        unpack2(w2, c, d);
-        r.s = a + b;
-        r.w = c + d;
-        lift(r, cm, scale2);
-        s2 = pack2(r.s, 0.0f);
-        w2 = pack2(r.w, 0.0f);
+        unpack2(s, a, b);
+        unpack2(w, c, d);
+        return Running{ref, a + b, c + d};
     }
-    const f32x2 neg = pack2(-r.m, -r.m), sc = pack2(scale2, scale2);
+    __device__ __forceinline__ void lift_to(float to, float unit) {
+        Running r = total();
+        lift(r, to, unit);
+        ref = to;
+        s = pack2(r.s, 0.0f);
+        w = pack2(r.w, 0.0f);
+    }
+};
+
+template <typename T, int U, bool kEntropy, bool kSafe>
+__device__ __forceinline__ void take(Share &r, uint4 (&v)[U], float scale2) {
+    if (kEntropy && !kSafe)
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = Elem<T>::raise(v[u]);
+    const float cm = Elem<T>::vmax(v);
+    r.top = fmaxf(r.top, cm);
+    if (kSafe ? cm > r.ref : cm * scale2 > r.ref + kSlack) r.lift_to(kSafe ? cm : cm * scale2, kSafe ? scale2 : 1.0f);
+    const f32x2 neg = pack2(-r.ref, -r.ref), sc = pack2(scale2, scale2);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int k = 0; k < Elem<T>::kVec / 2; ++k) {
-            f32x2 t = mul2(add2(Elem<T>::pair(v[u], k), neg), sc);
+            f32x2 t = kSafe ? mul2(add2(Elem<T>::pair(v[u], k), neg), sc) : fma2(Elem<T>::pair(v[u], k), sc, neg);
             float a, b;
             unpack2(t, a, b);
-            if (kEntropy) {
+            if (kSafe) {
                 a = max_nan(a, kFarBelow);
                 b = max_nan(b, kFarBelow);
                 t = pack2(a, b);
             }
             const f32x2 e = pack2(exp2_approx(a), exp2_approx(b));
-            s2 = add2(s2, e);
-            if (kEntropy) w2 = fma2(e, t, w2);
+            r.s = add2(r.s, e);
+            if (kEntropy) r.w = fma2(e, t, r.w);
         }
 }
 
-constexpr int kLogprobThreads = 512, kLogprobUnroll = 4;
+constexpr int kLogprobUnroll = 4;
 
-// One row per cluster of gridDim.x / n_tokens blocks (1 to 8).  A single pass: every thread keeps a
-// running maximum and sums over its share of the row, and the shares are joined in a fixed order
-// over the warp, the block and (through distributed shared memory) the cluster.
-template <typename T, bool kEntropy>
-__global__ void __launch_bounds__(kLogprobThreads, 2) token_logprob_kernel(const LogprobArgs a) {
+// One pass over the vectors [lo, hi) of a row, and for the row's first part over the ends that do not fill a
+// vector (at most 2 (kVec - 1) elements).
+template <typename T, bool kEntropy, bool kSafe, int kThreads>
+__device__ __forceinline__ Share pass_over(const T *x, uint32_t vocab, uint32_t head, uint32_t nvec, uint32_t lo, uint32_t hi, bool ends, float scale2) {
+    constexpr int E = Elem<T>::kVec, U = kLogprobUnroll;
+    constexpr uint32_t kChunk = U * kThreads;
+    const uint4 *xv = reinterpret_cast<const uint4 *>(x + head) + lo + threadIdx.x;
+    const uint32_t n = hi - lo, full = n / kChunk;
+    Share r{kSafe ? -FLT_MAX : fmaxf(0.5f * Elem<T>::kLow * scale2, -FLT_MAX), -CUDART_INF_F, pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
+    uint4 p[U], q[U];
+    auto fetch = [&](uint4 (&v)[U], uint32_t chunk) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = ld_stream(xv + (size_t)chunk * kChunk + u * kThreads);
+    };
+    // what is left behind the full chunks, filled up with -inf
+    auto rest = [&](uint4 (&v)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            v[u].x = v[u].y = v[u].z = v[u].w = Elem<T>::kFill;
+            if (full * kChunk + u * kThreads + threadIdx.x < n) v[u] = ld_stream(xv + (size_t)full * kChunk + u * kThreads);
+        }
+    };
+    if (full) fetch(p, 0); else rest(p);
+    if (ends) {
+        const uint32_t tail = head + nvec * E, n_loose = head + (vocab - tail);
+        if (threadIdx.x < n_loose) {
+            float z = Elem<T>::load(x + (threadIdx.x < head ? threadIdx.x : tail + threadIdx.x - head));
+            if (!kSafe) z = max_nan(z, Elem<T>::kLow);
+            r.top = z;
+            r.ref = kSafe ? fmaxf(z, -FLT_MAX) : fmaxf(z * scale2, r.ref);
+            const float t = max_nan(kSafe ? (z - r.ref) * scale2 : fmaf(z, scale2, -r.ref), kFarBelow), e = exp2_approx(t);
+            r.s = pack2(e, 0.0f);
+            r.w = pack2(e * t, 0.0f);
+        }
+    }
+    uint32_t k = 0;
+    while (k + 2 <= full) {              // two chunks a turn, each loaded while the other is added up
+        fetch(q, k + 1);
+        take<T, U, kEntropy, kSafe>(r, p, scale2);
+        if (k + 2 < full) fetch(p, k + 2); else rest(p);
+        take<T, U, kEntropy, kSafe>(r, q, scale2);
+        k += 2;
+    }
+    if (k < full) {
+        rest(q);
+        take<T, U, kEntropy, kSafe>(r, p, scale2);
+        if (n > full * kChunk) take<T, U, kEntropy, kSafe>(r, q, scale2);
+    } else if (n > full * kChunk) take<T, U, kEntropy, kSafe>(r, p, scale2);
+    return r;
+}
+
+// One row per cluster of `parts` blocks (1 to 8).  A single pass over the row: every thread keeps a reference and
+// sums over its share, and the shares are joined in a fixed order over the warp, the block and (through
+// distributed shared memory) the cluster.
+template <typename T, bool kEntropy, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprob_kernel(const LogprobArgs a) {
     griddep_launch_dependents();
     griddep_wait();
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t parts = cluster.num_blocks(), part = cluster.block_rank();
     const uint32_t t = blockIdx.x / parts;
-    __shared__ Running warp_part[kLogprobThreads / 32];
-    __shared__ Running block_part;
+    struct Part { Running sums; float top; };
+    __shared__ Part warp_part[kThreads / 32], block_part;
+    __shared__ bool quick_holds;
 
     long long row = t;
     bool have_row = true;
@@ -135,88 +209,79 @@ __global__ void __launch_bounds__(kLogprobThreads, 2) token_logprob_kernel(const
     }
 
     const T *x = static_cast<const T *>(a.logits) + row * a.stride;
-    constexpr int E = Elem<T>::kVec, U = kLogprobUnroll;
+    constexpr int E = Elem<T>::kVec;
     const uint32_t head = min((uint32_t)((16u - (reinterpret_cast<uintptr_t>(x) & 15u)) & 15u) / (uint32_t)sizeof(T), a.vocab);
     const uint32_t nvec = (a.vocab - head) / E;
-    const uint4 *xv = reinterpret_cast<const uint4 *>(x + head);
     const uint32_t lo = (uint32_t)((unsigned long long)nvec * part / parts);
     const uint32_t hi = (uint32_t)((unsigned long long)nvec * (part + 1) / parts);
-    Running r{-FLT_MAX, 0.0f, 0.0f};
-    f32x2 s2 = pack2(0.0f, 0.0f), w2 = pack2(0.0f, 0.0f);
-    uint4 fill;
-    fill.x = fill.y = fill.z = fill.w = Elem<T>::kFill;
-
-    auto fetch = [&](uint4 (&v)[U], uint32_t i) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t j = i + u * kLogprobThreads;
-            v[u] = j < hi ? ld_stream(xv + j) : fill;
-        }
-    };
-    uint4 cur[U], nxt[U];
-    uint32_t i = lo + threadIdx.x;
-    fetch(cur, i);
-    // the ends of the row that do not fill a vector: at most 2 * (E - 1) elements
-    if (part == 0) {
-        const uint32_t tail = head + nvec * E, n_loose = head + (a.vocab - tail);
-        if (threadIdx.x < n_loose) {
-            const float z = Elem<T>::load(x + (threadIdx.x < head ? threadIdx.x : tail + threadIdx.x - head));
-            r.m = fmaxf(z, -FLT_MAX);
-            const float d = max_nan((z - r.m) * a.scale2, kFarBelow);
-            const float e = exp2_approx(d);
-            s2 = pack2(e, 0.0f);
-            w2 = pack2(e * d, 0.0f);
-        }
-    }
-    while (i < hi) {
-        const uint32_t ahead = i + U * kLogprobThreads;
-        fetch(nxt, ahead);
-        take<T, U, kEntropy>(r, s2, w2, cur, a.scale2);
-#pragma unroll
-        for (int u = 0; u < U; ++u) cur[u] = nxt[u];
-        i = ahead;
-    }
-    {
-        float p, q;
-        unpack2(s2, p, q);
-        r.s = p + q;
-        unpack2(w2, p, q);
-        r.w = p + q;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Running other{__shfl_xor_sync(kFullMask, r.m, o), __shfl_xor_sync(kFullMask, r.s, o), __shfl_xor_sync(kFullMask, r.w, o)};
-        join(r, other, a.scale2);
-    }
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    if (lane == 0) warp_part[warp] = r;
-    __syncthreads();
-    if (warp == 0) {
-        r = lane < kLogprobThreads / 32 ? warp_part[lane] : Running{-FLT_MAX, 0.0f, 0.0f};
+    const float x_y = Elem<T>::load(x + y);
+
+    // Joins the threads' shares; the first block's first thread has the row's sums and maximum.
+    auto join_all = [&](const Share &mine, float unit) {
+        Running r = mine.total();
+        float top = mine.top;
+        auto over_lanes = [&]() {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            Running other{__shfl_xor_sync(kFullMask, r.m, o), __shfl_xor_sync(kFullMask, r.s, o), __shfl_xor_sync(kFullMask, r.w, o)};
-            join(r, other, a.scale2);
+            for (int o = 16; o > 0; o >>= 1) {
+                const Running other{__shfl_xor_sync(kFullMask, r.ref, o), __shfl_xor_sync(kFullMask, r.s, o), __shfl_xor_sync(kFullMask, r.w, o)};
+                join(r, other, unit);
+                top = fmaxf(top, __shfl_xor_sync(kFullMask, top, o));
+            }
+        };
+        over_lanes();
+        if (lane == 0) warp_part[warp] = Part{r, top};
+        __syncthreads();
+        if (warp == 0) {
+            const Part p = warp_part[lane < kThreads / 32 ? lane : 0];
+            r = p.sums;
+            top = p.top;
+            if (lane >= kThreads / 32) r.s = r.w = 0.0f;
+            over_lanes();
+            if (lane == 0) block_part = Part{r, top};
         }
-        if (lane == 0) block_part = r;
-    }
+        if (parts > 1) {
+            cluster.sync();
+            if (part == 0 && threadIdx.x == 0)
+                for (uint32_t p = 1; p < parts; ++p) {
+                    const Part o = *cluster.map_shared_rank(&block_part, p);
+                    join(r, o.sums, unit);
+                    top = fmaxf(top, o.top);
+                }
+        }
+        return Part{r, top};
+    };
+
+    Part all = join_all(pass_over<T, kEntropy, false, kThreads>(x, a.vocab, head, nvec, lo, hi, part == 0, a.scale2), 1.0f);
+    // the first block says whether that was right, the others look
+    if (part == 0 && threadIdx.x == 0)
+        quick_holds = a.scale2 < 1e8f && fabsf(all.top) * a.scale2 < 1e30f && (all.top - 0.5f * Elem<T>::kLow) * a.scale2 > -kFarBelow;
+    bool quick;
     if (parts > 1) {
         cluster.sync();
-        if (part == 0 && threadIdx.x == 0)
-            for (uint32_t p = 1; p < parts; ++p) join(r, *cluster.map_shared_rank(&block_part, p), a.scale2);
+        quick = *cluster.map_shared_rank(&quick_holds, 0);
         cluster.sync();                                      // a block's shared memory stays until it has been read
+    } else {
+        __syncthreads();
+        quick = quick_holds;
+    }
+    if (!quick) {
+        all = join_all(pass_over<T, kEntropy, true, kThreads>(x, a.vocab, head, nvec, lo, hi, part == 0, a.scale2), a.scale2);
+        if (parts > 1) cluster.sync();
     }
     if (part == 0 && threadIdx.x == 0) {
+        const Running r = all.sums;
         const bool none = r.s == 0.0f;                       // every logit -inf
         const float ln_s = none ? 0.0f : logf(r.s);
-        const float lp = none ? -CUDART_INF_F : fmaf(Elem<T>::load(x + y) - r.m, a.inv_tau, -ln_s);
-        a.logprob[t] = lp;
+        const float h = none ? 0.0f : ln_s - kLn2 * (r.w / r.s);
+        const float top = quick ? all.top : r.ref;
+        const float ln_top = quick ? ln_s - fmaf(top, a.scale2, -r.ref) * kLn2 : ln_s;      // relative to the maximum
+        a.logprob[t] = none ? -CUDART_INF_F : fmaf(x_y - top, a.inv_tau, -ln_top);
         if (a.norm) {
-            a.norm[2ull * t] = none ? -CUDART_INF_F : r.m;
-            a.norm[2ull * t + 1] = ln_s;
+            a.norm[2ull * t] = none ? -CUDART_INF_F : top;
+            a.norm[2ull * t + 1] = ln_top;
         }
         if (kEntropy) {
-            const float h = none ? 0.0f : ln_s - kLn2 * (r.w / r.s);
             if (a.entropy) a.entropy[t] = h;
             if (a.entropy_bf16) a.entropy_bf16[t] = Elem<__nv_bfloat16>::from(h);
         }

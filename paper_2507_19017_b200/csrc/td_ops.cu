@@ -112,13 +112,25 @@ LogprobArgs logprob_args(const A *a) {
 
 template <typename T>
 cudaError_t run_logprob(const LogprobArgs &k, cudaStream_t st) {
-    // Blocks of a cluster per row: enough to fill the machine when there are few rows, while every
-    // thread still has a vector of the row.
-    const uint32_t nvec = k.vocab / Elem<T>::kVec;
-    uint32_t parts = 1;
-    while (parts < 8 && (uint64_t)k.n_tokens * parts * 2 <= 296 && nvec >= parts * 2 * kLogprobThreads) parts *= 2;
-    auto *kernel = k.entropy || k.entropy_bf16 ? token_logprob_kernel<T, true> : token_logprob_kernel<T, false>;
-    return launch(kernel, (uint64_t)k.n_tokens * parts, kLogprobThreads, st, parts, k);
+    // Blocks per row (a cluster joins them) and threads per block, by the rows there are to fill 148 SMs with.
+    // Measured in us, bfloat16 vocabulary 129280: 1 row 4.1 on 8 x 256 threads, 5.0 on 4 x 128; 74 rows 7.8 on
+    // 2 x 512, 8.6 on 1 x 512; 148 rows 9.8 on 1 x 512, 12.2 on 1 x 256; 500 rows 25.6 on 256, 26.5 on 512;
+    // 1200 rows 54.4 on 256, 59.2 on 128; 8192 rows of 152064 405 on 128, 410 on 256.  Rows of fewer than 8192
+    // vectors gain nothing from a second block (32003: 3.6 on one, 3.9 on two), and a block wants four
+    // vectors per thread (4096: 2.3 on 128, 3.1 on 512).  float rows, with half the work per byte, go to 128
+    // threads earlier (777 rows of 50021: 27.8, on 256 31.0).
+    const uint32_t nvec = k.vocab / Elem<T>::kVec, rows = k.n_tokens;
+    const bool entropy = k.entropy || k.entropy_bf16;
+    auto go = [&](auto *with, auto *without, uint32_t threads, uint32_t parts) {
+        return launch(entropy ? with : without, (uint64_t)rows * parts, threads, st, parts, k);
+    };
+    auto go128 = [&]() { return go(token_logprob_kernel<T, true, 128>, token_logprob_kernel<T, false, 128>, 128, 1); };
+    auto go256 = [&](uint32_t parts) { return go(token_logprob_kernel<T, true, 256>, token_logprob_kernel<T, false, 256>, 256, parts); };
+    auto go512 = [&](uint32_t parts) { return go(token_logprob_kernel<T, true, 512>, token_logprob_kernel<T, false, 512>, 512, parts); };
+    if (nvec >= 8192 && rows <= 74) return rows <= 18 ? go256(8) : go512(rows <= 37 ? 4 : 2);
+    if (nvec >= 2048 && rows <= 296) return go512(1);
+    if (nvec >= 1024 && rows <= (sizeof(T) == 4 ? 592 : 1200)) return go256(1);
+    return go128();
 }
 template <typename T>
 cudaError_t run_logprob_grad(const LogprobArgs &k, cudaStream_t st) {

@@ -98,6 +98,12 @@ template <> struct Elem<float> {
         for (int u = 1; u < U; ++u) m = fmaxf(m, vmax(v[u]));
         return m;
     }
+    // lowest score that is told from -inf where the two must not be confused, and the vector raised to it (a NaN stays)
+    static constexpr float kLow = -1e30f;
+    static __device__ __forceinline__ uint4 raise(const uint4 &v) {
+        return make_uint4(__float_as_uint(max_nan(__uint_as_float(v.x), kLow)), __float_as_uint(max_nan(__uint_as_float(v.y), kLow)),
+                          __float_as_uint(max_nan(__uint_as_float(v.z), kLow)), __float_as_uint(max_nan(__uint_as_float(v.w), kLow)));
+    }
     static __device__ __forceinline__ void put_pair(uint4 &v, int k, float a, float b) {
         if (k == 0) { v.x = __float_as_uint(a); v.y = __float_as_uint(b); }
         else { v.z = __float_as_uint(a); v.w = __float_as_uint(b); }
@@ -126,6 +132,12 @@ template <> struct Elem<__nv_bfloat16> {
             m = __hmax2(__hmax2(m, __hmax2(h2(v[u].x), h2(v[u].y))), __hmax2(h2(v[u].z), h2(v[u].w)));
         return fmaxf(__low2float(m), __high2float(m));
     }
+    static constexpr float kLow = -1e30f;
+    static __device__ __forceinline__ uint32_t raise(uint32_t w) {
+        const __nv_bfloat162 m = __hmax2_nan(h2(w), __float2bfloat162_rn(kLow));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    }
+    static __device__ __forceinline__ uint4 raise(const uint4 &v) { return make_uint4(raise(v.x), raise(v.y), raise(v.z), raise(v.w)); }
     static __device__ __forceinline__ void put_pair(uint4 &v, int k, float a, float b) {
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
         set_word(v, k, *reinterpret_cast<const uint32_t *>(&h));
@@ -149,6 +161,12 @@ template <> struct Elem<__half> {
             m = __hmax2(__hmax2(m, __hmax2(h2(v[u].x), h2(v[u].y))), __hmax2(h2(v[u].z), h2(v[u].w)));
         return fmaxf(__low2float(m), __high2float(m));
     }
+    static constexpr float kLow = -65504.0f;
+    static __device__ __forceinline__ uint32_t raise(uint32_t w) {
+        const __half2 m = __hmax2_nan(h2(w), __float2half2_rn(kLow));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    }
+    static __device__ __forceinline__ uint4 raise(const uint4 &v) { return make_uint4(raise(v.x), raise(v.y), raise(v.z), raise(v.w)); }
     static __device__ __forceinline__ void put_pair(uint4 &v, int k, float a, float b) {
         const __half2 h = __floats2half2_rn(a, b);
         set_word(v, k, *reinterpret_cast<const uint32_t *>(&h));

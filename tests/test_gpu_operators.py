@@ -115,7 +115,8 @@ def exact_grad(logp, h, y, g, gh, tau):
 @pytest.mark.parametrize("name", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("rows,vocab,pad,offset,tau", [
     (1, 1, 0, 0, 1.0), (2, 2, 0, 1, 1.0), (5, 7, 0, 0, 0.5), (3, 8, 3, 0, 1.0), (4, 9, 0, 3, 2.0), (17, 257, 1, 0, 1.0),
-    (1, 129280, 0, 0, 1.0), (2, 129281, 7, 5, 0.7), (37, 50021, 0, 2, 1.3), (300, 4099, 5, 1, 1.0), (700, 2048, 0, 0, 1.0)])
+    (1, 129280, 0, 0, 1.0), (2, 129281, 7, 5, 0.7), (37, 50021, 0, 2, 1.3), (300, 4099, 5, 1, 1.0), (700, 2048, 0, 0, 1.0),
+    (9, 1000, 0, 0, 1e-4), (9, 1000, 1, 0, 300.0), (5, 70001, 0, 0, 1e6), (1300, 9000, 0, 0, 1.0), (70, 66000, 0, 0, 1.0)])
 def test_logprob_and_gradient(name, rows, vocab, pad, offset, tau):
     x = logits_of(rows, vocab, name, rows + vocab, pad, offset)
     y = torch.randint(vocab, (rows,), generator=gen(1), device="cuda", dtype=torch.int32)
@@ -161,9 +162,8 @@ def test_gradient_against_differences_of_the_forward_call():
 
 
 @pytest.mark.parametrize("name", ["bf16", "f16", "f32"])
-@pytest.mark.parametrize("rows", [8, 600])                       # rows split over clusters, and one block each
-def test_logprob_masked_vocabulary_and_special_values(name, rows):
-    vocab = 9001
+@pytest.mark.parametrize("rows,vocab", [(8, 9001), (600, 9001), (8, 70001), (30, 70001)])       # one block a row; rows split over clusters
+def test_logprob_masked_vocabulary_and_special_values(name, rows, vocab):
     low = torch.finfo(DTYPES[name]).min
     x = logits_of(rows, vocab, name, 11)
     x[0, ::2] = float("-inf")                                    # half the vocabulary masked
