@@ -22,7 +22,9 @@ struct EmbedArgs {
     uint32_t n_chunks;
     uint32_t *keys;                      // [n_tokens] sorted ids; vocab: no token
     uint32_t *pos;                       // [n_tokens] their positions
-    float *partial;                      // [2][n_chunks][dim]: sums of a run cut by the chunk's start / by its end
+    uint32_t *present;                   // [ceil(vocab / 32)] a bit per id that occurs, or nullptr
+    float *partial;                      // [2][n_chunks][partial_stride]: sums of a run cut by the chunk's start / by its end
+    size_t partial_stride;               // dim rounded up to a warp's columns
 };
 
 // Positions that hold a token of the batch.
@@ -104,279 +106,434 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a,
 
 // ---- sorting positions by id: least significant digit first, stable, so that the positions of one
 // id stay in ascending order ----
-constexpr int kSortThreads = 512, kSortItems = 8;
-constexpr uint32_t kSortTile = kSortThreads * kSortItems;
 constexpr int kSortBits = 9, kSortBins = 1 << kSortBits;
-constexpr int kSortWarps = kSortThreads / 32;
 
-struct SortPass {
-    uint32_t shift, first;               // first pass: keys come from the ids, positions are implicit
-    uint32_t n_tiles;
-    uint32_t *counts;                    // [n_tiles][kSortBins]
-    const uint32_t *keys_in, *pos_in;
-    uint32_t *keys_out, *pos_out;
-};
-
-__device__ __forceinline__ uint32_t sort_key(const EmbedArgs &a, const SortPass &s, uint32_t i, uint32_t n) {
-    return s.first ? id_at(a, i, n) : s.keys_in[i];
-}
-
-__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const EmbedArgs a, const SortPass s) {
-    griddep_launch_dependents();
-    griddep_wait();
-    __shared__ uint32_t bins[kSortBins];
-    for (int b = threadIdx.x; b < kSortBins; b += kSortThreads) bins[b] = 0;
-    __syncthreads();
-    const uint32_t n = tokens_in(a), base = blockIdx.x * kSortTile;
-#pragma unroll
-    for (int k = 0; k < kSortItems; ++k) {
-        const uint32_t i = base + k * kSortThreads + threadIdx.x;
-        if (i < a.n_tokens) atomicAdd(&bins[(sort_key(a, s, i, n) >> s.shift) & (kSortBins - 1)], 1u);
-    }
-    __syncthreads();
-    for (int b = threadIdx.x; b < kSortBins; b += kSortThreads) s.counts[(size_t)blockIdx.x * kSortBins + b] = bins[b];
-}
-
-__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const EmbedArgs a, const SortPass s) {
-    griddep_launch_dependents();
-    griddep_wait();
-    static_assert(kSortBins == kSortThreads, "one thread per bin");
-    __shared__ uint32_t warp_bins[kSortWarps][kSortBins];
-    __shared__ uint32_t warp_sum[kSortWarps];
+// Ranks of a block's entries among those of the same digit.  Entries are in registers, warp by warp, turn by turn,
+// lane by lane; warp_bins[w][d] ends up as the number of entries with digit d in the warp.
+template <int kItems, int kWarps, typename Count>
+__device__ __forceinline__ void rank_digits(const uint32_t (&key)[kItems], uint32_t (&rank)[kItems], uint32_t in_mask, uint32_t shift,
+                                            Count (*warp_bins)[kSortBins], uint32_t items) {
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     for (int b = lane; b < kSortBins; b += 32) warp_bins[warp][b] = 0;
     __syncwarp();
-    // a warp owns kSortItems * 32 consecutive entries of the tile
-    const uint32_t n = tokens_in(a), base = blockIdx.x * kSortTile + warp * (kSortItems * 32);
-    uint32_t key[kSortItems], at[kSortItems], rank[kSortItems];
 #pragma unroll
-    for (int k = 0; k < kSortItems; ++k) {
-        const uint32_t i = base + k * 32 + lane;
-        key[k] = i < a.n_tokens ? sort_key(a, s, i, n) : 0u;
-        at[k] = s.first || i >= a.n_tokens ? i : s.pos_in[i];
-    }
-#pragma unroll
-    for (int k = 0; k < kSortItems; ++k) {
-        const bool in = base + k * 32 + lane < a.n_tokens;
-        const uint32_t d = in ? (key[k] >> s.shift) & (kSortBins - 1) : kSortBins;      // absent entries match only each other
+    for (int k = 0; k < kItems; ++k) {
+        if ((uint32_t)k >= items) break;
+        const bool in = (in_mask >> k) & 1u;
+        const uint32_t d = in ? (key[k] >> shift) & (kSortBins - 1) : kSortBins;        // absent entries match only each other
         const uint32_t peers = __match_any_sync(kFullMask, d);
         const uint32_t before = in ? warp_bins[warp][d] : 0u;
         rank[k] = before + __popc(peers & ((1u << lane) - 1u));
         __syncwarp();
-        if (in && lane == (uint32_t)__ffs(peers) - 1u) warp_bins[warp][d] = before + __popc(peers);
+        if (in && lane == (uint32_t)__ffs(peers) - 1u) warp_bins[warp][d] = (Count)(before + __popc(peers));
         __syncwarp();
     }
-    __syncthreads();
-    // thread b: where bin b of this tile starts in the output
-    const uint32_t b = threadIdx.x;
-    uint32_t total = 0, ahead = 0;
-    for (uint32_t tile = 0; tile < s.n_tiles; ++tile) {
-        const uint32_t c = __ldcg(s.counts + (size_t)tile * kSortBins + b);
-        if (tile < blockIdx.x) ahead += c;
-        total += c;
-    }
-    uint32_t scan = total;
+}
+
+// Exclusive sum over a block's first kSortBins threads; every thread of the block calls it.
+__device__ __forceinline__ uint32_t scan_bins(uint32_t x, uint32_t *warp_sum) {
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    uint32_t scan = x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const uint32_t v = __shfl_up_sync(kFullMask, scan, o);
         if (lane >= (uint32_t)o) scan += v;
     }
-    if (lane == 31) warp_sum[warp] = scan;
+    if (lane == 31 && warp < kSortBins / 32) warp_sum[warp] = scan;
     __syncthreads();
-    uint32_t start = scan - total + ahead;
-    for (uint32_t w = 0; w < warp; ++w) start += warp_sum[w];
+    uint32_t before = scan - x;
+    for (uint32_t w = 0; w < min(warp, (uint32_t)(kSortBins / 32)); ++w) before += warp_sum[w];
+    return before;
+}
+
+// Zeros at [p, p + bytes) by n threads, of which this is number i; p and bytes are multiples of 2.
+__device__ __forceinline__ void fill_zero(uint8_t *p, size_t bytes, size_t i, size_t n) {
+    const size_t head = min(bytes, (size_t)((16u - (reinterpret_cast<uintptr_t>(p) & 15u)) & 15u)), nvec = (bytes - head) / 16;
+    for (size_t j = i; j < nvec; j += n) st_stream(p + head + j * 16, make_uint4(0u, 0u, 0u, 0u));
+    const size_t tail = head + nvec * 16;
+    if (i < head / 2) reinterpret_cast<uint16_t *>(p)[i] = 0;
+    if (i < (bytes - tail) / 2) reinterpret_cast<uint16_t *>(p + tail)[i] = 0;
+}
+
+// One block sorts everything: up to 8192 positions, in shared memory.  Blocks beyond the first clear the gradient
+// table meanwhile, where the launch has such blocks.
+constexpr int kSmallThreads = 1024, kSmallItems = 8, kSmallWarps = kSmallThreads / 32;
+constexpr uint32_t kSmallMax = kSmallThreads * kSmallItems;
+constexpr size_t kSmallSmem = (size_t)kSmallWarps * kSortBins * 2 + kSmallMax * (4 + 2) + 64;
+
+__global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedArgs a, uint32_t passes, uint32_t grad_size) {
+    griddep_launch_dependents();
+    griddep_wait();
+    if (blockIdx.x > 0) {
+        const size_t i = (size_t)(blockIdx.x - 1) * kSmallThreads + threadIdx.x, n = (size_t)(gridDim.x - 1) * kSmallThreads;
+        uint8_t *t = static_cast<uint8_t *>(a.grad_table);
+        const size_t row = (size_t)a.dim * grad_size, stride = (size_t)a.table_stride * grad_size;
+        if (row == stride) return fill_zero(t, row * a.vocab, i, n);
+        const size_t warp = i / 32, warps = n / 32, lane = threadIdx.x & 31u;
+        for (size_t v = warp; v < a.vocab; v += warps) fill_zero(t + v * stride, row, lane, 32);
+        return;
+    }
+    extern __shared__ __align__(16) uint8_t sort_smem[];
+    uint16_t(*warp_bins)[kSortBins] = reinterpret_cast<uint16_t(*)[kSortBins]>(sort_smem);
+    uint32_t *keys = reinterpret_cast<uint32_t *>(sort_smem + (size_t)kSmallWarps * kSortBins * 2);
+    uint16_t *pos = reinterpret_cast<uint16_t *>(keys + kSmallMax);
+    uint32_t *warp_sum = reinterpret_cast<uint32_t *>(pos + kSmallMax);
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t n = tokens_in(a), items = (a.n_tokens + kSmallThreads - 1) / kSmallThreads, base = warp * items * 32 + lane;
+    if (a.present) {
+        for (uint32_t w = threadIdx.x; w < (a.vocab + 31) / 32; w += kSmallThreads) a.present[w] = 0u;
+        __syncthreads();
+    }
+    uint32_t key[kSmallItems], at[kSmallItems], rank[kSmallItems], in_mask = 0;
+#pragma unroll
+    for (int k = 0; k < kSmallItems; ++k) {
+        if ((uint32_t)k >= items) break;
+        at[k] = base + k * 32;
+        if (at[k] < a.n_tokens) {
+            in_mask |= 1u << k;
+            key[k] = id_at(a, at[k], n);
+            if (a.present && key[k] < a.vocab) atomicOr(a.present + (key[k] >> 5), 1u << (key[k] & 31u));
+        }
+    }
+    for (uint32_t p = 0; p < passes; ++p) {
+        if (p) {
+#pragma unroll
+            for (int k = 0; k < kSmallItems; ++k) {
+                if ((uint32_t)k >= items) break;
+                if ((in_mask >> k) & 1u) {
+                    key[k] = keys[base + k * 32];
+                    at[k] = pos[base + k * 32];
+                }
+            }
+        }
+        const uint32_t shift = p * kSortBits;
+        rank_digits<kSmallItems, kSmallWarps>(key, rank, in_mask, shift, warp_bins, items);
+        __syncthreads();
+        uint32_t total = 0;
+        if (threadIdx.x < kSortBins)
+            for (int w = 0; w < kSmallWarps; ++w) {          // entries of the bin in earlier warps
+                const uint32_t c = warp_bins[w][threadIdx.x];
+                warp_bins[w][threadIdx.x] = (uint16_t)total;
+                total += c;
+            }
+        const uint32_t start = scan_bins(total, warp_sum);
+        if (threadIdx.x < kSortBins)
+            for (int w = 0; w < kSmallWarps; ++w) warp_bins[w][threadIdx.x] = (uint16_t)(warp_bins[w][threadIdx.x] + start);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kSmallItems; ++k) {
+            if ((uint32_t)k >= items) break;
+            if (!((in_mask >> k) & 1u)) continue;
+            const uint32_t to = warp_bins[warp][(key[k] >> shift) & (kSortBins - 1)] + rank[k];
+            if (p + 1 < passes) {
+                keys[to] = key[k];
+                pos[to] = (uint16_t)at[k];
+            } else {
+                a.keys[to] = key[k];
+                a.pos[to] = at[k];
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// More positions: tiles of kSortThreads * kItems entries.  A counting kernel for the first digit, then one
+// placing kernel per digit, which counts the next digit where its entries go.
+constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
+static_assert(kSortBins == kSortThreads, "one thread per bin");
+
+struct SortPass {
+    uint32_t shift, first, last;         // first: keys come from the ids, positions are implicit
+    uint32_t n_tiles, passes;
+    uint32_t *counts;                    // [passes][n_tiles][kSortBins]
+    const uint32_t *keys_in, *pos_in;
+    uint32_t *keys_out, *pos_out;
+};
+
+template <int kItems>
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const EmbedArgs a, const SortPass s) {
+    griddep_launch_dependents();
+    griddep_wait();
+    __shared__ uint32_t bins[kSortBins];
+    bins[threadIdx.x] = 0;
+    __syncthreads();
+    const uint32_t n = tokens_in(a), base = blockIdx.x * (kSortThreads * kItems);
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+        const uint32_t i = base + k * kSortThreads + threadIdx.x;
+        if (i < a.n_tokens) atomicAdd(&bins[id_at(a, i, n) & (kSortBins - 1)], 1u);
+    }
+    __syncthreads();
+    s.counts[(size_t)blockIdx.x * kSortBins + threadIdx.x] = bins[threadIdx.x];
+    // what the placing kernels add to
+    for (uint32_t p = 1; p < s.passes; ++p) s.counts[((size_t)p * s.n_tiles + blockIdx.x) * kSortBins + threadIdx.x] = 0u;
+    if (a.present)
+        for (uint32_t w = blockIdx.x * kSortThreads + threadIdx.x; w < (a.vocab + 31) / 32; w += gridDim.x * kSortThreads) a.present[w] = 0u;
+}
+
+template <int kItems>
+__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const EmbedArgs a, const SortPass s) {
+    griddep_launch_dependents();
+    griddep_wait();
+    __shared__ uint32_t warp_bins[kSortWarps][kSortBins];
+    __shared__ uint32_t warp_sum[kSortBins / 32];
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t pass = s.shift / kSortBits;
+    // a warp owns kItems * 32 consecutive entries of the tile
+    const uint32_t n = tokens_in(a), base = blockIdx.x * (kSortThreads * kItems) + warp * (kItems * 32) + lane;
+    uint32_t key[kItems], at[kItems], rank[kItems], in_mask = 0;
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+        at[k] = base + k * 32;
+        key[k] = 0;
+        if (at[k] < a.n_tokens) {
+            in_mask |= 1u << k;
+            key[k] = s.first ? id_at(a, at[k], n) : s.keys_in[at[k]];
+            if (!s.first) at[k] = s.pos_in[at[k]];
+        }
+    }
+    // thread b: entries of bin b in all tiles, and in the tiles before this one
+    uint32_t total = 0, ahead = 0;
+    const uint32_t *counts = s.counts + (size_t)pass * s.n_tiles * kSortBins + threadIdx.x;
+#pragma unroll 8
+    for (uint32_t tile = 0; tile < s.n_tiles; ++tile) {
+        const uint32_t c = __ldcg(counts + (size_t)tile * kSortBins);
+        if (tile < blockIdx.x) ahead += c;
+        total += c;
+    }
+    rank_digits<kItems, kSortWarps>(key, rank, in_mask, s.shift, warp_bins, kItems);
+    uint32_t start = scan_bins(total, warp_sum) + ahead;     // its barrier also ends the ranking
     for (int w = 0; w < kSortWarps; ++w) {
-        const uint32_t c = warp_bins[w][b];
-        warp_bins[w][b] = start;
+        const uint32_t c = warp_bins[w][threadIdx.x];
+        warp_bins[w][threadIdx.x] = start;
         start += c;
     }
     __syncthreads();
+    uint32_t *next = s.last ? nullptr : s.counts + (size_t)(pass + 1) * s.n_tiles * kSortBins;
 #pragma unroll
-    for (int k = 0; k < kSortItems; ++k) {
-        const uint32_t i = base + k * 32 + lane;
-        if (i >= a.n_tokens) continue;
+    for (int k = 0; k < kItems; ++k) {
+        if (!((in_mask >> k) & 1u)) continue;
         const uint32_t to = warp_bins[warp][(key[k] >> s.shift) & (kSortBins - 1)] + rank[k];
         s.keys_out[to] = key[k];
         s.pos_out[to] = at[k];
+        if (next) atomicAdd(next + (size_t)(to / (kSortThreads * kItems)) * kSortBins + ((key[k] >> (s.shift + kSortBits)) & (kSortBins - 1)), 1u);
+        if (s.first && a.present && key[k] < a.vocab) atomicOr(a.present + (key[k] >> 5), 1u << (key[k] & 31u));
     }
 }
 
 // ---- sums over the runs of equal ids ----
-// Row v of the gradient table, columns [c0, c0 + kCols) of this lane.
-template <typename T, int kCols>
+// kSumCols columns of a row per lane, kSumWarpCols per warp.  Wide: a lane's columns are consecutive, moved
+// 16 bytes at a time; else the warp's lanes take turns, element by element.
+constexpr int kSumThreads = 256, kSumCols = 8;
+constexpr uint32_t kSumWarpCols = 32 * kSumCols;
+
+template <typename T, bool kWide>
 struct Columns {
-    static __device__ __forceinline__ void load(float (&x)[kCols], const T *row, uint32_t c0, uint32_t dim, bool wide) {
-        if (wide) {
-            constexpr int E = Elem<T>::kVec;
+    static constexpr int kVecs = kWide ? kSumCols / Elem<T>::kVec : 0;
+    uint4 v[kWide ? kVecs : 1];
+    float x[kWide ? 1 : kSumCols];
+    // row: the warp's first column; n: columns of the row from there on
+    __device__ __forceinline__ void load(const T *row, uint32_t lane, uint32_t n, bool on) {
+        if constexpr (kWide) {
 #pragma unroll
-            for (int q = 0; q < kCols / E; ++q) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(row + c0 + q * E);
-#pragma unroll
-                for (int k = 0; k < E / 2; ++k) unpack2(Elem<T>::pair(v, k), x[q * E + 2 * k], x[q * E + 2 * k + 1]);
+            for (int q = 0; q < kVecs; ++q) {
+                v[q] = make_uint4(0u, 0u, 0u, 0u);
+                if (on && lane * kSumCols < n) v[q] = *reinterpret_cast<const uint4 *>(row + lane * kSumCols + q * Elem<T>::kVec);
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < kCols; ++j) x[j] = c0 + j < dim ? Elem<T>::load(row + c0 + j) : 0.0f;
+            for (int j = 0; j < kSumCols; ++j) x[j] = on && j * 32 + lane < n ? Elem<T>::load(row + j * 32 + lane) : 0.0f;
         }
     }
-    static __device__ __forceinline__ void store(T *row, const float (&x)[kCols], uint32_t c0, uint32_t dim, bool wide) {
-        if (wide) {
-            constexpr int E = Elem<T>::kVec;
+    __device__ __forceinline__ void add_to(f32x2 (&sum)[kSumCols / 2]) const {
+        if constexpr (kWide) {
 #pragma unroll
-            for (int q = 0; q < kCols / E; ++q) {
-                uint4 v;
+            for (int q = 0; q < kVecs; ++q)
 #pragma unroll
-                for (int k = 0; k < E / 2; ++k) Elem<T>::put_pair(v, k, x[q * E + 2 * k], x[q * E + 2 * k + 1]);
-                st_stream(row + c0 + q * E, v);
+                for (int k = 0; k < Elem<T>::kVec / 2; ++k) sum[q * Elem<T>::kVec / 2 + k] = add2(sum[q * Elem<T>::kVec / 2 + k], Elem<T>::pair(v[q], k));
+        } else {
+#pragma unroll
+            for (int k = 0; k < kSumCols / 2; ++k) sum[k] = add2(sum[k], pack2(x[2 * k], x[2 * k + 1]));
+        }
+    }
+    static __device__ __forceinline__ void store(T *row, const f32x2 (&sum)[kSumCols / 2], uint32_t lane, uint32_t n) {
+        if constexpr (kWide) {
+            if (lane * kSumCols >= n) return;
+#pragma unroll
+            for (int q = 0; q < kVecs; ++q) {
+                uint4 o;
+#pragma unroll
+                for (int k = 0; k < Elem<T>::kVec / 2; ++k) {
+                    float a, b;
+                    unpack2(sum[q * Elem<T>::kVec / 2 + k], a, b);
+                    Elem<T>::put_pair(o, k, a, b);
+                }
+                st_stream(row + lane * kSumCols + q * Elem<T>::kVec, o);
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < kCols; ++j)
-                if (c0 + j < dim) row[c0 + j] = Elem<T>::from(x[j]);
+            for (int k = 0; k < kSumCols / 2; ++k) {
+                float a, b;
+                unpack2(sum[k], a, b);
+                if (2 * k * 32 + lane < n) row[2 * k * 32 + lane] = Elem<T>::from(a);
+                if ((2 * k + 1) * 32 + lane < n) row[(2 * k + 1) * 32 + lane] = Elem<T>::from(b);
+            }
         }
     }
 };
 
-constexpr int kSumThreads = 256, kSumCols = 8;               // columns per lane: a warp covers 256
-constexpr uint32_t kSumWarpCols = 32 * kSumCols;
-
-template <typename G>
-__device__ __forceinline__ void write_row(const EmbedArgs &a, uint32_t v, const float (&sum)[kSumCols], uint32_t c0, bool wide) {
-    G *row = static_cast<G *>(a.grad_table) + (long long)v * a.table_stride;
-    float x[kSumCols];
+// scale * sum to row v of the gradient table, or added to what is there
+template <typename G, bool kWide>
+__device__ __forceinline__ void write_row(const EmbedArgs &a, uint32_t v, const f32x2 (&sum)[kSumCols / 2], uint32_t c0, uint32_t lane) {
+    G *row = static_cast<G *>(a.grad_table) + (long long)v * a.table_stride + c0;
+    f32x2 x[kSumCols / 2];
+    const f32x2 sc = pack2(a.scale, a.scale);
 #pragma unroll
-    for (int j = 0; j < kSumCols; ++j) x[j] = sum[j] * a.scale;
+    for (int k = 0; k < kSumCols / 2; ++k) x[k] = mul2(sum[k], sc);
     if (a.accumulate) {
-        float old[kSumCols];
-        Columns<G, kSumCols>::load(old, row, c0, a.dim, wide);
-#pragma unroll
-        for (int j = 0; j < kSumCols; ++j) x[j] += old[j];
+        Columns<G, kWide> old;
+        old.load(row, lane, a.dim - c0, true);
+        old.add_to(x);
     }
-    Columns<G, kSumCols>::store(row, x, c0, a.dim, wide);
+    Columns<G, kWide>::store(row, x, lane, a.dim - c0);
 }
 
 __device__ __forceinline__ float *partial_row(const EmbedArgs &a, uint32_t which, uint32_t chunk) {
-    return a.partial + ((size_t)which * a.n_chunks + chunk) * a.dim;
+    return a.partial + ((size_t)which * a.n_chunks + chunk) * a.partial_stride;
 }
 
-// A warp per (chunk of sorted positions, 256 columns).  A run that lies inside the chunk is written
-// out; the part of a run that began in an earlier chunk goes to partial 0, the part of one that
-// began here and goes on to partial 1.
-template <typename T, typename G>
-__global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const EmbedArgs a, uint32_t slices, bool wide_in, bool wide_out) {
+// Rows of the gradient table whose bit in a.present is not set, 32 per block.
+template <typename G>
+__device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t word) {
+    const uint32_t bits = a.present[word], lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    for (uint32_t k = warp; k < 32 && word * 32 + k < a.vocab; k += kSumThreads / 32)
+        if (!((bits >> k) & 1u))
+            fill_zero(reinterpret_cast<uint8_t *>(static_cast<G *>(a.grad_table) + (long long)(word * 32 + k) * a.table_stride), (size_t)a.dim * sizeof(G), lane, 32);
+}
+
+// A warp per (chunk of sorted positions, 256 columns).  A run that lies inside the chunk is written out; the part of
+// a run that began in an earlier chunk goes to partial 0, the part of one that began here and goes on to
+// partial 1.  Spread among the blocks that do this, as many as a.present has words clear rows without a token.
+template <typename T, typename G, bool kWide>
+__global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const EmbedArgs a, uint32_t slices, uint32_t sum_blocks) {
     griddep_launch_dependents();
     griddep_wait();
-    const unsigned long long item = (unsigned long long)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5);
+    const uint32_t sums_before = (uint32_t)((unsigned long long)blockIdx.x * sum_blocks / gridDim.x);
+    if ((uint32_t)((unsigned long long)(blockIdx.x + 1ull) * sum_blocks / gridDim.x) == sums_before)
+        return zero_rows<G>(a, blockIdx.x - sums_before);
+    const unsigned long long item = (unsigned long long)sums_before * (kSumThreads / 32) + (threadIdx.x >> 5);
     const unsigned long long chunk64 = item / slices;
     if (chunk64 >= a.n_chunks) return;
     const uint32_t chunk = (uint32_t)chunk64, lane = threadIdx.x & 31u;
-    const uint32_t c0 = (uint32_t)(item % slices) * kSumWarpCols + lane * kSumCols;
-    const bool full = c0 + kSumCols <= a.dim;                // this lane's columns all exist
+    const uint32_t c0 = (uint32_t)(item % slices) * kSumWarpCols, cols = a.dim - c0;
     const uint32_t lo = chunk * a.rows_per_chunk, hi = min(a.n_tokens, lo + a.rows_per_chunk);
     const uint32_t first = a.keys[lo];
     if (first >= a.vocab) return;                            // sorted behind all ids
     bool cont = lo > 0 && a.keys[lo - 1] == first;
-    float sum[kSumCols];
+    f32x2 sum[kSumCols / 2];
+    auto clear = [&]() {
 #pragma unroll
-    for (int j = 0; j < kSumCols; ++j) sum[j] = 0.0f;
+        for (int k = 0; k < kSumCols / 2; ++k) sum[k] = pack2(0.0f, 0.0f);
+    };
+    clear();
     uint32_t v = first;
+    const T *in = static_cast<const T *>(a.grad_out) + c0;
+    constexpr int kRows = kWide && sizeof(T) == 2 ? 8 : 4;   // rows on their way at a time
     for (uint32_t e0 = lo; e0 < hi; e0 += 32) {
         const uint32_t left = min(hi - e0, 32u);
         const uint32_t my_key = lane < left ? a.keys[e0 + lane] : a.vocab, my_pos = lane < left ? a.pos[e0 + lane] : 0u;
-        for (uint32_t k0 = 0; k0 < left; k0 += 4) {
-            float x[4][kSumCols];
+        for (uint32_t k0 = 0; k0 < left; k0 += kRows) {
+            Columns<T, kWide> x[kRows];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const uint32_t key = __shfl_sync(kFullMask, my_key, (k0 + u) & 31u), p = __shfl_sync(kFullMask, my_pos, (k0 + u) & 31u);
-#pragma unroll
-                for (int j = 0; j < kSumCols; ++j) x[u][j] = 0.0f;
-                if (k0 + u < left && key < a.vocab && c0 < a.dim)
-                    Columns<T, kSumCols>::load(x[u], static_cast<const T *>(a.grad_out) + (long long)p * a.out_stride, c0, a.dim, wide_in && full);
+            for (int u = 0; u < kRows; ++u) {
+                const uint32_t key = __shfl_sync(kFullMask, my_key, k0 + u), p = __shfl_sync(kFullMask, my_pos, k0 + u);
+                x[u].load(in + (long long)p * a.out_stride, lane, cols, key < a.vocab);
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < kRows; ++u) {
+                const uint32_t key = __shfl_sync(kFullMask, my_key, k0 + u);
                 if (k0 + u >= left) break;
-                const uint32_t key = __shfl_sync(kFullMask, my_key, (k0 + u) & 31u);
                 if (key != v) {                              // the run of v ends here
-                    if (c0 < a.dim && v < a.vocab) {
-                        if (cont) Columns<float, kSumCols>::store(partial_row(a, 0, chunk), sum, c0, a.dim, full && (a.dim & 3u) == 0);
-                        else write_row<G>(a, v, sum, c0, wide_out && full);
+                    if (v < a.vocab) {
+                        if (cont) Columns<float, kWide>::store(partial_row(a, 0, chunk) + c0, sum, lane, cols);
+                        else write_row<G, kWide>(a, v, sum, c0, lane);
                     }
                     cont = false;
                     v = key;
-#pragma unroll
-                    for (int j = 0; j < kSumCols; ++j) sum[j] = 0.0f;
+                    clear();
                 }
-#pragma unroll
-                for (int j = 0; j < kSumCols; ++j) sum[j] += x[u][j];
+                x[u].add_to(sum);
             }
         }
     }
-    if (v >= a.vocab || c0 >= a.dim) return;
+    if (v >= a.vocab) return;
     const bool goes_on = hi < a.n_tokens && a.keys[hi] == v;
-    if (cont) Columns<float, kSumCols>::store(partial_row(a, 0, chunk), sum, c0, a.dim, full && (a.dim & 3u) == 0);
-    else if (goes_on) Columns<float, kSumCols>::store(partial_row(a, 1, chunk), sum, c0, a.dim, full && (a.dim & 3u) == 0);
-    else write_row<G>(a, v, sum, c0, wide_out && full);
+    if (cont) Columns<float, kWide>::store(partial_row(a, 0, chunk) + c0, sum, lane, cols);
+    else if (goes_on) Columns<float, kWide>::store(partial_row(a, 1, chunk) + c0, sum, lane, cols);
+    else write_row<G, kWide>(a, v, sum, c0, lane);
 }
 
-// Runs that chunk borders cut: the chunk a run begins in adds the parts up in order.
-template <typename G>
-__global__ void __launch_bounds__(kSumThreads) embed_join_kernel(const EmbedArgs a, uint32_t slices, bool wide_out) {
+// Runs that chunk borders cut: the block of the chunk a run begins in adds the parts up.  Up to kJoinAlone parts one
+// warp adds in order, a slice of columns each; more are cut into one piece per warp, and the pieces' sums added
+// in order.
+constexpr uint32_t kJoinAlone = 8;
+template <typename G, bool kWide>
+__global__ void __launch_bounds__(kSumThreads) embed_join_kernel(const EmbedArgs a, uint32_t slices) {
     griddep_launch_dependents();
     griddep_wait();
-    const unsigned long long item = (unsigned long long)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5);
-    const unsigned long long chunk64 = item / slices;
-    if (chunk64 >= a.n_chunks) return;
-    const uint32_t chunk = (uint32_t)chunk64, lane = threadIdx.x & 31u;
-    const uint32_t c0 = (uint32_t)(item % slices) * kSumWarpCols + lane * kSumCols;
+    constexpr uint32_t kWarps = kSumThreads / 32;
+    __shared__ f32x2 piece[kWarps][kSumCols / 2][32];
+    const uint32_t chunk = blockIdx.x, lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t lo = chunk * a.rows_per_chunk;
     const unsigned long long hi = (unsigned long long)lo + a.rows_per_chunk;
     if (hi >= a.n_tokens) return;
     const uint32_t v = a.keys[hi - 1];
     if (v >= a.vocab || a.keys[hi] != v || (lo > 0 && a.keys[lo - 1] == v)) return;      // ends here, or began earlier
-    if (c0 >= a.dim) return;
-    const bool full = c0 + kSumCols <= a.dim, wide = full && (a.dim & 3u) == 0;
-    float sum[kSumCols], x[kSumCols];
-    Columns<float, kSumCols>::load(sum, partial_row(a, 1, chunk), c0, a.dim, wide);
-    for (uint32_t c = chunk + 1; c < a.n_chunks && a.keys[(size_t)c * a.rows_per_chunk] == v; ++c) {
-        Columns<float, kSumCols>::load(x, partial_row(a, 0, c), c0, a.dim, wide);
+    // chunks behind this one that begin with v
+    uint32_t parts = 0;
+    for (;;) {
+        const unsigned long long c = (unsigned long long)chunk + 1 + parts + lane;
+        const uint32_t same = __ballot_sync(kFullMask, c < a.n_chunks && a.keys[c * a.rows_per_chunk] == v);
+        if (same == kFullMask) { parts += 32; continue; }
+        parts += __ffs(~same) - 1;
+        break;
+    }
+    auto add_parts = [&](f32x2 (&sum)[kSumCols / 2], uint32_t from, uint32_t to, uint32_t c0) {
+        for (uint32_t p = from; p < to; p += 4) {
+            Columns<float, kWide> x[4];
 #pragma unroll
-        for (int j = 0; j < kSumCols; ++j) sum[j] += x[j];
-    }
-    write_row<G>(a, v, sum, c0, wide_out && full);
-}
-
-// Rows of the gradient table that no token has.
-template <typename G>
-__global__ void __launch_bounds__(kSumThreads) embed_zero_kernel(const EmbedArgs a, bool wide_out) {
-    griddep_launch_dependents();
-    griddep_wait();
-    constexpr uint32_t kRows = 32;
-    __shared__ uint32_t present;
-    const uint32_t v0 = blockIdx.x * kRows;
-    if (threadIdx.x < 32) {
-        const uint32_t v = v0 + threadIdx.x;
-        uint32_t lo = 0, hi = a.n_tokens;                    // first entry with key >= v
-        while (lo < hi) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (a.keys[mid] < v) lo = mid + 1; else hi = mid;
+            for (int u = 0; u < 4; ++u) x[u].load(partial_row(a, 0, chunk + 1 + min(p + u, to - 1)) + c0, lane, a.dim - c0, p + u < to);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[u].add_to(sum);
         }
-        const uint32_t bits = __ballot_sync(kFullMask, lo < a.n_tokens && a.keys[lo] == v);
-        if (threadIdx.x == 0) present = bits;
-    }
-    __syncthreads();
-    const uint32_t bits = present;
-    constexpr int E = Elem<G>::kVec;
-    for (uint32_t k = 0; k < kRows && v0 + k < a.vocab; ++k) {
-        if ((bits >> k) & 1u) continue;
-        G *row = static_cast<G *>(a.grad_table) + (long long)(v0 + k) * a.table_stride;
-        uint32_t done = 0;
-        if (wide_out) {
-            const uint32_t nvec = a.dim / E;
-            for (uint32_t j = threadIdx.x; j < nvec; j += kSumThreads) st_stream(reinterpret_cast<uint4 *>(row) + j, make_uint4(0u, 0u, 0u, 0u));
-            done = nvec * E;
+    };
+    const bool alone = parts <= kJoinAlone;
+    for (uint32_t s = alone ? warp : 0; s < slices; s += alone ? kWarps : 1) {
+        const uint32_t c0 = s * kSumWarpCols;
+        f32x2 sum[kSumCols / 2];
+#pragma unroll
+        for (int k = 0; k < kSumCols / 2; ++k) sum[k] = pack2(0.0f, 0.0f);
+        if (alone || warp == 0) {
+            Columns<float, kWide> x;
+            x.load(partial_row(a, 1, chunk) + c0, lane, a.dim - c0, true);
+            x.add_to(sum);
         }
-        for (uint32_t j = done + threadIdx.x; j < a.dim; j += kSumThreads) row[j] = Elem<G>::from(0.0f);
+        if (alone) {
+            add_parts(sum, 0, parts, c0);
+            write_row<G, kWide>(a, v, sum, c0, lane);
+            continue;
+        }
+        add_parts(sum, (uint32_t)((unsigned long long)parts * warp / kWarps), (uint32_t)((unsigned long long)parts * (warp + 1) / kWarps), c0);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kSumCols / 2; ++k) piece[warp][k][lane] = sum[k];
+        __syncthreads();
+        if (warp == 0) {
+            for (uint32_t w = 1; w < kWarps; ++w)
+#pragma unroll
+                for (int k = 0; k < kSumCols / 2; ++k) sum[k] = add2(sum[k], piece[w][k][lane]);
+            write_row<G, kWide>(a, v, sum, c0, lane);
+        }
     }
 }
 

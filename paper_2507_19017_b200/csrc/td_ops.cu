@@ -162,53 +162,84 @@ cudaError_t run_policy(const PolicyArgs &k, int kl, cudaStream_t st) {
     return kl == kNoKl ? run_policy<kVec, kNoKl>(k, st) : kl == kKlExp ? run_policy<kVec, kKlExp>(k, st) : run_policy<kVec, kKlPoly>(k, st);
 }
 
+// Sorted positions per chunk of the segment sums: short chunks while there are few positions to spread
+// over the machine, long ones later (a run cut by a border costs two float rows of extra traffic).
+uint32_t chunk_rows(uint32_t n_tokens, uint32_t slices) {
+    uint32_t r = 8;
+    while (r < 128 && (uint64_t)n_tokens * slices > (uint64_t)r * 148 * 48) r *= 2;
+    return r;
+}
 struct EmbedGradLayout {
-    size_t keys[2], pos[2], counts, partial, total;
-    uint32_t n_tiles, n_chunks, rows_per_chunk;
+    size_t keys[2], pos[2], counts, present, partial, partial_stride, total;
+    uint32_t n_tiles, n_chunks, rows_per_chunk, slices, passes;
+    bool small, big_tiles;
 };
-EmbedGradLayout embed_layout(uint32_t n_tokens, uint32_t dim) {
+EmbedGradLayout embed_layout(uint32_t n_tokens, uint32_t vocab, uint32_t dim) {
     EmbedGradLayout L{};
-    L.rows_per_chunk = n_tokens <= (1u << 17) ? 32u : 128u;
-    L.n_tiles = (n_tokens + kSortTile - 1) / kSortTile;
-    L.n_chunks = (n_tokens + L.rows_per_chunk - 1) / L.rows_per_chunk;
+    int bits = 0;
+    while (bits < 32 && (vocab >> bits) != 0) ++bits;        // the keys are 0 .. vocab
+    L.passes = (uint32_t)((bits + kSortBits - 1) / kSortBits);
+    L.small = n_tokens <= kSmallMax;
+    L.big_tiles = n_tokens > (1u << 17);                     // every block reads all tiles' counts: few of them
+    const uint32_t tile = kSortThreads * (L.big_tiles ? 16 : 4);
+    L.n_tiles = (uint32_t)(((uint64_t)n_tokens + tile - 1) / tile);
+    L.slices = (uint32_t)(((uint64_t)dim + kSumWarpCols - 1) / kSumWarpCols);
+    L.rows_per_chunk = chunk_rows(n_tokens, L.slices);
+    L.n_chunks = (uint32_t)(((uint64_t)n_tokens + L.rows_per_chunk - 1) / L.rows_per_chunk);
+    L.partial_stride = (size_t)L.slices * kSumWarpCols;
     size_t p = 0;
     auto take = [&](size_t bytes) { const size_t at = p; p = round_up(p + bytes, 256); return at; };
     for (int k = 0; k < 2; ++k) { L.keys[k] = take((size_t)n_tokens * 4); L.pos[k] = take((size_t)n_tokens * 4); }
-    L.counts = take((size_t)L.n_tiles * kSortBins * 4);
-    L.partial = take(2 * (size_t)L.n_chunks * dim * 4);
-    L.total = p ? p : 256;
+    L.counts = take((size_t)L.passes * L.n_tiles * kSortBins * 4);
+    L.present = take(((size_t)vocab + 31) / 32 * 4);
+    L.partial = take(2 * (size_t)L.n_chunks * L.partial_stride * 4);
+    L.total = p;
     return L;
 }
 
-template <typename T, typename G>
-cudaError_t run_embed_grad(EmbedArgs k, const EmbedGradLayout &L, uint8_t *ws, bool wide_in, bool wide_out, cudaStream_t st) {
-    cudaError_t rc;
-    if (k.n_tokens) {
-        int bits = 0;
-        while (bits < 32 && (k.vocab >> bits) != 0) ++bits;  // the keys are 0 .. vocab
-        const int passes = (bits + kSortBits - 1) / kSortBits;
-        for (int p = 0; p < passes; ++p) {
-            SortPass s{};
-            s.shift = (uint32_t)(p * kSortBits);
-            s.first = p == 0;
-            s.n_tiles = L.n_tiles;
-            s.counts = reinterpret_cast<uint32_t *>(ws + L.counts);
-            s.keys_in = reinterpret_cast<uint32_t *>(ws + L.keys[(p + 1) & 1]);
-            s.pos_in = reinterpret_cast<uint32_t *>(ws + L.pos[(p + 1) & 1]);
-            s.keys_out = reinterpret_cast<uint32_t *>(ws + L.keys[p & 1]);
-            s.pos_out = reinterpret_cast<uint32_t *>(ws + L.pos[p & 1]);
-            if ((rc = launch(sort_count_kernel, L.n_tiles, kSortThreads, st, 1u, k, s)) != cudaSuccess) return rc;
-            if ((rc = launch(sort_place_kernel, L.n_tiles, kSortThreads, st, 1u, k, s)) != cudaSuccess) return rc;
-            k.keys = s.keys_out;
-            k.pos = s.pos_out;
-        }
+template <int kItems>
+cudaError_t run_sort(EmbedArgs &k, const EmbedGradLayout &L, uint8_t *ws, cudaStream_t st) {
+    SortPass s{};
+    s.n_tiles = L.n_tiles;
+    s.passes = L.passes;
+    s.counts = reinterpret_cast<uint32_t *>(ws + L.counts);
+    cudaError_t rc = launch(sort_count_kernel<kItems>, L.n_tiles, kSortThreads, st, 1u, k, s);
+    for (uint32_t p = 0; p < L.passes && rc == cudaSuccess; ++p) {
+        s.shift = p * kSortBits;
+        s.first = p == 0;
+        s.last = p + 1 == L.passes;
+        s.keys_in = reinterpret_cast<uint32_t *>(ws + L.keys[(p + 1) & 1]);
+        s.pos_in = reinterpret_cast<uint32_t *>(ws + L.pos[(p + 1) & 1]);
+        s.keys_out = reinterpret_cast<uint32_t *>(ws + L.keys[p & 1]);
+        s.pos_out = reinterpret_cast<uint32_t *>(ws + L.pos[p & 1]);
+        rc = launch(sort_place_kernel<kItems>, L.n_tiles, kSortThreads, st, 1u, k, s);
     }
-    if (!k.accumulate && (rc = launch(embed_zero_kernel<G>, (k.vocab + 31ull) / 32, kSumThreads, st, 1u, k, wide_out)) != cudaSuccess) return rc;
-    if (!k.n_tokens) return cudaSuccess;
-    const uint32_t slices = (k.dim + kSumWarpCols - 1) / kSumWarpCols;
-    const uint64_t grid = ((uint64_t)k.n_chunks * slices + kSumThreads / 32 - 1) / (kSumThreads / 32);
-    if ((rc = launch(embed_sum_kernel<T, G>, grid, kSumThreads, st, 1u, k, slices, wide_in, wide_out)) != cudaSuccess) return rc;
-    return launch(embed_join_kernel<G>, grid, kSumThreads, st, 1u, k, slices, wide_out);
+    k.keys = s.keys_out;
+    k.pos = s.pos_out;
+    return rc;
+}
+
+template <typename T, typename G>
+cudaError_t run_embed_grad(EmbedArgs k, const EmbedGradLayout &L, uint8_t *ws, bool wide, cudaStream_t st) {
+    // Rows without a token are cleared one of two ways: all rows, by blocks that run beside the one-block sort, where
+    // that writes few rows twice; or those rows alone, by blocks that run among the sums.
+    const bool clear = !k.accumulate, clear_all = clear && L.small && k.n_tokens <= k.vocab / 8;
+    cudaError_t rc;
+    k.present = clear && !clear_all ? reinterpret_cast<uint32_t *>(ws + L.present) : nullptr;
+    if (L.small) {
+        rc = cudaFuncSetAttribute(sort_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem);
+        if (rc != cudaSuccess) return rc;
+        k.keys = reinterpret_cast<uint32_t *>(ws + L.keys[0]);
+        k.pos = reinterpret_cast<uint32_t *>(ws + L.pos[0]);
+        rc = launch_smem(sort_small_kernel, clear_all ? 148 * 2 : 1, kSmallThreads, kSmallSmem, st, 1u, k, L.passes, (uint32_t)sizeof(G));
+    } else rc = L.big_tiles ? run_sort<16>(k, L, ws, st) : run_sort<4>(k, L, ws, st);
+    if (rc != cudaSuccess) return rc;
+    const uint32_t sum_blocks = (uint32_t)(((uint64_t)L.n_chunks * L.slices + kSumThreads / 32 - 1) / (kSumThreads / 32));
+    const uint32_t zero_blocks = k.present ? (uint32_t)(((uint64_t)k.vocab + 31) / 32) : 0u;
+    if (sum_blocks + zero_blocks)
+        rc = launch(wide ? embed_sum_kernel<T, G, true> : embed_sum_kernel<T, G, false>, (uint64_t)sum_blocks + zero_blocks, kSumThreads, st, 1u, k, L.slices, sum_blocks);
+    if (rc != cudaSuccess || L.n_chunks < 2) return rc;
+    return launch(wide ? embed_join_kernel<G, true> : embed_join_kernel<G, false>, L.n_chunks - 1, kSumThreads, st, 1u, k, L.slices);
 }
 
 }  // namespace
@@ -371,8 +402,7 @@ int td_embed(const td_embed_args *a, void *stream) {
 }
 
 size_t td_embed_grad_workspace_bytes(uint32_t n_tokens, uint32_t vocab, uint32_t dim) {
-    (void)vocab;
-    return n_tokens < kIndexLimit && dim < kIndexLimit ? embed_layout(n_tokens, dim).total : 0;
+    return n_tokens < kIndexLimit && vocab < kIndexLimit && dim < kIndexLimit ? embed_layout(n_tokens, vocab, dim).total : 0;
 }
 
 int td_embed_grad(const td_embed_grad_args *a, void *stream) {
@@ -386,10 +416,9 @@ int td_embed_grad(const td_embed_grad_args *a, void *stream) {
     const uint32_t es = size_of(a->dtype), gs = size_of(a->grad_dtype);
     if (!a->grad_table || !aligned(a->grad_table, gs) || !aligned(a->status, 4)) return TD_EINVAL;
     if (a->n_tokens && (!a->ids || !a->grad_out || !aligned(a->ids, 4) || !aligned(a->grad_out, es))) return TD_EINVAL;
-    const EmbedGradLayout L = embed_layout(a->n_tokens, a->dim);
+    const EmbedGradLayout L = embed_layout(a->n_tokens, a->vocab, a->dim);
     if (!a->workspace || !aligned(a->workspace, 256) || a->workspace_bytes < L.total) return TD_EWORKSPACE;
-    const uint64_t slices = (a->dim + kSumWarpCols - 1) / kSumWarpCols;
-    if (((uint64_t)L.n_chunks * slices) / (kSumThreads / 32) >= kMaxGrid) return TD_EINVAL;
+    if ((uint64_t)L.n_chunks * L.slices + (uint64_t)a->vocab / 32 >= kMaxGrid) return TD_EINVAL;
     DeviceGuard dev(a->device);
     if (!dev.ok()) return TD_ECUDA;
     EmbedArgs k{};
@@ -410,17 +439,19 @@ int td_embed_grad(const td_embed_grad_args *a, void *stream) {
     k.n_chunks = L.n_chunks;
     uint8_t *ws = static_cast<uint8_t *>(a->workspace);
     k.partial = reinterpret_cast<float *>(ws + L.partial);
-    const bool wide_in = aligned(a->grad_out, 16) && a->out_stride * es % 16 == 0;
-    const bool wide_out = aligned(a->grad_table, 16) && a->table_stride * gs % 16 == 0;
+    k.partial_stride = L.partial_stride;
+    // rows of both sides start on 16-byte boundaries and are whole lanes' columns
+    const bool wide = a->dim % kSumCols == 0 && aligned(a->grad_out, 16) && a->out_stride * es % 16 == 0 && aligned(a->grad_table, 16) &&
+                      a->table_stride * gs % 16 == 0;
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t rc;
-    if (a->dtype == TD_F32) rc = run_embed_grad<float, float>(k, L, ws, wide_in, wide_out, st);
+    if (a->dtype == TD_F32) rc = run_embed_grad<float, float>(k, L, ws, wide, st);
     else if (a->dtype == TD_BF16)
-        rc = a->grad_dtype == TD_F32 ? run_embed_grad<__nv_bfloat16, float>(k, L, ws, wide_in, wide_out, st)
-                                     : run_embed_grad<__nv_bfloat16, __nv_bfloat16>(k, L, ws, wide_in, wide_out, st);
+        rc = a->grad_dtype == TD_F32 ? run_embed_grad<__nv_bfloat16, float>(k, L, ws, wide, st)
+                                     : run_embed_grad<__nv_bfloat16, __nv_bfloat16>(k, L, ws, wide, st);
     else
-        rc = a->grad_dtype == TD_F32 ? run_embed_grad<__half, float>(k, L, ws, wide_in, wide_out, st)
-                                     : run_embed_grad<__half, __half>(k, L, ws, wide_in, wide_out, st);
+        rc = a->grad_dtype == TD_F32 ? run_embed_grad<__half, float>(k, L, ws, wide, st)
+                                     : run_embed_grad<__half, __half>(k, L, ws, wide, st);
     return rc == cudaSuccess ? TD_OK : TD_ECUDA;
 }
 

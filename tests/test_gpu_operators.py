@@ -590,13 +590,24 @@ def test_embed_grad(name, gname, tokens, vocab, dim, pad, offset):
         assert torch.equal(first, check_embed_grad(ids, grad, vocab, gname, 0.5, pad, offset, accumulate))
 
 
-@pytest.mark.parametrize("tokens", [31, 32, 33, 64, 1000, 70000])
+@pytest.mark.parametrize("tokens", [7, 8, 9, 31, 32, 33, 64, 1000, 8192, 8193, 70000, 150000])
 def test_embed_grad_one_id_everywhere(tokens):
     """A single run over all chunks; next to it runs that end on chunk borders."""
     grad = table_of(tokens, 24, "bf16", 3)
     check_embed_grad(torch.full((tokens,), 2, dtype=torch.int32, device="cuda"), grad, 5, "f32")
     check_embed_grad((torch.arange(tokens, device="cuda") // 32).int(), grad, tokens // 32 + 1, "f32")
     check_embed_grad((torch.arange(tokens, device="cuda") // 96).flip(0).int(), grad, tokens // 96 + 2, "f32")
+
+
+@pytest.mark.parametrize("tokens,vocab", [(3000, 2 ** 19 + 7), (8192, 150), (20000, 2 ** 18 - 1), (20000, 2 ** 18), (140000, 2 ** 19), (140000, 300)])
+@pytest.mark.parametrize("dim", [8, 5])
+def test_embed_grad_sorts_of_every_size(tokens, vocab, dim):
+    r = np.random.default_rng(tokens)
+    ids = torch.from_numpy((vocab ** r.random(tokens)).astype(np.int32).clip(0, vocab - 1)).cuda()
+    ids[::17] = -1
+    ids[5] = vocab - 1
+    check_embed_grad(ids, table_of(tokens, dim, "bf16", 3), vocab, "f32")
+    check_embed_grad(ids.flip(0), table_of(tokens, dim, "f32", 3), vocab, "f32", scale=-2.0, accumulate=True)
 
 
 def test_embed_grad_of_broadcast_rows_and_wide_vocabularies():
