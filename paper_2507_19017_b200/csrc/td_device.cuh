@@ -26,27 +26,6 @@ enum : int {
     CNT_TOTAL = 112
 };
 
-// Division by a run-time constant d through a multiply and a shift, exact for n < 2^31:
-// n / d = (umulhi(n, mul) + n) >> shr with shr = ceil(log2 d), mul = floor(2^32 (2^shr - d) / d) + 1
-// (mul = 0 when d is a power of two).
-struct FastDiv {
-    uint32_t mul, shr;
-};
-static inline FastDiv make_fastdiv(uint32_t d) {
-    uint32_t l = 0;
-    while ((1ull << l) < d) ++l;
-    const uint64_t m = (1ull << l) == d ? 0 : ((1ull << 32) * ((1ull << l) - d)) / d + 1;
-    return FastDiv{(uint32_t)m, l};
-}
-__device__ __forceinline__ FastDiv make_fastdiv_dev(uint32_t d) {          // the same constants, computed on the device
-    const uint32_t l = d > 1u ? 32u - (uint32_t)__clz(d - 1u) : 0u;
-    const unsigned long long m = (1ull << l) == d ? 0ull : ((1ull << 32) * ((1ull << l) - d)) / d + 1ull;
-    return FastDiv{(uint32_t)m, l};
-}
-__device__ __forceinline__ uint32_t fast_div(uint32_t n, FastDiv f) {
-    return (__umulhi(n, f.mul) + n) >> f.shr;
-}
-
 // Everything a kernel needs to know about a dock; passed by value (constant bank).
 struct DockView {
     uint32_t G, N, S, n;

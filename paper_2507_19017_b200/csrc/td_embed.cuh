@@ -17,7 +17,7 @@ struct EmbedArgs {
     // gradient
     const void *grad_out;
     void *grad_table;
-    uint32_t accumulate;
+    uint32_t accumulate, grad_size;      // bytes of a gradient element
     uint32_t rows_per_chunk;             // sorted positions per chunk of the segment sums
     uint32_t n_chunks;
     uint32_t *keys;                      // [n_tokens] sorted ids; vocab: no token
@@ -25,6 +25,8 @@ struct EmbedArgs {
     uint32_t *present;                   // [ceil(vocab / 32)] a bit per id that occurs, or nullptr
     float *partial;                      // [2][n_chunks][partial_stride]: sums of a run cut by the chunk's start / by its end
     size_t partial_stride;               // dim rounded up to a warp's columns
+    uint32_t *arrived;                   // [n_chunks][slices] parts stored of the cut run that begins in the chunk
+    uint32_t n_arrived, zero_from;       // words of a.present whose rows were cleared before the sums
 };
 
 // Positions that hold a token of the batch.
@@ -50,57 +52,74 @@ __device__ __forceinline__ uint32_t id_at(const EmbedArgs &a, uint32_t t, uint32
     return (uint32_t)id;
 }
 
+// A team of 2^team lanes (4 to 32) per piece of a position's row; a lane moves kEmbedUnroll vectors of 16 bytes, the
+// team's lanes taking turns.  Aligned: rows of both sides start on 16-byte boundaries.  Else the vectors are
+// aligned on the output row and put together from two loads each, and the first piece's lanes move the elements
+// before the first and behind the last vector.
 constexpr int kEmbedThreads = 256, kEmbedUnroll = 4;
-constexpr uint32_t kEmbedVectors = 32 * kEmbedUnroll;        // 16-byte vectors of a row that one warp moves
 
-// A warp per (position, piece of the row).
-template <typename T, bool kWide>
-__global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a, uint32_t pieces) {
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a, uint32_t team, uint32_t pieces) {
     griddep_launch_dependents();
     griddep_wait();
-    const unsigned long long item = (unsigned long long)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5);
-    const unsigned long long t64 = item / pieces;
-    const uint32_t piece = (uint32_t)(item % pieces), lane = threadIdx.x & 31u;
+    constexpr int E = Elem<T>::kVec;
+    const uint32_t lanes = 1u << team, lane = threadIdx.x & (lanes - 1u);
+    unsigned long long t64 = (unsigned long long)blockIdx.x * (kEmbedThreads >> team) + (threadIdx.x >> team);
+    uint32_t piece = 0;
+    if (pieces > 1) {
+        piece = (uint32_t)(t64 % pieces);
+        t64 /= pieces;
+    }
     if (t64 >= a.n_tokens) return;
     const uint32_t t = (uint32_t)t64;
     const uint32_t id = id_at(a, t, tokens_in(a));
     const bool none = id >= a.vocab;
-    constexpr int E = Elem<T>::kVec;
-    const T *row = static_cast<const T *>(a.table) + (long long)(none ? 0 : id) * a.table_stride;
+    const T *table = static_cast<const T *>(a.table), *row = table + (long long)(none ? 0u : id) * a.table_stride;
     T *out = static_cast<T *>(a.out) + (long long)t * a.out_stride;
-    if constexpr (kWide) {
-        const uint32_t nvec = a.dim / E, lo = piece * kEmbedVectors;
-        const uint4 *rv = reinterpret_cast<const uint4 *>(row);
-        uint4 *ov = reinterpret_cast<uint4 *>(out);
-        uint4 v[kEmbedUnroll];
+    const uint32_t head = kAligned ? 0u : min((16u - (uint32_t)(reinterpret_cast<uintptr_t>(out) & 15u)) % 16u / (uint32_t)sizeof(T), a.dim);
+    const uint32_t nvec = (a.dim - head) / E, lo = piece * (kEmbedUnroll << team);
+    uint4 v[kEmbedUnroll];
+    if constexpr (kAligned) {
 #pragma unroll
         for (int u = 0; u < kEmbedUnroll; ++u) {
-            const uint32_t j = lo + u * 32 + lane;
+            const uint32_t j = lo + (u << team) + lane;
             v[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (j < nvec && !none) v[u] = __ldg(rv + j);
-        }
-        const f32x2 sc = pack2(a.scale, a.scale);
-#pragma unroll
-        for (int u = 0; u < kEmbedUnroll; ++u) {
-            const uint32_t j = lo + u * 32 + lane;
-            if (j >= nvec) break;
-            if (!none) {
-#pragma unroll
-                for (int k = 0; k < E / 2; ++k) {
-                    float p, q;
-                    unpack2(mul2(Elem<T>::pair(v[u], k), sc), p, q);
-                    Elem<T>::put_pair(v[u], k, p, q);
-                }
-            }
-            st_stream(ov + j, v[u]);
-        }
-        if (piece == pieces - 1 && lane < a.dim - nvec * E) {        // what does not fill a vector
-            const uint32_t j = nvec * E + lane;
-            out[j] = Elem<T>::from(none ? 0.0f : Elem<T>::load(row + j) * a.scale);
+            if (j < nvec && !none) v[u] = __ldg(reinterpret_cast<const uint4 *>(row) + j);
         }
     } else {
-        const uint32_t lo = piece * kEmbedVectors * E, hi = min(a.dim, lo + kEmbedVectors * E);
-        for (uint32_t j = lo + lane; j < hi; j += 32) out[j] = Elem<T>::from(none ? 0.0f : Elem<T>::load(row + j) * a.scale);
+        const T *end = table + (long long)(a.vocab - 1) * a.table_stride + a.dim;
+        Window<T> w[kEmbedUnroll];
+#pragma unroll
+        for (int u = 0; u < kEmbedUnroll; ++u) {
+            const uint32_t j = lo + (u << team) + lane;
+            if (j < nvec && !none) w[u].open(row + head + j * E, table, end);
+        }
+#pragma unroll
+        for (int u = 0; u < kEmbedUnroll; ++u) {
+            const uint32_t j = lo + (u << team) + lane;
+            v[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (j < nvec && !none) v[u] = w[u].close();
+        }
+    }
+    const f32x2 sc = pack2(a.scale, a.scale);
+#pragma unroll
+    for (int u = 0; u < kEmbedUnroll; ++u) {
+        const uint32_t j = lo + (u << team) + lane;
+        if (j >= nvec) break;
+#pragma unroll
+        for (int k = 0; k < E / 2; ++k) {
+            float p, q;
+            unpack2(mul2(Elem<T>::pair(v[u], k), sc), p, q);
+            Elem<T>::put_pair(v[u], k, p, q);
+        }
+        st_stream(out + head + j * E, v[u]);
+    }
+    if (piece == 0) {
+        const uint32_t tail = head + nvec * E, loose = head + (a.dim - tail);
+        for (uint32_t i = lane; i < loose; i += lanes) {
+            const uint32_t j = i < head ? i : tail + i - head;
+            out[j] = Elem<T>::from(none ? 0.0f : Elem<T>::load(row + j) * a.scale);
+        }
     }
 }
 
@@ -155,19 +174,27 @@ __device__ __forceinline__ void fill_zero(uint8_t *p, size_t bytes, size_t i, si
     if (i < (bytes - tail) / 2) reinterpret_cast<uint16_t *>(p + tail)[i] = 0;
 }
 
+// Rows of the gradient table whose bit in a.present is not set, 32 per block.
+__device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t word) {
+    const uint32_t bits = a.present[word], lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    for (uint32_t k = warp; k < 32 && word * 32 + k < a.vocab; k += blockDim.x >> 5)
+        if (!((bits >> k) & 1u))
+            fill_zero(static_cast<uint8_t *>(a.grad_table) + (size_t)(word * 32 + k) * a.table_stride * a.grad_size, (size_t)a.dim * a.grad_size, lane, 32);
+}
+
 // One block sorts everything: up to 8192 positions, in shared memory.  Blocks beyond the first clear the gradient
 // table meanwhile, where the launch has such blocks.
 constexpr int kSmallThreads = 1024, kSmallItems = 8, kSmallWarps = kSmallThreads / 32;
 constexpr uint32_t kSmallMax = kSmallThreads * kSmallItems;
 constexpr size_t kSmallSmem = (size_t)kSmallWarps * kSortBins * 2 + kSmallMax * (4 + 2) + 64;
 
-__global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedArgs a, uint32_t passes, uint32_t grad_size) {
+__global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedArgs a, uint32_t passes) {
     griddep_launch_dependents();
     griddep_wait();
     if (blockIdx.x > 0) {
         const size_t i = (size_t)(blockIdx.x - 1) * kSmallThreads + threadIdx.x, n = (size_t)(gridDim.x - 1) * kSmallThreads;
         uint8_t *t = static_cast<uint8_t *>(a.grad_table);
-        const size_t row = (size_t)a.dim * grad_size, stride = (size_t)a.table_stride * grad_size;
+        const size_t row = (size_t)a.dim * a.grad_size, stride = (size_t)a.table_stride * a.grad_size;
         if (row == stride) return fill_zero(t, row * a.vocab, i, n);
         const size_t warp = i / 32, warps = n / 32, lane = threadIdx.x & 31u;
         for (size_t v = warp; v < a.vocab; v += warps) fill_zero(t + v * stride, row, lane, 32);
@@ -180,6 +207,7 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedAr
     uint32_t *warp_sum = reinterpret_cast<uint32_t *>(pos + kSmallMax);
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t n = tokens_in(a), items = (a.n_tokens + kSmallThreads - 1) / kSmallThreads, base = warp * items * 32 + lane;
+    for (uint32_t w = threadIdx.x; w < a.n_arrived; w += kSmallThreads) a.arrived[w] = 0u;
     if (a.present) {
         for (uint32_t w = threadIdx.x; w < (a.vocab + 31) / 32; w += kSmallThreads) a.present[w] = 0u;
         __syncthreads();
@@ -238,7 +266,8 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedAr
 }
 
 // More positions: tiles of kSortThreads * kItems entries.  A counting kernel for the first digit, then one
-// placing kernel per digit, which counts the next digit where its entries go.
+// placing kernel per digit, which counts the next digit where its entries go.  Blocks beyond the tiles clear the
+// first rows without a token, where the last of several placing kernels has such blocks.
 constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
 static_assert(kSortBins == kSortThreads, "one thread per bin");
 
@@ -269,6 +298,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const EmbedArg
     for (uint32_t p = 1; p < s.passes; ++p) s.counts[((size_t)p * s.n_tiles + blockIdx.x) * kSortBins + threadIdx.x] = 0u;
     if (a.present)
         for (uint32_t w = blockIdx.x * kSortThreads + threadIdx.x; w < (a.vocab + 31) / 32; w += gridDim.x * kSortThreads) a.present[w] = 0u;
+    for (uint32_t w = blockIdx.x * kSortThreads + threadIdx.x; w < a.n_arrived; w += gridDim.x * kSortThreads) a.arrived[w] = 0u;
 }
 
 template <int kItems>
@@ -277,6 +307,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const EmbedArg
     griddep_wait();
     __shared__ uint32_t warp_bins[kSortWarps][kSortBins];
     __shared__ uint32_t warp_sum[kSortBins / 32];
+    if (blockIdx.x >= s.n_tiles) return zero_rows(a, blockIdx.x - s.n_tiles);
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t pass = s.shift / kSortBits;
     // a warp owns kItems * 32 consecutive entries of the tile
@@ -322,219 +353,263 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const EmbedArg
 }
 
 // ---- sums over the runs of equal ids ----
-// kSumCols columns of a row per lane, kSumWarpCols per warp.  Wide: a lane's columns are consecutive, moved
-// 16 bytes at a time; else the warp's lanes take turns, element by element.
-constexpr int kSumThreads = 256, kSumCols = 8;
+// A warp adds up kSumWarpCols columns of rows, kSumCols per lane, and keeps kSumAhead rows on their way through
+// shared memory.
+//   kWide: rows start on 16-byte boundaries and are whole lanes' columns; a lane copies and reads its own
+//     consecutive columns.
+//   else: the aligned 16-byte pieces that cover the warp's columns are copied, and a lane reads pairs of columns, 64 apart,
+//     from wherever in them the row begins; written rows go through shared memory too, to leave in vectors
+//     aligned on the row.
+constexpr int kSumThreads = 256, kSumWarps = kSumThreads / 32, kSumCols = 8, kSumPairs = kSumCols / 2;
 constexpr uint32_t kSumWarpCols = 32 * kSumCols;
 
 template <typename T, bool kWide>
-struct Columns {
-    static constexpr int kVecs = kWide ? kSumCols / Elem<T>::kVec : 0;
-    uint4 v[kWide ? kVecs : 1];
-    float x[kWide ? 1 : kSumCols];
-    // row: the warp's first column; n: columns of the row from there on
-    __device__ __forceinline__ void load(const T *row, uint32_t lane, uint32_t n, bool on) {
-        if constexpr (kWide) {
-#pragma unroll
-            for (int q = 0; q < kVecs; ++q) {
-                v[q] = make_uint4(0u, 0u, 0u, 0u);
-                if (on && lane * kSumCols < n) v[q] = *reinterpret_cast<const uint4 *>(row + lane * kSumCols + q * Elem<T>::kVec);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < kSumCols; ++j) x[j] = on && j * 32 + lane < n ? Elem<T>::load(row + j * 32 + lane) : 0.0f;
-        }
-    }
-    __device__ __forceinline__ void add_to(f32x2 (&sum)[kSumCols / 2]) const {
-        if constexpr (kWide) {
-#pragma unroll
-            for (int q = 0; q < kVecs; ++q)
-#pragma unroll
-                for (int k = 0; k < Elem<T>::kVec / 2; ++k) sum[q * Elem<T>::kVec / 2 + k] = add2(sum[q * Elem<T>::kVec / 2 + k], Elem<T>::pair(v[q], k));
-        } else {
-#pragma unroll
-            for (int k = 0; k < kSumCols / 2; ++k) sum[k] = add2(sum[k], pack2(x[2 * k], x[2 * k + 1]));
-        }
-    }
-    static __device__ __forceinline__ void store(T *row, const f32x2 (&sum)[kSumCols / 2], uint32_t lane, uint32_t n) {
-        if constexpr (kWide) {
-            if (lane * kSumCols >= n) return;
-#pragma unroll
-            for (int q = 0; q < kVecs; ++q) {
-                uint4 o;
-#pragma unroll
-                for (int k = 0; k < Elem<T>::kVec / 2; ++k) {
-                    float a, b;
-                    unpack2(sum[q * Elem<T>::kVec / 2 + k], a, b);
-                    Elem<T>::put_pair(o, k, a, b);
-                }
-                st_stream(row + lane * kSumCols + q * Elem<T>::kVec, o);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < kSumCols / 2; ++k) {
-                float a, b;
-                unpack2(sum[k], a, b);
-                if (2 * k * 32 + lane < n) row[2 * k * 32 + lane] = Elem<T>::from(a);
-                if ((2 * k + 1) * 32 + lane < n) row[(2 * k + 1) * 32 + lane] = Elem<T>::from(b);
-            }
-        }
-    }
+struct SumLayout {
+    static constexpr int kAhead = sizeof(T) == 2 ? 8 : 4;
+    static constexpr uint32_t kSlot = kSumWarpCols * sizeof(T) + (kWide ? 0 : 16);
+    static constexpr uint32_t kStage = kWide ? 0 : (kSumWarpCols + kSumWarpCols / 32) * 4;     // a word of padding per 32: lanes 8 apart in different banks
+    static constexpr uint32_t kWarpBytes = kAhead * kSlot + kStage;
 };
-
-// scale * sum to row v of the gradient table, or added to what is there
-template <typename G, bool kWide>
-__device__ __forceinline__ void write_row(const EmbedArgs &a, uint32_t v, const f32x2 (&sum)[kSumCols / 2], uint32_t c0, uint32_t lane) {
-    G *row = static_cast<G *>(a.grad_table) + (long long)v * a.table_stride + c0;
-    f32x2 x[kSumCols / 2];
-    const f32x2 sc = pack2(a.scale, a.scale);
-#pragma unroll
-    for (int k = 0; k < kSumCols / 2; ++k) x[k] = mul2(sum[k], sc);
-    if (a.accumulate) {
-        Columns<G, kWide> old;
-        old.load(row, lane, a.dim - c0, true);
-        old.add_to(x);
-    }
-    Columns<G, kWide>::store(row, x, lane, a.dim - c0);
+// column of a lane's pair k, from the warp's first
+template <bool kWide>
+__device__ __forceinline__ uint32_t pair_column(int k) {
+    const uint32_t lane = threadIdx.x & 31u;
+    return kWide ? lane * kSumCols + 2 * k : 64 * k + 2 * lane;
 }
 
+// A row's columns [c0, c0 + cols) on their way into a slot; the row lies in [begin, end).
+template <typename T, bool kWide>
+__device__ __forceinline__ void fetch_row(uint8_t *slot, const T *row, uint32_t c0, uint32_t cols, const T *begin, const T *end) {
+    const uint32_t lane = threadIdx.x & 31u;
+    constexpr uint32_t E = Elem<T>::kVec;
+    if constexpr (kWide) {
+        if (lane * kSumCols >= cols) return;
+#pragma unroll
+        for (uint32_t q = 0; q < kSumCols / E; ++q) copy_async<16>(slot + (lane * kSumCols + q * E) * sizeof(T), row + c0 + lane * kSumCols + q * E);
+    } else {
+        const T *from = row + c0;
+        const uint32_t skew = (uint32_t)(reinterpret_cast<uintptr_t>(from) & 15u) / (uint32_t)sizeof(T), pieces = (skew + cols + E - 1) / E;
+        for (uint32_t i = lane; i < pieces; i += 32) {
+            const T *at = from - skew + i * E;
+            if (at >= begin && at + E <= end) copy_async<16>(slot + i * 16, at);
+            else                                             // a piece that reaches over an end of the array
+                for (uint32_t k = 0; k < E; ++k)
+                    if (at + k >= begin && at + k < end) reinterpret_cast<T *>(slot + i * 16)[k] = at[k];
+        }
+    }
+}
+template <typename T, bool kWide>
+__device__ __forceinline__ void add_row(f32x2 (&sum)[kSumPairs], const uint8_t *slot, const T *from) {
+    const uint32_t lane = threadIdx.x & 31u;
+    constexpr int E = Elem<T>::kVec;
+    if constexpr (kWide) {
+#pragma unroll
+        for (int q = 0; q < kSumCols / E; ++q) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(slot + (lane * kSumCols + q * E) * sizeof(T));
+#pragma unroll
+            for (int k = 0; k < E / 2; ++k) sum[q * E / 2 + k] = add2(sum[q * E / 2 + k], Elem<T>::pair(v, k));
+        }
+    } else {
+        const uint32_t skew = (uint32_t)(reinterpret_cast<uintptr_t>(from) & 15u);          // bytes
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(slot + (skew & ~3u));
+#pragma unroll
+        for (int k = 0; k < kSumPairs; ++k) {
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if constexpr (sizeof(T) == 4) {
+                v.x = w[64 * k + 2 * lane];
+                v.y = w[64 * k + 2 * lane + 1];
+            } else if (skew & 2u) v.x = __funnelshift_r(w[32 * k + lane], w[32 * k + lane + 1], 16);
+            else v.x = w[32 * k + lane];
+            sum[k] = add2(sum[k], Elem<T>::pair(v, 0));
+        }
+    }
+}
+
+// scale * sum to columns [c0, c0 + cols) of row v of the gradient table, or added to what is there.
+template <typename G, bool kWide>
+__device__ __forceinline__ void write_row(const EmbedArgs &a, uint32_t v, const f32x2 (&sum)[kSumPairs], uint32_t c0, uint32_t cols, float *stage) {
+    G *out = static_cast<G *>(a.grad_table) + (long long)v * a.table_stride + c0;
+    const uint32_t lane = threadIdx.x & 31u;
+    constexpr uint32_t E = Elem<G>::kVec;
+    float x[kSumCols];
+#pragma unroll
+    for (int k = 0; k < kSumPairs; ++k) {
+        const uint32_t c = pair_column<kWide>(k);
+        unpack2(mul2(sum[k], pack2(a.scale, a.scale)), x[2 * k], x[2 * k + 1]);
+        if (a.accumulate) {
+            if (c < cols) x[2 * k] += Elem<G>::load(out + c);
+            if (c + 1 < cols) x[2 * k + 1] += Elem<G>::load(out + c + 1);
+        }
+    }
+    if constexpr (kWide) {
+        if (lane * kSumCols >= cols) return;
+#pragma unroll
+        for (uint32_t q = 0; q < kSumCols / E; ++q) {
+            uint4 o;
+#pragma unroll
+            for (uint32_t k = 0; k < E / 2; ++k) Elem<G>::put_pair(o, k, x[q * E + 2 * k], x[q * E + 2 * k + 1]);
+            st_stream(out + lane * kSumCols + q * E, o);
+        }
+    } else {
+        auto at = [](uint32_t c) { return c + c / 32; };
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < kSumPairs; ++k) {
+            stage[at(pair_column<false>(k))] = x[2 * k];
+            stage[at(pair_column<false>(k) + 1)] = x[2 * k + 1];
+        }
+        __syncwarp();
+        const uint32_t head = min((16u - (uint32_t)(reinterpret_cast<uintptr_t>(out) & 15u)) % 16u / (uint32_t)sizeof(G), cols), nvec = (cols - head) / E;
+        for (uint32_t j = lane; j < nvec; j += 32) {
+            uint4 o;
+#pragma unroll
+            for (uint32_t k = 0; k < E / 2; ++k) Elem<G>::put_pair(o, k, stage[at(head + j * E + 2 * k)], stage[at(head + j * E + 2 * k + 1)]);
+            st_stream(out + head + j * E, o);
+        }
+        const uint32_t tail = head + nvec * E;
+        if (lane < head) out[lane] = Elem<G>::from(stage[at(lane)]);
+        if (lane < cols - tail) out[tail + lane] = Elem<G>::from(stage[at(tail + lane)]);
+    }
+}
+
+// Sums of a run's part: which = 0 cut by the chunk's start, 1 by its end.  A row has room for whole warps' columns.
 __device__ __forceinline__ float *partial_row(const EmbedArgs &a, uint32_t which, uint32_t chunk) {
     return a.partial + ((size_t)which * a.n_chunks + chunk) * a.partial_stride;
 }
 
-// Rows of the gradient table whose bit in a.present is not set, 32 per block.
-template <typename G>
-__device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t word) {
-    const uint32_t bits = a.present[word], lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    for (uint32_t k = warp; k < 32 && word * 32 + k < a.vocab; k += kSumThreads / 32)
-        if (!((bits >> k) & 1u))
-            fill_zero(reinterpret_cast<uint8_t *>(static_cast<G *>(a.grad_table) + (long long)(word * 32 + k) * a.table_stride), (size_t)a.dim * sizeof(G), lane, 32);
+// The parts of a run that chunk borders cut, of which this warp has just stored one (run v; cont: it began before
+// `chunk`): whichever warp stores the last one adds them up, in the order of the chunks.  True for that warp.
+template <bool kWide>
+__device__ __noinline__ bool join_run(const EmbedArgs &a, uint32_t v, uint32_t chunk, bool cont, uint32_t slice, uint32_t slices, f32x2 (&sum)[kSumPairs]) {
+    const uint32_t lane = threadIdx.x & 31u, c0 = slice * kSumWarpCols;
+    // chunks that continue the run: behind this one (those that begin with v), and before it back to the one
+    // it begins in (the last whose predecessor does not end with v)
+    uint32_t behind = 0, back = 0;
+    for (;;) {
+        const unsigned long long c = (unsigned long long)chunk + 1 + behind + lane;
+        const uint32_t same = __ballot_sync(kFullMask, c < a.n_chunks && __ldg(a.keys + c * a.rows_per_chunk) == v);
+        if (same != kFullMask) { behind += __ffs(~same) - 1; break; }
+        behind += 32;
+    }
+    if (cont)
+        for (;;) {
+            const long long c = (long long)chunk - 1 - back - lane;
+            const uint32_t same = __ballot_sync(kFullMask, c > 0 && __ldg(a.keys + (size_t)c * a.rows_per_chunk - 1) == v);
+            if (same != kFullMask) { back += __ffs(~same); break; }
+            back += 32;
+        }
+    const uint32_t owner = chunk - back, parts = back + behind;      // `parts` partial 0, and the owner's partial 1
+    __threadfence();
+    __syncwarp();
+    uint32_t before = 0;
+    if (lane == 0) before = atomicAdd(a.arrived + (size_t)owner * slices + slice, 1u);
+    if (__shfl_sync(kFullMask, before, 0) != parts) return false;
+    __threadfence();
+    constexpr uint32_t kAhead = 8;
+    for (uint32_t p = 0; p <= parts; p += kAhead) {
+        float2 x[kAhead][kSumPairs];
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u) {
+            const uint32_t q = min(p + u, parts);
+            const float *from = (q ? partial_row(a, 0, owner + q) : partial_row(a, 1, owner)) + c0;
+#pragma unroll
+            for (int k = 0; k < kSumPairs; ++k) x[u][k] = __ldcg(reinterpret_cast<const float2 *>(from + pair_column<kWide>(k)));
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u) {
+            if (p + u > parts) break;
+#pragma unroll
+            for (int k = 0; k < kSumPairs; ++k) {
+                const f32x2 y = pack2(x[u][k].x, x[u][k].y);
+                sum[k] = p + u ? add2(sum[k], y) : y;
+            }
+        }
+    }
+    return true;
 }
 
 // A warp per (chunk of sorted positions, 256 columns).  A run that lies inside the chunk is written out; the part of
 // a run that began in an earlier chunk goes to partial 0, the part of one that began here and goes on to
-// partial 1.  Spread among the blocks that do this, as many as a.present has words clear rows without a token.
+// partial 1, and the last part to arrive writes the run out.  Spread among the blocks that do this, as many as
+// a.present has words left clear rows without a token.
 template <typename T, typename G, bool kWide>
-__global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const EmbedArgs a, uint32_t slices, uint32_t sum_blocks) {
+__global__ void __launch_bounds__(kSumThreads, 4) embed_sum_kernel(const __grid_constant__ EmbedArgs a, uint32_t slices, uint32_t sum_blocks) {
     griddep_launch_dependents();
     griddep_wait();
     const uint32_t sums_before = (uint32_t)((unsigned long long)blockIdx.x * sum_blocks / gridDim.x);
     if ((uint32_t)((unsigned long long)(blockIdx.x + 1ull) * sum_blocks / gridDim.x) == sums_before)
-        return zero_rows<G>(a, blockIdx.x - sums_before);
-    const unsigned long long item = (unsigned long long)sums_before * (kSumThreads / 32) + (threadIdx.x >> 5);
+        return zero_rows(a, blockIdx.x - sums_before + a.zero_from);
+    using Layout = SumLayout<T, kWide>;
+    constexpr int kAhead = Layout::kAhead;
+    extern __shared__ __align__(16) uint8_t sum_smem[];
+    uint8_t *ring = sum_smem + (threadIdx.x >> 5) * Layout::kWarpBytes;
+    float *stage = reinterpret_cast<float *>(ring + kAhead * Layout::kSlot);
+    const unsigned long long item = (unsigned long long)sums_before * kSumWarps + (threadIdx.x >> 5);
     const unsigned long long chunk64 = item / slices;
     if (chunk64 >= a.n_chunks) return;
-    const uint32_t chunk = (uint32_t)chunk64, lane = threadIdx.x & 31u;
-    const uint32_t c0 = (uint32_t)(item % slices) * kSumWarpCols, cols = a.dim - c0;
-    const uint32_t lo = chunk * a.rows_per_chunk, hi = min(a.n_tokens, lo + a.rows_per_chunk);
-    const uint32_t first = a.keys[lo];
-    if (first >= a.vocab) return;                            // sorted behind all ids
-    bool cont = lo > 0 && a.keys[lo - 1] == first;
-    f32x2 sum[kSumCols / 2];
+    const uint32_t chunk = (uint32_t)chunk64, slice = (uint32_t)(item % slices), lane = threadIdx.x & 31u;
+    const uint32_t c0 = slice * kSumWarpCols, cols = min(a.dim - c0, kSumWarpCols);
+    const uint32_t lo = chunk * a.rows_per_chunk, n = min(a.n_tokens - lo, a.rows_per_chunk);
+    const T *in = static_cast<const T *>(a.grad_out), *in_end = in + (long long)(a.n_tokens - 1) * a.out_stride + a.dim;
+
+    // keys and positions, 32 entries at a time; the rows' fetching runs kAhead entries ahead of their adding
+    const uint32_t *keys = a.keys + lo, *pos = a.pos + lo;
+    auto batch = [&](const uint32_t *p, uint32_t b, uint32_t none) { return b + lane < n ? __ldg(p + b + lane) : none; };
+    uint32_t my_key = batch(keys, 0, a.vocab), my_pos = batch(pos, 0, 0u), next_key = 0, next_pos = 0;
+    const uint32_t before = lo > 0 ? __ldg(keys - 1) : a.vocab, after = lo + n < a.n_tokens ? __ldg(keys + n) : a.vocab;
+    uint32_t v = __shfl_sync(kFullMask, my_key, 0);
+    if (v >= a.vocab) return;                                // sorted behind all ids
+    bool cont = before == v;
+    uint32_t fetch_pos = my_pos, fetch_key = my_key;         // the batch that is being fetched from
+    auto issue = [&](uint32_t f, uint32_t slot) {
+        if (f < n) {
+            if (f && (f & 31u) == 0) { fetch_key = next_key; fetch_pos = next_pos; }
+            const uint32_t key = __shfl_sync(kFullMask, fetch_key, f & 31u), p = __shfl_sync(kFullMask, fetch_pos, f & 31u);
+            if ((f & 31u) == 0) { next_key = batch(keys, f + 32, a.vocab); next_pos = batch(pos, f + 32, 0u); }
+            if (key < a.vocab) fetch_row<T, kWide>(ring + slot * Layout::kSlot, in + (long long)p * a.out_stride, c0, cols, in, in_end);
+        }
+        copy_commit();
+    };
+#pragma unroll 1
+    for (int k = 0; k < kAhead; ++k) issue(k, k);
+    f32x2 sum[kSumPairs];
     auto clear = [&]() {
 #pragma unroll
-        for (int k = 0; k < kSumCols / 2; ++k) sum[k] = pack2(0.0f, 0.0f);
+        for (int k = 0; k < kSumPairs; ++k) sum[k] = pack2(0.0f, 0.0f);
     };
     clear();
-    uint32_t v = first;
-    const T *in = static_cast<const T *>(a.grad_out) + c0;
-    constexpr int kRows = kWide && sizeof(T) == 2 ? 8 : 4;   // rows on their way at a time
-    for (uint32_t e0 = lo; e0 < hi; e0 += 32) {
-        const uint32_t left = min(hi - e0, 32u);
-        const uint32_t my_key = lane < left ? a.keys[e0 + lane] : a.vocab, my_pos = lane < left ? a.pos[e0 + lane] : 0u;
-        for (uint32_t k0 = 0; k0 < left; k0 += kRows) {
-            Columns<T, kWide> x[kRows];
+    uint32_t slot = 0;
+#pragma unroll 1
+    for (uint32_t e = 0;; ++e) {
+        if (e && (e & 31u) == 0 && e < n) { my_key = batch(keys, e, a.vocab); my_pos = batch(pos, e, 0u); }
+        const uint32_t key = e < n ? __shfl_sync(kFullMask, my_key, e & 31u) : a.vocab;
+        if (key != v || e == n) {                            // the run of v ends, or the chunk does
+            const bool goes_on = e == n && after == v;
+            bool whole = true;
+            if (cont || goes_on) {
+                float *to = partial_row(a, cont ? 0u : 1u, chunk) + c0;
 #pragma unroll
-            for (int u = 0; u < kRows; ++u) {
-                const uint32_t key = __shfl_sync(kFullMask, my_key, k0 + u), p = __shfl_sync(kFullMask, my_pos, k0 + u);
-                x[u].load(in + (long long)p * a.out_stride, lane, cols, key < a.vocab);
-            }
-#pragma unroll
-            for (int u = 0; u < kRows; ++u) {
-                const uint32_t key = __shfl_sync(kFullMask, my_key, k0 + u);
-                if (k0 + u >= left) break;
-                if (key != v) {                              // the run of v ends here
-                    if (v < a.vocab) {
-                        if (cont) Columns<float, kWide>::store(partial_row(a, 0, chunk) + c0, sum, lane, cols);
-                        else write_row<G, kWide>(a, v, sum, c0, lane);
-                    }
-                    cont = false;
-                    v = key;
-                    clear();
+                for (int k = 0; k < kSumPairs; ++k) {
+                    float x, y;
+                    unpack2(sum[k], x, y);
+                    __stcg(reinterpret_cast<float2 *>(to + pair_column<kWide>(k)), make_float2(x, y));
                 }
-                x[u].add_to(sum);
+                whole = join_run<kWide>(a, v, chunk, cont, slice, slices, sum);
             }
+            if (whole) write_row<G, kWide>(a, v, sum, c0, cols, stage);
+            if (key >= a.vocab) break;                       // the chunk's end, or positions without a token
+            cont = false;
+            v = key;
+            clear();
         }
+        copy_wait<kAhead - 1>();
+        if (!kWide) __syncwarp();
+        add_row<T, kWide>(sum, ring + slot * Layout::kSlot, in + (long long)__shfl_sync(kFullMask, my_pos, e & 31u) * a.out_stride + c0);
+        if (!kWide) __syncwarp();
+        issue(e + kAhead, slot);
+        slot = slot + 1 == kAhead ? 0 : slot + 1;
     }
-    if (v >= a.vocab) return;
-    const bool goes_on = hi < a.n_tokens && a.keys[hi] == v;
-    if (cont) Columns<float, kWide>::store(partial_row(a, 0, chunk) + c0, sum, lane, cols);
-    else if (goes_on) Columns<float, kWide>::store(partial_row(a, 1, chunk) + c0, sum, lane, cols);
-    else write_row<G, kWide>(a, v, sum, c0, lane);
-}
-
-// Runs that chunk borders cut: the block of the chunk a run begins in adds the parts up.  Up to kJoinAlone parts one
-// warp adds in order, a slice of columns each; more are cut into one piece per warp, and the pieces' sums added
-// in order.
-constexpr uint32_t kJoinAlone = 8;
-template <typename G, bool kWide>
-__global__ void __launch_bounds__(kSumThreads) embed_join_kernel(const EmbedArgs a, uint32_t slices) {
-    griddep_launch_dependents();
-    griddep_wait();
-    constexpr uint32_t kWarps = kSumThreads / 32;
-    __shared__ f32x2 piece[kWarps][kSumCols / 2][32];
-    const uint32_t chunk = blockIdx.x, lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    const uint32_t lo = chunk * a.rows_per_chunk;
-    const unsigned long long hi = (unsigned long long)lo + a.rows_per_chunk;
-    if (hi >= a.n_tokens) return;
-    const uint32_t v = a.keys[hi - 1];
-    if (v >= a.vocab || a.keys[hi] != v || (lo > 0 && a.keys[lo - 1] == v)) return;      // ends here, or began earlier
-    // chunks behind this one that begin with v
-    uint32_t parts = 0;
-    for (;;) {
-        const unsigned long long c = (unsigned long long)chunk + 1 + parts + lane;
-        const uint32_t same = __ballot_sync(kFullMask, c < a.n_chunks && a.keys[c * a.rows_per_chunk] == v);
-        if (same == kFullMask) { parts += 32; continue; }
-        parts += __ffs(~same) - 1;
-        break;
-    }
-    auto add_parts = [&](f32x2 (&sum)[kSumCols / 2], uint32_t from, uint32_t to, uint32_t c0) {
-        for (uint32_t p = from; p < to; p += 4) {
-            Columns<float, kWide> x[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) x[u].load(partial_row(a, 0, chunk + 1 + min(p + u, to - 1)) + c0, lane, a.dim - c0, p + u < to);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) x[u].add_to(sum);
-        }
-    };
-    const bool alone = parts <= kJoinAlone;
-    for (uint32_t s = alone ? warp : 0; s < slices; s += alone ? kWarps : 1) {
-        const uint32_t c0 = s * kSumWarpCols;
-        f32x2 sum[kSumCols / 2];
-#pragma unroll
-        for (int k = 0; k < kSumCols / 2; ++k) sum[k] = pack2(0.0f, 0.0f);
-        if (alone || warp == 0) {
-            Columns<float, kWide> x;
-            x.load(partial_row(a, 1, chunk) + c0, lane, a.dim - c0, true);
-            x.add_to(sum);
-        }
-        if (alone) {
-            add_parts(sum, 0, parts, c0);
-            write_row<G, kWide>(a, v, sum, c0, lane);
-            continue;
-        }
-        add_parts(sum, (uint32_t)((unsigned long long)parts * warp / kWarps), (uint32_t)((unsigned long long)parts * (warp + 1) / kWarps), c0);
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kSumCols / 2; ++k) piece[warp][k][lane] = sum[k];
-        __syncthreads();
-        if (warp == 0) {
-            for (uint32_t w = 1; w < kWarps; ++w)
-#pragma unroll
-                for (int k = 0; k < kSumCols / 2; ++k) sum[k] = add2(sum[k], piece[w][k][lane]);
-            write_row<G, kWide>(a, v, sum, c0, lane);
-        }
-    }
+    copy_wait<0>();                                          // nothing of this warp's is still on its way
 }
 
 }  // namespace td

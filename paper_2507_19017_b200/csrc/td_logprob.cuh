@@ -291,9 +291,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprob_kerne
 constexpr int kGradThreads = 256, kGradUnroll = 4;
 constexpr uint32_t kGradVectors = kGradThreads * kGradUnroll * 4;        // vectors of a row per block
 
-// One block per (row, chunk of the row).
-template <typename T>
-__global__ void __launch_bounds__(kGradThreads, 4) token_logprob_grad_kernel(const LogprobArgs a) {
+// One block per (row, chunk of the row).  kSame: a row of logits and its gradient's start at the same offset
+// from a 16-byte boundary; else the logits' vectors are put together from two loads each.
+template <typename T, bool kSame>
+__global__ void __launch_bounds__(kGradThreads, kSame ? 4 : 3) token_logprob_grad_kernel(const LogprobArgs a) {
     griddep_launch_dependents();
     griddep_wait();
     const uint32_t chunk = blockIdx.x % a.chunks;
@@ -331,11 +332,9 @@ __global__ void __launch_bounds__(kGradThreads, 4) token_logprob_grad_kernel(con
         cb = -h * kLn2 * a.inv_tau;
         if ((g == 0.0f && h == 0.0f) || m == -CUDART_INF_F) y = -1;
     }
-    const uint32_t phase_x = (uint32_t)(reinterpret_cast<uintptr_t>(x) & 15u), phase_o = (uint32_t)(reinterpret_cast<uintptr_t>(out) & 15u);
     const bool zero = y < 0;
-    const bool wide = zero || phase_x == phase_o;
-    // where the row's vectors start, by the place it is written to
-    const uint32_t head = wide ? min(((16u - phase_o) & 15u) / (uint32_t)sizeof(T), a.vocab) : 0u;
+    // the row's vectors are aligned on the place it is written to
+    const uint32_t head = min((16u - (uint32_t)(reinterpret_cast<uintptr_t>(out) & 15u)) % 16u / (uint32_t)sizeof(T), a.vocab);
     const uint32_t nvec = (a.vocab - head) / E;
     const uint32_t lo = chunk * kGradVectors, hi = min(nvec, lo + kGradVectors);
     const float gy = g * a.inv_tau;
@@ -356,19 +355,24 @@ __global__ void __launch_bounds__(kGradThreads, 4) token_logprob_grad_kernel(con
         for (uint32_t i = lo + threadIdx.x; i < hi; i += kGradThreads) st_stream(ov + i, z);
         return;
     }
-    if (!wide) {                                             // logits and gradient rows at different phases: element by element
-        const uint32_t end = min(nvec * E, hi * E);
-        for (uint32_t v = lo * E + threadIdx.x; v < end; v += kGradThreads) out[v] = Elem<T>::from(value(Elem<T>::load(x + v), v));
-        return;
-    }
-    const uint4 *xv = reinterpret_cast<const uint4 *>(x + head);
+    const T *xh = x + head, *begin = static_cast<const T *>(a.logits), *end = begin + (long long)(a.n_rows - 1) * a.stride + a.vocab;
     const uint32_t y_vec = (uint32_t)y >= head ? ((uint32_t)y - head) / E : 0xffffffffu, y_in = ((uint32_t)y - head) % E;
     const f32x2 neg = pack2(-m, -m), sc = pack2(a.scale2, a.scale2), off = pack2(-log2_s, -log2_s), c0 = pack2(ca, ca), c1 = pack2(cb, cb);
     for (uint32_t i = lo + threadIdx.x; i < hi; i += kGradThreads * U) {
         uint4 v[U];
+        if constexpr (kSame) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i + u * kGradThreads < hi) v[u] = ld_stream(xv + i + u * kGradThreads);
+            for (int u = 0; u < U; ++u)
+                if (i + u * kGradThreads < hi) v[u] = ld_stream(xh + (size_t)(i + u * kGradThreads) * E);
+        } else {
+            Window<T> w[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * kGradThreads < hi) w[u].open(xh + (size_t)(i + u * kGradThreads) * E, begin, end);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * kGradThreads < hi) v[u] = w[u].close();
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint32_t j = i + u * kGradThreads;

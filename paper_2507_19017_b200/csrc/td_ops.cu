@@ -51,15 +51,16 @@ cudaError_t launch_smem(void (*kernel)(KArgs...), uint64_t grid, uint32_t block,
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+#ifndef TD_NO_PDL
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+#endif
     if (cluster > 1) {
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = cluster;
-        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-        cfg.numAttrs = 2;
+        attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        attr[cfg.numAttrs].val.clusterDim.x = cluster;
+        attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+        ++cfg.numAttrs;
     }
     return cudaLaunchKernelEx(&cfg, kernel, KArgs(std::forward<Args>(args))...);
 }
@@ -134,7 +135,9 @@ cudaError_t run_logprob(const LogprobArgs &k, cudaStream_t st) {
 }
 template <typename T>
 cudaError_t run_logprob_grad(const LogprobArgs &k, cudaStream_t st) {
-    return launch(token_logprob_grad_kernel<T>, (uint64_t)k.n_rows * k.chunks, kGradThreads, st, 1u, k);
+    const bool same = ((reinterpret_cast<uintptr_t>(k.logits) ^ reinterpret_cast<uintptr_t>(k.grad)) & 15u) == 0 &&
+                      (k.stride - k.grad_stride) * (long long)sizeof(T) % 16 == 0;
+    return launch(same ? token_logprob_grad_kernel<T, true> : token_logprob_grad_kernel<T, false>, (uint64_t)k.n_rows * k.chunks, kGradThreads, st, 1u, k);
 }
 
 uint32_t policy_blocks(uint64_t n_tokens) {
@@ -162,15 +165,27 @@ cudaError_t run_policy(const PolicyArgs &k, int kl, cudaStream_t st) {
     return kl == kNoKl ? run_policy<kVec, kNoKl>(k, st) : kl == kKlExp ? run_policy<kVec, kKlExp>(k, st) : run_policy<kVec, kKlPoly>(k, st);
 }
 
-// Sorted positions per chunk of the segment sums: short chunks while there are few positions to spread
-// over the machine, long ones later (a run cut by a border costs two float rows of extra traffic).
+template <typename T>
+cudaError_t run_embed(const EmbedArgs &k, bool whole, cudaStream_t st) {
+    const uint32_t nvec = k.dim / Elem<T>::kVec + 1;
+    uint32_t team = 2;                                       // lanes per row, as a power of two: a quarter of its vectors
+    while (team < 5 && (kEmbedUnroll << team) < nvec) ++team;
+    const uint32_t pieces = (nvec + (kEmbedUnroll << team) - 1) / (kEmbedUnroll << team), teams = kEmbedThreads >> team;
+    const uint64_t grid = ((uint64_t)k.n_tokens * pieces + teams - 1) / teams;
+    if (grid > kMaxGrid) return cudaErrorInvalidValue;
+    return launch(whole ? embed_kernel<T, true> : embed_kernel<T, false>, grid, kEmbedThreads, st, 1u, k, team, pieces);
+}
+
+// Sorted positions per chunk of the segment sums: short chunks while there are few positions to spread over the
+// machine, long ones later (a run cut by a border costs two float rows of extra traffic, and one warp joins
+// its parts).  65536 positions x 8 slices: 295 us with 64, 327 with 32, 309 with 128.
 uint32_t chunk_rows(uint32_t n_tokens, uint32_t slices) {
-    uint32_t r = 8;
-    while (r < 128 && (uint64_t)n_tokens * slices > (uint64_t)r * 148 * 48) r *= 2;
+    uint32_t r = n_tokens <= 2048 ? 8 : 32;
+    while (r < 512 && (uint64_t)n_tokens * slices > (uint64_t)r * 148 * 64) r *= 2;
     return r;
 }
 struct EmbedGradLayout {
-    size_t keys[2], pos[2], counts, present, partial, partial_stride, total;
+    size_t keys[2], pos[2], counts, present, arrived, partial, partial_stride, total;
     uint32_t n_tiles, n_chunks, rows_per_chunk, slices, passes;
     bool small, big_tiles;
 };
@@ -192,6 +207,7 @@ EmbedGradLayout embed_layout(uint32_t n_tokens, uint32_t vocab, uint32_t dim) {
     for (int k = 0; k < 2; ++k) { L.keys[k] = take((size_t)n_tokens * 4); L.pos[k] = take((size_t)n_tokens * 4); }
     L.counts = take((size_t)L.passes * L.n_tiles * kSortBins * 4);
     L.present = take(((size_t)vocab + 31) / 32 * 4);
+    L.arrived = take((size_t)L.n_chunks * L.slices * 4);
     L.partial = take(2 * (size_t)L.n_chunks * L.partial_stride * 4);
     L.total = p;
     return L;
@@ -212,7 +228,7 @@ cudaError_t run_sort(EmbedArgs &k, const EmbedGradLayout &L, uint8_t *ws, cudaSt
         s.pos_in = reinterpret_cast<uint32_t *>(ws + L.pos[(p + 1) & 1]);
         s.keys_out = reinterpret_cast<uint32_t *>(ws + L.keys[p & 1]);
         s.pos_out = reinterpret_cast<uint32_t *>(ws + L.pos[p & 1]);
-        rc = launch(sort_place_kernel<kItems>, L.n_tiles, kSortThreads, st, 1u, k, s);
+        rc = launch(sort_place_kernel<kItems>, L.n_tiles + (s.last ? k.zero_from : 0u), kSortThreads, st, 1u, k, s);
     }
     k.keys = s.keys_out;
     k.pos = s.pos_out;
@@ -226,20 +242,32 @@ cudaError_t run_embed_grad(EmbedArgs k, const EmbedGradLayout &L, uint8_t *ws, b
     const bool clear = !k.accumulate, clear_all = clear && L.small && k.n_tokens <= k.vocab / 8;
     cudaError_t rc;
     k.present = clear && !clear_all ? reinterpret_cast<uint32_t *>(ws + L.present) : nullptr;
+    const uint32_t words = k.present ? (uint32_t)(((uint64_t)k.vocab + 31) / 32) : 0u;
+    k.arrived = reinterpret_cast<uint32_t *>(ws + L.arrived);
+    k.n_arrived = L.n_chunks * L.slices;
     if (L.small) {
         rc = cudaFuncSetAttribute(sort_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem);
         if (rc != cudaSuccess) return rc;
         k.keys = reinterpret_cast<uint32_t *>(ws + L.keys[0]);
         k.pos = reinterpret_cast<uint32_t *>(ws + L.pos[0]);
-        rc = launch_smem(sort_small_kernel, clear_all ? 148 * 2 : 1, kSmallThreads, kSmallSmem, st, 1u, k, L.passes, (uint32_t)sizeof(G));
-    } else rc = L.big_tiles ? run_sort<16>(k, L, ws, st) : run_sort<4>(k, L, ws, st);
+        rc = launch_smem(sort_small_kernel, clear_all ? 148 * 2 : 1, kSmallThreads, kSmallSmem, st, 1u, k, L.passes);
+    } else {
+        // the last placing kernel leaves most of the machine idle for about 8 us: room to clear some 40 MB of rows
+        if (L.passes > 1) {
+            const uint64_t some = (40ull << 20) / (32 * (uint64_t)k.dim * sizeof(G)) + 1;
+            k.zero_from = some < words ? (uint32_t)some : words;
+        }
+        rc = L.big_tiles ? run_sort<16>(k, L, ws, st) : run_sort<4>(k, L, ws, st);
+    }
     if (rc != cudaSuccess) return rc;
     const uint32_t sum_blocks = (uint32_t)(((uint64_t)L.n_chunks * L.slices + kSumThreads / 32 - 1) / (kSumThreads / 32));
-    const uint32_t zero_blocks = k.present ? (uint32_t)(((uint64_t)k.vocab + 31) / 32) : 0u;
-    if (sum_blocks + zero_blocks)
-        rc = launch(wide ? embed_sum_kernel<T, G, true> : embed_sum_kernel<T, G, false>, (uint64_t)sum_blocks + zero_blocks, kSumThreads, st, 1u, k, L.slices, sum_blocks);
-    if (rc != cudaSuccess || L.n_chunks < 2) return rc;
-    return launch(wide ? embed_join_kernel<G, true> : embed_join_kernel<G, false>, L.n_chunks - 1, kSumThreads, st, 1u, k, L.slices);
+    const uint32_t zero_blocks = words - k.zero_from;
+    if (sum_blocks + zero_blocks == 0) return cudaSuccess;
+    const uint64_t grid = (uint64_t)sum_blocks + zero_blocks;
+    const size_t smem = sum_blocks ? kSumWarps * (wide ? SumLayout<T, true>::kWarpBytes : SumLayout<T, false>::kWarpBytes) : 0;
+    auto *kernel = wide ? embed_sum_kernel<T, G, true> : embed_sum_kernel<T, G, false>;
+    if (smem > 48 * 1024 && (rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return rc;
+    return launch_smem(kernel, grid, kSumThreads, smem, st, 1u, k, L.slices, sum_blocks);
 }
 
 }  // namespace
@@ -372,10 +400,8 @@ int td_embed(const td_embed_args *a, void *stream) {
     const uint32_t es = size_of(a->dtype);
     if (!a->ids || !a->table || !a->out || !aligned(a->ids, 4) || !aligned(a->table, es) || !aligned(a->out, es) || !aligned(a->status, 4))
         return TD_EINVAL;
-    const uint32_t per_piece = kEmbedVectors * (16u / es);
-    const uint32_t pieces = (a->dim + per_piece - 1) / per_piece;
-    const uint64_t grid = ((uint64_t)a->n_tokens * pieces + kEmbedThreads / 32 - 1) / (kEmbedThreads / 32);
-    if (grid > kMaxGrid) return TD_EINVAL;
+    // rows of both sides start on 16-byte boundaries
+    const bool whole = aligned(a->table, 16) && aligned(a->out, 16) && a->table_stride * es % 16 == 0 && a->out_stride * es % 16 == 0;
     DeviceGuard dev(a->device);
     if (!dev.ok()) return TD_ECUDA;
     EmbedArgs k{};
@@ -391,13 +417,10 @@ int td_embed(const td_embed_args *a, void *stream) {
     k.out = a->out;
     k.table_stride = a->table_stride;
     k.out_stride = a->out_stride;
-    // rows of both sides start on 16-byte boundaries
-    const bool wide = aligned(a->table, 16) && aligned(a->out, 16) && a->table_stride * es % 16 == 0 && a->out_stride * es % 16 == 0;
     cudaStream_t st = (cudaStream_t)stream;
-    auto go = [&](auto *wide_kernel, auto *narrow_kernel) { return launch(wide ? wide_kernel : narrow_kernel, grid, kEmbedThreads, st, 1u, k, pieces); };
-    const cudaError_t rc = a->dtype == TD_F32 ? go(embed_kernel<float, true>, embed_kernel<float, false>)
-                         : a->dtype == TD_BF16 ? go(embed_kernel<__nv_bfloat16, true>, embed_kernel<__nv_bfloat16, false>)
-                                               : go(embed_kernel<__half, true>, embed_kernel<__half, false>);
+    const cudaError_t rc = a->dtype == TD_F32 ? run_embed<float>(k, whole, st)
+                         : a->dtype == TD_BF16 ? run_embed<__nv_bfloat16>(k, whole, st) : run_embed<__half>(k, whole, st);
+    if (rc == cudaErrorInvalidValue) return TD_EINVAL;
     return rc == cudaSuccess ? TD_OK : TD_ECUDA;
 }
 
@@ -418,7 +441,7 @@ int td_embed_grad(const td_embed_grad_args *a, void *stream) {
     if (a->n_tokens && (!a->ids || !a->grad_out || !aligned(a->ids, 4) || !aligned(a->grad_out, es))) return TD_EINVAL;
     const EmbedGradLayout L = embed_layout(a->n_tokens, a->vocab, a->dim);
     if (!a->workspace || !aligned(a->workspace, 256) || a->workspace_bytes < L.total) return TD_EWORKSPACE;
-    if ((uint64_t)L.n_chunks * L.slices + (uint64_t)a->vocab / 32 >= kMaxGrid) return TD_EINVAL;
+    if ((uint64_t)L.n_chunks * L.slices + (uint64_t)a->vocab / 32 >= kMaxGrid) return TD_EINVAL;          // also keeps n_arrived in 32 bits
     DeviceGuard dev(a->device);
     if (!dev.ok()) return TD_ECUDA;
     EmbedArgs k{};
@@ -435,6 +458,7 @@ int td_embed_grad(const td_embed_grad_args *a, void *stream) {
     k.grad_table = a->grad_table;
     k.table_stride = a->table_stride;
     k.accumulate = (uint32_t)a->accumulate;
+    k.grad_size = gs;
     k.rows_per_chunk = L.rows_per_chunk;
     k.n_chunks = L.n_chunks;
     uint8_t *ws = static_cast<uint8_t *>(a->workspace);

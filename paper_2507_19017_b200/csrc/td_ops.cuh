@@ -175,6 +175,43 @@ template <> struct Elem<__half> {
     static __device__ __forceinline__ __half from(float x) { return __float2half_rn(x); }
 };
 
+// 16 bytes that start `phase` bytes (even, below 16) into a and end in b.
+__device__ __forceinline__ uint4 shifted(const uint4 &a, const uint4 &b, uint32_t phase) {
+    const bool one = phase & 4u, two = phase & 8u;
+    const uint32_t half = (phase & 2u) * 8u;
+    const uint32_t t0 = one ? a.y : a.x, t1 = one ? a.z : a.y, t2 = one ? a.w : a.z, t3 = one ? b.x : a.w, t4 = one ? b.y : b.x,
+                   t5 = one ? b.z : b.y, t6 = one ? b.w : b.z;
+    const uint32_t u0 = two ? t2 : t0, u1 = two ? t3 : t1, u2 = two ? t4 : t2, u3 = two ? t5 : t3, u4 = two ? t6 : t4;
+    return make_uint4(__funnelshift_r(u0, u1, half), __funnelshift_r(u1, u2, half), __funnelshift_r(u2, u3, half), __funnelshift_r(u3, u4, half));
+}
+// kVec elements at p, whatever its alignment, put together from two aligned loads that stay within [begin, end), the
+// buffer they lie in; at the buffer's ends, where they would not, element by element.  open() issues the loads and
+// close() takes what they brought, so that several can be on their way.
+template <typename T>
+struct Window {
+    uint4 a, b;
+    const T *p;
+    uint32_t phase;
+    bool whole;
+    __device__ __forceinline__ void open(const T *from, const T *begin, const T *end) {
+        p = from;
+        phase = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u);
+        const T *at = p - phase / sizeof(T);
+        const bool a_in = at >= begin, b_in = phase == 0 || at + 2 * Elem<T>::kVec <= end;
+        whole = a_in && b_in;
+        a = b = make_uint4(0u, 0u, 0u, 0u);
+        if (whole) a = *reinterpret_cast<const uint4 *>(at);
+        if (whole && phase != 0) b = *(reinterpret_cast<const uint4 *>(at) + 1);
+    }
+    __device__ __forceinline__ uint4 close() const {
+        if (whole) return shifted(a, b, phase);
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int k = 0; k < Elem<T>::kVec / 2; ++k) Elem<T>::put_pair(v, k, Elem<T>::load(p + 2 * k), Elem<T>::load(p + 2 * k + 1));
+        return v;
+    }
+};
+
 // 16-byte accesses that data used once goes through: read past L1, written without being kept.
 __device__ __forceinline__ uint4 ld_stream(const void *p) {
     uint4 v;
@@ -185,5 +222,19 @@ __device__ __forceinline__ uint4 ld_stream(const void *p) {
 __device__ __forceinline__ void st_stream(void *p, const uint4 &v) {
     asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+
+// Asynchronous copy of kBytes (4, 8 or 16) from global to shared memory.  What a thread has copied it may read after
+// copy_wait; others also need a barrier.
+template <int kBytes>
+__device__ __forceinline__ void copy_async(void *shared, const void *global) {
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(shared);
+    if constexpr (kBytes == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(global) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(global), "n"(kBytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
 
 }  // namespace td

@@ -189,20 +189,6 @@ __device__ __forceinline__ f32x2 policy_pair(const PolicyArgs &a, const Seat &se
     return d;
 }
 
-// Asynchronous copy of kBytes (4, 8 or 16) from global to shared memory by one thread, which alone reads
-// them later: no barrier is needed between.
-template <int kBytes>
-__device__ __forceinline__ void copy_async(void *shared, const void *global) {
-    const uint32_t to = (uint32_t)__cvta_generic_to_shared(shared);
-    if constexpr (kBytes == 16)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(global) : "memory");
-    else
-        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(global), "n"(kBytes) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kPending>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
-
 // Positions rel .. rel + kVec of a per-token array that ends at `limit`; `whole`: all of them exist, and the
 // array is aligned for one access of kVec.  A slot is the kVec elements' place in shared memory.
 template <int kVec>
