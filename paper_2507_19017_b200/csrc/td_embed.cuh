@@ -26,7 +26,7 @@ struct EmbedArgs {
     float *partial;                      // [2][n_chunks][partial_stride]: sums of a run cut by the chunk's start / by its end
     size_t partial_stride;               // dim rounded up to a warp's columns
     uint32_t *arrived;                   // [n_chunks][slices] parts stored of the cut run that begins in the chunk
-    uint32_t n_arrived, zero_from;       // words of a.present whose rows were cleared before the sums
+    uint32_t n_arrived, zero_from;       // blocks of zero_rows that ran before the sums
 };
 
 // Positions that hold a token of the batch.
@@ -139,9 +139,16 @@ __device__ __forceinline__ void rank_digits(const uint32_t (&key)[kItems], uint3
     for (int k = 0; k < kItems; ++k) {
         if ((uint32_t)k >= items) break;
         const bool in = (in_mask >> k) & 1u;
-        const uint32_t d = in ? (key[k] >> shift) & (kSortBins - 1) : kSortBins;        // absent entries match only each other
-        const uint32_t peers = __match_any_sync(kFullMask, d);
-        const uint32_t before = in ? warp_bins[warp][d] : 0u;
+        const uint32_t d = (key[k] >> shift) & (kSortBins - 1);
+        // lanes with the same digit, one vote per bit (a match instruction took 300 to 400 cycles here)
+        uint32_t peers = __ballot_sync(kFullMask, in);
+#pragma unroll
+        for (int b = 0; b < kSortBits; ++b) {
+            const bool set = (d >> b) & 1u;
+            const uint32_t v = __ballot_sync(kFullMask, set);
+            peers &= set ? v : ~v;
+        }
+        const uint32_t before = in ? (uint32_t)warp_bins[warp][d] : 0u;
         rank[k] = before + __popc(peers & ((1u << lane) - 1u));
         __syncwarp();
         if (in && lane == (uint32_t)__ffs(peers) - 1u) warp_bins[warp][d] = (Count)(before + __popc(peers));
@@ -165,6 +172,8 @@ __device__ __forceinline__ uint32_t scan_bins(uint32_t x, uint32_t *warp_sum) {
     return before;
 }
 
+constexpr uint32_t kZeroWords = 8;       // words of a.present per block, where rows are short
+
 // Zeros at [p, p + bytes) by n threads, of which this is number i; p and bytes are multiples of 2.
 __device__ __forceinline__ void fill_zero(uint8_t *p, size_t bytes, size_t i, size_t n) {
     const size_t head = min(bytes, (size_t)((16u - (reinterpret_cast<uintptr_t>(p) & 15u)) & 15u)), nvec = (bytes - head) / 16;
@@ -174,19 +183,36 @@ __device__ __forceinline__ void fill_zero(uint8_t *p, size_t bytes, size_t i, si
     if (i < (bytes - tail) / 2) reinterpret_cast<uint16_t *>(p + tail)[i] = 0;
 }
 
-// Rows of the gradient table whose bit in a.present is not set, 32 per block.
-__device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t word) {
-    const uint32_t bits = a.present[word], lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    for (uint32_t k = warp; k < 32 && word * 32 + k < a.vocab; k += blockDim.x >> 5)
-        if (!((bits >> k) & 1u))
-            fill_zero(static_cast<uint8_t *>(a.grad_table) + (size_t)(word * 32 + k) * a.table_stride * a.grad_size, (size_t)a.dim * a.grad_size, lane, 32);
+// Clears the rows of the gradient table whose bit in a.present is not set.  Long rows: the block takes 32 rows,
+// a warp at a time one of them.  Short ones: every warp takes 32, neighbours without a gap between them at once.
+constexpr uint32_t kLongRow = 1024;      // bytes
+__device__ __forceinline__ bool long_rows(const EmbedArgs &a) { return a.dim * (unsigned long long)a.grad_size >= kLongRow; }
+__device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t block) {
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const size_t row = (size_t)a.dim * a.grad_size, stride = (size_t)a.table_stride * a.grad_size;
+    uint8_t *table = static_cast<uint8_t *>(a.grad_table);
+    if (long_rows(a)) {
+        const uint32_t bits = a.present[block];
+        for (uint32_t k = warp; k < 32 && block * 32 + k < a.vocab; k += blockDim.x >> 5)
+            if (!((bits >> k) & 1u)) fill_zero(table + (size_t)(block * 32 + k) * stride, row, lane, 32);
+        return;
+    }
+    const uint32_t word = block * kZeroWords + warp;
+    if (warp >= kZeroWords || word >= (a.vocab + 31) / 32) return;
+    const uint32_t rows = min(32u, a.vocab - word * 32);
+    uint32_t absent = ~a.present[word] & (rows == 32 ? kFullMask : (1u << rows) - 1u);
+    while (absent) {
+        const uint32_t from = __ffs(absent) - 1, free = ~(absent >> from), n = row == stride ? (free ? __ffs(free) - 1 : 32) : 1;
+        fill_zero(table + (size_t)(word * 32 + from) * stride, row * n, lane, 32);
+        absent &= from + n >= 32 ? 0u : kFullMask << (from + n);
+    }
 }
 
 // One block sorts everything: up to 8192 positions, in shared memory.  Blocks beyond the first clear the gradient
 // table meanwhile, where the launch has such blocks.
 constexpr int kSmallThreads = 1024, kSmallItems = 8, kSmallWarps = kSmallThreads / 32;
 constexpr uint32_t kSmallMax = kSmallThreads * kSmallItems;
-constexpr size_t kSmallSmem = (size_t)kSmallWarps * kSortBins * 2 + kSmallMax * (4 + 2) + 64;
+constexpr size_t kSmallSmem = (size_t)kSmallWarps * kSortBins * 2 + kSmallMax * (4 + 2) + kSortBins * 2 + 64;
 
 __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedArgs a, uint32_t passes) {
     griddep_launch_dependents();
@@ -204,7 +230,8 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedAr
     uint16_t(*warp_bins)[kSortBins] = reinterpret_cast<uint16_t(*)[kSortBins]>(sort_smem);
     uint32_t *keys = reinterpret_cast<uint32_t *>(sort_smem + (size_t)kSmallWarps * kSortBins * 2);
     uint16_t *pos = reinterpret_cast<uint16_t *>(keys + kSmallMax);
-    uint32_t *warp_sum = reinterpret_cast<uint32_t *>(pos + kSmallMax);
+    uint16_t *bin_start = pos + kSmallMax;
+    uint32_t *warp_sum = reinterpret_cast<uint32_t *>(bin_start + kSortBins);
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t n = tokens_in(a), items = (a.n_tokens + kSmallThreads - 1) / kSmallThreads, base = warp * items * 32 + lane;
     for (uint32_t w = threadIdx.x; w < a.n_arrived; w += kSmallThreads) a.arrived[w] = 0u;
@@ -212,11 +239,13 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedAr
         for (uint32_t w = threadIdx.x; w < (a.vocab + 31) / 32; w += kSmallThreads) a.present[w] = 0u;
         __syncthreads();
     }
+    const uint32_t busy = items ? (a.n_tokens + items * 32 - 1) / (items * 32) : 0;        // warps that have entries
     uint32_t key[kSmallItems], at[kSmallItems], rank[kSmallItems], in_mask = 0;
 #pragma unroll
     for (int k = 0; k < kSmallItems; ++k) {
         if ((uint32_t)k >= items) break;
         at[k] = base + k * 32;
+        key[k] = 0;
         if (at[k] < a.n_tokens) {
             in_mask |= 1u << k;
             key[k] = id_at(a, at[k], n);
@@ -235,24 +264,24 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedAr
             }
         }
         const uint32_t shift = p * kSortBits;
-        rank_digits<kSmallItems, kSmallWarps>(key, rank, in_mask, shift, warp_bins, items);
+        if (warp < busy) rank_digits<kSmallItems, kSmallWarps>(key, rank, in_mask, shift, warp_bins, items);
         __syncthreads();
         uint32_t total = 0;
         if (threadIdx.x < kSortBins)
-            for (int w = 0; w < kSmallWarps; ++w) {          // entries of the bin in earlier warps
+#pragma unroll 4
+            for (uint32_t w = 0; w < busy; ++w) {            // entries of the bin in earlier warps
                 const uint32_t c = warp_bins[w][threadIdx.x];
                 warp_bins[w][threadIdx.x] = (uint16_t)total;
                 total += c;
             }
         const uint32_t start = scan_bins(total, warp_sum);
-        if (threadIdx.x < kSortBins)
-            for (int w = 0; w < kSmallWarps; ++w) warp_bins[w][threadIdx.x] = (uint16_t)(warp_bins[w][threadIdx.x] + start);
+        if (threadIdx.x < kSortBins) bin_start[threadIdx.x] = (uint16_t)start;
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kSmallItems; ++k) {
             if ((uint32_t)k >= items) break;
             if (!((in_mask >> k) & 1u)) continue;
-            const uint32_t to = warp_bins[warp][(key[k] >> shift) & (kSortBins - 1)] + rank[k];
+            const uint32_t d = (key[k] >> shift) & (kSortBins - 1), to = bin_start[d] + warp_bins[warp][d] + rank[k];
             if (p + 1 < passes) {
                 keys[to] = key[k];
                 pos[to] = (uint16_t)at[k];
@@ -326,7 +355,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const EmbedArg
     // thread b: entries of bin b in all tiles, and in the tiles before this one
     uint32_t total = 0, ahead = 0;
     const uint32_t *counts = s.counts + (size_t)pass * s.n_tiles * kSortBins + threadIdx.x;
-#pragma unroll 8
+#pragma unroll 16
     for (uint32_t tile = 0; tile < s.n_tiles; ++tile) {
         const uint32_t c = __ldcg(counts + (size_t)tile * kSortBins);
         if (tile < blockIdx.x) ahead += c;
@@ -353,22 +382,21 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const EmbedArg
 }
 
 // ---- sums over the runs of equal ids ----
-// A warp adds up kSumWarpCols columns of rows, kSumCols per lane, and keeps kSumAhead rows on their way through
-// shared memory.
-//   kWide: rows start on 16-byte boundaries and are whole lanes' columns; a lane copies and reads its own
-//     consecutive columns.
-//   else: the aligned 16-byte pieces that cover the warp's columns are copied, and a lane reads pairs of columns, 64 apart,
-//     from wherever in them the row begins; written rows go through shared memory too, to leave in vectors
-//     aligned on the row.
+// A warp adds up kSumWarpCols columns of rows, kSumCols per lane.
+//   kWide: rows start on 16-byte boundaries and are whole lanes' columns; a lane loads its own consecutive columns
+//     of kRows rows at a time into registers.
+//   else: the aligned 16-byte pieces that cover the warp's columns of a row are copied to shared memory, two groups of
+//     kRows rows in turn, and a lane reads pairs of columns, 64 apart, from wherever in them the row begins;
+//     written rows go through shared memory too, to leave in vectors aligned on the row.
 constexpr int kSumThreads = 256, kSumWarps = kSumThreads / 32, kSumCols = 8, kSumPairs = kSumCols / 2;
 constexpr uint32_t kSumWarpCols = 32 * kSumCols;
 
 template <typename T, bool kWide>
 struct SumLayout {
-    static constexpr int kAhead = sizeof(T) == 2 ? 8 : 4;
-    static constexpr uint32_t kSlot = kSumWarpCols * sizeof(T) + (kWide ? 0 : 16);
-    static constexpr uint32_t kStage = kWide ? 0 : (kSumWarpCols + kSumWarpCols / 32) * 4;     // a word of padding per 32: lanes 8 apart in different banks
-    static constexpr uint32_t kWarpBytes = kAhead * kSlot + kStage;
+    static constexpr int kRows = kWide && sizeof(T) == 2 ? 8 : 4;
+    static constexpr uint32_t kSlot = kSumWarpCols * sizeof(T) + 16;
+    static constexpr uint32_t kStage = (kSumWarpCols + kSumWarpCols / 32) * 4;     // a word of padding per 32: lanes 8 apart in different banks
+    static constexpr uint32_t kWarpBytes = kWide ? 0 : 2 * kRows * kSlot + kStage;
 };
 // column of a lane's pair k, from the warp's first
 template <bool kWide>
@@ -378,51 +406,38 @@ __device__ __forceinline__ uint32_t pair_column(int k) {
 }
 
 // A row's columns [c0, c0 + cols) on their way into a slot; the row lies in [begin, end).
-template <typename T, bool kWide>
+template <typename T>
 __device__ __forceinline__ void fetch_row(uint8_t *slot, const T *row, uint32_t c0, uint32_t cols, const T *begin, const T *end) {
-    const uint32_t lane = threadIdx.x & 31u;
     constexpr uint32_t E = Elem<T>::kVec;
-    if constexpr (kWide) {
-        if (lane * kSumCols >= cols) return;
-#pragma unroll
-        for (uint32_t q = 0; q < kSumCols / E; ++q) copy_async<16>(slot + (lane * kSumCols + q * E) * sizeof(T), row + c0 + lane * kSumCols + q * E);
-    } else {
-        const T *from = row + c0;
-        const uint32_t skew = (uint32_t)(reinterpret_cast<uintptr_t>(from) & 15u) / (uint32_t)sizeof(T), pieces = (skew + cols + E - 1) / E;
-        for (uint32_t i = lane; i < pieces; i += 32) {
-            const T *at = from - skew + i * E;
-            if (at >= begin && at + E <= end) copy_async<16>(slot + i * 16, at);
-            else                                             // a piece that reaches over an end of the array
-                for (uint32_t k = 0; k < E; ++k)
-                    if (at + k >= begin && at + k < end) reinterpret_cast<T *>(slot + i * 16)[k] = at[k];
-        }
+    const T *from = row + c0;
+    const uint32_t skew = (uint32_t)(reinterpret_cast<uintptr_t>(from) & 15u) / (uint32_t)sizeof(T), pieces = (skew + cols + E - 1) / E;
+    for (uint32_t i = threadIdx.x & 31u; i < pieces; i += 32) {
+        const T *at = from - skew + i * E;
+        if (at >= begin && at + E <= end) copy_async<16>(slot + i * 16, at);
+        else                                                 // a piece that reaches over an end of the array
+            for (uint32_t k = 0; k < E; ++k)
+                if (at + k >= begin && at + k < end) reinterpret_cast<T *>(slot + i * 16)[k] = at[k];
     }
 }
-template <typename T, bool kWide>
-__device__ __forceinline__ void add_row(f32x2 (&sum)[kSumPairs], const uint8_t *slot, const T *from) {
-    const uint32_t lane = threadIdx.x & 31u;
-    constexpr int E = Elem<T>::kVec;
-    if constexpr (kWide) {
+// skew: bytes from the slot's start to the row's first column
+template <typename T>
+__device__ __forceinline__ void add_slot(f32x2 (&sum)[kSumPairs], const uint8_t *slot, uint32_t skew) {
+    const uint32_t lane = threadIdx.x & 31u, *w = reinterpret_cast<const uint32_t *>(slot + (skew & ~3u));
 #pragma unroll
-        for (int q = 0; q < kSumCols / E; ++q) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(slot + (lane * kSumCols + q * E) * sizeof(T));
-#pragma unroll
-            for (int k = 0; k < E / 2; ++k) sum[q * E / 2 + k] = add2(sum[q * E / 2 + k], Elem<T>::pair(v, k));
-        }
-    } else {
-        const uint32_t skew = (uint32_t)(reinterpret_cast<uintptr_t>(from) & 15u);          // bytes
-        const uint32_t *w = reinterpret_cast<const uint32_t *>(slot + (skew & ~3u));
-#pragma unroll
-        for (int k = 0; k < kSumPairs; ++k) {
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if constexpr (sizeof(T) == 4) {
-                v.x = w[64 * k + 2 * lane];
-                v.y = w[64 * k + 2 * lane + 1];
-            } else if (skew & 2u) v.x = __funnelshift_r(w[32 * k + lane], w[32 * k + lane + 1], 16);
-            else v.x = w[32 * k + lane];
-            sum[k] = add2(sum[k], Elem<T>::pair(v, 0));
-        }
+    for (int k = 0; k < kSumPairs; ++k) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (sizeof(T) == 4) {
+            v.x = w[64 * k + 2 * lane];
+            v.y = w[64 * k + 2 * lane + 1];
+        } else v.x = __funnelshift_r(w[32 * k + lane], w[32 * k + lane + 1], (skew & 2u) * 8u);
+        sum[k] = add2(sum[k], Elem<T>::pair(v, 0));
     }
+}
+
+// Four floats added to those at p (16-byte aligned).
+__device__ __forceinline__ void add_vector(void *p, const uint4 &v) {
+    asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(__uint_as_float(v.x)), "f"(__uint_as_float(v.y)),
+                 "f"(__uint_as_float(v.z)), "f"(__uint_as_float(v.w)) : "memory");
 }
 
 // scale * sum to columns [c0, c0 + cols) of row v of the gradient table, or added to what is there.
@@ -436,11 +451,13 @@ __device__ __forceinline__ void write_row(const EmbedArgs &a, uint32_t v, const 
     for (int k = 0; k < kSumPairs; ++k) {
         const uint32_t c = pair_column<kWide>(k);
         unpack2(mul2(sum[k], pack2(a.scale, a.scale)), x[2 * k], x[2 * k + 1]);
-        if (a.accumulate) {
+        if (sizeof(G) == 2 && a.accumulate) {
             if (c < cols) x[2 * k] += Elem<G>::load(out + c);
             if (c + 1 < cols) x[2 * k + 1] += Elem<G>::load(out + c + 1);
         }
     }
+    // a float row is added to where it lies: one addition per element, so the order of the warps is nothing to it
+    const bool add = sizeof(G) == 4 && a.accumulate;
     if constexpr (kWide) {
         if (lane * kSumCols >= cols) return;
 #pragma unroll
@@ -448,7 +465,7 @@ __device__ __forceinline__ void write_row(const EmbedArgs &a, uint32_t v, const 
             uint4 o;
 #pragma unroll
             for (uint32_t k = 0; k < E / 2; ++k) Elem<G>::put_pair(o, k, x[q * E + 2 * k], x[q * E + 2 * k + 1]);
-            st_stream(out + lane * kSumCols + q * E, o);
+            if (add) add_vector(out + lane * kSumCols + q * E, o); else st_stream(out + lane * kSumCols + q * E, o);
         }
     } else {
         auto at = [](uint32_t c) { return c + c / 32; };
@@ -464,11 +481,14 @@ __device__ __forceinline__ void write_row(const EmbedArgs &a, uint32_t v, const 
             uint4 o;
 #pragma unroll
             for (uint32_t k = 0; k < E / 2; ++k) Elem<G>::put_pair(o, k, stage[at(head + j * E + 2 * k)], stage[at(head + j * E + 2 * k + 1)]);
-            st_stream(out + head + j * E, o);
+            if (add) add_vector(out + head + j * E, o); else st_stream(out + head + j * E, o);
         }
         const uint32_t tail = head + nvec * E;
-        if (lane < head) out[lane] = Elem<G>::from(stage[at(lane)]);
-        if (lane < cols - tail) out[tail + lane] = Elem<G>::from(stage[at(tail + lane)]);
+        auto loose = [&](uint32_t c) {
+            if (add) atomicAdd(reinterpret_cast<float *>(out) + c, stage[at(c)]); else out[c] = Elem<G>::from(stage[at(c)]);
+        };
+        if (lane < head) loose(lane);
+        if (lane < cols - tail) loose(tail + lane);
     }
 }
 
@@ -480,7 +500,7 @@ __device__ __forceinline__ float *partial_row(const EmbedArgs &a, uint32_t which
 // The parts of a run that chunk borders cut, of which this warp has just stored one (run v; cont: it began before
 // `chunk`): whichever warp stores the last one adds them up, in the order of the chunks.  True for that warp.
 template <bool kWide>
-__device__ __noinline__ bool join_run(const EmbedArgs &a, uint32_t v, uint32_t chunk, bool cont, uint32_t slice, uint32_t slices, f32x2 (&sum)[kSumPairs]) {
+__device__ __forceinline__ bool join_run(const EmbedArgs &a, uint32_t v, uint32_t chunk, bool cont, uint32_t slice, uint32_t slices, f32x2 (&sum)[kSumPairs]) {
     const uint32_t lane = threadIdx.x & 31u, c0 = slice * kSumWarpCols;
     // chunks that continue the run: behind this one (those that begin with v), and before it back to the one
     // it begins in (the last whose predecessor does not end with v)
@@ -528,23 +548,36 @@ __device__ __noinline__ bool join_run(const EmbedArgs &a, uint32_t v, uint32_t c
     return true;
 }
 
+template <bool kWide>
+__device__ __forceinline__ void store_partial(const EmbedArgs &a, uint32_t which, uint32_t chunk, uint32_t c0, const f32x2 (&sum)[kSumPairs]) {
+    float *to = partial_row(a, which, chunk) + c0, x[kSumCols];
+#pragma unroll
+    for (int k = 0; k < kSumPairs; ++k) unpack2(sum[k], x[2 * k], x[2 * k + 1]);
+    if constexpr (kWide) {
+        float4 *p = reinterpret_cast<float4 *>(to + pair_column<true>(0));
+        __stcg(p, make_float4(x[0], x[1], x[2], x[3]));
+        __stcg(p + 1, make_float4(x[4], x[5], x[6], x[7]));
+    } else {
+#pragma unroll
+        for (int k = 0; k < kSumPairs; ++k) __stcg(reinterpret_cast<float2 *>(to + pair_column<false>(k)), make_float2(x[2 * k], x[2 * k + 1]));
+    }
+}
+
 // A warp per (chunk of sorted positions, 256 columns).  A run that lies inside the chunk is written out; the part of
 // a run that began in an earlier chunk goes to partial 0, the part of one that began here and goes on to
-// partial 1, and the last part to arrive writes the run out.  Spread among the blocks that do this, as many as
-// a.present has words left clear rows without a token.
+// partial 1, and the last part to arrive writes the run out.  The blocks behind the sum_blocks that do this clear
+// rows without a token (before them or spread among them they cost 65536 x 2048 into float 5 to 10 % more).
 template <typename T, typename G, bool kWide>
-__global__ void __launch_bounds__(kSumThreads, 4) embed_sum_kernel(const __grid_constant__ EmbedArgs a, uint32_t slices, uint32_t sum_blocks) {
+__global__ void __launch_bounds__(kSumThreads, kWide ? 3 : 4) embed_sum_kernel(const __grid_constant__ EmbedArgs a, uint32_t slices, uint32_t sum_blocks) {
     griddep_launch_dependents();
     griddep_wait();
-    const uint32_t sums_before = (uint32_t)((unsigned long long)blockIdx.x * sum_blocks / gridDim.x);
-    if ((uint32_t)((unsigned long long)(blockIdx.x + 1ull) * sum_blocks / gridDim.x) == sums_before)
-        return zero_rows(a, blockIdx.x - sums_before + a.zero_from);
+    if (blockIdx.x >= sum_blocks) return zero_rows(a, blockIdx.x - sum_blocks + a.zero_from);
     using Layout = SumLayout<T, kWide>;
-    constexpr int kAhead = Layout::kAhead;
+    constexpr int kRows = Layout::kRows, E = Elem<T>::kVec;
     extern __shared__ __align__(16) uint8_t sum_smem[];
     uint8_t *ring = sum_smem + (threadIdx.x >> 5) * Layout::kWarpBytes;
-    float *stage = reinterpret_cast<float *>(ring + kAhead * Layout::kSlot);
-    const unsigned long long item = (unsigned long long)sums_before * kSumWarps + (threadIdx.x >> 5);
+    float *stage = kWide ? nullptr : reinterpret_cast<float *>(ring + 2 * kRows * Layout::kSlot);
+    const unsigned long long item = (unsigned long long)blockIdx.x * kSumWarps + (threadIdx.x >> 5);
     const unsigned long long chunk64 = item / slices;
     if (chunk64 >= a.n_chunks) return;
     const uint32_t chunk = (uint32_t)chunk64, slice = (uint32_t)(item % slices), lane = threadIdx.x & 31u;
@@ -552,64 +585,108 @@ __global__ void __launch_bounds__(kSumThreads, 4) embed_sum_kernel(const __grid_
     const uint32_t lo = chunk * a.rows_per_chunk, n = min(a.n_tokens - lo, a.rows_per_chunk);
     const T *in = static_cast<const T *>(a.grad_out), *in_end = in + (long long)(a.n_tokens - 1) * a.out_stride + a.dim;
 
-    // keys and positions, 32 entries at a time; the rows' fetching runs kAhead entries ahead of their adding
+    // keys and positions, 32 entries at a time; the rows of the next group are on their way while one is added
     const uint32_t *keys = a.keys + lo, *pos = a.pos + lo;
     auto batch = [&](const uint32_t *p, uint32_t b, uint32_t none) { return b + lane < n ? __ldg(p + b + lane) : none; };
-    uint32_t my_key = batch(keys, 0, a.vocab), my_pos = batch(pos, 0, 0u), next_key = 0, next_pos = 0;
+    uint32_t my_key = batch(keys, 0, a.vocab), my_pos = batch(pos, 0, 0u);
     const uint32_t before = lo > 0 ? __ldg(keys - 1) : a.vocab, after = lo + n < a.n_tokens ? __ldg(keys + n) : a.vocab;
     uint32_t v = __shfl_sync(kFullMask, my_key, 0);
     if (v >= a.vocab) return;                                // sorted behind all ids
-    bool cont = before == v;
-    uint32_t fetch_pos = my_pos, fetch_key = my_key;         // the batch that is being fetched from
-    auto issue = [&](uint32_t f, uint32_t slot) {
-        if (f < n) {
-            if (f && (f & 31u) == 0) { fetch_key = next_key; fetch_pos = next_pos; }
-            const uint32_t key = __shfl_sync(kFullMask, fetch_key, f & 31u), p = __shfl_sync(kFullMask, fetch_pos, f & 31u);
-            if ((f & 31u) == 0) { next_key = batch(keys, f + 32, a.vocab); next_pos = batch(pos, f + 32, 0u); }
-            if (key < a.vocab) fetch_row<T, kWide>(ring + slot * Layout::kSlot, in + (long long)p * a.out_stride, c0, cols, in, in_end);
-        }
-        copy_commit();
-    };
-#pragma unroll 1
-    for (int k = 0; k < kAhead; ++k) issue(k, k);
+    const uint32_t first = v;
+    const bool began_before = before == first;
+    bool cont = began_before;                                // still in that run
     f32x2 sum[kSumPairs];
     auto clear = [&]() {
 #pragma unroll
         for (int k = 0; k < kSumPairs; ++k) sum[k] = pack2(0.0f, 0.0f);
     };
     clear();
-    uint32_t slot = 0;
-#pragma unroll 1
-    for (uint32_t e = 0;; ++e) {
-        if (e && (e & 31u) == 0 && e < n) { my_key = batch(keys, e, a.vocab); my_pos = batch(pos, e, 0u); }
-        const uint32_t key = e < n ? __shfl_sync(kFullMask, my_key, e & 31u) : a.vocab;
-        if (key != v || e == n) {                            // the run of v ends, or the chunk does
-            const bool goes_on = e == n && after == v;
-            bool whole = true;
-            if (cont || goes_on) {
-                float *to = partial_row(a, cont ? 0u : 1u, chunk) + c0;
-#pragma unroll
-                for (int k = 0; k < kSumPairs; ++k) {
-                    float x, y;
-                    unpack2(sum[k], x, y);
-                    __stcg(reinterpret_cast<float2 *>(to + pair_column<kWide>(k)), make_float2(x, y));
-                }
-                whole = join_run<kWide>(a, v, chunk, cont, slice, slices, sum);
-            }
-            if (whole) write_row<G, kWide>(a, v, sum, c0, cols, stage);
-            if (key >= a.vocab) break;                       // the chunk's end, or positions without a token
-            cont = false;
-            v = key;
-            clear();
+    auto next_run = [&](uint32_t key) {  // ends the run of v, unless key is v
+        if (key == v) return;
+        if (v < a.vocab) {
+            if (cont) store_partial<kWide>(a, 0u, chunk, c0, sum);
+            else write_row<G, kWide>(a, v, sum, c0, cols, stage);
         }
-        copy_wait<kAhead - 1>();
-        if (!kWide) __syncwarp();
-        add_row<T, kWide>(sum, ring + slot * Layout::kSlot, in + (long long)__shfl_sync(kFullMask, my_pos, e & 31u) * a.out_stride + c0);
-        if (!kWide) __syncwarp();
-        issue(e + kAhead, slot);
-        slot = slot + 1 == kAhead ? 0 : slot + 1;
+        cont = false;
+        v = key;
+        clear();
+    };
+
+    if constexpr (kWide) {
+        constexpr int kVecs = kSumCols / E;
+        const T *mine = in + c0 + lane * kSumCols;
+        const bool on = lane * kSumCols < cols;
+        for (uint32_t e0 = 0; e0 < n; e0 += 32) {
+            if (e0) { my_key = batch(keys, e0, a.vocab); my_pos = batch(pos, e0, 0u); }
+            const uint32_t left = min(n - e0, 32u);
+            for (uint32_t k0 = 0; k0 < left; k0 += kRows) {
+                uint4 x[kRows][kVecs];
+#pragma unroll
+                for (int u = 0; u < kRows; ++u) {
+                    const uint32_t key = __shfl_sync(kFullMask, my_key, k0 + u), p = __shfl_sync(kFullMask, my_pos, k0 + u);
+                    const bool some = on && key < a.vocab;
+                    const T *row = mine + (long long)p * a.out_stride;
+#pragma unroll
+                    for (int q = 0; q < kVecs; ++q) {
+                        x[u][q] = make_uint4(0u, 0u, 0u, 0u);
+                        if (some) x[u][q] = ld_stream(row + q * E);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kRows; ++u) {
+                    if (k0 + u >= left) break;
+                    next_run(__shfl_sync(kFullMask, my_key, k0 + u));
+#pragma unroll
+                    for (int q = 0; q < kVecs; ++q)
+#pragma unroll
+                        for (int k = 0; k < E / 2; ++k) sum[q * E / 2 + k] = add2(sum[q * E / 2 + k], Elem<T>::pair(x[u][q], k));
+                }
+            }
+        }
+    } else {
+        const uint32_t in_skew = (uint32_t)reinterpret_cast<uintptr_t>(in + c0), stride_skew = (uint32_t)a.out_stride * (uint32_t)sizeof(T);
+        uint32_t far_key = my_key, far_pos = my_pos;         // the batch that rows are fetched from
+        auto issue = [&](uint32_t f) {   // the group of kRows rows from entry f on
+            if (f < n) {
+                if (f && (f & 31u) == 0) { far_key = batch(keys, f, a.vocab); far_pos = batch(pos, f, 0u); }
+#pragma unroll
+                for (int u = 0; u < kRows; ++u) {
+                    const uint32_t key = __shfl_sync(kFullMask, far_key, (f + u) & 31u), p = __shfl_sync(kFullMask, far_pos, (f + u) & 31u);
+                    if (key < a.vocab) fetch_row(ring + ((f / kRows) % 2 * kRows + u) * Layout::kSlot, in + (long long)p * a.out_stride, c0, cols, in, in_end);
+                }
+            }
+            copy_commit();
+        };
+        issue(0);
+        issue(kRows);
+        for (uint32_t e = 0; e < n; e += kRows) {
+            if (e && (e & 31u) == 0) { my_key = batch(keys, e, a.vocab); my_pos = batch(pos, e, 0u); }
+            copy_wait<1>();
+            __syncwarp();
+#pragma unroll 1
+            for (int u = 0; u < kRows; ++u) {
+                const uint32_t key = __shfl_sync(kFullMask, my_key, (e + u) & 31u), p = __shfl_sync(kFullMask, my_pos, (e + u) & 31u);
+                if (e + u >= n) break;
+                next_run(key);
+                if (key < a.vocab) add_slot<T>(sum, ring + ((e / kRows) % 2 * kRows + u) * Layout::kSlot, (in_skew + p * stride_skew) & 15u);
+            }
+            __syncwarp();
+            issue(e + 2 * kRows);
+        }
+        copy_wait<0>();                                      // nothing of this warp's is still on its way
     }
-    copy_wait<0>();                                          // nothing of this warp's is still on its way
+    const bool goes_on = v < a.vocab && after == v;
+    if (v < a.vocab) {
+        if (cont || goes_on) store_partial<kWide>(a, cont ? 0u : 1u, chunk, c0, sum);
+        else write_row<G, kWide>(a, v, sum, c0, cols, stage);
+    }
+    // the runs of which this chunk had a part: the one it began in, and the one it ended in
+#pragma unroll 1
+    for (int side = 0; side < 2; ++side) {
+        const bool part = side == 0 ? began_before : goes_on && !cont;
+        const uint32_t run = side == 0 ? first : v;
+        if (part && join_run<kWide>(a, run, chunk, side == 0, slice, slices, sum)) write_row<G, kWide>(a, run, sum, c0, cols, stage);
+    }
 }
 
 }  // namespace td

@@ -242,7 +242,8 @@ cudaError_t run_embed_grad(EmbedArgs k, const EmbedGradLayout &L, uint8_t *ws, b
     const bool clear = !k.accumulate, clear_all = clear && L.small && k.n_tokens <= k.vocab / 8;
     cudaError_t rc;
     k.present = clear && !clear_all ? reinterpret_cast<uint32_t *>(ws + L.present) : nullptr;
-    const uint32_t words = k.present ? (uint32_t)(((uint64_t)k.vocab + 31) / 32) : 0u;
+    const uint32_t per_block = (uint64_t)k.dim * sizeof(G) >= kLongRow ? 1u : kZeroWords;         // words of k.present
+    const uint32_t zeroing = k.present ? (uint32_t)(((uint64_t)k.vocab + 32 * per_block - 1) / (32 * per_block)) : 0u;
     k.arrived = reinterpret_cast<uint32_t *>(ws + L.arrived);
     k.n_arrived = L.n_chunks * L.slices;
     if (L.small) {
@@ -254,14 +255,14 @@ cudaError_t run_embed_grad(EmbedArgs k, const EmbedGradLayout &L, uint8_t *ws, b
     } else {
         // the last placing kernel leaves most of the machine idle for about 8 us: room to clear some 40 MB of rows
         if (L.passes > 1) {
-            const uint64_t some = (40ull << 20) / (32 * (uint64_t)k.dim * sizeof(G)) + 1;
-            k.zero_from = some < words ? (uint32_t)some : words;
+            const uint64_t some = (40ull << 20) / (32 * per_block * (uint64_t)k.dim * sizeof(G)) + 1;
+            k.zero_from = some < zeroing ? (uint32_t)some : zeroing;
         }
         rc = L.big_tiles ? run_sort<16>(k, L, ws, st) : run_sort<4>(k, L, ws, st);
     }
     if (rc != cudaSuccess) return rc;
     const uint32_t sum_blocks = (uint32_t)(((uint64_t)L.n_chunks * L.slices + kSumThreads / 32 - 1) / (kSumThreads / 32));
-    const uint32_t zero_blocks = words - k.zero_from;
+    const uint32_t zero_blocks = zeroing - k.zero_from;
     if (sum_blocks + zero_blocks == 0) return cudaSuccess;
     const uint64_t grid = (uint64_t)sum_blocks + zero_blocks;
     const size_t smem = sum_blocks ? kSumWarps * (wide ? SumLayout<T, true>::kWarpBytes : SumLayout<T, false>::kWarpBytes) : 0;
