@@ -25,7 +25,7 @@ struct EmbedArgs {
     uint32_t *present;                   // [ceil(vocab / 32)] a bit per id that occurs, or nullptr
     float *partial;                      // [2][n_chunks][partial_stride]: sums of a run cut by the chunk's start / by its end
     size_t partial_stride;               // dim rounded up to a warp's columns
-    uint32_t *arrived;                   // [n_chunks][slices] parts stored of the cut run that begins in the chunk
+    uint32_t *arrived;                   // [3][n_chunks][slices] parts, and groups of parts, stored of cut runs
     uint32_t n_arrived, zero_from;       // blocks of zero_rows that ran before the sums
 };
 
@@ -235,8 +235,12 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedAr
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t n = tokens_in(a), items = (a.n_tokens + kSmallThreads - 1) / kSmallThreads, base = warp * items * 32 + lane;
     for (uint32_t w = threadIdx.x; w < a.n_arrived; w += kSmallThreads) a.arrived[w] = 0u;
+    // the bits of the ids that occur: in shared memory (the place of the counts) where there is room for the vocabulary
+    const uint32_t words = (a.vocab + 31) / 32;
+    const bool near = words <= kSmallWarps * kSortBins / 2;
+    uint32_t *bits = near ? reinterpret_cast<uint32_t *>(sort_smem) : a.present;
     if (a.present) {
-        for (uint32_t w = threadIdx.x; w < (a.vocab + 31) / 32; w += kSmallThreads) a.present[w] = 0u;
+        for (uint32_t w = threadIdx.x; w < words; w += kSmallThreads) bits[w] = 0u;
         __syncthreads();
     }
     const uint32_t busy = items ? (a.n_tokens + items * 32 - 1) / (items * 32) : 0;        // warps that have entries
@@ -249,8 +253,13 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedAr
         if (at[k] < a.n_tokens) {
             in_mask |= 1u << k;
             key[k] = id_at(a, at[k], n);
-            if (a.present && key[k] < a.vocab) atomicOr(a.present + (key[k] >> 5), 1u << (key[k] & 31u));
+            if (a.present && key[k] < a.vocab) atomicOr(bits + (key[k] >> 5), 1u << (key[k] & 31u));
         }
+    }
+    if (a.present && near) {
+        __syncthreads();
+        for (uint32_t w = threadIdx.x; w < words; w += kSmallThreads) a.present[w] = bits[w];
+        __syncthreads();
     }
     for (uint32_t p = 0; p < passes; ++p) {
         if (p) {
@@ -282,15 +291,15 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedAr
             if ((uint32_t)k >= items) break;
             if (!((in_mask >> k) & 1u)) continue;
             const uint32_t d = (key[k] >> shift) & (kSortBins - 1), to = bin_start[d] + warp_bins[warp][d] + rank[k];
-            if (p + 1 < passes) {
-                keys[to] = key[k];
-                pos[to] = (uint16_t)at[k];
-            } else {
-                a.keys[to] = key[k];
-                a.pos[to] = at[k];
-            }
+            keys[to] = key[k];
+            pos[to] = (uint16_t)at[k];
         }
         __syncthreads();
+    }
+    // stores to scattered places take one block about a cycle each: out in order, from shared memory
+    for (uint32_t i = threadIdx.x; i < a.n_tokens; i += kSmallThreads) {
+        a.keys[i] = keys[i];
+        a.pos[i] = pos[i];
     }
 }
 
@@ -497,8 +506,24 @@ __device__ __forceinline__ float *partial_row(const EmbedArgs &a, uint32_t which
     return a.partial + ((size_t)which * a.n_chunks + chunk) * a.partial_stride;
 }
 
+template <bool kWide>
+__device__ __forceinline__ void store_partial(const EmbedArgs &a, uint32_t which, uint32_t chunk, uint32_t c0, const f32x2 (&sum)[kSumPairs]) {
+    float *to = partial_row(a, which, chunk) + c0, x[kSumCols];
+#pragma unroll
+    for (int k = 0; k < kSumPairs; ++k) unpack2(sum[k], x[2 * k], x[2 * k + 1]);
+    if constexpr (kWide) {
+        float4 *p = reinterpret_cast<float4 *>(to + pair_column<true>(0));
+        __stcg(p, make_float4(x[0], x[1], x[2], x[3]));
+        __stcg(p + 1, make_float4(x[4], x[5], x[6], x[7]));
+    } else {
+#pragma unroll
+        for (int k = 0; k < kSumPairs; ++k) __stcg(reinterpret_cast<float2 *>(to + pair_column<false>(k)), make_float2(x[2 * k], x[2 * k + 1]));
+    }
+}
+
 // The parts of a run that chunk borders cut, of which this warp has just stored one (run v; cont: it began before
 // `chunk`): whichever warp stores the last one adds them up, in the order of the chunks.  True for that warp.
+constexpr uint32_t kJoinGroup = 16;
 template <bool kWide>
 __device__ __forceinline__ bool join_run(const EmbedArgs &a, uint32_t v, uint32_t chunk, bool cont, uint32_t slice, uint32_t slices, f32x2 (&sum)[kSumPairs]) {
     const uint32_t lane = threadIdx.x & 31u, c0 = slice * kSumWarpCols;
@@ -519,47 +544,44 @@ __device__ __forceinline__ bool join_run(const EmbedArgs &a, uint32_t v, uint32_
             back += 32;
         }
     const uint32_t owner = chunk - back, parts = back + behind;      // `parts` partial 0, and the owner's partial 1
-    __threadfence();
-    __syncwarp();
-    uint32_t before = 0;
-    if (lane == 0) before = atomicAdd(a.arrived + (size_t)owner * slices + slice, 1u);
-    if (__shfl_sync(kFullMask, before, 0) != parts) return false;
-    __threadfence();
-    constexpr uint32_t kAhead = 8;
-    for (uint32_t p = 0; p <= parts; p += kAhead) {
-        float2 x[kAhead][kSumPairs];
+    const size_t counters = (size_t)a.n_chunks * slices;
+    // part q: the owner's partial 1, then the following chunks' partial 0.  Groups of kJoinGroup parts are added up
+    // first, each by the last to arrive, then the groups' sums, which take the place of their first part.
+    uint32_t group = back / kJoinGroup;
+#pragma unroll 1
+    for (uint32_t level = 0;; ++level) {
+        const uint32_t from = level == 0 ? group * kJoinGroup : 0u, step = level == 0 ? 1u : kJoinGroup;
+        const uint32_t terms = level == 0 ? min(kJoinGroup, parts + 1 - from) : parts / kJoinGroup + 1;
+        // a chunk may begin one run and start a group of another: three sets of counters
+        uint32_t *counter = a.arrived + (level ? 2 * counters : group ? counters : 0u) + (size_t)(owner + from) * slices + slice;
+        __threadfence();
+        __syncwarp();
+        uint32_t before = 0;
+        if (lane == 0) before = atomicAdd(counter, 1u);
+        if (__shfl_sync(kFullMask, before, 0) != terms - 1) return false;
+        __threadfence();
+        constexpr uint32_t kAhead = 8;
+        for (uint32_t t = 0; t < terms; t += kAhead) {
+            float2 x[kAhead][kSumPairs];
 #pragma unroll
-        for (uint32_t u = 0; u < kAhead; ++u) {
-            const uint32_t q = min(p + u, parts);
-            const float *from = (q ? partial_row(a, 0, owner + q) : partial_row(a, 1, owner)) + c0;
+            for (uint32_t u = 0; u < kAhead; ++u) {
+                const uint32_t q = from + min(t + u, terms - 1) * step;
+                const float *p = (q ? partial_row(a, 0, owner + q) : partial_row(a, 1, owner)) + c0;
 #pragma unroll
-            for (int k = 0; k < kSumPairs; ++k) x[u][k] = __ldcg(reinterpret_cast<const float2 *>(from + pair_column<kWide>(k)));
-        }
+                for (int k = 0; k < kSumPairs; ++k) x[u][k] = __ldcg(reinterpret_cast<const float2 *>(p + pair_column<kWide>(k)));
+            }
 #pragma unroll
-        for (uint32_t u = 0; u < kAhead; ++u) {
-            if (p + u > parts) break;
+            for (uint32_t u = 0; u < kAhead; ++u) {
+                if (t + u >= terms) break;
 #pragma unroll
-            for (int k = 0; k < kSumPairs; ++k) {
-                const f32x2 y = pack2(x[u][k].x, x[u][k].y);
-                sum[k] = p + u ? add2(sum[k], y) : y;
+                for (int k = 0; k < kSumPairs; ++k) {
+                    const f32x2 y = pack2(x[u][k].x, x[u][k].y);
+                    sum[k] = t + u ? add2(sum[k], y) : y;
+                }
             }
         }
-    }
-    return true;
-}
-
-template <bool kWide>
-__device__ __forceinline__ void store_partial(const EmbedArgs &a, uint32_t which, uint32_t chunk, uint32_t c0, const f32x2 (&sum)[kSumPairs]) {
-    float *to = partial_row(a, which, chunk) + c0, x[kSumCols];
-#pragma unroll
-    for (int k = 0; k < kSumPairs; ++k) unpack2(sum[k], x[2 * k], x[2 * k + 1]);
-    if constexpr (kWide) {
-        float4 *p = reinterpret_cast<float4 *>(to + pair_column<true>(0));
-        __stcg(p, make_float4(x[0], x[1], x[2], x[3]));
-        __stcg(p + 1, make_float4(x[4], x[5], x[6], x[7]));
-    } else {
-#pragma unroll
-        for (int k = 0; k < kSumPairs; ++k) __stcg(reinterpret_cast<float2 *>(to + pair_column<false>(k)), make_float2(x[2 * k], x[2 * k + 1]));
+        if (level == 1 || parts < kJoinGroup) return true;
+        store_partial<kWide>(a, from ? 0u : 1u, owner + from, c0, sum);
     }
 }
 

@@ -31,10 +31,10 @@ constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kFarBelow = -1000.0f;    // 2^-1000 is 0 in float: scores below it contribute nothing, and stay finite
 
 // Target of token t, or -1; a target past the vocabulary is reported.
-__device__ __forceinline__ int32_t target_of(const LogprobArgs &a, uint32_t t) {
+__device__ __forceinline__ int32_t target_of(const LogprobArgs &a, uint32_t t, bool report) {
     const int32_t y = __ldg(a.targets + t);
     if (y >= 0 && (uint32_t)y >= a.vocab) {
-        if (a.status && threadIdx.x == 0) atomicOr(a.status, TD_ERR_OOB_INDEX);
+        if (a.status && report) atomicOr(a.status, TD_ERR_OOB_INDEX);
         return -1;
     }
     return y;
@@ -122,10 +122,10 @@ constexpr int kLogprobUnroll = 4;
 // One pass over the vectors [lo, hi) of a row, and for the row's first part over the ends that do not fill a
 // vector (at most 2 (kVec - 1) elements).
 template <typename T, bool kEntropy, bool kSafe, int kThreads>
-__device__ __forceinline__ Share pass_over(const T *x, uint32_t vocab, uint32_t head, uint32_t nvec, uint32_t lo, uint32_t hi, bool ends, float scale2) {
+__device__ __forceinline__ Share pass_over(const T *x, uint32_t vocab, uint32_t head, uint32_t nvec, uint32_t lo, uint32_t hi, bool ends, float scale2, uint32_t tid) {
     constexpr int E = Elem<T>::kVec, U = kLogprobUnroll;
     constexpr uint32_t kChunk = U * kThreads;
-    const uint4 *xv = reinterpret_cast<const uint4 *>(x + head) + lo + threadIdx.x;
+    const uint4 *xv = reinterpret_cast<const uint4 *>(x + head) + lo + tid;
     const uint32_t n = hi - lo, full = n / kChunk;
     Share r{kSafe ? -FLT_MAX : fmaxf(0.5f * Elem<T>::kLow * scale2, -FLT_MAX), -CUDART_INF_F, pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
     uint4 p[U], q[U];
@@ -138,14 +138,14 @@ __device__ __forceinline__ Share pass_over(const T *x, uint32_t vocab, uint32_t 
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             v[u].x = v[u].y = v[u].z = v[u].w = Elem<T>::kFill;
-            if (full * kChunk + u * kThreads + threadIdx.x < n) v[u] = ld_stream(xv + (size_t)full * kChunk + u * kThreads);
+            if (full * kChunk + u * kThreads + tid < n) v[u] = ld_stream(xv + (size_t)full * kChunk + u * kThreads);
         }
     };
     if (full) fetch(p, 0); else rest(p);
     if (ends) {
         const uint32_t tail = head + nvec * E, n_loose = head + (vocab - tail);
-        if (threadIdx.x < n_loose) {
-            float z = Elem<T>::load(x + (threadIdx.x < head ? threadIdx.x : tail + threadIdx.x - head));
+        if (tid < n_loose) {
+            float z = Elem<T>::load(x + (tid < head ? tid : tail + tid - head));
             if (!kSafe) z = max_nan(z, Elem<T>::kLow);
             r.top = z;
             r.ref = kSafe ? fmaxf(z, -FLT_MAX) : fmaxf(z * scale2, r.ref);
@@ -170,17 +170,21 @@ __device__ __forceinline__ Share pass_over(const T *x, uint32_t vocab, uint32_t 
     return r;
 }
 
-// One row per cluster of `parts` blocks (1 to 8).  A single pass over the row: every thread keeps a reference and
+// One row per cluster of `parts` blocks (1 to 8); or, kThreads = 32, per warp, kWarpRows rows a block.  A single pass over the row: every thread keeps a reference and
 // sums over its share, and the shares are joined in a fixed order over the warp, the block and (through
 // distributed shared memory) the cluster.
+constexpr int kWarpRows = 4;
 template <typename T, bool kEntropy, int kThreads>
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprob_kernel(const LogprobArgs a) {
+__global__ void __launch_bounds__(kThreads == 32 ? 32 * kWarpRows : kThreads, kThreads == 32 ? 32 / kWarpRows : 1024 / kThreads)
+token_logprob_kernel(const LogprobArgs a) {
     griddep_launch_dependents();
     griddep_wait();
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
-    const uint32_t parts = cluster.num_blocks(), part = cluster.block_rank();
-    const uint32_t t = blockIdx.x / parts;
+    constexpr bool kWarpRow = kThreads == 32;
+    const uint32_t parts = kWarpRow ? 1u : cluster.num_blocks(), part = kWarpRow ? 0u : cluster.block_rank();
+    const uint32_t t = kWarpRow ? blockIdx.x * kWarpRows + threadIdx.x / 32 : blockIdx.x / parts, tid = kWarpRow ? threadIdx.x & 31u : threadIdx.x;
+    if (kWarpRow && t >= a.n_tokens) return;
     struct Part { Running sums; float top; };
     __shared__ Part warp_part[kThreads / 32], block_part;
     __shared__ bool quick_holds;
@@ -197,9 +201,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprob_kerne
             have_row = row >= (long long)a.batch.cu_prompt[i] + a.batch.cu_response[i] && row < (long long)a.n_rows;
         }
     }
-    const int32_t y = target_of(a, t);
+    const int32_t y = target_of(a, t, tid == 0);
     if (!have_row || y < 0) {
-        if (part == 0 && threadIdx.x == 0) {
+        if (part == 0 && tid == 0) {
             a.logprob[t] = 0.0f;
             if (a.norm) { a.norm[2ull * t] = 0.0f; a.norm[2ull * t + 1] = 0.0f; }
             if (a.entropy) a.entropy[t] = 0.0f;
@@ -230,6 +234,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprob_kerne
             }
         };
         over_lanes();
+        if constexpr (kWarpRow) return Part{r, top};         // the same in all lanes
         if (lane == 0) warp_part[warp] = Part{r, top};
         __syncthreads();
         if (warp == 0) {
@@ -252,24 +257,24 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) token_logprob_kerne
         return Part{r, top};
     };
 
-    Part all = join_all(pass_over<T, kEntropy, false, kThreads>(x, a.vocab, head, nvec, lo, hi, part == 0, a.scale2), 1.0f);
-    // the first block says whether that was right, the others look
-    if (part == 0 && threadIdx.x == 0)
-        quick_holds = a.scale2 < 1e8f && fabsf(all.top) * a.scale2 < 1e30f && (all.top - 0.5f * Elem<T>::kLow) * a.scale2 > -kFarBelow;
-    bool quick;
-    if (parts > 1) {
-        cluster.sync();
-        quick = *cluster.map_shared_rank(&quick_holds, 0);
-        cluster.sync();                                      // a block's shared memory stays until it has been read
-    } else {
-        __syncthreads();
-        quick = quick_holds;
+    Part all = join_all(pass_over<T, kEntropy, false, kThreads>(x, a.vocab, head, nvec, lo, hi, part == 0, a.scale2, tid), 1.0f);
+    bool quick = a.scale2 < 1e8f && fabsf(all.top) * a.scale2 < 1e30f && (all.top - 0.5f * Elem<T>::kLow) * a.scale2 > -kFarBelow;
+    if constexpr (!kWarpRow) {           // the first block's first thread has the maximum and says; the others look
+        if (part == 0 && threadIdx.x == 0) quick_holds = quick;
+        if (parts > 1) {
+            cluster.sync();
+            quick = *cluster.map_shared_rank(&quick_holds, 0);
+            cluster.sync();                                  // a block's shared memory stays until it has been read
+        } else {
+            __syncthreads();
+            quick = quick_holds;
+        }
     }
     if (!quick) {
-        all = join_all(pass_over<T, kEntropy, true, kThreads>(x, a.vocab, head, nvec, lo, hi, part == 0, a.scale2), a.scale2);
+        all = join_all(pass_over<T, kEntropy, true, kThreads>(x, a.vocab, head, nvec, lo, hi, part == 0, a.scale2, tid), a.scale2);
         if (parts > 1) cluster.sync();
     }
-    if (part == 0 && threadIdx.x == 0) {
+    if (part == 0 && tid == 0) {
         const Running r = all.sums;
         const bool none = r.s == 0.0f;                       // every logit -inf
         const float ln_s = none ? 0.0f : logf(r.s);
@@ -292,13 +297,17 @@ constexpr int kGradThreads = 256, kGradUnroll = 4;
 constexpr uint32_t kGradVectors = kGradThreads * kGradUnroll * 4;        // vectors of a row per block
 
 // One block per (row, chunk of the row).  kSame: a row of logits and its gradient's start at the same offset
-// from a 16-byte boundary; else the logits' vectors are put together from two loads each.
-template <typename T, bool kSame>
+// from a 16-byte boundary; else the logits' vectors are put together from two loads each.  kTeam = 32: a row
+// per warp.
+template <typename T, bool kSame, int kTeam>
 __global__ void __launch_bounds__(kGradThreads, kSame ? 4 : 3) token_logprob_grad_kernel(const LogprobArgs a) {
     griddep_launch_dependents();
     griddep_wait();
-    const uint32_t chunk = blockIdx.x % a.chunks;
-    const long long row = blockIdx.x / a.chunks;
+    constexpr bool kWarpRow = kTeam == 32;
+    const uint32_t tid = kWarpRow ? threadIdx.x & 31u : threadIdx.x;
+    const uint32_t chunk = kWarpRow ? 0u : blockIdx.x % a.chunks;
+    const long long row = kWarpRow ? (long long)blockIdx.x * (kGradThreads / 32) + threadIdx.x / 32 : blockIdx.x / a.chunks;
+    if (kWarpRow && row >= (long long)a.n_rows) return;
     const T *x = static_cast<const T *>(a.logits) + row * a.stride;
     T *out = static_cast<T *>(a.grad) + row * a.grad_stride;
     constexpr int E = Elem<T>::kVec, U = kGradUnroll;
@@ -323,7 +332,7 @@ __global__ void __launch_bounds__(kGradThreads, kSame ? 4 : 3) token_logprob_gra
     float ca = 0.0f, cb = 0.0f, g = 0.0f, m = 0.0f, log2_s = 0.0f;
     int32_t y = -1;
     if (t >= 0) {
-        y = target_of(a, (uint32_t)t);
+        y = target_of(a, (uint32_t)t, tid == 0 && chunk == 0);
         g = a.grad_logprob ? a.grad_logprob[t] : 0.0f;
         const float h = a.grad_entropy ? a.grad_entropy[t] : 0.0f;
         m = a.norm_in[2 * t];
@@ -336,7 +345,7 @@ __global__ void __launch_bounds__(kGradThreads, kSame ? 4 : 3) token_logprob_gra
     // the row's vectors are aligned on the place it is written to
     const uint32_t head = min((16u - (uint32_t)(reinterpret_cast<uintptr_t>(out) & 15u)) % 16u / (uint32_t)sizeof(T), a.vocab);
     const uint32_t nvec = (a.vocab - head) / E;
-    const uint32_t lo = chunk * kGradVectors, hi = min(nvec, lo + kGradVectors);
+    const uint32_t lo = chunk * kGradVectors, hi = kWarpRow ? nvec : min(nvec, lo + kGradVectors);
     const float gy = g * a.inv_tau;
     auto value = [&](float z, uint32_t v) {
         const float d = max_nan(fmaf(z - m, a.scale2, -log2_s), kFarBelow);
@@ -344,38 +353,38 @@ __global__ void __launch_bounds__(kGradThreads, kSame ? 4 : 3) token_logprob_gra
     };
     if (chunk == 0) {                                        // the ends that do not fill a vector
         const uint32_t tail = head + nvec * E, n_loose = head + (a.vocab - tail);
-        if (threadIdx.x < n_loose) {
-            const uint32_t v = threadIdx.x < head ? threadIdx.x : tail + threadIdx.x - head;
+        if (tid < n_loose) {
+            const uint32_t v = tid < head ? tid : tail + tid - head;
             out[v] = Elem<T>::from(zero ? 0.0f : value(Elem<T>::load(x + v), v));
         }
     }
     uint4 *ov = reinterpret_cast<uint4 *>(out + head);
     if (zero) {
         const uint4 z = make_uint4(0u, 0u, 0u, 0u);
-        for (uint32_t i = lo + threadIdx.x; i < hi; i += kGradThreads) st_stream(ov + i, z);
+        for (uint32_t i = lo + tid; i < hi; i += kTeam) st_stream(ov + i, z);
         return;
     }
     const T *xh = x + head, *begin = static_cast<const T *>(a.logits), *end = begin + (long long)(a.n_rows - 1) * a.stride + a.vocab;
     const uint32_t y_vec = (uint32_t)y >= head ? ((uint32_t)y - head) / E : 0xffffffffu, y_in = ((uint32_t)y - head) % E;
     const f32x2 neg = pack2(-m, -m), sc = pack2(a.scale2, a.scale2), off = pack2(-log2_s, -log2_s), c0 = pack2(ca, ca), c1 = pack2(cb, cb);
-    for (uint32_t i = lo + threadIdx.x; i < hi; i += kGradThreads * U) {
+    for (uint32_t i = lo + tid; i < hi; i += kTeam * U) {
         uint4 v[U];
         if constexpr (kSame) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (i + u * kGradThreads < hi) v[u] = ld_stream(xh + (size_t)(i + u * kGradThreads) * E);
+                if (i + u * kTeam < hi) v[u] = ld_stream(xh + (size_t)(i + u * kTeam) * E);
         } else {
             Window<T> w[U];
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (i + u * kGradThreads < hi) w[u].open(xh + (size_t)(i + u * kGradThreads) * E, begin, end);
+                if (i + u * kTeam < hi) w[u].open(xh + (size_t)(i + u * kTeam) * E, begin, end);
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (i + u * kGradThreads < hi) v[u] = w[u].close();
+                if (i + u * kTeam < hi) v[u] = w[u].close();
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint32_t j = i + u * kGradThreads;
+            const uint32_t j = i + u * kTeam;
             if (j >= hi) break;
             uint4 o;
 #pragma unroll

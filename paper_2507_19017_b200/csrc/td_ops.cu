@@ -114,7 +114,7 @@ LogprobArgs logprob_args(const A *a) {
 template <typename T>
 cudaError_t run_logprob(const LogprobArgs &k, cudaStream_t st) {
     // Blocks per row (a cluster joins them) and threads per block, by the rows there are to fill 148 SMs with.
-    // Measured in us, bfloat16 vocabulary 129280: 1 row 4.1 on 8 x 256 threads, 5.0 on 4 x 128; 74 rows 7.8 on
+    // In us, bfloat16, a vocabulary of 129280: 1 row 4.1 on 8 x 256 threads, 5.0 on 4 x 128; 74 rows 7.8 on
     // 2 x 512, 8.6 on 1 x 512; 148 rows 9.8 on 1 x 512, 12.2 on 1 x 256; 500 rows 25.6 on 256, 26.5 on 512;
     // 1200 rows 54.4 on 256, 59.2 on 128; 8192 rows of 152064 405 on 128, 410 on 256.  Rows of fewer than 8192
     // vectors gain nothing from a second block (32003: 3.6 on one, 3.9 on two), and a block wants four
@@ -128,6 +128,10 @@ cudaError_t run_logprob(const LogprobArgs &k, cudaStream_t st) {
     auto go128 = [&]() { return go(token_logprob_kernel<T, true, 128>, token_logprob_kernel<T, false, 128>, 128, 1); };
     auto go256 = [&](uint32_t parts) { return go(token_logprob_kernel<T, true, 256>, token_logprob_kernel<T, false, 256>, 256, parts); };
     auto go512 = [&](uint32_t parts) { return go(token_logprob_kernel<T, true, 512>, token_logprob_kernel<T, false, 512>, 512, parts); };
+    // Short rows go a warp each, four to a block: 8000 rows of 1000 6.9 (a block each 22.0), of 6000 19.2 (29.1);
+    // 2000 rows of 6000 9.6 both ways, 200 rows 3.5 (3.2).
+    if (nvec < (rows >= 4096 ? 1024 : 512))
+        return launch(entropy ? token_logprob_kernel<T, true, 32> : token_logprob_kernel<T, false, 32>, ((uint64_t)rows + 3) / 4, 128, st, 1u, k);
     if (nvec >= 8192 && rows <= 74) return rows <= 18 ? go256(8) : go512(rows <= 37 ? 4 : 2);
     if (nvec >= 2048 && rows <= 296) return go512(1);
     if (nvec >= 1024 && rows <= (sizeof(T) == 4 ? 592 : 1200)) return go256(1);
@@ -137,7 +141,15 @@ template <typename T>
 cudaError_t run_logprob_grad(const LogprobArgs &k, cudaStream_t st) {
     const bool same = ((reinterpret_cast<uintptr_t>(k.logits) ^ reinterpret_cast<uintptr_t>(k.grad)) & 15u) == 0 &&
                       (k.stride - k.grad_stride) * (long long)sizeof(T) % 16 == 0;
-    return launch(same ? token_logprob_grad_kernel<T, true> : token_logprob_grad_kernel<T, false>, (uint64_t)k.n_rows * k.chunks, kGradThreads, st, 1u, k);
+    // Short rows go a warp each: 40000 rows of 1000 bfloat16 29 us (a block each 87), of 6000 154 (178); 2000 rows of
+    // 4000 9.9 (9.4), of 1000 3.3 (5.4); 200 rows of 2000 2.9 (2.1).
+    if (k.vocab / Elem<T>::kVec < (k.n_rows >= 4096 ? 1024u : k.n_rows >= 1024 ? 256u : 128u)) {
+        constexpr uint32_t kRows = kGradThreads / 32;
+        return launch(same ? token_logprob_grad_kernel<T, true, 32> : token_logprob_grad_kernel<T, false, 32>, ((uint64_t)k.n_rows + kRows - 1) / kRows,
+                      kGradThreads, st, 1u, k);
+    }
+    return launch(same ? token_logprob_grad_kernel<T, true, kGradThreads> : token_logprob_grad_kernel<T, false, kGradThreads>,
+                  (uint64_t)k.n_rows * k.chunks, kGradThreads, st, 1u, k);
 }
 
 uint32_t policy_blocks(uint64_t n_tokens) {
@@ -148,7 +160,7 @@ uint32_t policy_blocks(uint64_t n_tokens) {
 // The instance for a call: positions per access, the KL term's form, mask and entropy or none.
 template <int kVec, int kKl, bool kMask, bool kEnt>
 cudaError_t run_policy(const PolicyArgs &k, cudaStream_t st) {
-    constexpr size_t smem = kPolicyStages * PolicyStage<kVec, kKl, kMask, kEnt>::kBytes;
+    constexpr size_t smem = PolicyStage<kVec, kKl, kMask, kEnt>::kStages * PolicyStage<kVec, kKl, kMask, kEnt>::kBytes;
     if (smem > 40 * 1024) {                                  // with the fixed arrays, beyond the 48 KB a launch gets unasked
         const cudaError_t rc = cudaFuncSetAttribute(policy_loss_kernel<kVec, kKl, kMask, kEnt>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (rc != cudaSuccess) return rc;
@@ -180,7 +192,7 @@ cudaError_t run_embed(const EmbedArgs &k, bool whole, cudaStream_t st) {
 // machine, long ones later (a run cut by a border costs two float rows of extra traffic, and one warp joins
 // its parts).  65536 positions x 8 slices: 295 us with 64, 327 with 32, 309 with 128.
 uint32_t chunk_rows(uint32_t n_tokens, uint32_t slices) {
-    uint32_t r = n_tokens <= 2048 ? 8 : 32;
+    uint32_t r = 8;
     while (r < 512 && (uint64_t)n_tokens * slices > (uint64_t)r * 148 * 64) r *= 2;
     return r;
 }
@@ -207,7 +219,7 @@ EmbedGradLayout embed_layout(uint32_t n_tokens, uint32_t vocab, uint32_t dim) {
     for (int k = 0; k < 2; ++k) { L.keys[k] = take((size_t)n_tokens * 4); L.pos[k] = take((size_t)n_tokens * 4); }
     L.counts = take((size_t)L.passes * L.n_tiles * kSortBins * 4);
     L.present = take(((size_t)vocab + 31) / 32 * 4);
-    L.arrived = take((size_t)L.n_chunks * L.slices * 4);
+    L.arrived = take(3 * (size_t)L.n_chunks * L.slices * 4);
     L.partial = take(2 * (size_t)L.n_chunks * L.partial_stride * 4);
     L.total = p;
     return L;
@@ -245,7 +257,7 @@ cudaError_t run_embed_grad(EmbedArgs k, const EmbedGradLayout &L, uint8_t *ws, b
     const uint32_t per_block = (uint64_t)k.dim * sizeof(G) >= kLongRow ? 1u : kZeroWords;         // words of k.present
     const uint32_t zeroing = k.present ? (uint32_t)(((uint64_t)k.vocab + 32 * per_block - 1) / (32 * per_block)) : 0u;
     k.arrived = reinterpret_cast<uint32_t *>(ws + L.arrived);
-    k.n_arrived = L.n_chunks * L.slices;
+    k.n_arrived = 3 * L.n_chunks * L.slices;
     if (L.small) {
         rc = cudaFuncSetAttribute(sort_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem);
         if (rc != cudaSuccess) return rc;
@@ -442,7 +454,7 @@ int td_embed_grad(const td_embed_grad_args *a, void *stream) {
     if (a->n_tokens && (!a->ids || !a->grad_out || !aligned(a->ids, 4) || !aligned(a->grad_out, es))) return TD_EINVAL;
     const EmbedGradLayout L = embed_layout(a->n_tokens, a->vocab, a->dim);
     if (!a->workspace || !aligned(a->workspace, 256) || a->workspace_bytes < L.total) return TD_EWORKSPACE;
-    if ((uint64_t)L.n_chunks * L.slices + (uint64_t)a->vocab / 32 >= kMaxGrid) return TD_EINVAL;          // also keeps n_arrived in 32 bits
+    if (3 * (uint64_t)L.n_chunks * L.slices + (uint64_t)a->vocab / 32 >= kMaxGrid) return TD_EINVAL;          // also keeps n_arrived in 32 bits
     DeviceGuard dev(a->device);
     if (!dev.ok()) return TD_ECUDA;
     EmbedArgs k{};

@@ -245,13 +245,13 @@ struct PolicyArrays {
     float *grad_logprob, *grad_entropy;
     int limit;                           // positions up to the arrays' end, or more than the share has
 };
-// What is on its way for a block: kPolicyStages turns of every array in use, each thread's elements in
-// a slot of its own.
-constexpr int kPolicyStages = 3;
+// What is on its way for a block: kStages turns of every array in use, each thread's elements in a slot of its own.
+// Three, or two where three would leave no room for four blocks on an SM (the whole grid is resident at once).
 template <int kVec, int kKl, bool kMask, bool kEnt>
 struct PolicyStage {
     static constexpr int kArrays = 2 + (kKl != kNoKl) + kEnt;
     static constexpr size_t kBytes = (size_t)kPolicyThreads * (kArrays * kVec * 4 + (kMask ? 4 : 0));      // of one turn
+    static constexpr int kStages = 3 * kBytes > 48 * 1024 ? 2 : 3;
     float *at;
     __device__ __forceinline__ PolicyStage(uint8_t *smem, int stage) : at(reinterpret_cast<float *>(smem + stage * kBytes)) {}
     __device__ __forceinline__ float *slot(int array) const { return at + ((size_t)array * kPolicyThreads + threadIdx.x) * kVec; }
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kPolicyThreads, kPolicyBlocksPerSm) policy_los
     constexpr int kTurn = kPolicyThreads * kVec;
     int rel = (int)threadIdx.x * kVec;
 #pragma unroll
-    for (int k = 0; k < kPolicyStages; ++k) {
+    for (int k = 0; k < Stage::kStages; ++k) {
         if (rel + k * kTurn < size) Stage(policy_smem, k).fetch(arr, a.bf16_columns, rel + k * kTurn);
         copy_commit();
     }
@@ -400,13 +400,13 @@ __global__ void __launch_bounds__(kPolicyThreads, kPolicyBlocksPerSm) policy_los
         seat.most = adv < 0.0f ? -adv * a.dual_clip : CUDART_INF_F;         // dual_clip = inf: no limit
     };
 
-    for (int k = 0; rel < size; k = k + 1 == kPolicyStages ? 0 : k + 1) {
+    for (int k = 0; rel < size; k = k + 1 == Stage::kStages ? 0 : k + 1) {
         // kPairs pairs of positions; a single position goes as a pair whose second is off
         constexpr int kPairs = (kVec + 1) / 2;
         f32x2 raw[kPairs], gap[kPairs];
         float en[kVec], gl[2 * kPairs], ge[2 * kPairs];
         uint32_t on = 0xffffffffu;
-        copy_wait<kPolicyStages - 1>();
+        copy_wait<Stage::kStages - 1>();
         {
             const Stage stage(policy_smem, k);
             float lp[kVec], old[kVec], ref[kVec];
@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(kPolicyThreads, kPolicyBlocksPerSm) policy_los
                 raw[j] = arr.old_logprob ? pack2(lp[x] - old[x], lp[y] - old[y]) : both(0.0f);
                 gap[j] = kKl != kNoKl ? pack2(ref[x] - lp[x], ref[y] - lp[y]) : both(0.0f);
             }
-            const int ahead = rel + kPolicyStages * kTurn;
+            const int ahead = rel + Stage::kStages * kTurn;
             if (ahead < size) stage.fetch(arr, a.bf16_columns, ahead);
             copy_commit();
         }
