@@ -88,17 +88,18 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a,
         }
     } else {
         const T *end = table + (long long)(a.vocab - 1) * a.table_stride + a.dim;
+        const bool edge = id == 0 || id == a.vocab - 1;
         Window<T> w[kEmbedUnroll];
 #pragma unroll
         for (int u = 0; u < kEmbedUnroll; ++u) {
             const uint32_t j = lo + (u << team) + lane;
-            if (j < nvec && !none) w[u].open(row + head + j * E, table, end);
+            if (j < nvec && !none) w[u].open(row + head + j * E, table, end, edge);
         }
 #pragma unroll
         for (int u = 0; u < kEmbedUnroll; ++u) {
             const uint32_t j = lo + (u << team) + lane;
             v[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (j < nvec && !none) v[u] = w[u].close();
+            if (j < nvec && !none) v[u] = w[u].close(row + head + j * E);
         }
     }
     const f32x2 sc = pack2(a.scale, a.scale);

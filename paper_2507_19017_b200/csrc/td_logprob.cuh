@@ -364,6 +364,7 @@ __global__ void __launch_bounds__(kGradThreads, kSame ? 4 : 3) token_logprob_gra
         for (uint32_t i = lo + tid; i < hi; i += kTeam) st_stream(ov + i, z);
         return;
     }
+    const bool edge = row == 0 || row == (long long)a.n_rows - 1 || a.stride < (long long)a.vocab;      // rows may overlap
     const T *xh = x + head, *begin = static_cast<const T *>(a.logits), *end = begin + (long long)(a.n_rows - 1) * a.stride + a.vocab;
     const uint32_t y_vec = (uint32_t)y >= head ? ((uint32_t)y - head) / E : 0xffffffffu, y_in = ((uint32_t)y - head) % E;
     const f32x2 neg = pack2(-m, -m), sc = pack2(a.scale2, a.scale2), off = pack2(-log2_s, -log2_s), c0 = pack2(ca, ca), c1 = pack2(cb, cb);
@@ -377,10 +378,10 @@ __global__ void __launch_bounds__(kGradThreads, kSame ? 4 : 3) token_logprob_gra
             Window<T> w[U];
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (i + u * kTeam < hi) w[u].open(xh + (size_t)(i + u * kTeam) * E, begin, end);
+                if (i + u * kTeam < hi) w[u].open(xh + (size_t)(i + u * kTeam) * E, begin, end, edge);
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (i + u * kTeam < hi) v[u] = w[u].close();
+                if (i + u * kTeam < hi) v[u] = w[u].close(xh + (size_t)(i + u * kTeam) * E);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {

@@ -175,36 +175,38 @@ template <> struct Elem<__half> {
     static __device__ __forceinline__ __half from(float x) { return __float2half_rn(x); }
 };
 
-// 16 bytes that start `phase` bytes (even, below 16) into a and end in b.
+// 16 bytes that start `phase` bytes (even, below 16) into a and end in b.  A warp works on one row at a time and its lanes'
+// places are 16 bytes apart, so phase is the same in all of them.
 __device__ __forceinline__ uint4 shifted(const uint4 &a, const uint4 &b, uint32_t phase) {
-    const bool one = phase & 4u, two = phase & 8u;
     const uint32_t half = (phase & 2u) * 8u;
-    const uint32_t t0 = one ? a.y : a.x, t1 = one ? a.z : a.y, t2 = one ? a.w : a.z, t3 = one ? b.x : a.w, t4 = one ? b.y : b.x,
-                   t5 = one ? b.z : b.y, t6 = one ? b.w : b.z;
-    const uint32_t u0 = two ? t2 : t0, u1 = two ? t3 : t1, u2 = two ? t4 : t2, u3 = two ? t5 : t3, u4 = two ? t6 : t4;
-    return make_uint4(__funnelshift_r(u0, u1, half), __funnelshift_r(u1, u2, half), __funnelshift_r(u2, u3, half), __funnelshift_r(u3, u4, half));
+    uint32_t w0 = a.x, w1 = a.y, w2 = a.z, w3 = a.w, w4 = b.x;
+    switch (phase >> 2) {
+        case 1: w0 = a.y; w1 = a.z; w2 = a.w; w3 = b.x; w4 = b.y; break;
+        case 2: w0 = a.z; w1 = a.w; w2 = b.x; w3 = b.y; w4 = b.z; break;
+        case 3: w0 = a.w; w1 = b.x; w2 = b.y; w3 = b.z; w4 = b.w; break;
+        default: break;
+    }
+    return make_uint4(__funnelshift_r(w0, w1, half), __funnelshift_r(w1, w2, half), __funnelshift_r(w2, w3, half), __funnelshift_r(w3, w4, half));
 }
-// kVec elements at p, whatever its alignment, put together from two aligned loads that stay within [begin, end), the
-// buffer they lie in; at the buffer's ends, where they would not, element by element.  open() issues the loads and
-// close() takes what they brought, so that several can be on their way.
+// kVec elements at p, whatever its alignment, put together from two aligned loads.  Those may reach up to 14 bytes over
+// the ends of the elements' row, into the rows before and behind; `edge`: there may be none, so they are made only where
+// they stay within [begin, end), the buffer, and elsewhere the elements are loaded one by one.  open() issues the loads
+// and close() takes what they brought, so that several can be on their way.
 template <typename T>
 struct Window {
     uint4 a, b;
-    const T *p;
-    uint32_t phase;
     bool whole;
-    __device__ __forceinline__ void open(const T *from, const T *begin, const T *end) {
-        p = from;
-        phase = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u);
-        const T *at = p - phase / sizeof(T);
-        const bool a_in = at >= begin, b_in = phase == 0 || at + 2 * Elem<T>::kVec <= end;
-        whole = a_in && b_in;
+    __device__ __forceinline__ void open(const T *p, const T *begin, const T *end, bool edge) {
+        const uint32_t phase = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u);
+        const uint4 *at = reinterpret_cast<const uint4 *>(p - phase / sizeof(T));
+        whole = true;
+        if (edge) whole = p - phase / sizeof(T) >= begin && (phase == 0 || p - phase / sizeof(T) + 2 * Elem<T>::kVec <= end);
         a = b = make_uint4(0u, 0u, 0u, 0u);
-        if (whole) a = *reinterpret_cast<const uint4 *>(at);
-        if (whole && phase != 0) b = *(reinterpret_cast<const uint4 *>(at) + 1);
+        if (whole) a = at[0];
+        if (whole && phase != 0) b = at[1];
     }
-    __device__ __forceinline__ uint4 close() const {
-        if (whole) return shifted(a, b, phase);
+    __device__ __forceinline__ uint4 close(const T *p) const {
+        if (whole) return shifted(a, b, (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u));
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
         for (int k = 0; k < Elem<T>::kVec / 2; ++k) Elem<T>::put_pair(v, k, Elem<T>::load(p + 2 * k), Elem<T>::load(p + 2 * k + 1));

@@ -280,6 +280,21 @@ def test_logprob_token_rows_of_a_batch_end_with_it():
     assert (grad[7:] == 0).all() and (grad[:7] != 0).any(1).all()
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+def test_logprob_of_broadcast_rows(name):
+    """One row of logits for all tokens (row stride 0), at an odd place in memory; the gradients are rows of their own."""
+    rows, vocab = 9, 333
+    x = logits_of(1, vocab, name, 3, offset=3).expand(rows, vocab)
+    assert x.stride(0) == 0
+    y = torch.randint(vocab, (rows,), generator=gen(4), device="cuda", dtype=torch.int32)
+    out, logp, h = check_forward(x, y)
+    g, gh = (torch.randn(rows, generator=gen(k), device="cuda") for k in (2, 3))
+    grad = torch.empty(rows, vocab, dtype=x.dtype, device="cuda")
+    td.token_logprob_grad(grad, x, y, out.norm, g, entropy=out.entropy, grad_entropy=gh)
+    want = exact_grad(logp, h, y, g.double(), gh.double(), 1.0)
+    assert ((grad.double() - want).abs() <= grad_bound(logp, h, g.double(), gh.double(), 1.0, vocab, name, want)).all()
+
+
 def test_logprob_rows_beyond_32_bit_offsets():
     rows, vocab, stride = 33000, 130, 65600                      # the last rows start past 2^31 elements
     flat = torch.empty(rows * stride, dtype=torch.bfloat16, device="cuda")
