@@ -209,8 +209,8 @@ __device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t block) {
     }
 }
 
-// One block sorts everything: up to 8192 positions, in shared memory.  Blocks beyond the first clear the gradient
-// table meanwhile, where the launch has such blocks.
+// One block sorts everything: up to 8192 positions, in shared memory.  Blocks beyond the first clear the first rows of
+// the gradient table meanwhile, with a token or without, where the launch has such blocks.
 constexpr int kSmallThreads = 1024, kSmallItems = 8, kSmallWarps = kSmallThreads / 32;
 constexpr uint32_t kSmallMax = kSmallThreads * kSmallItems;
 constexpr size_t kSmallSmem = (size_t)kSmallWarps * kSortBins * 2 + kSmallMax * (4 + 2) + kSortBins * 2 + 64;
@@ -222,9 +222,10 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedAr
         const size_t i = (size_t)(blockIdx.x - 1) * kSmallThreads + threadIdx.x, n = (size_t)(gridDim.x - 1) * kSmallThreads;
         uint8_t *t = static_cast<uint8_t *>(a.grad_table);
         const size_t row = (size_t)a.dim * a.grad_size, stride = (size_t)a.table_stride * a.grad_size;
-        if (row == stride) return fill_zero(t, row * a.vocab, i, n);
+        const size_t rows = min((size_t)a.vocab, (size_t)a.zero_from * 32 * (long_rows(a) ? 1 : kZeroWords));
+        if (row == stride) return fill_zero(t, row * rows, i, n);
         const size_t warp = i / 32, warps = n / 32, lane = threadIdx.x & 31u;
-        for (size_t v = warp; v < a.vocab; v += warps) fill_zero(t + v * stride, row, lane, 32);
+        for (size_t v = warp; v < rows; v += warps) fill_zero(t + v * stride, row, lane, 32);
         return;
     }
     extern __shared__ __align__(16) uint8_t sort_smem[];

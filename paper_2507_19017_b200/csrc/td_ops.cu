@@ -249,13 +249,16 @@ cudaError_t run_sort(EmbedArgs &k, const EmbedGradLayout &L, uint8_t *ws, cudaSt
 
 template <typename T, typename G>
 cudaError_t run_embed_grad(EmbedArgs k, const EmbedGradLayout &L, uint8_t *ws, bool wide, cudaStream_t st) {
-    // Rows without a token are cleared one of two ways: all rows, by blocks that run beside the one-block sort, where
-    // that writes few rows twice; or those rows alone, by blocks that run among the sums.
-    const bool clear = !k.accumulate, clear_all = clear && L.small && k.n_tokens <= k.vocab / 8;
+    // Rows without a token are cleared by blocks behind those of the sums; the first of them earlier, beside the sort,
+    // which leaves most of the machine idle for 5 to 8 us, time for some 30 MB.
     cudaError_t rc;
-    k.present = clear && !clear_all ? reinterpret_cast<uint32_t *>(ws + L.present) : nullptr;
+    k.present = k.accumulate ? nullptr : reinterpret_cast<uint32_t *>(ws + L.present);
     const uint32_t per_block = (uint64_t)k.dim * sizeof(G) >= kLongRow ? 1u : kZeroWords;         // words of k.present
     const uint32_t zeroing = k.present ? (uint32_t)(((uint64_t)k.vocab + 32 * per_block - 1) / (32 * per_block)) : 0u;
+    const uint64_t early = (30ull << 20) / (32 * per_block * (uint64_t)k.dim * sizeof(G)) + 1;
+    // The one-block sort does not know the rows yet and clears all, which is only worth it while few of them are written again;
+    // the last of several placing kernels knows.
+    if (L.small ? k.n_tokens <= k.vocab / 8 : L.passes > 1) k.zero_from = early < zeroing ? (uint32_t)early : zeroing;
     k.arrived = reinterpret_cast<uint32_t *>(ws + L.arrived);
     k.n_arrived = 3 * L.n_chunks * L.slices;
     if (L.small) {
@@ -263,15 +266,8 @@ cudaError_t run_embed_grad(EmbedArgs k, const EmbedGradLayout &L, uint8_t *ws, b
         if (rc != cudaSuccess) return rc;
         k.keys = reinterpret_cast<uint32_t *>(ws + L.keys[0]);
         k.pos = reinterpret_cast<uint32_t *>(ws + L.pos[0]);
-        rc = launch_smem(sort_small_kernel, clear_all ? 148 * 2 : 1, kSmallThreads, kSmallSmem, st, 1u, k, L.passes);
-    } else {
-        // the last placing kernel leaves most of the machine idle for about 8 us: room to clear some 40 MB of rows
-        if (L.passes > 1) {
-            const uint64_t some = (40ull << 20) / (32 * per_block * (uint64_t)k.dim * sizeof(G)) + 1;
-            k.zero_from = some < zeroing ? (uint32_t)some : zeroing;
-        }
-        rc = L.big_tiles ? run_sort<16>(k, L, ws, st) : run_sort<4>(k, L, ws, st);
-    }
+        rc = launch_smem(sort_small_kernel, k.zero_from ? 148 * 2 : 1, kSmallThreads, kSmallSmem, st, 1u, k, L.passes);
+    } else rc = L.big_tiles ? run_sort<16>(k, L, ws, st) : run_sort<4>(k, L, ws, st);
     if (rc != cudaSuccess) return rc;
     const uint32_t sum_blocks = (uint32_t)(((uint64_t)L.n_chunks * L.slices + kSumThreads / 32 - 1) / (kSumThreads / 32));
     const uint32_t zero_blocks = zeroing - k.zero_from;
