@@ -1,6 +1,8 @@
 // Embedding rows of token ids, and the gradient with respect to the table by sorted tokens.
 #pragma once
 
+#include <cooperative_groups.h>
+
 #include "td_ops.cuh"
 
 namespace td {
@@ -188,12 +190,12 @@ __device__ __forceinline__ void fill_zero(uint8_t *p, size_t bytes, size_t i, si
 // a warp at a time one of them.  Short ones: every warp takes 32, neighbours without a gap between them at once.
 constexpr uint32_t kLongRow = 1024;      // bytes
 __device__ __forceinline__ bool long_rows(const EmbedArgs &a) { return a.dim * (unsigned long long)a.grad_size >= kLongRow; }
-__device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t block) {
+__device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t block, const uint32_t *present) {       // the block's words
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const size_t row = (size_t)a.dim * a.grad_size, stride = (size_t)a.table_stride * a.grad_size;
     uint8_t *table = static_cast<uint8_t *>(a.grad_table);
     if (long_rows(a)) {
-        const uint32_t bits = a.present[block];
+        const uint32_t bits = present[0];
         for (uint32_t k = warp; k < 32 && block * 32 + k < a.vocab; k += blockDim.x >> 5)
             if (!((bits >> k) & 1u)) fill_zero(table + (size_t)(block * 32 + k) * stride, row, lane, 32);
         return;
@@ -201,51 +203,64 @@ __device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t block) {
     const uint32_t word = block * kZeroWords + warp;
     if (warp >= kZeroWords || word >= (a.vocab + 31) / 32) return;
     const uint32_t rows = min(32u, a.vocab - word * 32);
-    uint32_t absent = ~a.present[word] & (rows == 32 ? kFullMask : (1u << rows) - 1u);
+    uint32_t absent = ~present[warp] & (rows == 32 ? kFullMask : (1u << rows) - 1u);
     while (absent) {
         const uint32_t from = __ffs(absent) - 1, free = ~(absent >> from), n = row == stride ? (free ? __ffs(free) - 1 : 32) : 1;
         fill_zero(table + (size_t)(word * 32 + from) * stride, row * n, lane, 32);
         absent &= from + n >= 32 ? 0u : kFullMask << (from + n);
     }
 }
+__device__ __forceinline__ uint32_t zero_words(const EmbedArgs &a) { return long_rows(a) ? 1u : kZeroWords; }       // per block
 
-// One block sorts everything: up to 8192 positions, in shared memory.  Blocks beyond the first clear the first rows of
-// the gradient table meanwhile, with a token or without, where the launch has such blocks.
+// One cluster of one or eight blocks sorts up to 65536 positions in its shared memory: a block holds a
+// consecutive share of the entries, and places them in whichever block's share they belong.  Blocks beyond the
+// cluster's clear the first rows of the gradient table meanwhile, with a token or without, where the launch has such
+// blocks.
 constexpr int kSmallThreads = 1024, kSmallItems = 8, kSmallWarps = kSmallThreads / 32;
-constexpr uint32_t kSmallMax = kSmallThreads * kSmallItems;
-constexpr size_t kSmallSmem = (size_t)kSmallWarps * kSortBins * 2 + kSmallMax * (4 + 2) + kSortBins * 2 + 64;
+constexpr uint32_t kSmallBlocks = 8;
+struct SmallSort {
+    uint16_t warp_bins[kSmallWarps][kSortBins];
+    uint32_t keys[kSmallThreads * kSmallItems];
+    uint16_t pos[kSmallThreads * kSmallItems];
+    uint32_t bin_total[kSortBins], bin_start[kSortBins], warp_sum[kSortBins / 32];
+};
 
-__global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedArgs a, uint32_t passes) {
+// log_items: entries per thread, as a power of two
+__global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedArgs a, uint32_t passes, uint32_t log_items) {
     griddep_launch_dependents();
     griddep_wait();
-    if (blockIdx.x > 0) {
-        const size_t i = (size_t)(blockIdx.x - 1) * kSmallThreads + threadIdx.x, n = (size_t)(gridDim.x - 1) * kSmallThreads;
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    const uint32_t blocks = cluster.num_blocks(), me = cluster.block_rank();
+    if (blockIdx.x >= blocks) {
+        const size_t i = (size_t)(blockIdx.x - blocks) * kSmallThreads + threadIdx.x, n = (size_t)(gridDim.x - blocks) * kSmallThreads;
         uint8_t *t = static_cast<uint8_t *>(a.grad_table);
         const size_t row = (size_t)a.dim * a.grad_size, stride = (size_t)a.table_stride * a.grad_size;
-        const size_t rows = min((size_t)a.vocab, (size_t)a.zero_from * 32 * (long_rows(a) ? 1 : kZeroWords));
+        const size_t rows = min((size_t)a.vocab, (size_t)a.zero_from * 32 * zero_words(a));
         if (row == stride) return fill_zero(t, row * rows, i, n);
         const size_t warp = i / 32, warps = n / 32, lane = threadIdx.x & 31u;
         for (size_t v = warp; v < rows; v += warps) fill_zero(t + v * stride, row, lane, 32);
         return;
     }
     extern __shared__ __align__(16) uint8_t sort_smem[];
-    uint16_t(*warp_bins)[kSortBins] = reinterpret_cast<uint16_t(*)[kSortBins]>(sort_smem);
-    uint32_t *keys = reinterpret_cast<uint32_t *>(sort_smem + (size_t)kSmallWarps * kSortBins * 2);
-    uint16_t *pos = reinterpret_cast<uint16_t *>(keys + kSmallMax);
-    uint16_t *bin_start = pos + kSmallMax;
-    uint32_t *warp_sum = reinterpret_cast<uint32_t *>(bin_start + kSortBins);
+    SmallSort &s = *reinterpret_cast<SmallSort *>(sort_smem);
+    auto all_blocks = [&]() { if (blocks > 1) cluster.sync(); else __syncthreads(); };
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    const uint32_t n = tokens_in(a), items = (a.n_tokens + kSmallThreads - 1) / kSmallThreads, base = warp * items * 32 + lane;
-    for (uint32_t w = threadIdx.x; w < a.n_arrived; w += kSmallThreads) a.arrived[w] = 0u;
+    const uint32_t n = tokens_in(a), items = 1u << log_items, log_share = log_items + 10;
+    static_assert(kSmallThreads == 1 << 10, "a block's share is its threads' items");
+    const uint32_t first = me << log_share, base = first + warp * (items * 32) + lane;
+    const uint32_t mine = a.n_tokens > first ? min(a.n_tokens - first, 1u << log_share) : 0u;
+    const uint32_t busy = (mine + items * 32 - 1) >> (log_items + 5);        // warps that have entries
+    for (uint32_t w = me * kSmallThreads + threadIdx.x; w < a.n_arrived; w += blocks * kSmallThreads) a.arrived[w] = 0u;
     // the bits of the ids that occur: in shared memory (the place of the counts) where there is room for the vocabulary
     const uint32_t words = (a.vocab + 31) / 32;
     const bool near = words <= kSmallWarps * kSortBins / 2;
-    uint32_t *bits = near ? reinterpret_cast<uint32_t *>(sort_smem) : a.present;
+    uint32_t *bits = near ? reinterpret_cast<uint32_t *>(s.warp_bins) : a.present;
     if (a.present) {
-        for (uint32_t w = threadIdx.x; w < words; w += kSmallThreads) bits[w] = 0u;
-        __syncthreads();
+        if (near) for (uint32_t w = threadIdx.x; w < words; w += kSmallThreads) bits[w] = 0u;
+        else for (uint32_t w = me * kSmallThreads + threadIdx.x; w < words; w += blocks * kSmallThreads) bits[w] = 0u;
+        all_blocks();
     }
-    const uint32_t busy = items ? (a.n_tokens + items * 32 - 1) / (items * 32) : 0;        // warps that have entries
     uint32_t key[kSmallItems], at[kSmallItems], rank[kSmallItems], in_mask = 0;
 #pragma unroll
     for (int k = 0; k < kSmallItems; ++k) {
@@ -259,9 +274,13 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedAr
         }
     }
     if (a.present && near) {
-        __syncthreads();
-        for (uint32_t w = threadIdx.x; w < words; w += kSmallThreads) a.present[w] = bits[w];
-        __syncthreads();
+        all_blocks();
+        for (uint32_t w = me * kSmallThreads + threadIdx.x; w < words; w += blocks * kSmallThreads) {
+            uint32_t any = 0;
+            for (uint32_t c = 0; c < blocks; ++c) any |= cluster.map_shared_rank(bits, c)[w];
+            a.present[w] = any;
+        }
+        all_blocks();
     }
     for (uint32_t p = 0; p < passes; ++p) {
         if (p) {
@@ -269,39 +288,54 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedAr
             for (int k = 0; k < kSmallItems; ++k) {
                 if ((uint32_t)k >= items) break;
                 if ((in_mask >> k) & 1u) {
-                    key[k] = keys[base + k * 32];
-                    at[k] = pos[base + k * 32];
+                    key[k] = s.keys[base - first + k * 32];
+                    at[k] = s.pos[base - first + k * 32];
                 }
             }
         }
         const uint32_t shift = p * kSortBits;
-        if (warp < busy) rank_digits<kSmallItems, kSmallWarps>(key, rank, in_mask, shift, warp_bins, items);
+        if (warp < busy) rank_digits<kSmallItems, kSmallWarps>(key, rank, in_mask, shift, s.warp_bins, items);
         __syncthreads();
-        uint32_t total = 0;
-        if (threadIdx.x < kSortBins)
+        uint32_t total = 0, ahead = 0;
+        if (threadIdx.x < kSortBins) {
 #pragma unroll 4
             for (uint32_t w = 0; w < busy; ++w) {            // entries of the bin in earlier warps
-                const uint32_t c = warp_bins[w][threadIdx.x];
-                warp_bins[w][threadIdx.x] = (uint16_t)total;
+                const uint32_t c = s.warp_bins[w][threadIdx.x];
+                s.warp_bins[w][threadIdx.x] = (uint16_t)total;
                 total += c;
             }
-        const uint32_t start = scan_bins(total, warp_sum);
-        if (threadIdx.x < kSortBins) bin_start[threadIdx.x] = (uint16_t)start;
+            s.bin_total[threadIdx.x] = total;
+        }
+        if (blocks > 1) {                // and in earlier blocks; from here on all entries are in registers
+            cluster.sync();
+            if (threadIdx.x < kSortBins) {
+                total = 0;
+#pragma unroll
+                for (uint32_t c = 0; c < kSmallBlocks; ++c) {
+                    const uint32_t x = cluster.map_shared_rank(s.bin_total, c)[threadIdx.x];
+                    ahead += c < me ? x : 0u;
+                    total += x;
+                }
+            }
+        }
+        const uint32_t start = scan_bins(total, s.warp_sum) + ahead;
+        if (threadIdx.x < kSortBins) s.bin_start[threadIdx.x] = start;
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kSmallItems; ++k) {
             if ((uint32_t)k >= items) break;
             if (!((in_mask >> k) & 1u)) continue;
-            const uint32_t d = (key[k] >> shift) & (kSortBins - 1), to = bin_start[d] + warp_bins[warp][d] + rank[k];
-            keys[to] = key[k];
-            pos[to] = (uint16_t)at[k];
+            const uint32_t d = (key[k] >> shift) & (kSortBins - 1), to = s.bin_start[d] + s.warp_bins[warp][d] + rank[k];
+            const uint32_t block = to >> log_share, slot = to & ((1u << log_share) - 1u);
+            cluster.map_shared_rank(s.keys, block)[slot] = key[k];
+            cluster.map_shared_rank(s.pos, block)[slot] = (uint16_t)at[k];
         }
-        __syncthreads();
+        all_blocks();
     }
-    // stores to scattered places take one block about a cycle each: out in order, from shared memory
-    for (uint32_t i = threadIdx.x; i < a.n_tokens; i += kSmallThreads) {
-        a.keys[i] = keys[i];
-        a.pos[i] = pos[i];
+    // stores to scattered places take a block about a cycle each: out in order, from shared memory
+    for (uint32_t i = threadIdx.x; i < mine; i += kSmallThreads) {
+        a.keys[first + i] = s.keys[i];
+        a.pos[first + i] = s.pos[i];
     }
 }
 
@@ -347,7 +381,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const EmbedArg
     griddep_wait();
     __shared__ uint32_t warp_bins[kSortWarps][kSortBins];
     __shared__ uint32_t warp_sum[kSortBins / 32];
-    if (blockIdx.x >= s.n_tiles) return zero_rows(a, blockIdx.x - s.n_tiles);
+    if (blockIdx.x >= s.n_tiles) return zero_rows(a, blockIdx.x - s.n_tiles, a.present + (size_t)(blockIdx.x - s.n_tiles) * zero_words(a));
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t pass = s.shift / kSortBits;
     // a warp owns kItems * 32 consecutive entries of the tile
@@ -595,7 +629,10 @@ template <typename T, typename G, bool kWide>
 __global__ void __launch_bounds__(kSumThreads, kWide ? 3 : 4) embed_sum_kernel(const __grid_constant__ EmbedArgs a, uint32_t slices, uint32_t sum_blocks) {
     griddep_launch_dependents();
     griddep_wait();
-    if (blockIdx.x >= sum_blocks) return zero_rows(a, blockIdx.x - sum_blocks + a.zero_from);
+    if (blockIdx.x >= sum_blocks) {
+        const uint32_t block = blockIdx.x - sum_blocks + a.zero_from;
+        return zero_rows(a, block, a.present + (size_t)block * zero_words(a));
+    }
     using Layout = SumLayout<T, kWide>;
     constexpr int kRows = Layout::kRows, E = Elem<T>::kVec;
     extern __shared__ __align__(16) uint8_t sum_smem[];
@@ -711,6 +748,96 @@ __global__ void __launch_bounds__(kSumThreads, kWide ? 3 : 4) embed_sum_kernel(c
         const uint32_t run = side == 0 ? first : v;
         if (part && join_run<kWide>(a, run, chunk, side == 0, slice, slices, sum)) write_row<G, kWide>(a, run, sum, c0, cols, stage);
     }
+}
+
+// ---- few positions: no sort, one launch ----
+// A block per (position, 256 columns) looks its id up among all positions, a share of them per warp, and stops unless
+// the position is the id's first.  Each warp adds up the id's rows in its share, and the shares' sums are added in
+// order.  Blocks behind the sum_blocks clear rows without a token; they look through the ids for their own rows.
+// The looking costs positions^2 comparisons: nothing for hundreds of positions, too much for many thousands.
+template <typename T, typename G, bool kWide>
+__global__ void __launch_bounds__(kSumThreads) embed_few_kernel(const EmbedArgs a, uint32_t slices, uint32_t sum_blocks) {
+    griddep_launch_dependents();
+    griddep_wait();
+    __shared__ f32x2 piece[kSumWarps][kSumPairs][32];
+    __shared__ bool found[kSumWarps];
+    __shared__ float stage[SumLayout<T, false>::kStage / 4];
+    __shared__ uint32_t bits[kZeroWords];
+    const uint32_t n = tokens_in(a), lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    if (blockIdx.x >= sum_blocks) {
+        const uint32_t block = blockIdx.x - sum_blocks, words = zero_words(a);
+        const uint32_t v0 = block * words * 32;
+        if (threadIdx.x < kZeroWords) bits[threadIdx.x] = 0u;
+        __syncthreads();
+        for (uint32_t t = threadIdx.x; t < a.n_tokens; t += kSumThreads) {
+            const uint32_t id = id_at(a, t, n);
+            if (id < a.vocab && id >= v0 && id - v0 < words * 32) atomicOr(bits + (id - v0) / 32, 1u << ((id - v0) & 31u));
+        }
+        __syncthreads();
+        return zero_rows(a, block, bits);
+    }
+    const uint32_t t = blockIdx.x / slices, c0 = blockIdx.x % slices * kSumWarpCols, cols = min(a.dim - c0, kSumWarpCols);
+    const uint32_t v = id_at(a, t, n);
+    if (v >= a.vocab) return;
+    const uint32_t share = (a.n_tokens + kSumThreads - 1) / kSumThreads * 32, lo = warp * share, hi = min(a.n_tokens, lo + share);
+    auto matches = [&](uint32_t g) { return __ballot_sync(kFullMask, g + lane < hi && id_at(a, g + lane, n) == v); };
+    bool earlier = false;
+    for (uint32_t g = lo; g < hi && g < t; g += 32) earlier |= (matches(g) & (t - g < 32 ? (1u << (t - g)) - 1u : kFullMask)) != 0;
+    if (__syncthreads_or(earlier)) return;
+
+    constexpr int E = Elem<T>::kVec, kRows = 4;
+    const T *in = static_cast<const T *>(a.grad_out) + c0;
+    f32x2 sum[kSumPairs];
+#pragma unroll
+    for (int k = 0; k < kSumPairs; ++k) sum[k] = pack2(0.0f, 0.0f);
+    bool any = false;
+    for (uint32_t g = lo; g < hi; g += 32) {
+        uint32_t mask = matches(g);
+        any |= mask != 0;
+        while (mask) {                   // kRows rows at a time, in ascending order of position
+            f32x2 x[kRows][kSumPairs];
+            uint32_t taken = 0;
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) {
+                if (!mask) break;
+                const T *row = in + (long long)(g + __ffs(mask) - 1) * a.out_stride;
+                mask &= mask - 1;
+                ++taken;
+                if constexpr (kWide) {
+#pragma unroll
+                    for (int q = 0; q < kSumCols / E; ++q) {
+                        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                        if (lane * kSumCols < cols) w = *reinterpret_cast<const uint4 *>(row + lane * kSumCols + q * E);
+#pragma unroll
+                        for (int k = 0; k < E / 2; ++k) x[u][q * E / 2 + k] = Elem<T>::pair(w, k);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < kSumPairs; ++k) {
+                        const uint32_t c = pair_column<false>(k);
+                        x[u][k] = pack2(c < cols ? Elem<T>::load(row + c) : 0.0f, c + 1 < cols ? Elem<T>::load(row + c + 1) : 0.0f);
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) {
+                if ((uint32_t)u >= taken) break;
+#pragma unroll
+                for (int k = 0; k < kSumPairs; ++k) sum[k] = add2(sum[k], x[u][k]);
+            }
+        }
+    }
+    if (lane == 0) found[warp] = any;
+    if (any && warp)
+#pragma unroll
+        for (int k = 0; k < kSumPairs; ++k) piece[warp][k][lane] = sum[k];
+    __syncthreads();
+    if (warp) return;
+    for (int w = 1; w < kSumWarps; ++w)
+        if (found[w])
+#pragma unroll
+            for (int k = 0; k < kSumPairs; ++k) sum[k] = add2(sum[k], piece[w][k][lane]);
+    write_row<G, kWide>(a, v, sum, c0, cols, stage);
 }
 
 }  // namespace td
