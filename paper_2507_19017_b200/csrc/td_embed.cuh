@@ -213,11 +213,11 @@ __device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t block, co
 }
 __device__ __forceinline__ uint32_t zero_words(const EmbedArgs &a) { return long_rows(a) ? 1u : kZeroWords; }       // per block
 
-// One cluster of one or eight blocks sorts up to 65536 positions in its shared memory: a block holds a
+// One cluster of one or eight blocks sorts up to 32768 positions (4096 with one block) in its shared memory: a block holds a
 // consecutive share of the entries, and places them in whichever block's share they belong.  Blocks beyond the
 // cluster's clear the first rows of the gradient table meanwhile, with a token or without, where the launch has such
 // blocks.
-constexpr int kSmallThreads = 1024, kSmallItems = 8, kSmallWarps = kSmallThreads / 32;
+constexpr int kSmallThreads = 1024, kSmallItems = 4, kSmallWarps = kSmallThreads / 32;
 constexpr uint32_t kSmallBlocks = 8;
 struct SmallSort {
     uint16_t warp_bins[kSmallWarps][kSortBins];

@@ -301,8 +301,8 @@ constexpr uint32_t kGradVectors = kGradThreads * kGradUnroll * 4;        // vect
 
 // Elementwise over the rows: p = 2^d with d = (x - max) c - log2 S, gradient p (ca + cb d), and g / tau more at the target.
 // Bound by memory: the stream of four 7B-shaped samples, 7774 rows of 152064 bfloat16 of which 5057 have a gradient and the
-// others are only cleared (3.9 GB), in 605 us, 6.45 TB/s.  One block per (row, chunk of the row).  kSame: a row of logits and its gradient's start at the same offset
-// from a 16-byte boundary; else the logits' vectors are put together from two loads each.  kTeam = 32: a row
+// others are only cleared (3.9 GB), in 605 us, 6.45 TB/s.  One block per (row, chunk of the row).  kSame: a row of
+// logits and its gradient's start at the same offset from a 16-byte boundary; else the logits' vectors are put together from two loads each.  kTeam = 32: a row
 // per warp.
 template <typename T, bool kSame, int kTeam>
 __global__ void __launch_bounds__(kGradThreads, kSame ? 4 : 3) token_logprob_grad_kernel(const LogprobArgs a) {
