@@ -1,8 +1,6 @@
 // Embedding rows of token ids, and the gradient with respect to the table by sorted tokens.
 #pragma once
 
-#include <cooperative_groups.h>
-
 #include "td_ops.cuh"
 
 namespace td {
@@ -24,7 +22,7 @@ struct EmbedArgs {
     uint32_t n_chunks;
     uint32_t *keys;                      // [n_tokens] sorted ids; vocab: no token
     uint32_t *pos;                       // [n_tokens] their positions
-    uint32_t *present;                   // [ceil(vocab / 32)] a bit per id that occurs, or nullptr
+    uint32_t *present;                   // [ceil(vocab / 32)] a bit per id that occurs, or nullptr: found in the keys
     float *partial;                      // [2][n_chunks][partial_stride]: sums of a run cut by the chunk's start / by its end
     size_t partial_stride;               // dim rounded up to a warp's columns
     uint32_t *arrived;                   // [3][n_chunks][slices] parts, and groups of parts, stored of cut runs
@@ -133,15 +131,14 @@ constexpr int kSortBits = 9, kSortBins = 1 << kSortBits;
 
 // Ranks of a block's entries among those of the same digit.  Entries are in registers, warp by warp, turn by turn,
 // lane by lane; warp_bins[w][d] ends up as the number of entries with digit d in the warp.
-template <int kItems, int kWarps, typename Count>
+template <int kItems>
 __device__ __forceinline__ void rank_digits(const uint32_t (&key)[kItems], uint32_t (&rank)[kItems], uint32_t in_mask, uint32_t shift,
-                                            Count (*warp_bins)[kSortBins], uint32_t items) {
+                                            uint32_t (*warp_bins)[kSortBins]) {
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     for (int b = lane; b < kSortBins; b += 32) warp_bins[warp][b] = 0;
     __syncwarp();
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
-        if ((uint32_t)k >= items) break;
         const bool in = (in_mask >> k) & 1u;
         const uint32_t d = (key[k] >> shift) & (kSortBins - 1);
         // lanes with the same digit, one vote per bit (a match instruction took 300 to 400 cycles here)
@@ -152,10 +149,10 @@ __device__ __forceinline__ void rank_digits(const uint32_t (&key)[kItems], uint3
             const uint32_t v = __ballot_sync(kFullMask, set);
             peers &= set ? v : ~v;
         }
-        const uint32_t before = in ? (uint32_t)warp_bins[warp][d] : 0u;
+        const uint32_t before = in ? warp_bins[warp][d] : 0u;
         rank[k] = before + __popc(peers & ((1u << lane) - 1u));
         __syncwarp();
-        if (in && lane == (uint32_t)__ffs(peers) - 1u) warp_bins[warp][d] = (Count)(before + __popc(peers));
+        if (in && lane == (uint32_t)__ffs(peers) - 1u) warp_bins[warp][d] = before + __popc(peers);
         __syncwarp();
     }
 }
@@ -213,130 +210,65 @@ __device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t block, co
 }
 __device__ __forceinline__ uint32_t zero_words(const EmbedArgs &a) { return long_rows(a) ? 1u : kZeroWords; }       // per block
 
-// One cluster of one or eight blocks sorts up to 32768 positions (4096 with one block) in its shared memory: a block holds a
-// consecutive share of the entries, and places them in whichever block's share they belong.  Blocks beyond the
-// cluster's clear the first rows of the gradient table meanwhile, with a token or without, where the launch has such
-// blocks.
-constexpr int kSmallThreads = 1024, kSmallItems = 4, kSmallWarps = kSmallThreads / 32;
-constexpr uint32_t kSmallBlocks = 8;
-struct SmallSort {
-    uint16_t warp_bins[kSmallWarps][kSortBins];
-    uint32_t keys[kSmallThreads * kSmallItems];
-    uint16_t pos[kSmallThreads * kSmallItems];
-    uint32_t bin_total[kSortBins], bin_start[kSortBins], warp_sum[kSortBins / 32];
-};
+// The bits of the block's rows, from the sorted keys; for all threads of a block of kSumThreads.
+constexpr int kSumThreads = 256, kSumWarps = kSumThreads / 32;
+__device__ __forceinline__ void present_in_keys(const EmbedArgs &a, uint32_t block, uint32_t *bits) {
+    const uint32_t v0 = block * zero_words(a) * 32, v1 = v0 + zero_words(a) * 32;
+    if (threadIdx.x < kZeroWords) bits[threadIdx.x] = 0u;
+    uint32_t lo = 0, hi = a.n_tokens;                        // the first entry that is not below v0 lies in [lo, hi]
+    while (lo < hi) {
+        const uint32_t step = (hi - lo + kSumThreads - 1) / kSumThreads, at = lo + threadIdx.x * step;
+        const uint32_t below = __syncthreads_count(at < hi && __ldg(a.keys + at) < v0);
+        if (below == 0) break;
+        hi = min(hi, lo + below * step);
+        lo += (below - 1) * step + 1;
+    }
+    for (uint32_t e = lo + threadIdx.x;; e += kSumThreads) {
+        const uint32_t id = e < a.n_tokens ? __ldg(a.keys + e) : a.vocab;
+        const bool in = id < min(v1, a.vocab);
+        if (in) atomicOr(bits + (id - v0) / 32, 1u << ((id - v0) & 31u));
+        if (__syncthreads_count(in) < kSumThreads) break;
+    }
+}
 
-// log_items: entries per thread, as a power of two
-__global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(const EmbedArgs a, uint32_t passes, uint32_t log_items) {
+// Up to kRankMax positions: a position's place among the sorted ones is the number of smaller ids, and of equal ids at
+// earlier positions.  A block counts it for 32 positions, one per lane, its warps going through a share of all ids
+// each.  positions^2 comparisons: 4000 positions 6 us, 8192 15 us, where sorting by digits takes 17 for any number.
+constexpr int kRankThreads = 1024, kRankWarps = kRankThreads / 32;
+constexpr uint32_t kRankMax = 8192;
+
+__global__ void __launch_bounds__(kRankThreads) embed_rank_kernel(const EmbedArgs a) {
     griddep_launch_dependents();
     griddep_wait();
-    namespace cg = cooperative_groups;
-    cg::cluster_group cluster = cg::this_cluster();
-    const uint32_t blocks = cluster.num_blocks(), me = cluster.block_rank();
-    if (blockIdx.x >= blocks) {
-        const size_t i = (size_t)(blockIdx.x - blocks) * kSmallThreads + threadIdx.x, n = (size_t)(gridDim.x - blocks) * kSmallThreads;
-        uint8_t *t = static_cast<uint8_t *>(a.grad_table);
-        const size_t row = (size_t)a.dim * a.grad_size, stride = (size_t)a.table_stride * a.grad_size;
-        const size_t rows = min((size_t)a.vocab, (size_t)a.zero_from * 32 * zero_words(a));
-        if (row == stride) return fill_zero(t, row * rows, i, n);
-        const size_t warp = i / 32, warps = n / 32, lane = threadIdx.x & 31u;
-        for (size_t v = warp; v < rows; v += warps) fill_zero(t + v * stride, row, lane, 32);
-        return;
-    }
-    extern __shared__ __align__(16) uint8_t sort_smem[];
-    SmallSort &s = *reinterpret_cast<SmallSort *>(sort_smem);
-    auto all_blocks = [&]() { if (blocks > 1) cluster.sync(); else __syncthreads(); };
-    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    const uint32_t n = tokens_in(a), items = 1u << log_items, log_share = log_items + 10;
-    static_assert(kSmallThreads == 1 << 10, "a block's share is its threads' items");
-    const uint32_t first = me << log_share, base = first + warp * (items * 32) + lane;
-    const uint32_t mine = a.n_tokens > first ? min(a.n_tokens - first, 1u << log_share) : 0u;
-    const uint32_t busy = (mine + items * 32 - 1) >> (log_items + 5);        // warps that have entries
-    for (uint32_t w = me * kSmallThreads + threadIdx.x; w < a.n_arrived; w += blocks * kSmallThreads) a.arrived[w] = 0u;
-    // the bits of the ids that occur: in shared memory (the place of the counts) where there is room for the vocabulary
-    const uint32_t words = (a.vocab + 31) / 32;
-    const bool near = words <= kSmallWarps * kSortBins / 2;
-    uint32_t *bits = near ? reinterpret_cast<uint32_t *>(s.warp_bins) : a.present;
-    if (a.present) {
-        if (near) for (uint32_t w = threadIdx.x; w < words; w += kSmallThreads) bits[w] = 0u;
-        else for (uint32_t w = me * kSmallThreads + threadIdx.x; w < words; w += blocks * kSmallThreads) bits[w] = 0u;
-        all_blocks();
-    }
-    uint32_t key[kSmallItems], at[kSmallItems], rank[kSmallItems], in_mask = 0;
-#pragma unroll
-    for (int k = 0; k < kSmallItems; ++k) {
-        if ((uint32_t)k >= items) break;
-        at[k] = base + k * 32;
-        key[k] = 0;
-        if (at[k] < a.n_tokens) {
-            in_mask |= 1u << k;
-            key[k] = id_at(a, at[k], n);
-            if (a.present && key[k] < a.vocab) atomicOr(bits + (key[k] >> 5), 1u << (key[k] & 31u));
-        }
-    }
-    if (a.present && near) {
-        all_blocks();
-        for (uint32_t w = me * kSmallThreads + threadIdx.x; w < words; w += blocks * kSmallThreads) {
-            uint32_t any = 0;
-            for (uint32_t c = 0; c < blocks; ++c) any |= cluster.map_shared_rank(bits, c)[w];
-            a.present[w] = any;
-        }
-        all_blocks();
-    }
-    for (uint32_t p = 0; p < passes; ++p) {
-        if (p) {
-#pragma unroll
-            for (int k = 0; k < kSmallItems; ++k) {
-                if ((uint32_t)k >= items) break;
-                if ((in_mask >> k) & 1u) {
-                    key[k] = s.keys[base - first + k * 32];
-                    at[k] = s.pos[base - first + k * 32];
-                }
-            }
-        }
-        const uint32_t shift = p * kSortBits;
-        if (warp < busy) rank_digits<kSmallItems, kSmallWarps>(key, rank, in_mask, shift, s.warp_bins, items);
-        __syncthreads();
-        uint32_t total = 0, ahead = 0;
-        if (threadIdx.x < kSortBins) {
+    __shared__ __align__(16) uint32_t ids[kRankMax];
+    __shared__ uint32_t place[32];
+    const uint32_t n = tokens_in(a), lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    for (uint32_t w = blockIdx.x * kRankThreads + threadIdx.x; w < a.n_arrived; w += gridDim.x * kRankThreads) a.arrived[w] = 0u;
+    const uint32_t padded = (a.n_tokens + 3) & ~3u;
+    for (uint32_t t = threadIdx.x; t < padded; t += kRankThreads) ids[t] = t < a.n_tokens ? id_at(a, t, n) : 0xffffffffu;
+    if (threadIdx.x < 32) place[threadIdx.x] = 0u;
+    __syncthreads();
+    const uint32_t t0 = blockIdx.x * 32, t = t0 + lane, mine = t < a.n_tokens ? ids[t] : 0u;
+    const uint32_t share = (padded / 4 + kRankWarps - 1) / kRankWarps * 4, lo = min(padded, warp * share), hi = min(padded, lo + share);
+    uint32_t count = 0;
+    const uint4 *v = reinterpret_cast<const uint4 *>(ids);
 #pragma unroll 4
-            for (uint32_t w = 0; w < busy; ++w) {            // entries of the bin in earlier warps
-                const uint32_t c = s.warp_bins[w][threadIdx.x];
-                s.warp_bins[w][threadIdx.x] = (uint16_t)total;
-                total += c;
-            }
-            s.bin_total[threadIdx.x] = total;
-        }
-        if (blocks > 1) {                // and in earlier blocks; from here on all entries are in registers
-            cluster.sync();
-            if (threadIdx.x < kSortBins) {
-                total = 0;
-#pragma unroll
-                for (uint32_t c = 0; c < kSmallBlocks; ++c) {
-                    const uint32_t x = cluster.map_shared_rank(s.bin_total, c)[threadIdx.x];
-                    ahead += c < me ? x : 0u;
-                    total += x;
-                }
-            }
-        }
-        const uint32_t start = scan_bins(total, s.warp_sum) + ahead;
-        if (threadIdx.x < kSortBins) s.bin_start[threadIdx.x] = start;
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kSmallItems; ++k) {
-            if ((uint32_t)k >= items) break;
-            if (!((in_mask >> k) & 1u)) continue;
-            const uint32_t d = (key[k] >> shift) & (kSortBins - 1), to = s.bin_start[d] + s.warp_bins[warp][d] + rank[k];
-            const uint32_t block = to >> log_share, slot = to & ((1u << log_share) - 1u);
-            cluster.map_shared_rank(s.keys, block)[slot] = key[k];
-            cluster.map_shared_rank(s.pos, block)[slot] = (uint16_t)at[k];
-        }
-        all_blocks();
+    for (uint32_t s = lo; s < min(hi, t0); s += 4) {         // before the block's positions: equal ids come first
+        const uint4 x = v[s / 4];
+        count += (uint32_t)(x.x <= mine) + (uint32_t)(x.y <= mine) + (uint32_t)(x.z <= mine) + (uint32_t)(x.w <= mine);
     }
-    // stores to scattered places take a block about a cycle each: out in order, from shared memory
-    for (uint32_t i = threadIdx.x; i < mine; i += kSmallThreads) {
-        a.keys[first + i] = s.keys[i];
-        a.pos[first + i] = s.pos[i];
+#pragma unroll 4
+    for (uint32_t s = max(lo, t0 + 32); s < hi; s += 4) {
+        const uint4 x = v[s / 4];
+        count += (uint32_t)(x.x < mine) + (uint32_t)(x.y < mine) + (uint32_t)(x.z < mine) + (uint32_t)(x.w < mine);
+    }
+    if (warp == 0)
+        for (uint32_t s = t0; s < min(t0 + 32, a.n_tokens); ++s) count += ids[s] < mine || (ids[s] == mine && s < t);
+    atomicAdd(place + lane, count);
+    __syncthreads();
+    if (warp == 0 && t < a.n_tokens) {
+        a.keys[place[lane]] = mine;
+        a.pos[place[lane]] = t;
     }
 }
 
@@ -407,7 +339,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const EmbedArg
         if (tile < blockIdx.x) ahead += c;
         total += c;
     }
-    rank_digits<kItems, kSortWarps>(key, rank, in_mask, s.shift, warp_bins, kItems);
+    rank_digits<kItems>(key, rank, in_mask, s.shift, warp_bins);
     uint32_t start = scan_bins(total, warp_sum) + ahead;     // its barrier also ends the ranking
     for (int w = 0; w < kSortWarps; ++w) {
         const uint32_t c = warp_bins[w][threadIdx.x];
@@ -434,7 +366,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const EmbedArg
 //   else: the aligned 16-byte pieces that cover the warp's columns of a row are copied to shared memory, two groups of
 //     kRows rows in turn, and a lane reads pairs of columns, 64 apart, from wherever in them the row begins;
 //     written rows go through shared memory too, to leave in vectors aligned on the row.
-constexpr int kSumThreads = 256, kSumWarps = kSumThreads / 32, kSumCols = 8, kSumPairs = kSumCols / 2;
+constexpr int kSumCols = 8, kSumPairs = kSumCols / 2;
 constexpr uint32_t kSumWarpCols = 32 * kSumCols;
 
 template <typename T, bool kWide>
@@ -635,7 +567,10 @@ __global__ void __launch_bounds__(kSumThreads, kWide ? 3 : 4) embed_sum_kernel(c
     griddep_wait();
     if (blockIdx.x >= sum_blocks) {
         const uint32_t block = blockIdx.x - sum_blocks + a.zero_from;
-        return zero_rows(a, block, a.present + (size_t)block * zero_words(a));
+        if (a.present) return zero_rows(a, block, a.present + (size_t)block * zero_words(a));
+        __shared__ uint32_t bits[kZeroWords];
+        present_in_keys(a, block, bits);
+        return zero_rows(a, block, bits);
     }
     using Layout = SumLayout<T, kWide>;
     constexpr int kRows = Layout::kRows, E = Elem<T>::kVec;

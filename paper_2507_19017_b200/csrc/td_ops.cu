@@ -199,14 +199,13 @@ uint32_t chunk_rows(uint32_t n_tokens, uint32_t slices) {
 struct EmbedGradLayout {
     size_t keys[2], pos[2], counts, present, arrived, partial, partial_stride, total;
     uint32_t n_tiles, n_chunks, rows_per_chunk, slices, passes;
-    bool small, big_tiles;
+    bool big_tiles;
 };
 EmbedGradLayout embed_layout(uint32_t n_tokens, uint32_t vocab, uint32_t dim) {
     EmbedGradLayout L{};
     int bits = 0;
     while (bits < 32 && (vocab >> bits) != 0) ++bits;        // the keys are 0 .. vocab
     L.passes = (uint32_t)((bits + kSortBits - 1) / kSortBits);
-    L.small = n_tokens <= 16384;                             // 33000 positions: 38 us in one cluster, 20 in tiles
     L.big_tiles = n_tokens > (1u << 17);                     // every block reads all tiles' counts: few of them
     const uint32_t tile = kSortThreads * (L.big_tiles ? 16 : 4);
     L.n_tiles = (uint32_t)(((uint64_t)n_tokens + tile - 1) / tile);
@@ -249,36 +248,33 @@ cudaError_t run_sort(EmbedArgs &k, const EmbedGradLayout &L, uint8_t *ws, cudaSt
 
 template <typename T, typename G>
 cudaError_t run_embed_grad(EmbedArgs k, const EmbedGradLayout &L, uint8_t *ws, bool wide, cudaStream_t st) {
-    // Rows without a token are cleared by blocks behind those of the sums; the first of them earlier, beside the sort,
-    // which leaves most of the machine idle for 5 to 8 us, time for some 30 MB.
+    // Rows without a token are cleared by blocks behind those of the sums, 32 rows each or 32 kZeroWords.
     cudaError_t rc;
-    k.present = k.accumulate ? nullptr : reinterpret_cast<uint32_t *>(ws + L.present);
-    const uint32_t per_block = (uint64_t)k.dim * sizeof(G) >= kLongRow ? 1u : kZeroWords;         // words of k.present
-    const uint32_t zeroing = k.present ? (uint32_t)(((uint64_t)k.vocab + 32 * per_block - 1) / (32 * per_block)) : 0u;
-    // Few positions need no sort.  By blocks there would be, in us (without / with one), added into float rows: 300 of 40
-    // columns 3.7 / 11.6, 2000 of 40 13.9 / 18.7, 600 of 1001 11.2 / 17.1, 30 of 4096 3.0 / 9.1; but 1000 of 1001
-    // 18.6 / 18.5, 4000 of 40 34.6 / 23.3, 300 of 4096 15.5 / 12.9.
+    const uint32_t per_block = (uint64_t)k.dim * sizeof(G) >= kLongRow ? 1u : kZeroWords;
+    const uint32_t zeroing = k.accumulate ? 0u : (uint32_t)(((uint64_t)k.vocab + 32 * per_block - 1) / (32 * per_block));
+    // Few positions need no sort.  Without / with one, in us, added into float rows: 300 of 40 columns 4.2 / 9.5, 2000 of 40
+    // 13.9 / 14.6, 600 of 1001 11.2 / 13.9, 30 of 4096 3.3 / 8.3; but 1000 of 1001 18.6 / 15.3, 4000 of 40 34.6 / 19.5,
+    // 300 of 4096 15.5 / 10.0.
     if ((uint64_t)k.n_tokens * L.slices <= 2400) {
         const uint32_t positions = k.n_tokens * L.slices;
         if (positions + zeroing == 0) return cudaSuccess;
         return launch(wide ? embed_few_kernel<T, G, true> : embed_few_kernel<T, G, false>, (uint64_t)positions + zeroing, kSumThreads, st, 1u, k, L.slices, positions);
     }
-    const uint64_t early = (30ull << 20) / (32 * per_block * (uint64_t)k.dim * sizeof(G)) + 1;
-    // The one-block sort does not know the rows yet and clears all, which is only worth it while few of them are written again;
-    // the last of several placing kernels knows.
-    if (L.small ? k.n_tokens <= k.vocab / 8 : L.passes > 1) k.zero_from = early < zeroing ? (uint32_t)early : zeroing;
     k.arrived = reinterpret_cast<uint32_t *>(ws + L.arrived);
     k.n_arrived = 3 * L.n_chunks * L.slices;
-    if (L.small) {
-        rc = cudaFuncSetAttribute(sort_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SmallSort));
-        if (rc != cudaSuccess) return rc;
+    if (k.n_tokens <= kRankMax) {
         k.keys = reinterpret_cast<uint32_t *>(ws + L.keys[0]);
         k.pos = reinterpret_cast<uint32_t *>(ws + L.pos[0]);
-        const uint32_t blocks = k.n_tokens <= 4096 ? 1u : kSmallBlocks;       // 3000: 12.1 us on one, 13.6 on eight; 5000: 15 and 14.0
-        uint32_t log_items = 0;
-        while ((blocks * kSmallThreads << log_items) < k.n_tokens) ++log_items;
-        rc = launch_smem(sort_small_kernel, blocks + (k.zero_from ? 148 * 2 : 0), kSmallThreads, sizeof(SmallSort), st, blocks, k, L.passes, log_items);
-    } else rc = L.big_tiles ? run_sort<16>(k, L, ws, st) : run_sort<4>(k, L, ws, st);
+        rc = launch(embed_rank_kernel, (k.n_tokens + 31) / 32, kRankThreads, st, 1u, k);
+    } else {
+        if (zeroing) {
+            k.present = reinterpret_cast<uint32_t *>(ws + L.present);
+            // the last of several placing kernels leaves most of the machine idle for 8 us: time to clear the first 30 MB
+            const uint64_t early = (30ull << 20) / (32 * per_block * (uint64_t)k.dim * sizeof(G)) + 1;
+            if (L.passes > 1) k.zero_from = early < zeroing ? (uint32_t)early : zeroing;
+        }
+        rc = L.big_tiles ? run_sort<16>(k, L, ws, st) : run_sort<4>(k, L, ws, st);
+    }
     if (rc != cudaSuccess) return rc;
     const uint32_t sum_blocks = (uint32_t)(((uint64_t)L.n_chunks * L.slices + kSumThreads / 32 - 1) / (kSumThreads / 32));
     const uint32_t zero_blocks = zeroing - k.zero_from;

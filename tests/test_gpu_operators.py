@@ -614,7 +614,7 @@ def test_embed_grad_one_id_everywhere(tokens):
     check_embed_grad((torch.arange(tokens, device="cuda") // 96).flip(0).int(), grad, tokens // 96 + 2, "f32")
 
 
-@pytest.mark.parametrize("tokens,vocab", [(2400, 5000), (2401, 90), (3000, 2 ** 19 + 7), (8192, 150), (16384, 2 ** 18 + 1), (20000, 2 ** 18 - 1), (20000, 2 ** 18), (140000, 2 ** 19), (140000, 300)])
+@pytest.mark.parametrize("tokens,vocab", [(2400, 5000), (2401, 90), (2403, 40000), (4999, 7), (3000, 2 ** 19 + 7), (8192, 150), (16384, 2 ** 18 + 1), (20000, 2 ** 18 - 1), (20000, 2 ** 18), (140000, 2 ** 19), (140000, 300)])
 @pytest.mark.parametrize("dim", [8, 5])
 def test_embed_grad_sorts_of_every_size(tokens, vocab, dim):
     r = np.random.default_rng(tokens)
