@@ -170,7 +170,7 @@ __device__ __forceinline__ Share pass_over(const T *x, uint32_t vocab, uint32_t 
     return r;
 }
 
-// Bound by reading the logits once: 8192 rows of 152064 bfloat16 in 400 to 425 us, 5.9 to 6.2 TB/s (0.91 to 0.96 of
+// Bound by reading the logits once: 8192 rows of 152064 bfloat16 in 400 to 431 us, 5.8 to 6.2 TB/s (0.89 to 0.96 of
 // a plain copy's rate), the spread being the clock under power limit, because next to the memory the exponential unit is
 // 78 % busy (one exponential per score) at 5.7 instructions per score.
 // One row per cluster of `parts` blocks (1 to 8); or, kThreads = 32, per warp, kWarpRows rows a block.  A single pass over the row: every thread keeps a reference and
