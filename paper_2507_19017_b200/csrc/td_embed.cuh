@@ -43,7 +43,7 @@ __device__ __forceinline__ uint32_t tokens_in(const EmbedArgs &a) {
 // Id at position t, or vocab when there is no token.
 __device__ __forceinline__ uint32_t id_at(const EmbedArgs &a, uint32_t t, uint32_t n) {
     if (t >= n) return a.vocab;
-    const int32_t id = __ldg(a.ids + t);
+    const int32_t id = a.ids[t];
     if (id < 0) return a.vocab;
     if ((uint32_t)id >= a.vocab) {
         if (a.status) atomicOr(a.status, TD_ERR_OOB_INDEX);
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a,
         for (int u = 0; u < kEmbedUnroll; ++u) {
             const uint32_t j = lo + (u << team) + lane;
             v[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (j < nvec && !none) v[u] = __ldg(reinterpret_cast<const uint4 *>(row) + j);
+            if (j < nvec && !none) v[u] = reinterpret_cast<const uint4 *>(row)[j];
         }
     } else {
         const T *end = table + (long long)(a.vocab - 1) * a.table_stride + a.dim;
@@ -218,13 +218,13 @@ __device__ __forceinline__ void present_in_keys(const EmbedArgs &a, uint32_t blo
     uint32_t lo = 0, hi = a.n_tokens;                        // the first entry that is not below v0 lies in [lo, hi]
     while (lo < hi) {
         const uint32_t step = (hi - lo + kSumThreads - 1) / kSumThreads, at = lo + threadIdx.x * step;
-        const uint32_t below = __syncthreads_count(at < hi && __ldg(a.keys + at) < v0);
+        const uint32_t below = __syncthreads_count(at < hi && a.keys[at] < v0);
         if (below == 0) break;
         hi = min(hi, lo + below * step);
         lo += (below - 1) * step + 1;
     }
     for (uint32_t e = lo + threadIdx.x;; e += kSumThreads) {
-        const uint32_t id = e < a.n_tokens ? __ldg(a.keys + e) : a.vocab;
+        const uint32_t id = e < a.n_tokens ? a.keys[e] : a.vocab;
         const bool in = id < min(v1, a.vocab);
         if (in) atomicOr(bits + (id - v0) / 32, 1u << ((id - v0) & 31u));
         if (__syncthreads_count(in) < kSumThreads) break;
@@ -501,14 +501,14 @@ __device__ __forceinline__ bool join_run(const EmbedArgs &a, uint32_t v, uint32_
     uint32_t behind = 0, back = 0;
     for (;;) {
         const unsigned long long c = (unsigned long long)chunk + 1 + behind + lane;
-        const uint32_t same = __ballot_sync(kFullMask, c < a.n_chunks && __ldg(a.keys + c * a.rows_per_chunk) == v);
+        const uint32_t same = __ballot_sync(kFullMask, c < a.n_chunks && a.keys[c * a.rows_per_chunk] == v);
         if (same != kFullMask) { behind += __ffs(~same) - 1; break; }
         behind += 32;
     }
     if (cont)
         for (;;) {
             const long long c = (long long)chunk - 1 - back - lane;
-            const uint32_t same = __ballot_sync(kFullMask, c > 0 && __ldg(a.keys + (size_t)c * a.rows_per_chunk - 1) == v);
+            const uint32_t same = __ballot_sync(kFullMask, c > 0 && a.keys[(size_t)c * a.rows_per_chunk - 1] == v);
             if (same != kFullMask) { back += __ffs(~same); break; }
             back += 32;
         }
@@ -587,9 +587,9 @@ __global__ void __launch_bounds__(kSumThreads, kWide ? 3 : 4) embed_sum_kernel(c
 
     // keys and positions, 32 entries at a time; the rows of the next group are on their way while one is added
     const uint32_t *keys = a.keys + lo, *pos = a.pos + lo;
-    auto batch = [&](const uint32_t *p, uint32_t b, uint32_t none) { return b + lane < n ? __ldg(p + b + lane) : none; };
+    auto batch = [&](const uint32_t *p, uint32_t b, uint32_t none) { return b + lane < n ? p[b + lane] : none; };
     uint32_t my_key = batch(keys, 0, a.vocab), my_pos = batch(pos, 0, 0u);
-    const uint32_t before = lo > 0 ? __ldg(keys - 1) : a.vocab, after = lo + n < a.n_tokens ? __ldg(keys + n) : a.vocab;
+    const uint32_t before = lo > 0 ? a.keys[lo - 1] : a.vocab, after = lo + n < a.n_tokens ? keys[n] : a.vocab;
     uint32_t v = __shfl_sync(kFullMask, my_key, 0);
     if (v >= a.vocab) return;                                // sorted behind all ids
     const uint32_t first = v;

@@ -32,7 +32,7 @@ constexpr float kFarBelow = -1000.0f;    // 2^-1000 is 0 in float: scores below 
 
 // Target of token t, or -1; a target past the vocabulary is reported.
 __device__ __forceinline__ int32_t target_of(const LogprobArgs &a, uint32_t t, bool report) {
-    const int32_t y = __ldg(a.targets + t);
+    const int32_t y = a.targets[t];
     if (y >= 0 && (uint32_t)y >= a.vocab) {
         if (a.status && report) atomicOr(a.status, TD_ERR_OOB_INDEX);
         return -1;

@@ -25,6 +25,11 @@ __device__ __forceinline__ uint32_t batch_samples(const BatchView &b) {
     return b.result ? min(b.result->n_samples, b.max_samples) : b.max_samples;
 }
 
+// Operands are read with ordinary loads, never through the read-only path (__ldg, ld.global.nc): that path is
+// defined only for memory that nothing writes while the kernel runs, and a kernel here is let in while the one
+// ahead of it, which may be what writes an operand, is still running.  Behind griddep_wait() an ordinary load
+// has that kernel's results.
+
 // The sample whose row [cu[s], cu[s + 1]) holds position t: the last s in [lo, n) with cu[s] <= t.
 // Rows of length zero are passed over; for a cu array that is not non-decreasing the answer is some
 // index of [lo, n).
@@ -32,7 +37,7 @@ __device__ __forceinline__ uint32_t sample_of(const int32_t *cu, uint32_t lo, ui
     uint32_t hi = n;
     while (hi - lo > 1) {
         const uint32_t mid = lo + (hi - lo) / 2;
-        if ((long long)__ldg(cu + mid) <= t) lo = mid; else hi = mid;
+        if ((long long)cu[mid] <= t) lo = mid; else hi = mid;
     }
     return lo;
 }

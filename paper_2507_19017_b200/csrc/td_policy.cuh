@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_count_kernel(const Poli
             const uint4 *mv = reinterpret_cast<const uint4 *>(m + head);
 #pragma unroll 4
             for (long long i = lane; i < nvec; i += 32) {
-                const uint4 v = __ldg(mv + i);
+                const uint4 v = mv[i];
                 c += (__popc(__vcmpne4(v.x, 0u)) + __popc(__vcmpne4(v.y, 0u)) + __popc(__vcmpne4(v.z, 0u)) + __popc(__vcmpne4(v.w, 0u))) >> 3;
             }
             const long long tail = head + nvec * 16;
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(kPolicyThreads, kPolicyBlocksPerSm) policy_los
         while (hi - lo > 1) {
             const uint32_t step = (hi - lo + kPolicyThreads - 1) / kPolicyThreads;
             const uint64_t at = lo + (uint64_t)(threadIdx.x + 1) * step;
-            const int below = __syncthreads_count(at < hi && (long long)__ldg(a.batch.cu_response + at) <= base);
+            const int below = __syncthreads_count(at < hi && (long long)a.batch.cu_response[at] <= base);
             lo += (uint32_t)below * step;
             hi = min(hi, lo + step);
         }
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(kPolicyThreads, kPolicyBlocksPerSm) policy_los
     else {
         long long c = 0;
         if (a.need_counts) {
-            for (uint32_t s = threadIdx.x; s < n; s += kPolicyThreads) c += __ldg(a.counts + s);
+            for (uint32_t s = threadIdx.x; s < n; s += kPolicyThreads) c += a.counts[s];
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(kFullMask, c, o);
             if (lane == 0) warp_counts[warp] = c;
@@ -354,7 +354,8 @@ __global__ void __launch_bounds__(kPolicyThreads, kPolicyBlocksPerSm) policy_los
     }
     auto weight = [&](uint32_t s, const Span &p) {
         if (!a.mean_samples) return common;
-        const int32_t c = a.need_counts ? __ldg(a.counts + s) : (int32_t)(p.valid_end - p.first);
+        // (with a load that passes by L1, ld.global.cg, the kernel took 8 us more whether or not it has counts)
+        const int32_t c = a.need_counts ? a.counts[s] : (int32_t)(p.valid_end - p.first);
         return c > 0 ? common / (float)c : 0.0f;
     };
     auto from_base = [&](long long p) { return (int)max(-1ll, min(p - base, (long long)size)); };
@@ -363,7 +364,7 @@ __global__ void __launch_bounds__(kPolicyThreads, kPolicyBlocksPerSm) policy_los
         const Span p = span_of(a, s);
         win_first[threadIdx.x] = from_base(p.first);
         win_end[threadIdx.x] = from_base(p.valid_end);
-        win_adv[threadIdx.x] = __ldg(a.advantages + s);
+        win_adv[threadIdx.x] = a.advantages[s];
         win_w[threadIdx.x] = weight(s, p);
     }
     __syncthreads();
@@ -376,7 +377,7 @@ __global__ void __launch_bounds__(kPolicyThreads, kPolicyBlocksPerSm) policy_los
         const uint32_t left = n - s0;
         auto starts = [&](uint32_t i) {
             if (i < in_window) return win_first[i];
-            return a.row_width ? from_base((long long)(s0 + i) * (long long)a.row_width) : from_base(__ldg(a.batch.cu_response + s0 + i));
+            return a.row_width ? from_base((long long)(s0 + i) * (long long)a.row_width) : from_base(a.batch.cu_response[s0 + i]);
         };
         uint32_t lo = at, step = 1;      // gallop: the next sample is usually near
         while (lo + step < left && starts(lo + step) <= q) { lo += step; step <<= 1; }
@@ -397,7 +398,7 @@ __global__ void __launch_bounds__(kPolicyThreads, kPolicyBlocksPerSm) policy_los
             const Span p = span_of(a, s0 + lo);
             seat.first = from_base(p.first);
             seat.end = from_base(p.valid_end);
-            adv = __ldg(a.advantages + s0 + lo);
+            adv = a.advantages[s0 + lo];
             seat.w = weight(s0 + lo, p);
         }
         seat.neg_adv = -adv;

@@ -685,3 +685,64 @@ def test_operators_run_on_the_stream_they_are_given():
         assert torch.equal(rows_out, table[y.long()])
         want = torch.zeros(vocab, dim, dtype=torch.float64, device="cuda").index_add_(0, y.long(), rows_out.double())
         assert ((dtable - want).abs() <= 64 * U * want.abs().clamp(min=8.0)).all()
+
+
+# ------------------------------------------------------------------ one call's output as the next one's operand
+def test_calls_read_what_the_call_before_them_has_just_written():
+    """Rounds without a synchronisation in which every operand of a call but the first's was written by the kernel right
+    ahead of it, in buffers that the rounds share; each round's results against 64 bits afterwards."""
+    rounds, tokens, vocab, dim = 6, 9000, 700, 96
+    ids = [torch.randint(vocab, (tokens,), generator=gen(k), device="cuda", dtype=torch.int32) for k in range(rounds)]
+    table = table_of(vocab, dim, "f32", 1)
+    y = torch.randint(dim, (tokens,), generator=gen(20), device="cuda", dtype=torch.int32)
+    g = torch.randn(tokens, generator=gen(21), device="cuda")
+    rows, grad = torch.empty(tokens, dim, device="cuda"), torch.empty(tokens, dim, device="cuda")
+    dtable, back = torch.empty(vocab, dim, device="cuda"), torch.empty(tokens, dim, device="cuda")
+    lp, ws = td.LogprobBuffers(tokens), td.EmbedGradWorkspace(tokens, vocab, dim)
+    kept = []
+    for k in range(rounds):
+        td.embed(rows, ids[k], table, scale=1.0 + k)
+        td.token_logprob(lp, rows, y)
+        td.token_logprob_grad(grad, rows, y, lp.norm, g)
+        td.embed_grad(dtable, ids[k], grad, ws)
+        td.embed(back, ids[k], dtable)
+        kept.append([t.clone() for t in (rows, lp.logprob, grad, dtable, back)])
+    for k, (rows_k, lp_k, grad_k, dtable_k, back_k) in enumerate(kept):
+        x = table[ids[k].long()].float() * (1.0 + k)
+        assert torch.equal(rows_k, x)
+        want_lp, _, _, h, logp = exact_logprob(x, y)
+        assert ((lp_k - want_lp).abs() <= logprob_tol(dim) + 4 * U * want_lp.abs()).all()
+        want = exact_grad(logp, h, y, g.double(), 0 * g.double(), 1.0)
+        assert ((grad_k - want).abs() <= grad_bound(logp, h, g.double(), 0 * g.double(), 1.0, dim, "f32", want)).all()
+        at = ids[k].long()
+        total = torch.zeros(vocab, dim, dtype=torch.float64, device="cuda").index_add_(0, at, grad_k.double())
+        size = torch.zeros(vocab, dim, dtype=torch.float64, device="cuda").index_add_(0, at, grad_k.double().abs())
+        many = torch.bincount(at, minlength=vocab).double()[:, None]
+        assert ((dtable_k - total).abs() <= (many + 4) * U * size + rounding(total, "f32")).all()
+        assert torch.equal(back_k, dtable_k[at])
+
+
+@pytest.mark.parametrize("mean", [td.MEAN_TOKENS, td.MEAN_SAMPLES])
+def test_policy_loss_counts_of_a_mask_that_changes_between_calls(mean):
+    """Rounds without a synchronisation on one set of buffers; every round's mask leaves another number of tokens."""
+    lens = [40, 0, 700, 3, 2500, 61]
+    lp, old, _, _, _, adv = policy_inputs(lens, 4)
+    n = sum(lens)
+    draw = np.random.default_rng(9)
+    masks = [draw.random(n) < p for p in (0.9, 0.1, 0.5, 0.0, 0.7, 0.01, 1.0, 0.3)]
+    cfg = td.PolicyLossConfig(reduction=mean)
+    batch, out = td.Batch(None, cu_of(lens)), td.PolicyLossBuffers(n, len(lens))
+    dev = [torch.from_numpy(a).cuda() for a in (lp, old, adv)]
+    sources = [torch.from_numpy(m).cuda() for m in masks]
+    mask, kept = torch.empty(n, dtype=torch.bool, device="cuda"), []
+    for source in sources:
+        mask.copy_(source)
+        td.policy_loss(out, batch, dev[0], dev[2], old_logprob=dev[1], mask=mask, config=cfg)
+        kept.append((out.stats.clone(), out.grad_logprob.clone()))
+    for m, (stats, grad_lp) in zip(masks, kept):
+        if not m.any():
+            assert (stats == 0).all() and (grad_lp == 0).all()
+            continue
+        sums, mags, grad, _, size = exact_policy(cfg, lens, lp, old, None, None, m, adv, 0, len(lens))
+        assert (np.abs(stats.double().cpu().numpy() - sums) <= 2.0 ** -18 * mags + 1e-30).all()
+        assert (np.abs(grad_lp.double().cpu().numpy() - grad) <= 2.0 ** -18 * size + 1e-30).all()

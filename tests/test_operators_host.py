@@ -188,3 +188,13 @@ def test_binding_refuses_what_is_not_on_a_device(td):
         td.Batch(None, None)
     with pytest.raises(ValueError):
         td.Batch(None, y)
+
+
+def test_operator_kernels_do_not_read_through_the_read_only_path():
+    """That path (__ldg, ld.global.nc) is defined only for memory nothing writes while the kernel runs; these kernels
+    are let in while the one ahead of them, which may write their operands, is still running."""
+    csrc = os.path.join(ROOT, "paper_2507_19017_b200", "csrc")
+    for name in ("td_ops.cu", "td_ops.cuh", "td_logprob.cuh", "td_policy.cuh", "td_embed.cuh"):
+        with open(os.path.join(csrc, name)) as f:
+            code = "\n".join(line.split("//")[0] for line in f)
+        assert "__ldg" not in code and "global.nc" not in code and "tex." not in code, name
