@@ -604,6 +604,8 @@ typedef struct {
     uint64_t workspace_bytes;              /* >= td_embed_grad_workspace_bytes(n_tokens, vocab, dim) */
     uint32_t *status;
 } td_embed_grad_args;
+/* Never falls as an argument grows: a workspace for the largest call serves every call with no more
+ * positions, vocabulary and columns.  0 where an argument is 2^31 or more. */
 size_t td_embed_grad_workspace_bytes(uint32_t n_tokens, uint32_t vocab, uint32_t dim);
 int td_embed_grad(const td_embed_grad_args *args, void *stream);
 

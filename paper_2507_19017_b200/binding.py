@@ -877,7 +877,7 @@ def embed(out, ids, table, scale: float = 1.0, batch: Optional[Batch] = None, to
 
 
 class EmbedGradWorkspace:
-    """Workspace of embed_grad for up to n_tokens positions and rows of dim columns."""
+    """Workspace of embed_grad for up to n_tokens positions, vocab table rows and dim columns."""
 
     def __init__(self, n_tokens: int, vocab: int, dim: int, device: int = 0):
         import torch

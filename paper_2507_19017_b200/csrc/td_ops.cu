@@ -1,5 +1,6 @@
 // Host side of the operators on a served batch (include/td.h): argument checks and launches.
 // Nothing is allocated and nothing synchronises.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <utility>
@@ -191,22 +192,37 @@ cudaError_t run_embed(const EmbedArgs &k, bool whole, cudaStream_t st) {
 // Sorted positions per chunk of the segment sums: short chunks while there are few positions to spread over the
 // machine, long ones later (a run cut by a border costs two float rows of extra traffic, and one warp joins
 // its parts).  65536 positions x 8 slices: 295 us with 64, 327 with 32, 309 with 128.
+constexpr uint32_t kMinChunk = 8, kMaxChunk = 512, kWantParts = 148 * 64;
 uint32_t chunk_rows(uint32_t n_tokens, uint32_t slices) {
-    uint32_t r = 8;
-    while (r < 512 && (uint64_t)n_tokens * slices > (uint64_t)r * 148 * 64) r *= 2;
+    uint32_t r = kMinChunk;
+    while (r < kMaxChunk && (uint64_t)n_tokens * slices > (uint64_t)r * kWantParts) r *= 2;
     return r;
+}
+// The most (chunk, slice) pairs of a call of up to n_tokens positions and up to so many slices: with the shortest chunks
+// ceil(n / 8) slices; with longer ones kWantParts and the last, partly filled chunk's, or ceil(n / 512) slices
+// where even the longest chunks are more.
+uint64_t most_parts(uint32_t n_tokens, uint32_t slices) {
+    const uint64_t shortest = ((uint64_t)n_tokens + kMinChunk - 1) / kMinChunk * slices, longest = ((uint64_t)n_tokens + kMaxChunk - 1) / kMaxChunk * slices;
+    return std::min<uint64_t>(shortest, std::max<uint64_t>((uint64_t)kWantParts + slices, longest));
+}
+constexpr uint32_t kFewTiles = 1u << 17;                     // positions up to which a tile of the sort is kSortThreads * 4, beyond * 16
+uint32_t most_tiles(uint32_t n_tokens) {                     // of a call of up to n_tokens positions
+    const uint32_t small = (std::min(n_tokens, kFewTiles) + kSortThreads * 4 - 1) / (kSortThreads * 4);
+    return std::max(small, (uint32_t)(((uint64_t)n_tokens + kSortThreads * 16 - 1) / (kSortThreads * 16)));
 }
 struct EmbedGradLayout {
     size_t keys[2], pos[2], counts, present, arrived, partial, partial_stride, total;
     uint32_t n_tiles, n_chunks, rows_per_chunk, slices, passes;
     bool big_tiles;
 };
+// Areas have room for what any call with no more positions, vocabulary and columns would take, so that a workspace for the
+// largest call holds for all.
 EmbedGradLayout embed_layout(uint32_t n_tokens, uint32_t vocab, uint32_t dim) {
     EmbedGradLayout L{};
     int bits = 0;
     while (bits < 32 && (vocab >> bits) != 0) ++bits;        // the keys are 0 .. vocab
     L.passes = (uint32_t)((bits + kSortBits - 1) / kSortBits);
-    L.big_tiles = n_tokens > (1u << 17);                     // every block reads all tiles' counts: few of them
+    L.big_tiles = n_tokens > kFewTiles;                      // every block reads all tiles' counts: few of them
     const uint32_t tile = kSortThreads * (L.big_tiles ? 16 : 4);
     L.n_tiles = (uint32_t)(((uint64_t)n_tokens + tile - 1) / tile);
     L.slices = (uint32_t)(((uint64_t)dim + kSumWarpCols - 1) / kSumWarpCols);
@@ -216,10 +232,11 @@ EmbedGradLayout embed_layout(uint32_t n_tokens, uint32_t vocab, uint32_t dim) {
     size_t p = 0;
     auto take = [&](size_t bytes) { const size_t at = p; p = round_up(p + bytes, 256); return at; };
     for (int k = 0; k < 2; ++k) { L.keys[k] = take((size_t)n_tokens * 4); L.pos[k] = take((size_t)n_tokens * 4); }
-    L.counts = take((size_t)L.passes * L.n_tiles * kSortBins * 4);
+    const size_t parts = most_parts(n_tokens, L.slices);
+    L.counts = take((size_t)L.passes * most_tiles(n_tokens) * kSortBins * 4);
     L.present = take(((size_t)vocab + 31) / 32 * 4);
-    L.arrived = take(3 * (size_t)L.n_chunks * L.slices * 4);
-    L.partial = take(2 * (size_t)L.n_chunks * L.partial_stride * 4);
+    L.arrived = take(3 * parts * 4);
+    L.partial = take(2 * parts * kSumWarpCols * 4);
     L.total = p;
     return L;
 }

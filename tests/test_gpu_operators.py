@@ -746,3 +746,20 @@ def test_policy_loss_counts_of_a_mask_that_changes_between_calls(mean):
         sums, mags, grad, _, size = exact_policy(cfg, lens, lp, old, None, None, m, adv, 0, len(lens))
         assert (np.abs(stats.double().cpu().numpy() - sums) <= 2.0 ** -18 * mags + 1e-30).all()
         assert (np.abs(grad_lp.double().cpu().numpy() - grad) <= 2.0 ** -18 * size + 1e-30).all()
+
+
+def test_embed_grad_smaller_calls_in_the_workspace_of_the_largest():
+    """One workspace; calls on both sides of every size at which their layout of it changes."""
+    vocab, dim = 3001, 1024
+    ws = td.EmbedGradWorkspace(19500, vocab, dim)
+    r = np.random.default_rng(3)
+    ids = torch.from_numpy((vocab ** r.random(19500)).astype(np.int32).clip(0, vocab - 1)).cuda()
+    grad = table_of(19500, dim, "bf16", 3)
+    for n in (19500, 18945, 18944, 18000, 9500, 8193, 8192, 601, 600, 5):     # 18944 positions x 4 slices: the longest of 8 a chunk
+        dtable = torch.empty(vocab, dim, device="cuda")
+        td.embed_grad(dtable, ids[:n], grad[:n], ws)
+        at = ids[:n].long()
+        want = torch.zeros(vocab, dim, dtype=torch.float64, device="cuda").index_add_(0, at, grad[:n].double())
+        size = torch.zeros(vocab, dim, dtype=torch.float64, device="cuda").index_add_(0, at, grad[:n].double().abs())
+        many = torch.bincount(at, minlength=vocab).double()[:, None]
+        assert ((dtable - want).abs() <= (many + 4) * U * size + rounding(want, "f32")).all(), n

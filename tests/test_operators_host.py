@@ -198,3 +198,37 @@ def test_operator_kernels_do_not_read_through_the_read_only_path():
         with open(os.path.join(csrc, name)) as f:
             code = "\n".join(line.split("//")[0] for line in f)
         assert "__ldg" not in code and "global.nc" not in code and "tex." not in code, name
+
+
+def thresholds(vocab, dim):
+    """Numbers of positions around which the call's layout changes: chunks of the sums double, tiles of the sort grow."""
+    slices = -(-dim // 256)
+    at = {1, 8, 100, 2400, 8192, 2 ** 17, 2 ** 20, 3 * 10 ** 6}
+    for r in (8, 16, 32, 64, 128, 256, 512):
+        at.add(r * 148 * 64 // slices)
+    return sorted({n + k for n in at for k in (-1, 0, 1, 2, 500) if n + k >= 0})
+
+
+@pytest.mark.parametrize("vocab", [1, 511, 512, 32003, 129280, 2 ** 20])
+def test_embed_grad_workspace_holds_for_every_smaller_call(td, vocab):
+    """The size never falls as positions, vocabulary or columns grow."""
+    size = td.lib().td_embed_grad_workspace_bytes
+    dims = [1, 23, 255, 256, 257, 512, 1001, 1024, 2048, 4096, 5000, 8192, 70000]
+    last = None
+    for dim in dims:
+        at = thresholds(vocab, dim)
+        now = [size(n, vocab, dim) for n in at]
+        assert all(a <= b for a, b in zip(now, now[1:])), dim
+        assert all(size(n, v, dim) <= size(n, vocab, dim) for n in at[::7] for v in (1, 500, vocab // 2 + 1) if v <= vocab)
+        common = [size(n, vocab, dim) for n in thresholds(vocab, 2048)]
+        assert last is None or all(a <= b for a, b in zip(last, common)), dim
+        last = common
+
+
+def test_embed_grad_takes_a_larger_calls_workspace(td):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is present")
+    room = td.lib().td_embed_grad_workspace_bytes(65536, 129280, 2048)
+    for n in (37888, 37000, 9472, 8700, 20000, 65535, 1):
+        assert embed_grad(td, n_tokens=n, vocab=129280, dim=2048, table_stride=2048, out_stride=2048, workspace_bytes=room) == td.ECUDA, n
