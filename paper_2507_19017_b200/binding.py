@@ -881,6 +881,7 @@ class EmbedGradWorkspace:
 
     def __init__(self, n_tokens: int, vocab: int, dim: int, device: int = 0):
         import torch
+        self.device = device
         self.nbytes = lib().td_embed_grad_workspace_bytes(n_tokens, vocab, dim)
         self.memory = torch.empty(self.nbytes, dtype=torch.uint8, device=torch.device("cuda", device))
         self.address = self.memory.data_ptr()
@@ -896,6 +897,8 @@ def embed_grad(grad_table, ids, grad_out, workspace: EmbedGradWorkspace, scale: 
     o, ostride, tag, out_rows, out_dim = _matrix(grad_out, "grad_out", device)
     if out_rows != n or out_dim != dim:
         raise ValueError(f"grad_out: needs shape ({n}, {dim})")
+    if workspace.device != device:
+        raise ValueError(f"workspace: on cuda:{workspace.device}, the operands are on cuda:{device}")
     _EMBED_GRAD(_op_stream(stream, device), _vector(ids, 0, "ids", "i32", device), n, vocab, dim, tag, o, ostride, gtag,
                 1 if accumulate else 0, g, gstride, scale, tokens, device, 0, _batch_address(batch, device),
                 workspace.address, workspace.nbytes, _vector(status, 1, "status", "i32", device))

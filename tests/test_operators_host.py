@@ -232,3 +232,34 @@ def test_embed_grad_takes_a_larger_calls_workspace(td):
     room = td.lib().td_embed_grad_workspace_bytes(65536, 129280, 2048)
     for n in (37888, 37000, 9472, 8700, 20000, 65535, 1):
         assert embed_grad(td, n_tokens=n, vocab=129280, dim=2048, table_stride=2048, out_stride=2048, workspace_bytes=room) == td.ECUDA, n
+
+
+class OnDevice:
+    """What the binding asks of a tensor, for one that would be on a device."""
+
+    def __init__(self, dtype, *shape, device=0):
+        self.dtype, self.shape, self.device = dtype, shape, device
+
+    def get_device(self):
+        return self.device
+
+    def stride(self):
+        return (self.shape[1], 1) if len(self.shape) == 2 else (1,)
+
+    def numel(self):
+        return math.prod(self.shape)
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return A
+
+
+def test_embed_grad_refuses_a_workspace_on_another_device(td):
+    import torch
+    ws = object.__new__(td.EmbedGradWorkspace)
+    ws.device, ws.address, ws.nbytes = 1, A, td.lib().td_embed_grad_workspace_bytes(8, 50, 16)
+    ids, grad, table = OnDevice(torch.int32, 8), OnDevice(torch.float32, 8, 16), OnDevice(torch.float32, 50, 16)
+    with pytest.raises(ValueError, match="workspace"):
+        td.embed_grad(table, ids, grad, ws, stream=0)
