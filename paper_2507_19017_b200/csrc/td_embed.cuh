@@ -108,12 +108,13 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a,
     for (int u = 0; u < kEmbedUnroll; ++u) {
         const uint32_t j = lo + (u << team) + lane;
         if (j >= nvec) break;
+        if (!none)                       // zeros stay zeros, whatever the scale's sign or value
 #pragma unroll
-        for (int k = 0; k < E / 2; ++k) {
-            float p, q;
-            unpack2(mul2(Elem<T>::pair(v[u], k), sc), p, q);
-            Elem<T>::put_pair(v[u], k, p, q);
-        }
+            for (int k = 0; k < E / 2; ++k) {
+                float p, q;
+                unpack2(mul2(Elem<T>::pair(v[u], k), sc), p, q);
+                Elem<T>::put_pair(v[u], k, p, q);
+            }
         st_stream(out + head + j * E, v[u]);
     }
     if (piece == 0) {

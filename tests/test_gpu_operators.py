@@ -763,3 +763,19 @@ def test_embed_grad_smaller_calls_in_the_workspace_of_the_largest():
         size = torch.zeros(vocab, dim, dtype=torch.float64, device="cuda").index_add_(0, at, grad[:n].double().abs())
         many = torch.bincount(at, minlength=vocab).double()[:, None]
         assert ((dtable - want).abs() <= (many + 4) * U * size + rounding(want, "f32")).all(), n
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dim,pad,offset", [(64, 0, 0), (4096, 0, 0), (61, 0, 0), (1001, 3, 1), (5, 0, 0)])
+@pytest.mark.parametrize("scale", [-2.0, math.inf, math.nan])
+def test_embed_rows_without_a_token_are_plain_zeros(name, dim, pad, offset, scale):
+    """Bit for bit, at every alignment, whatever the scale is."""
+    table = table_of(20, dim, name, 1, pad, offset)
+    ids = torch.tensor([3, -1, 19, 20, 0, -5, 7, 2], dtype=torch.int32, device="cuda")
+    batch = td.Batch(cu_of([2, 3]), cu_of([1, 1]))               # 7 of the 8 positions
+    out = table_of(8, dim, name, 2, pad, offset)
+    td.embed(out, ids, table, scale=scale, batch=batch)
+    bits = out[[1, 3, 5, 7]].contiguous().view(torch.int32 if name == "f32" else torch.int16)
+    assert (bits == 0).all()
+    if scale == -2.0:
+        assert torch.equal(out[[0, 2, 4, 6]], (table[[3, 19, 0, 7]].float() * scale).to(table.dtype))
