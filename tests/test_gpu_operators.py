@@ -779,3 +779,70 @@ def test_embed_rows_without_a_token_are_plain_zeros(name, dim, pad, offset, scal
     assert (bits == 0).all()
     if scale == -2.0:
         assert torch.equal(out[[0, 2, 4, 6]], (table[[3, 19, 0, 7]].float() * scale).to(table.dtype))
+
+
+# Beyond 2400 (position, 256 columns) pairs, so that the sorted sums run, with several slices of columns: positions ordered by
+# counting (3000) and by digits in two passes (9000), a last slice that is whole, one vector, or odd; tables beyond the 30 MB that are
+# cleared beside the last placing pass, of long rows and of short ones, with the rest behind the sums.
+WIDE_SUMS = [(3000, 700, 1024, 0, 0), (3000, 700, 1001, 0, 0), (3000, 700, 1000, 24, 8), (2500, 40, 264, 0, 0), (2500, 40, 257, 5, 3),
+             (9000, 2000, 513, 0, 1), (9000, 40000, 600, 0, 0), (9000, 40000, 601, 0, 0), (9000, 20000, 2048, 0, 0), (9000, 170000, 100, 0, 0),
+             (9000, 170000, 100, 4, 0)]
+
+
+@pytest.mark.parametrize("name,gname", [("bf16", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("f16", "f16"), ("f32", "f32")])
+@pytest.mark.parametrize("tokens,vocab,dim,pad,offset", WIDE_SUMS)
+def test_embed_grad_sums_of_several_slices(name, gname, tokens, vocab, dim, pad, offset):
+    r = np.random.default_rng(dim)
+    skewed = torch.from_numpy((vocab ** r.random(tokens)).astype(np.int32).clip(0, vocab - 1)).cuda()
+    skewed[::29] = -1
+    skewed[-1] = vocab - 1
+    grad = table_of(tokens, dim, name, 3, pad, offset)
+    for accumulate in (False, True):
+        first = check_embed_grad(skewed, grad, vocab, gname, 0.5, pad, offset, accumulate)
+        assert torch.equal(first, check_embed_grad(skewed, grad, vocab, gname, 0.5, pad, offset, accumulate))
+        del first
+        # one id for all, and runs whose ends fall on chunk borders and inside chunks
+        check_embed_grad(torch.full_like(skewed, vocab // 2), grad, vocab, gname, -1.0, pad, offset, accumulate)
+        runs = (torch.arange(tokens, device="cuda") // 40 * 7 % vocab).int()
+        check_embed_grad(runs[torch.randperm(tokens, generator=gen(6), device="cuda")], grad, vocab, gname, 1.0, pad, offset, accumulate)
+
+
+def test_embed_grad_of_rows_at_different_strides_and_alignments():
+    """Rows further apart than they are long, in both tensors by different amounts, at places of different alignment."""
+    tokens, vocab, dim = 3000, 500, 777
+    grad, dtable = table_of(tokens, dim, "bf16", 3, 11, 5), table_of(vocab, dim, "f32", 4, 3, 1)
+    ids = torch.randint(vocab, (tokens,), generator=gen(7), device="cuda", dtype=torch.int32)
+    td.embed_grad(dtable, ids, grad, td.EmbedGradWorkspace(tokens, vocab, dim))
+    want = torch.zeros(vocab, dim, dtype=torch.float64, device="cuda").index_add_(0, ids.long(), grad.double())
+    size = torch.zeros(vocab, dim, dtype=torch.float64, device="cuda").index_add_(0, ids.long(), grad.double().abs())
+    many = torch.bincount(ids.long(), minlength=vocab).double()[:, None]
+    assert ((dtable - want).abs() <= (many + 4) * U * size + rounding(want, "f32")).all()
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("dim,gap,offset", [(64, 8, 0), (300, 3, 0), (1001, 5, 1), (20, 1, 3)])
+def test_operators_leave_what_lies_between_rows_alone(name, dim, gap, offset):
+    def home_of(rows):
+        flat = torch.full((rows * (dim + gap) + offset + 8,), 7.0, dtype=DTYPES[name], device="cuda")
+        return flat, flat[offset:offset + rows * (dim + gap)].view(rows, dim + gap)
+
+    def untouched(flat, home):
+        inside = torch.zeros_like(flat, dtype=torch.bool)
+        inside[offset:offset + home.numel()].view(home.shape)[:, :dim] = True
+        return bool((flat[~inside] == 7.0).all())
+
+    for tokens in (30, 3000):
+        table, ids = table_of(90, dim, name, 1), torch.randint(90, (tokens,), generator=gen(5), device="cuda", dtype=torch.int32)
+        flat, home = home_of(tokens)
+        td.embed(home[:, :dim], ids, table)
+        assert untouched(flat, home) and torch.equal(home[:, :dim], table[ids.long()])
+        grad = table_of(tokens, dim, name, 2)
+        flat, home = home_of(2000)
+        td.embed_grad(home[:, :dim], ids, grad, td.EmbedGradWorkspace(tokens, 2000, dim))
+        assert untouched(flat, home) and (home[90:, :dim] == 0).all()
+        flat, home = home_of(tokens)
+        y = torch.randint(dim, (tokens,), generator=gen(6), device="cuda", dtype=torch.int32)
+        lp = td.LogprobBuffers(tokens)
+        td.token_logprob(lp, grad, y)
+        td.token_logprob_grad(home[:, :dim], grad, y, lp.norm, torch.ones(tokens, device="cuda"))
+        assert untouched(flat, home)
