@@ -846,3 +846,139 @@ def test_operators_leave_what_lies_between_rows_alone(name, dim, gap, offset):
         td.token_logprob(lp, grad, y)
         td.token_logprob_grad(home[:, :dim], grad, y, lp.norm, torch.ones(tokens, device="cuda"))
         assert untouched(flat, home)
+
+
+# ------------------------------------------------------------------ policy loss of many samples
+def wide_policy(cfg, lens, lp, old, ref, ent, mask, adv, width, served):
+    """exact_policy for large batches: the same formulas in 64 bits over whole tensors."""
+    n, dev = lp.numel(), lp.device
+    lens = torch.as_tensor(lens, device=dev)
+    count = lens[:served].clamp(max=width) if width else lens[:served]
+    first = torch.arange(served, device=dev) * width if width else lens[:served].cumsum(0) - lens[:served]
+    sample = torch.repeat_interleave(torch.arange(served, device=dev), count)
+    p = first[sample] + torch.arange(sample.numel(), device=dev) - (count.cumsum(0) - count)[sample]
+    inside = p < n
+    if mask is not None:
+        inside &= mask[p.clamp(max=n - 1)]
+    sample, p = sample[inside], p[inside]
+    kept = torch.bincount(sample, minlength=served).double()
+    total = float(p.numel())
+    if cfg.reduction == td.MEAN_TOKENS:
+        w = torch.full((p.numel(),), 1.0 / (cfg.norm if cfg.norm > 0 else total), dtype=torch.float64, device=dev)
+    else:
+        w = 1.0 / ((cfg.norm if cfg.norm > 0 else served) * kept[sample])
+    A, x = adv[sample].double(), lp[p].double()
+    raw = x - old[p].double() if old is not None else torch.zeros_like(x)
+    limited = raw.clamp(-30, 30)
+    r = limited.exp()
+    lo, hi = float(np.float32(1) - np.float32(cfg.clip_low)), float(np.float32(1) + np.float32(cfg.clip_high))
+    free, held = -A * r, -A * r.clamp(lo, hi)
+    clipped = free < held
+    pg = torch.maximum(free, held)
+    d = torch.where(clipped | (raw != limited), 0.0, free)
+    if cfg.dual_clip > 0:
+        over = (A < 0) & (pg > -A * cfg.dual_clip)
+        pg, d, clipped = torch.where(over, -A * cfg.dual_clip, pg), torch.where(over, 0.0, d), clipped | over
+    kl, size = torch.zeros_like(x), w * A.abs() * r
+    if ref is not None:
+        gap = ref[p].double() - x
+        k = gap.clamp(-30, 30)
+        kl, dk = {td.KL_K1: (-k, torch.ones_like(k)), td.KL_K2: (k * k / 2, -k), td.KL_K3: (torch.expm1(k) - k, -torch.expm1(k))}[cfg.kl_kind]
+        d = d + torch.where(k == gap, cfg.kl_coef * dk, 0.0)
+        size = size + w * abs(cfg.kl_coef) * (k.exp() + k.abs() + 1)
+    e = ent[p].double() if ent is not None else torch.zeros_like(x)
+    ones = torch.ones_like(x)
+    each = torch.stack([w * (pg + cfg.kl_coef * kl - cfg.entropy_coef * e), w * pg, w * kl, w * e, clipped.double() / total, -raw / total, r / total, ones])
+    mags = each.abs().sum(1)
+    mags[0] += (size + w * (cfg.entropy_coef * e).abs()).sum()
+    mags[2] += 3 * w.sum()
+    full = [torch.zeros(n, dtype=torch.float64, device=dev) for _ in range(3)]
+    full[0][p], full[2][p] = w * d * cfg.grad_scale, size * abs(cfg.grad_scale)
+    if ent is not None:
+        full[1][p] = -cfg.entropy_coef * w * cfg.grad_scale
+    return each.sum(1), mags, full
+
+
+def check_wide(cfg, lens, arrays, width=0, served=None, bf16=False, offset=0, terms="all"):
+    lp, old, ref, ent, mask, adv = arrays
+    if "e" not in terms and terms != "all":
+        ent = None
+    if "m" not in terms and terms != "all":
+        mask = None
+    count = len(lens) if served is None else min(served, len(lens))
+    out = run_policy(cfg, lens, lp, old, ref, ent, mask, adv, width=width, served=served, bf16=bf16, offset=offset)
+    dev = [None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda() for a in (lp, old, ref, ent, mask, adv)]
+    sums, mags, (grad, gent, size) = wide_policy(cfg, np.asarray(lens), *dev, width, count)
+    rel = 2.0 ** -18                                             # as in check_policy; a thread adds up some 20 tokens here
+    assert ((out.stats.double() - sums).abs() <= rel * mags + 1e-30).all(), (out.stats, sums)
+    assert ((out.grad_logprob - grad).abs() <= rel * size + 1e-30).all()
+    assert ((out.grad_entropy - gent).abs() <= rel * gent.abs()).all()
+    return out
+
+
+def test_the_two_policy_references_agree():
+    lens = [33, 0, 250, 1, 18]
+    for width, served in ((0, 5), (0, 3), (40, 5), (300, 4)):
+        lp, old, ref, ent, mask, adv = policy_inputs(lens, 3, width=width)
+        for mean in (td.MEAN_TOKENS, td.MEAN_SAMPLES):
+            cfg = td.PolicyLossConfig(clip_high=0.28, dual_clip=1.5, kl_coef=0.3, entropy_coef=-0.02, reduction=mean, grad_scale=3.0)
+            sums, mags, grad, gent, size = exact_policy(cfg, lens, lp, old, ref, ent, mask, adv, width, served)
+            s2, m2, (g2, e2, z2) = wide_policy(cfg, np.asarray(lens), *(torch.from_numpy(a) for a in (lp, old, ref, ent, mask, adv)), width, served)
+            for a, b in ((sums, s2), (mags, m2), (grad, g2), (gent, e2), (size, z2)):
+                assert np.allclose(a, b.numpy(), rtol=1e-10, atol=1e-14)
+
+
+# Samples in numbers beyond the 256 a block keeps at hand, over many blocks: of similar length, mostly empty or of one token (a block's
+# share holds thousands), one long sample among many short ones.
+def many_lens(kind):
+    r = np.random.default_rng(5)
+    if kind == "even":
+        return r.integers(1, 4000, 300)
+    if kind == "short":
+        return r.integers(0, 3, 40000)
+    lens = r.integers(0, 40, 3000)
+    lens[[0, 1500, 2999]] = [0, 200000, 0]
+    return lens
+
+
+@pytest.mark.parametrize("kind", ["even", "short", "mixed"])
+@pytest.mark.parametrize("mean", [td.MEAN_TOKENS, td.MEAN_SAMPLES])
+@pytest.mark.parametrize("terms", ["all", "", "e", "m"])
+def test_policy_loss_of_many_samples(kind, mean, terms):
+    lens = many_lens(kind)
+    arrays = policy_inputs(lens, 6, slack=11)
+    arrays[0][lens.sum():] = np.nan
+    cfg = td.PolicyLossConfig(clip_high=0.28, dual_clip=1.5, kl_coef=0.1, entropy_coef=0.01, reduction=mean, grad_scale=-2.0)
+    for served in (None, len(lens) - 30):
+        check_wide(cfg, lens, arrays, served=served, terms=terms)
+    check_wide(cfg, lens, arrays, offset=1, terms=terms)         # a position at a time
+
+
+@pytest.mark.parametrize("samples,width", [(300, 700), (5000, 13), (2000, 64)])
+@pytest.mark.parametrize("mean", [td.MEAN_TOKENS, td.MEAN_SAMPLES])
+@pytest.mark.parametrize("terms", ["all", "", "m"])
+def test_policy_loss_of_many_padded_rows(samples, width, mean, terms):
+    lens = np.random.default_rng(7).integers(0, width * 5 // 4, samples)
+    arrays = policy_inputs(lens, 8, width=width, bf16=True)
+    pad = np.arange(samples * width) % width >= np.repeat(lens, width)
+    arrays[0][pad] = np.nan
+    for kind in (td.KL_K1, td.KL_K2, td.KL_K3):
+        cfg = td.PolicyLossConfig(kl_coef=0.1, kl_kind=kind, entropy_coef=0.01, reduction=mean)
+        check_wide(cfg, lens, arrays, width=width, terms=terms, bf16=True)
+        check_wide(cfg, lens, arrays, width=width, served=samples - 47, terms=terms, bf16=True)
+    check_wide(cfg, lens, arrays, width=width, terms=terms, offset=1)
+
+
+@pytest.mark.parametrize("terms", ["all", "", "e", "m"])
+@pytest.mark.parametrize("padded", [False, True])
+def test_policy_loss_of_millions_of_tokens(terms, padded):
+    """Beyond 592 x 1024 x 3 positions a block goes round its staging memory more than once."""
+    lens = np.random.default_rng(2).integers(1, 5200, 1000)
+    width = 2900 if padded else 0
+    arrays = policy_inputs(lens, 4, width=width)
+    assert len(arrays[0]) > 2_500_000
+    for mean in (td.MEAN_TOKENS, td.MEAN_SAMPLES):
+        for kind in (td.KL_K3, td.KL_K2):
+            cfg = td.PolicyLossConfig(dual_clip=1.5, kl_coef=0.1, kl_kind=kind, entropy_coef=0.01, reduction=mean)
+            check_wide(cfg, lens, arrays, width=width, terms=terms)
+    check_wide(cfg, lens, (arrays[0], arrays[1], None) + arrays[3:], width=width, terms=terms)
