@@ -585,7 +585,8 @@ int td_embed(const td_embed_args *args, void *stream);
  * sorted positions, so that the result does not depend on timing.
  *   accumulate = 0: every row of grad_table is written, 0 where no token is;
  *   accumulate = 1: the sum is added to the rows that occur (in float, rounded once), others keep
- *                   their contents and are not touched. */
+ *                   their contents and are not touched.  Float rows are added to where they lie, by
+ *                   additions in memory, which take numbers below 2^-126 as zero. */
 typedef struct {
     const int32_t *ids;
     uint32_t n_tokens, vocab, dim;

@@ -556,8 +556,8 @@ __device__ __forceinline__ bool join_run(const EmbedArgs &a, uint32_t v, uint32_
 }
 
 // Bound by memory: 65536 rows of 2048 bfloat16 into a table of 129280 float rows (268 MB read, 1059 MB written) 207 us of
-// the call's 244, the rest being the sort (one counting kernel of 3 us and two placing kernels of 8); rows of 2047, which go
-// through shared memory, 278 us a call.
+// the call's 239, the rest being the sort (one counting kernel of 3 us and two placing kernels of 8); rows of 2047, which go
+// through shared memory, 281 us a call.
 // A warp per (chunk of sorted positions, 256 columns).  A run that lies inside the chunk is written out; the part of
 // a run that began in an earlier chunk goes to partial 0, the part of one that began here and goes on to
 // partial 1, and the last part to arrive writes the run out.  The blocks behind the sum_blocks that do this clear

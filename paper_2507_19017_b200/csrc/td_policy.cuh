@@ -278,10 +278,10 @@ struct PolicyStage {
 constexpr int kPolicyWindow = 256;
 static_assert(kPolicyWindow == kPolicyThreads, "one thread fills one entry");
 
-// 12 to 25 bytes and some 80 instructions per token.  75 million tokens of the R1-shaped batch: 250 us, 4.9 TB/s (0.76 of
+// 12 to 25 bytes and some 80 instructions per token.  75 million tokens of the R1-shaped batch: 246 us, 5.0 TB/s (0.77 of
 // a plain copy's rate) at 73 % of the instruction issue slots; a separate path for small log ratios, more or fewer resident
-// blocks and deeper staging measured the same or worse.  Small batches are latency: 8 samples 5.8 us, 64 masked ones
-// 9.9 us with the counting kernel.
+// blocks and deeper staging measured the same or worse.  Small batches are latency: 8 samples 6.1 us, 64 masked ones
+// 10.1 us with the counting kernel.
 // A block's consecutive share of the positions, kVec (4 or 1) per thread and turn.  Positions are
 // counted from the share's start; the next turn's loads are under way while a turn is worked on.
 template <int kVec, int kKl, bool kMask, bool kEnt>
