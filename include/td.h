@@ -610,6 +610,113 @@ typedef struct {
 size_t td_embed_grad_workspace_bytes(uint32_t n_tokens, uint32_t vocab, uint32_t dim);
 int td_embed_grad(const td_embed_grad_args *args, void *stream);
 
+/* ---- A paged key-value cache for generation ----------------------------------------------------
+ * What a generation state keeps between two tokens, and the steps on it: keys and values of every
+ * token lie in pages of page_size tokens; a table row per sequence names its pages in order, so
+ * token j of sequence s lies in page table[s][j / page_size] at place j % page_size; holders[p] counts the
+ * table rows that name page p, and a page without a holder is free.  The responses of a GRPO group
+ * share their prompt's full pages (td_cache_fork).
+ *
+ * The conventions of the operators above hold: caller-owned device memory, work on `stream` only, no
+ * synchronisation, no allocation.  All of it is device state that the calls read and write in stream order,
+ * so that a whole generation step can stand in a CUDA graph; calls on one cache are ordered by the
+ * caller (attention calls may overlap each other).  Empty cache: lengths and holders zero; the
+ * table may hold anything.  Which sequences a call is about is said by one entry per sequence, so
+ * that none is named twice.  A table entry outside [0, n_pages) never causes an access outside the cache: the
+ * token or page is passed over and TD_ERR_OOB_INDEX is OR-ed into *status (device, may be NULL,
+ * never cleared here).  A sequence whose length lies outside [0, max_pages * page_size] is passed over with
+ * TD_ERR_BAD_LENGTH. */
+typedef struct {
+    int32_t  dtype;                        /* TD_F32 | TD_BF16 | TD_F16 */
+    uint32_t n_pages, page_size;           /* page_size < 2^16; n_pages * page_size < 2^40 */
+    uint32_t n_layers, n_heads, dim;       /* of keys and values, >= 1; n_layers, n_heads < 2^16, dim < 2^16 */
+    int64_t  layer_stride, page_stride, token_stride, head_stride;   /* elements, >= 0, the same for both; dim is contiguous */
+    void *keys, *values;                   /* device, layer 0; both NULL: tables only (extend, free) */
+    uint32_t max_seqs, max_pages;          /* table rows < 2^24, and entries of a row; max_pages * page_size < 2^31 */
+    int32_t *table;                        /* device [max_seqs][max_pages] */
+    int32_t *length;                       /* device [max_seqs], tokens */
+    int32_t *holders;                      /* device [n_pages] */
+    uint32_t *status;
+    void    *workspace;                    /* device, 256-byte aligned, any contents, for extend, fork and compact;
+                                              private to the call while in flight */
+    uint64_t workspace_bytes;              /* >= td_cache_workspace_bytes(n_pages, max_seqs) */
+    int32_t  device;
+    uint32_t reserved;
+} td_cache;
+/* Never falls as an argument grows. 0 where an argument is out of range. */
+size_t td_cache_workspace_bytes(uint32_t n_pages, uint32_t max_seqs);
+
+/* Room for new tokens: length[s] += add[s], and the pages that takes, the lowest free ones first, in
+ * order of s.  add: device [max_seqs], or NULL: one token for every sequence that has any.  cu: device
+ * [max_seqs + 1] or NULL: written with the running sum of the tokens given, as td_cache_write takes it.
+ * Negative entries and sequences that would pass max_pages get nothing (TD_ERR_BAD_LENGTH).  Where
+ * the free pages do not suffice for the whole call nothing is changed, cu is zeros, and
+ * TD_ERR_ARENA_FULL is raised.  The last page of a sequence must be its own unless it is full (a fork leaves
+ * it so). */
+int td_cache_extend(const td_cache *cache, const int32_t *add, int32_t *cu, void *stream);
+
+/* Sequence s becomes a copy of sequence parent[s] (device [max_seqs], negative: none): it holds the parent's
+ * full pages too, and a partly filled last page is copied, in every layer, to a page of its own (the
+ * lowest free ones, in order of s).  s must be empty, else it is passed over with TD_ERR_DUP_PUT; a
+ * parent >= max_seqs is passed over with TD_ERR_OOB_INDEX; a parent that is itself forked to by this
+ * call counts as it was before it.  Too few free pages: nothing is changed, TD_ERR_ARENA_FULL. */
+int td_cache_fork(const td_cache *cache, const int32_t *parent, void *stream);
+
+/* Sequences with release[s] != 0 (device bytes [max_seqs]; NULL: all) give their pages back and
+ * have length 0.  A page that is given back more often than it is held stays free (TD_ERR_DUP_PUT). */
+int td_cache_free(const td_cache *cache, const uint8_t *release, void *stream);
+
+/* The U pages that are held move to numbers 0 .. U - 1: the i-th held page with a number >= U, from below,
+ * goes to the i-th free number < U, with its contents in every layer and its holders; the tables follow.
+ * used: device word, written with U, or NULL.  moved: device [n_pages], written with every page's new number,
+ * -1 for a free one, or NULL.  Pages that are left keep their contents. */
+int td_cache_compact(const td_cache *cache, uint32_t *used, int32_t *moved, void *stream);
+
+/* Keys and values of new tokens into their pages.  Row t of keys / values belongs to the sequence s with
+ * cu[s] <= t < cu[s + 1] (cu: device [max_seqs + 1], from td_cache_extend) and is its token
+ * length[s] - (cu[s + 1] - t): the newest tokens, whose room the extend has made.  Rows from n_rows or
+ * cu[max_seqs] on are not stored; a row that would be a token before the first is passed over with
+ * TD_ERR_BAD_LENGTH. */
+typedef struct {
+    const td_cache *cache;
+    uint32_t layer, n_rows;                /* n_rows < 2^31 */
+    const void *keys, *values;             /* device [n_rows][cache->n_heads][cache->dim] of the cache's dtype */
+    int64_t  row_stride, head_stride;      /* elements, >= 0; dim is contiguous */
+    const int32_t *cu;
+} td_cache_write_args;
+int td_cache_write(const td_cache_write_args *args, void *stream);
+
+/* Attention of one new token per row over the cache: with kv = h / (n_heads / cache->n_heads),
+ *   x_j = scale * q[r][h] . K[j][kv],  lse = ln sum_j e^(x_j),  out[r][h] = sum_j e^(x_j - lse) V[j][kv]
+ * over the tokens j of sequence seqs[r] (seqs == NULL: r), with window > 0 its last `window` ones only.
+ * Scores, their maximum and both sums are float; the weights e^(x_j - max) are rounded to the cache's
+ * type for the product with V (bfloat16, half).  A row without a token (seqs[r] < 0, length 0, or every score -inf)
+ * has out 0 and lse -inf; seqs[r] >= max_seqs is the same with TD_ERR_OOB_INDEX.  A score of -inf has weight 0; NaN or +inf
+ * among a row's scores makes that row's head NaN.  What lies in a page behind a sequence's last token is never used.
+ * group > 1: rows i * group .. i * group + group - 1 are likely to share leading pages, as the
+ * responses of a GRPO group do; full pages that all of a group's rows (with a token) have in common are
+ * then read once for all.  Only time depends on it. */
+typedef struct {
+    const td_cache *cache;
+    uint32_t layer, n_rows, n_heads;       /* n_heads: a multiple of cache->n_heads; n_rows < 2^24 */
+    uint32_t group;                        /* >= 1 */
+    uint32_t window, reserved;
+    float    scale;                        /* finite */
+    uint32_t reserved2;
+    const int32_t *seqs;                   /* device [n_rows] */
+    const void *q;                         /* device [n_rows][n_heads][dim] of the cache's dtype */
+    int64_t  q_row_stride, q_head_stride;  /* elements, >= 0 */
+    void    *out;                          /* device, the same shape and type; rows and heads must not overlap */
+    int64_t  out_row_stride, out_head_stride;
+    float   *lse;                          /* device [n_rows][n_heads], or NULL */
+    void    *workspace;                    /* device, 256-byte aligned, zero-filled once after allocation, private
+                                              to this call while it is in flight */
+    uint64_t workspace_bytes;              /* >= td_cache_attention_workspace_bytes(n_rows, n_heads, dim) */
+} td_cache_attention_args;
+/* Never falls as an argument grows. 0 where an argument is out of range. */
+size_t td_cache_attention_workspace_bytes(uint32_t n_rows, uint32_t n_heads, uint32_t dim);
+int td_cache_attention(const td_cache_attention_args *args, void *stream);
+
 const char *td_strerror(int code);
 
 #ifdef __cplusplus

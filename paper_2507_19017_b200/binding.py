@@ -45,7 +45,9 @@ EXPORTS = ["td_query_workspace", "td_create", "td_destroy", "td_put", "td_get",
            "td_model_bytes", "td_put_back", "td_put_back_many", "td_put_many_host", "td_get_many_host", "td_get_many_host_stage_bytes", "td_debug_validate",
            "td_debug_lookback",
            "td_token_logprob", "td_token_logprob_grad", "td_policy_loss_workspace_bytes", "td_policy_loss",
-           "td_embed", "td_embed_grad_workspace_bytes", "td_embed_grad"]
+           "td_embed", "td_embed_grad_workspace_bytes", "td_embed_grad",
+           "td_cache_workspace_bytes", "td_cache_extend", "td_cache_fork", "td_cache_free", "td_cache_compact", "td_cache_write",
+           "td_cache_attention_workspace_bytes", "td_cache_attention"]
 
 
 class TdModel(C.Structure):
@@ -167,6 +169,28 @@ class TdEmbedGradArgs(C.Structure):
                 ("status", C.c_void_p)]
 
 
+class TdCache(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_pages", C.c_uint32), ("page_size", C.c_uint32), ("n_layers", C.c_uint32),
+                ("n_heads", C.c_uint32), ("dim", C.c_uint32), ("layer_stride", C.c_int64), ("page_stride", C.c_int64),
+                ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("keys", C.c_void_p), ("values", C.c_void_p),
+                ("max_seqs", C.c_uint32), ("max_pages", C.c_uint32), ("table", C.c_void_p), ("length", C.c_void_p),
+                ("holders", C.c_void_p), ("status", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+                ("device", C.c_int32), ("reserved", C.c_uint32)]
+
+
+class TdCacheWriteArgs(C.Structure):
+    _fields_ = [("cache", C.POINTER(TdCache)), ("layer", C.c_uint32), ("n_rows", C.c_uint32), ("keys", C.c_void_p),
+                ("values", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("cu", C.c_void_p)]
+
+
+class TdCacheAttentionArgs(C.Structure):
+    _fields_ = [("cache", C.POINTER(TdCache)), ("layer", C.c_uint32), ("n_rows", C.c_uint32), ("n_heads", C.c_uint32),
+                ("group", C.c_uint32), ("window", C.c_uint32), ("reserved", C.c_uint32), ("scale", C.c_float),
+                ("reserved2", C.c_uint32), ("seqs", C.c_void_p), ("q", C.c_void_p), ("q_row_stride", C.c_int64),
+                ("q_head_stride", C.c_int64), ("out", C.c_void_p), ("out_row_stride", C.c_int64),
+                ("out_head_stride", C.c_int64), ("lse", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
 class TdError(RuntimeError):
     def __init__(self, call: str, code: int):
         self.code = code
@@ -254,13 +278,21 @@ def lib():
         L.td_model_bytes.restype = C.c_int
         L.td_model_bytes.argtypes = [C.POINTER(TdModel), C.POINTER(u64), C.POINTER(u64), C.POINTER(C.c_double)]
         for name, args in (("td_token_logprob", TdLogprobArgs), ("td_token_logprob_grad", TdLogprobGradArgs),
-                           ("td_policy_loss", TdPolicyArgs), ("td_embed", TdEmbedArgs), ("td_embed_grad", TdEmbedGradArgs)):
+                           ("td_policy_loss", TdPolicyArgs), ("td_embed", TdEmbedArgs), ("td_embed_grad", TdEmbedGradArgs),
+                           ("td_cache_write", TdCacheWriteArgs), ("td_cache_attention", TdCacheAttentionArgs)):
             getattr(L, name).restype = C.c_int
             getattr(L, name).argtypes = [C.POINTER(args), vp]
         L.td_policy_loss_workspace_bytes.restype = C.c_size_t
         L.td_policy_loss_workspace_bytes.argtypes = [u32]
         L.td_embed_grad_workspace_bytes.restype = C.c_size_t
         L.td_embed_grad_workspace_bytes.argtypes = [u32, u32, u32]
+        for name, extra in (("td_cache_extend", 2), ("td_cache_fork", 1), ("td_cache_free", 1), ("td_cache_compact", 2)):
+            getattr(L, name).restype = C.c_int
+            getattr(L, name).argtypes = [vp] * (extra + 2)
+        L.td_cache_workspace_bytes.restype = C.c_size_t
+        L.td_cache_workspace_bytes.argtypes = [u32, u32]
+        L.td_cache_attention_workspace_bytes.restype = C.c_size_t
+        L.td_cache_attention_workspace_bytes.argtypes = [u32, u32, u32]
         _lib = L
     return _lib
 
@@ -903,3 +935,153 @@ def embed_grad(grad_table, ids, grad_out, workspace: EmbedGradWorkspace, scale: 
                 1 if accumulate else 0, g, gstride, scale, tokens, device, 0, _batch_address(batch, device),
                 workspace.address, workspace.nbytes, _vector(status, 1, "status", "i32", device))
     return grad_table
+
+
+# -- a paged key-value cache for generation ---------------------------------------
+_CACHE_WRITE, _CACHE_ATTENTION = _Op("td_cache_write", TdCacheWriteArgs), _Op("td_cache_attention", TdCacheAttentionArgs)
+
+
+def _strides(t) -> Tuple:
+    """Element strides; torch may give an axis of one entry, or of none, any."""
+    return tuple(s if n > 1 else 0 for n, s in zip(t.shape, t.stride()))
+
+
+class Cache:
+    """A paged key-value cache: keys and values [layers, pages, page_size, heads, dim] (float32, bfloat16 or
+    float16; the same strides, dim contiguous; None, None with a page_size: tables only), table int32
+    [max_seqs, max_pages], length int32 [max_seqs], holders int32 [pages].  All are the caller's tensors and are read and written
+    in place; an empty cache has zero lengths and holders.  status collects ERR_* bits."""
+
+    def __init__(self, keys, values, table, length, holders, page_size: Optional[int] = None):
+        import torch
+        device = self.device = _device_of(holders, "holders")
+        self.keys, self.values, self.table, self.length, self.holders = keys, values, table, length, holders     # kept alive
+        if len(table.shape) != 2:
+            raise ValueError(f"table: needs a matrix, got {tuple(table.shape)}")
+        (self.max_seqs, self.max_pages), self.n_pages = table.shape, holders.numel()
+        shape, strides, addresses, tag = (0, self.n_pages, page_size, 0, 0), (0, 0, 0, 0, 0), (None, None), F32
+        if (keys is None) != (values is None) or (keys is None and page_size is None):
+            raise ValueError("a cache needs keys and values, or neither and a page_size")
+        if keys is not None:
+            shape, strides, tag = tuple(keys.shape), _strides(keys), _tag(keys, "keys", _FLOATS)
+            if (len(shape) != 5 or tuple(values.shape) != shape or values.dtype != keys.dtype or _strides(values) != strides
+                    or keys.get_device() != device or values.get_device() != device):
+                raise ValueError(f"keys, values: need the same shape [layers, pages, page_size, heads, dim], strides and type on "
+                                 f"cuda:{device}, got {shape} and {tuple(values.shape)}")
+            if shape[1] != self.n_pages or (page_size is not None and page_size != shape[2]):
+                raise ValueError(f"keys: {shape[1]} pages of {shape[2]} tokens, holders and page_size say {self.n_pages} of {page_size}")
+            if strides[4] > 1 or (shape[4] > 1 and strides[4] != 1) or any(n > 1 and s == 0 for n, s in zip(shape, strides)):
+                raise ValueError(f"keys: dim must be contiguous and no axis broadcast, got strides {strides}")
+            addresses = keys.data_ptr(), values.data_ptr()
+        self.n_layers, _, self.page_size, self.n_heads, self.dim = shape
+        self.tag = tag
+        self.status = torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", device))
+        nbytes = lib().td_cache_workspace_bytes(self.n_pages, self.max_seqs)
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", device))
+        self.struct = TdCache(tag, self.n_pages, self.page_size, self.n_layers, self.n_heads, self.dim, *strides[:4], *addresses,
+                              self.max_seqs, self.max_pages, _vector(table, 0, "table", "i32", device),
+                              _vector(length, self.max_seqs, "length", "i32", device), _vector(holders, 0, "holders", "i32", device),
+                              self.status.data_ptr(), self.workspace.data_ptr(), nbytes, device, 0)
+        self.address = C.addressof(self.struct)
+
+    @classmethod
+    def empty(cls, n_layers: int, n_pages: int, page_size: int, n_heads: int, dim: int, max_seqs: int, max_pages: int, dtype,
+              device: int = 0, heads_first: bool = True) -> "Cache":
+        """An empty cache of its own memory; heads_first: a token's heads lie side by side, otherwise a head's tokens of a page."""
+        import torch
+        dev = torch.device("cuda", device)
+        shape = (n_layers, n_pages, page_size, n_heads, dim) if heads_first else (n_layers, n_pages, n_heads, page_size, dim)
+        keys, values = (torch.zeros(shape, dtype=dtype, device=dev) for _ in range(2))
+        if not heads_first:
+            keys, values = keys.transpose(2, 3), values.transpose(2, 3)
+        table, length, holders = (torch.zeros(n, dtype=torch.int32, device=dev) for n in ((max_seqs, max_pages), max_seqs, n_pages))
+        return cls(keys, values, table, length, holders)
+
+
+def _cache_call(name: str, cache: Cache, stream, *addresses):
+    rc = getattr(lib(), name)(cache.address, *addresses, _op_stream(stream, cache.device))
+    if rc != 0:
+        raise TdError(name, rc)
+
+
+def cache_extend(cache: Cache, add=None, cu=None, stream=None):
+    """Room for add[s] more tokens (int32 [max_seqs]; None: one for every sequence that has any): lengths grow, and the
+    pages that takes are the lowest free ones, in order of sequence.  cu (int32 [max_seqs + 1]): written with the
+    running sum of the tokens, as cache_write takes it."""
+    _cache_call("td_cache_extend", cache, stream, _vector(add, cache.max_seqs, "add", "i32", cache.device) or None,
+                _vector(cu, cache.max_seqs + 1, "cu", "i32", cache.device) or None)
+
+
+def cache_fork(cache: Cache, parent, stream=None):
+    """Empty sequences s with parent[s] >= 0 (int32 [max_seqs]) become copies of parent[s]: full pages shared, a partly
+    filled last page copied in every layer."""
+    _cache_call("td_cache_fork", cache, stream, _vector(parent, cache.max_seqs, "parent", "i32", cache.device) or None)
+
+
+def cache_free(cache: Cache, release=None, stream=None):
+    """Sequences with release[s] (bool or uint8 [max_seqs]; None: all) give back their pages and become empty."""
+    _cache_call("td_cache_free", cache, stream, _vector(release, cache.max_seqs, "release", "mask", cache.device) or None)
+
+
+def cache_compact(cache: Cache, used=None, moved=None, stream=None):
+    """Held pages move to the lowest numbers, tables and holders follow.  used (int32 [1]): how many they are;
+    moved (int32 [pages]): every page's new number, -1 for a free one."""
+    _cache_call("td_cache_compact", cache, stream, _vector(used, 1, "used", "i32", cache.device) or None,
+                _vector(moved, cache.n_pages, "moved", "i32", cache.device) or None)
+
+
+def _rows_of_heads(t, what: str, cache: Cache, heads: Optional[int] = None):
+    """(address, row stride, head stride, rows, heads) of [rows, heads, dim] in the cache's type."""
+    shape, strides = tuple(t.shape), _strides(t)
+    if (len(shape) != 3 or shape[2] != cache.dim or (heads is not None and shape[1] != heads) or t.get_device() != cache.device
+            or (shape[2] > 1 and strides[2] != 1)):
+        raise ValueError(f"{what}: needs [rows, {heads or 'heads'}, {cache.dim}] with contiguous rows on cuda:{cache.device}, got {shape} "
+                         f"strides {strides} on {t.device}")
+    if _tag(t, what, _FLOATS) != cache.tag:
+        raise ValueError(f"{what}: {t.dtype}, the cache has another type")
+    return t.data_ptr(), strides[0], strides[1], shape[0], shape[1]
+
+
+def cache_write(cache: Cache, keys, values, cu, layer: int = 0, stream=None):
+    """Keys and values [rows, heads, dim] of new tokens into a layer: rows cu[s] .. cu[s + 1] - 1 are the newest tokens of
+    sequence s, in order (cu int32 [max_seqs + 1], from cache_extend)."""
+    k, row, head, n, _ = _rows_of_heads(keys, "keys", cache, cache.n_heads)
+    v, row_v, head_v, n_v, _ = _rows_of_heads(values, "values", cache, cache.n_heads)
+    if (row, head, n) != (row_v, head_v, n_v):
+        raise ValueError("keys, values: need the same shape and strides")
+    _CACHE_WRITE(_op_stream(stream, cache.device), cache.address, layer, n, k, v, row, head,
+                 _vector(cu, cache.max_seqs + 1, "cu", "i32", cache.device))
+
+
+class AttentionBuffers:
+    """Outputs and workspace of cache_attention for up to n_rows rows of n_heads heads: out [n_rows, n_heads, dim]
+    (a tensor of the caller's, or allocated), lse (lse=True: float32 [n_rows, n_heads])."""
+
+    def __init__(self, n_rows: int, n_heads: int, dim: int, dtype, lse: bool = False, device: int = 0, out=None):
+        import torch
+        dev = torch.device("cuda", device)
+        self.n_rows, self.n_heads, self.dim, self.device = n_rows, n_heads, dim, device
+        self.out = out if out is not None else torch.zeros(n_rows, n_heads, dim, dtype=dtype, device=dev)
+        strides = _strides(self.out)
+        if (tuple(self.out.shape) != (n_rows, n_heads, dim) or self.out.dtype != dtype or self.out.get_device() != device
+                or (dim > 1 and strides[2] != 1)):
+            raise ValueError(f"out: needs {dtype} [{n_rows}, {n_heads}, {dim}] with contiguous rows on cuda:{device}")
+        self.lse = torch.zeros(n_rows, n_heads, dtype=torch.float32, device=dev) if lse else None
+        nbytes = lib().td_cache_attention_workspace_bytes(n_rows, n_heads, dim)
+        self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=dev)
+        self._addresses = (self.out.data_ptr(), strides[0], strides[1], self.lse.data_ptr() if lse else 0, self.workspace.data_ptr(), nbytes)
+
+
+def cache_attention(out: AttentionBuffers, cache: Cache, q, seqs=None, layer: int = 0, window: int = 0, group: int = 1,
+                    scale: Optional[float] = None, stream=None) -> AttentionBuffers:
+    """Attention of one new token per row over a layer of the cache: q [rows, heads, dim] against the tokens of sequence
+    seqs[row] (int32; None: the row's number; negative: none), the last `window` of them if it is not 0.  scale:
+    1 / sqrt(dim) unless given.  group > 1: rows come in groups that share leading pages, which are read once."""
+    address, row, head, n, heads = _rows_of_heads(q, "q", cache)
+    if n > out.n_rows or heads != out.n_heads or cache.dim != out.dim or out.device != cache.device or out.out.dtype != q.dtype:
+        raise ValueError(f"q: {n} rows of {heads} x {cache.dim} {q.dtype}, the buffers hold {out.n_rows} of {out.n_heads} x {out.dim} "
+                         f"{out.out.dtype} on cuda:{out.device}")
+    _CACHE_ATTENTION(_op_stream(stream, cache.device), cache.address, layer, n, heads, group, window, 0,
+                     cache.dim ** -0.5 if scale is None else scale, 0, _vector(seqs, n, "seqs", "i32", cache.device), address, row, head,
+                     *out._addresses)
+    return out
