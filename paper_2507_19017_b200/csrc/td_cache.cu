@@ -148,10 +148,37 @@ cudaError_t run_write(const CacheView &v, const PoolView &p, WriteArgs k, cudaSt
     k.rows_per_block = rows;
     return launch(cache_write_kernel<V>, (k.n_rows + rows - 1) / rows, kCacheThreads, st, 1u, v, p, k);
 }
+
+// ---- attention ----
+constexpr uint32_t kBlocks = 148;                             // one per SM
+template <int kChunks>
+constexpr size_t part_bytes() { return (size_t)(2 * AttendShape<kChunks>::kWarps + 2) * kBlocks * AttendShape<kChunks>::kPartFloats * 4; }
+size_t attend_bytes(uint32_t dim) {                           // never falls as dim grows
+    size_t n = part_bytes<4>();
+    if (dim > 64) n = std::max(n, part_bytes<6>());
+    if (dim > 96) n = std::max(n, part_bytes<8>());
+    if (dim > 128) n = std::max(n, part_bytes<12>());
+    if (dim > 192) n = std::max(n, part_bytes<16>());
+    return round_up(kBlocks * 4, 256) + n;
+}
+template <typename T, int kChunks>
+cudaError_t run_attend(const CacheView &v, const AttendArgs &k, cudaStream_t st) {
+    using S = AttendShape<kChunks>;
+    const cudaError_t rc = cudaFuncSetAttribute(attend_kernel<T, kChunks>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes);
+    if (rc != cudaSuccess) return rc;
+    return launch_smem(attend_kernel<T, kChunks>, kBlocks, S::kThreads, S::kBytes, st, 1u, v, k);
+}
 template <typename T>
 cudaError_t run_attend(const CacheView &v, const AttendArgs &k, cudaStream_t st) {
-    const uint64_t units = (uint64_t)k.n_rows * k.n_heads, blocks = (units + kAttendThreads / 32 - 1) / (kAttendThreads / 32);
-    return launch(attend_kernel<T>, blocks, kAttendThreads, st, 1u, v, k);
+    if (k.dim <= 64) return run_attend<T, 4>(v, k, st);
+    if (k.dim <= 96) return run_attend<T, 6>(v, k, st);
+    if (k.dim <= 128) return run_attend<T, 8>(v, k, st);
+    if (k.dim <= 192) return run_attend<T, 12>(v, k, st);
+    return run_attend<T, 16>(v, k, st);
+}
+cudaError_t run_attend_float(const CacheView &v, const AttendArgs &k, cudaStream_t st) {
+    const uint64_t units = (uint64_t)k.n_rows * k.n_heads, blocks = (units + kFloatThreads / 32 - 1) / (kFloatThreads / 32);
+    return launch(attend_float_kernel<float>, blocks, kFloatThreads, st, 1u, v, k);
 }
 
 }  // namespace
@@ -258,7 +285,7 @@ int td_cache_write(const td_cache_write_args *a, void *stream) {
 
 size_t td_cache_attention_workspace_bytes(uint32_t n_rows, uint32_t n_heads, uint32_t dim) {
     if (n_rows >= kMaxRows || n_heads >= (1u << 16) || dim > kMaxDim) return 0;
-    return 256;
+    return attend_bytes(dim);
 }
 
 int td_cache_attention(const td_cache_attention_args *a, void *stream) {
@@ -301,10 +328,15 @@ int td_cache_attention(const td_cache_attention_args *a, void *stream) {
     k.ratio = a->n_heads / c->n_heads;
     k.dim = c->dim;
     k.window = a->window;
+    k.units = k.kv_heads * ((k.ratio + kHeadRows - 1) / kHeadRows);
     k.scale = a->scale;
+    k.scale2 = (float)(1.4426950408889634 * (double)a->scale);
+    uint8_t *ws = static_cast<uint8_t *>(a->workspace);
+    k.arrived = reinterpret_cast<uint32_t *>(ws);
+    k.parts = reinterpret_cast<float *>(ws + round_up(kBlocks * 4, 256));
     cudaStream_t st = (cudaStream_t)stream;
     const CacheView v = cache_view(c);
-    return result(c->dtype == TD_F32 ? run_attend<float>(v, k, st) : c->dtype == TD_BF16 ? run_attend<__nv_bfloat16>(v, k, st)
+    return result(c->dtype == TD_F32 ? run_attend_float(v, k, st) : c->dtype == TD_BF16 ? run_attend<__nv_bfloat16>(v, k, st)
                                                                                           : run_attend<__half>(v, k, st));
 }
 
