@@ -25,8 +25,15 @@ struct AttendArgs {
     uint32_t n_rows, n_heads, kv_heads, ratio, dim, window;
     uint32_t units;                                           // of a row: key heads times sixteens of heads of each
     float scale, scale2;                                      // scale2 = scale * log2(e)
-    float *parts;                                             // [2 per warp, then 2 per block][part_floats]
+    float *parts;                                             // [2 per warp, then 2 per block][part floats]
     uint32_t *arrived;                                        // [blocks], zero between calls
+    // groups of rows with common pages; group == 1: none
+    uint32_t group, n_groups, m_blocks, m_rows;               // a group's heads over one key head in m_blocks blocks of m_rows (128 at most)
+    FastDiv by_group, by_ratio;
+    int2 *shared;                                             // [n_groups] common tokens, and a sequence that has them
+    float *common;                                            // [rows * heads][dim, then maximum, sum] what the common tokens give
+    float *share_parts;                                       // [2 per block]
+    uint32_t *share_arrived;                                  // [blocks], zero between calls
 };
 
 constexpr uint32_t kTile = 16;                                // tokens of a tile
@@ -56,6 +63,8 @@ struct Span {                                                 // the tokens [lo,
     int32_t s, lo, n;
     __device__ __forceinline__ uint32_t tiles() const { return (uint32_t)(n - lo + (int32_t)kTile - 1) / kTile; }
 };
+// kOwn: without the tokens that the row's group has in common.
+template <bool kOwn>
 __device__ __forceinline__ Span span_of(const CacheView &c, const AttendArgs &a, uint32_t row, bool flag) {
     Span p{a.seqs ? a.seqs[row] : (int32_t)row, 0, 0};
     if (p.s < 0) return p;
@@ -70,6 +79,7 @@ __device__ __forceinline__ Span span_of(const CacheView &c, const AttendArgs &a,
     }
     p.n = n;
     p.lo = a.window && (uint32_t)n > a.window ? n - (int32_t)a.window : 0;
+    if (kOwn && a.group > 1 && n > 0) p.lo = max(p.lo, a.shared[fast_div(row, a.by_group)].x);          // never both: see share_plan_kernel
     return p;
 }
 
@@ -84,6 +94,36 @@ struct Line {
     }
 };
 
+// Places of n items, per_thread consecutive ones to a thread: sums[i] those up to and with thread i's.
+template <uint32_t kThreads, typename Places>
+__device__ __forceinline__ void sum_places(unsigned long long *sums, uint32_t n, uint32_t per_thread, Places places) {
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    unsigned long long mine = 0;
+    for (uint32_t i = threadIdx.x * per_thread; i < min(n, (threadIdx.x + 1) * per_thread); ++i) mine += places(i);
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const unsigned long long y = __shfl_up_sync(kFullMask, mine, d);
+        if (lane >= (uint32_t)d) mine += y;
+    }
+    sums[threadIdx.x] = mine;
+    __syncthreads();
+    unsigned long long before = 0;
+    for (uint32_t w = 0; w < warp; ++w) before += sums[w * 32 + 31];
+    __syncthreads();
+    sums[threadIdx.x] = mine + before;
+    __syncthreads();
+}
+// The thread whose items `place` is among.
+template <uint32_t kThreads>
+__device__ __forceinline__ uint32_t thread_of(const unsigned long long *sums, unsigned long long place) {
+    uint32_t lo = 0, hi = kThreads - 1;
+    while (lo < hi) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (sums[mid] > place) hi = mid; else lo = mid + 1;
+    }
+    return lo;
+}
+
 // A unit that a cut went through: its first place and tiles.
 struct Cut {
     unsigned long long place;
@@ -96,6 +136,14 @@ __device__ __forceinline__ uint32_t heads_of(const AttendArgs &a, uint32_t unit,
     return min(kHeadRows, a.ratio - at);
 }
 
+// What a row's head has from the tokens its group has in common; nullptr: there are none.
+template <uint32_t kDim>
+__device__ __forceinline__ const float *common_of(const AttendArgs &a, uint32_t row, uint32_t head) {
+    if (a.group <= 1 || a.shared[fast_div(row, a.by_group)].x == 0) return nullptr;
+    return a.common + ((size_t)row * a.n_heads + head) * (kDim + 2);
+}
+
+constexpr uint32_t kNoTokens = 0xffffffffu;
 // Joins the parts k = 0 .. count - 1 of a unit (slot(k) of `parts`) into out and lse, or into another part; `me` of `all` threads.
 // A maximum of -inf means that a part has nothing; NaN stays.
 template <typename T, uint32_t kDim, typename Slot>
@@ -104,6 +152,8 @@ __device__ __forceinline__ void join_parts(const AttendArgs &a, uint32_t row, ui
     constexpr uint32_t kFloats = kHeadRows * (kDim + 2);
     uint32_t first;
     const uint32_t heads = heads_of(a, unit, first), pairs = kDim / 2;
+    const bool nothing = count == kNoTokens;                  // the row has no tokens, its group may
+    if (nothing) count = 0;
     for (uint32_t i = me; i < heads * pairs; i += all) {
         const uint32_t h = i / pairs, d = (i - h * pairs) * 2;
         if (d >= a.dim) continue;
@@ -120,6 +170,16 @@ __device__ __forceinline__ void join_parts(const AttendArgs &a, uint32_t row, ui
             x = fmaf(v.x, e, x);
             y = fmaf(v.y, e, y);
         }
+        if (!to && !nothing) {
+            if (const float *w = common_of<kDim>(a, row, first + h)) {
+                const float2 ml = *reinterpret_cast<const float2 *>(w + kDim), v = *reinterpret_cast<const float2 *>(w + d);
+                const float most = max_nan(top, ml.x), all_ref = most == -CUDART_INF_F ? 0.0f : most, e = exp2_approx(ref - all_ref), f = exp2_approx(ml.x - all_ref);
+                sum = fmaf(ml.y, f, sum * e);
+                x = fmaf(v.x, f, x * e);
+                y = fmaf(v.y, f, y * e);
+                top = most;
+            }
+        }
         if (to) {
             *reinterpret_cast<float2 *>(to + h * kDim + d) = make_float2(x, y);
             if (d == 0) *reinterpret_cast<float2 *>(to + kHeadRows * kDim + 2 * h) = make_float2(top, sum);
@@ -130,6 +190,146 @@ __device__ __forceinline__ void join_parts(const AttendArgs &a, uint32_t row, ui
         if (a.lse && d == 0) a.lse[(size_t)row * a.n_heads + first + h] = sum == 0.0f ? -CUDART_INF_F : (top + log2f(sum)) * 0.69314718055994531f;
     }
 }
+
+// Sixteen rows' running maximum (in units of log2), sum and weighted values, in the layout of the matrix instructions: lane
+// 4 g + t has rows g and g + 8.
+template <typename T, int kChunks>
+struct Fold {
+    using S = AttendShape<kChunks>;
+    uint32_t qf[S::kQueryInRegisters ? kChunks : 1][4];
+    float o[2 * kChunks][4], m[2], l[2];
+
+    __device__ __forceinline__ void begin() {
+#pragma unroll
+        for (int k = 0; k < 2 * kChunks; ++k) o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.0f;
+        m[0] = m[1] = -CUDART_INF_F;
+        l[0] = l[1] = 0.0f;
+    }
+    // The rows' queries, from q + offset(row) on (negative: zeros), into registers or, for long heads, into the warp's shared memory.
+    template <typename Offset>
+    __device__ __forceinline__ void query(const T *q, uint32_t shared, uint32_t dim, Offset offset) {
+        const uint32_t lane = threadIdx.x & 31u, g = lane >> 2, t = lane & 3u;
+        if constexpr (S::kQueryInRegisters) {
+            const int64_t at[2] = {offset(g), offset(g + 8)};
+#pragma unroll
+            for (int k = 0; k < kChunks; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t d = k * 16 + t * 2 + (i >> 1) * 8;
+                    qf[k][i] = at[i & 1] >= 0 && d < dim ? *reinterpret_cast<const uint32_t *>(q + at[i & 1] + d) : 0u;
+                }
+        } else {
+            __syncwarp();
+            for (uint32_t i = lane; i < kHeadRows * S::kDim / 8; i += 32) {
+                const uint32_t h = i / (S::kDim / 8), v = i - h * (S::kDim / 8);
+                const int64_t at = offset(h);
+                uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                if (at >= 0 && v * 8 < dim) x = *reinterpret_cast<const uint4 *>(q + at + v * 8);
+                store_shared(shared + h * S::kPitch + v * 16, x);
+            }
+            __syncwarp();
+        }
+    }
+    // Sixteen more tokens: keys and values in shared memory, bit i of `counts`: token i counts.
+    __device__ __forceinline__ void add(uint32_t keys, uint32_t values, uint32_t shared, uint32_t counts, float scale2) {
+        const uint32_t lane = threadIdx.x & 31u, t = lane & 3u;
+        // scores of 16 heads and 16 tokens, two products of 8 tokens
+        float s[2][4] = {};
+#pragma unroll
+        for (int k = 0; k < kChunks; ++k) {
+            uint32_t b[4], qa[4];
+            load_matrices(b, keys + ((lane & 7u) + (lane >> 4) * 8) * S::kPitch + k * 32 + (lane >> 3 & 1u) * 16);
+            if constexpr (S::kQueryInRegisters) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) qa[i] = qf[k][i];
+            } else {
+                load_matrices(qa, shared + (lane & 15u) * S::kPitch + k * 32 + (lane >> 4) * 16);
+            }
+            multiply_add<T>(s[0], qa, b[0], b[1]);
+            multiply_add<T>(s[1], qa, b[2], b[3]);
+        }
+        float top[2] = {m[0], m[1]};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool on = counts >> (i * 8 + t * 2 + (k & 1)) & 1u;
+                s[i][k] = on ? s[i][k] * scale2 : -CUDART_INF_F;
+                top[k >> 1] = max_nan(top[k >> 1], s[i][k]);
+            }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            top[r] = max_nan(top[r], __shfl_xor_sync(kFullMask, top[r], 1));
+            top[r] = max_nan(top[r], __shfl_xor_sync(kFullMask, top[r], 2));
+        }
+        // the sums so far are brought to the new maximum where it has moved (or is NaN), which is seldom
+        if (__any_sync(kFullMask, !(top[0] == m[0]) || !(top[1] == m[1]))) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const float keep = m[r] == -CUDART_INF_F ? 0.0f : exp2_approx(m[r] - top[r]);
+                l[r] *= keep;
+#pragma unroll
+                for (int k = 0; k < 2 * kChunks; ++k) {
+                    o[k][2 * r] *= keep;
+                    o[k][2 * r + 1] *= keep;
+                }
+                m[r] = top[r];
+            }
+        }
+        uint32_t p[4];
+        {
+            const float ref[2] = {m[0] == -CUDART_INF_F ? 0.0f : m[0], m[1] == -CUDART_INF_F ? 0.0f : m[1]};
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    s[i][k] = exp2_approx(s[i][k] - ref[k >> 1]);
+                    l[k >> 1] += s[i][k];
+                }
+            // Weights are rounded to the type of the values, as the matrix instruction takes them; their sum is not.
+            p[0] = pair_of<T>(s[0][0], s[0][1]);
+            p[1] = pair_of<T>(s[0][2], s[0][3]);
+            p[2] = pair_of<T>(s[1][0], s[1][1]);
+            p[3] = pair_of<T>(s[1][2], s[1][3]);
+        }
+#pragma unroll
+        for (int k = 0; k < kChunks; ++k) {
+            uint32_t b[4];
+            load_matrices_transposed(b, values + ((lane & 7u) + (lane >> 3 & 1u) * 8) * S::kPitch + k * 32 + (lane >> 4) * 16);
+            multiply_add<T>(o[2 * k], p, b[0], b[1]);
+            multiply_add<T>(o[2 * k + 1], p, b[2], b[3]);
+        }
+    }
+    // The sums over a row, in all four of its lanes.
+    __device__ __forceinline__ void end() {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            l[r] += __shfl_xor_sync(kFullMask, l[r], 1);
+            l[r] += __shfl_xor_sync(kFullMask, l[r], 2);
+        }
+    }
+    // Row g + 8 r joined with a part of it.
+    __device__ __forceinline__ void join(const float *from, const float *ml, int r) {
+        const uint32_t t = threadIdx.x & 3u;
+        const float2 other = *reinterpret_cast<const float2 *>(ml);
+        const float top = max_nan(m[r], other.x), ref = top == -CUDART_INF_F ? 0.0f : top, e = exp2_approx(m[r] - ref), f = exp2_approx(other.x - ref);
+#pragma unroll
+        for (int k = 0; k < 2 * kChunks; ++k) {
+            const float2 v = *reinterpret_cast<const float2 *>(from + k * 8 + t * 2);
+            o[k][2 * r] = fmaf(v.x, f, o[k][2 * r] * e);
+            o[k][2 * r + 1] = fmaf(v.y, f, o[k][2 * r + 1] * e);
+        }
+        l[r] = fmaf(other.y, f, l[r] * e);
+        m[r] = top;
+    }
+    // Row g + 8 r as a part: values to `to`, {maximum, sum} to `ml`.
+    __device__ __forceinline__ void store(float *to, float *ml, int r) const {
+        const uint32_t t = threadIdx.x & 3u;
+#pragma unroll
+        for (int k = 0; k < 2 * kChunks; ++k) *reinterpret_cast<float2 *>(to + k * 8 + t * 2) = make_float2(o[k][2 * r], o[k][2 * r + 1]);
+        if (t == 0) *reinterpret_cast<float2 *>(ml) = make_float2(m[r], l[r]);
+    }
+};
 
 template <typename T, int kChunks>
 __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kernel(CacheView c, AttendArgs a) {
@@ -144,24 +344,10 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
 
     // ---- this warp's share ----
     const uint32_t per_thread = (a.n_rows + S::kThreads - 1) / S::kThreads;
-    {
-        unsigned long long mine = 0;
-        for (uint32_t r = threadIdx.x * per_thread; r < min(a.n_rows, (threadIdx.x + 1) * per_thread); ++r)
-            mine += (unsigned long long)a.units * (span_of(c, a, r, blockIdx.x == 0).tiles() + 1);
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const unsigned long long y = __shfl_up_sync(kFullMask, mine, d);
-            if (lane >= (uint32_t)d) mine += y;
-        }
-        sums[threadIdx.x] = mine;
-        __syncthreads();
-        unsigned long long before = 0;
-        for (uint32_t w = 0; w < warp; ++w) before += sums[w * 32 + 31];
-        __syncthreads();
-        sums[threadIdx.x] = mine + before;
-        if (lane == 0) cut_in.valid = cut_out[warp].valid = 0;
-        __syncthreads();
-    }
+    if (lane == 0) cut_in.valid = cut_out[warp].valid = 0;
+    sum_places<S::kThreads>(sums, a.n_rows, per_thread, [&](uint32_t r) {
+        return (unsigned long long)a.units * (span_of<true>(c, a, r, blockIdx.x == 0).tiles() + 1);
+    });
     Line line;
     line.total = sums[S::kThreads - 1];
     const uint32_t blocks = (uint32_t)min((unsigned long long)gridDim.x, line.total / (S::kWarps * kLeastTiles) + 1);
@@ -179,16 +365,12 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
 
     if (begin < end) {
         // where `begin` lies: the thread whose rows it is among, then the row
-        uint32_t lo = 0, hi = S::kThreads - 1;                // the first thread with sums > begin
-        while (lo < hi) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (sums[mid] > begin) hi = mid; else lo = mid + 1;
-        }
+        const uint32_t lo = thread_of<S::kThreads>(sums, begin);
         unsigned long long row_place = lo ? sums[lo - 1] : 0;
         uint32_t row = lo * per_thread;
         Span span;
         for (;; ++row) {
-            span = span_of(c, a, row, false);
+            span = span_of<true>(c, a, row, false);
             const unsigned long long places = (unsigned long long)a.units * (span.tiles() + 1);
             if (row_place + places > begin) break;
             row_place += places;
@@ -197,7 +379,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
         uint32_t unit = (uint32_t)((begin - row_place) / (tiles + 1));
         int32_t tile = (int32_t)(begin - row_place - (unsigned long long)unit * (tiles + 1)) - 1;          // -1: the place ahead
         unsigned long long place = begin;                     // of the next tile to bring
-        Span next = row + 1 < a.n_rows ? span_of(c, a, row + 1, false) : Span{-1, 0, 0};
+        Span next = row + 1 < a.n_rows ? span_of<true>(c, a, row + 1, false) : Span{-1, 0, 0};
 
         uint32_t kv, first, heads;
         auto enter = [&]() {                                  // a unit's key head and its heads
@@ -211,7 +393,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
                 ++row;
                 span = next;
                 tiles = span.tiles();
-                next = row + 1 < a.n_rows ? span_of(c, a, row + 1, false) : Span{-1, 0, 0};
+                next = row + 1 < a.n_rows ? span_of<true>(c, a, row + 1, false) : Span{-1, 0, 0};
             }
             enter();
         };
@@ -223,12 +405,8 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
                 if (tile >= 0) break;
                 ++place;
                 if (tiles == 0) {
-                    const uint32_t pairs = a.dim / 2;
-                    for (uint32_t i = lane; i < heads * pairs; i += 32) {
-                        const uint32_t h = i / pairs, d = (i - h * pairs) * 2;
-                        *reinterpret_cast<uint32_t *>(static_cast<T *>(a.out) + row * a.out_row + (first + h) * a.out_head + d) = 0u;
-                    }
-                    if (a.lse && lane < heads) a.lse[(size_t)row * a.n_heads + first + lane] = -CUDART_INF_F;
+                    // nothing of its own: zeros, or what its group has in common
+                    join_parts<T, S::kDim>(a, row, unit, nullptr, span.n > 0 ? 0u : kNoTokens, [](uint32_t) { return 0u; }, nullptr, lane, 32);
                     leave();
                 } else {
                     tile = 0;
@@ -280,8 +458,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
             if (more) ++brought;
             copy_commit();
         }
-        uint32_t qf[S::kQueryInRegisters ? kChunks : 1][4];
-        float o[2 * kChunks][4], m[2], l[2];
+        Fold<T, kChunks> f;
         bool head_whole = false;
         uint32_t stage = 0, put = S::kStages - 1;
 #pragma unroll 1
@@ -299,100 +476,12 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
             if (note.z >> 16 & 1u) {                          // a unit begins here
                 head_whole = note.z >> 18 & 1u;
                 const T *q = static_cast<const T *>(a.q) + note.x * a.q_row + first * a.q_head;
-                if constexpr (S::kQueryInRegisters) {
-#pragma unroll
-                    for (int k = 0; k < kChunks; ++k)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t h = g + (i & 1) * 8, d = k * 16 + t * 2 + (i >> 1) * 8;
-                            qf[k][i] = h < heads && d < a.dim ? *reinterpret_cast<const uint32_t *>(q + h * a.q_head + d) : 0u;
-                        }
-                } else {
-                    for (uint32_t i = lane; i < kHeadRows * S::kDim / 8; i += 32) {
-                        const uint32_t h = i / (S::kDim / 8), v = i - h * (S::kDim / 8);
-                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                        if (h < heads && v * 8 < a.dim) x = *reinterpret_cast<const uint4 *>(q + h * a.q_head + v * 8);
-                        *reinterpret_cast<uint4 *>(mem + S::kStages * S::kStage + h * S::kPitch + v * 16) = x;
-                    }
-                    __syncwarp();
-                }
-#pragma unroll
-                for (int k = 0; k < 2 * kChunks; ++k) o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.0f;
-                m[0] = m[1] = -CUDART_INF_F;
-                l[0] = l[1] = 0.0f;
+                f.begin();
+                f.query(q, query, a.dim, [&](uint32_t h) { return h < heads ? (int64_t)h * a.q_head : (int64_t)-1; });
             }
-            // scores of 16 heads and 16 tokens, two products of 8 tokens
-            float s[2][4] = {};
-#pragma unroll
-            for (int k = 0; k < kChunks; ++k) {
-                uint32_t b[4], qa[4];
-                load_matrices(b, at + ((lane & 7u) + (lane >> 4) * 8) * S::kPitch + k * 32 + (lane >> 3 & 1u) * 16);
-                if constexpr (S::kQueryInRegisters) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) qa[i] = qf[k][i];
-                } else {
-                    load_matrices(qa, query + (lane & 15u) * S::kPitch + k * 32 + (lane >> 4) * 16);
-                }
-                multiply_add<T>(s[0], qa, b[0], b[1]);
-                multiply_add<T>(s[1], qa, b[2], b[3]);
-            }
-            float top[2] = {m[0], m[1]};
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const bool counts = note.z >> (i * 8 + t * 2 + (k & 1)) & 1u;
-                    s[i][k] = counts ? s[i][k] * a.scale2 : -CUDART_INF_F;
-                    top[k >> 1] = max_nan(top[k >> 1], s[i][k]);
-                }
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                top[r] = max_nan(top[r], __shfl_xor_sync(kFullMask, top[r], 1));
-                top[r] = max_nan(top[r], __shfl_xor_sync(kFullMask, top[r], 2));
-            }
-            // the sums so far are brought to the new maximum where it has moved (or is NaN), which is seldom
-            if (__any_sync(kFullMask, !(top[0] == m[0]) || !(top[1] == m[1]))) {
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const float keep = m[r] == -CUDART_INF_F ? 0.0f : exp2_approx(m[r] - top[r]);
-                    l[r] *= keep;
-#pragma unroll
-                    for (int k = 0; k < 2 * kChunks; ++k) {
-                        o[k][2 * r] *= keep;
-                        o[k][2 * r + 1] *= keep;
-                    }
-                    m[r] = top[r];
-                }
-            }
-            uint32_t p[4];
-            {
-                const float ref[2] = {m[0] == -CUDART_INF_F ? 0.0f : m[0], m[1] == -CUDART_INF_F ? 0.0f : m[1]};
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        s[i][k] = exp2_approx(s[i][k] - ref[k >> 1]);
-                        l[k >> 1] += s[i][k];
-                    }
-                // Weights are rounded to the type of the values, as the matrix instruction takes them; their sum is not.
-                p[0] = pair_of<T>(s[0][0], s[0][1]);
-                p[1] = pair_of<T>(s[0][2], s[0][3]);
-                p[2] = pair_of<T>(s[1][0], s[1][1]);
-                p[3] = pair_of<T>(s[1][2], s[1][3]);
-            }
-#pragma unroll
-            for (int k = 0; k < kChunks; ++k) {
-                uint32_t b[4];
-                load_matrices_transposed(b, at + S::kSide + ((lane & 7u) + (lane >> 3 & 1u) * 8) * S::kPitch + k * 32 + (lane >> 4) * 16);
-                multiply_add<T>(o[2 * k], p, b[0], b[1]);
-                multiply_add<T>(o[2 * k + 1], p, b[2], b[3]);
-            }
+            f.add(at, at + S::kSide, query, note.z, a.scale2);
             if (note.z >> 17 & 1u) {                          // the unit, or this warp's part of it, ends here
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    l[r] += __shfl_xor_sync(kFullMask, l[r], 1);
-                    l[r] += __shfl_xor_sync(kFullMask, l[r], 2);
-                }
+                f.end();
                 const bool whole = head_whole && (note.z >> 19 & 1u);
                 float *part = a.parts + ((size_t)2 * w_global + (head_whole ? 1 : 0)) * S::kPartFloats;
 #pragma unroll
@@ -400,18 +489,30 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
                     const uint32_t h = g + r * 8;
                     if (h >= heads) continue;
                     if (whole) {
-                        const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
+                        float keep = 1.0f, sum = f.l[r], top = f.m[r], also = 0.0f;
+                        const float *w = common_of<S::kDim>(a, note.x, first + h);
+                        if (w) {
+                            const float2 ml = *reinterpret_cast<const float2 *>(w + S::kDim);
+                            const float most = max_nan(top, ml.x), ref = most == -CUDART_INF_F ? 0.0f : most;
+                            keep = exp2_approx(top - ref);
+                            also = exp2_approx(ml.x - ref);
+                            sum = fmaf(ml.y, also, sum * keep);
+                            top = most;
+                        }
+                        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
                         T *out = static_cast<T *>(a.out) + note.x * a.out_row + (first + h) * a.out_head;
 #pragma unroll
-                        for (int k = 0; k < 2 * kChunks; ++k)
-                            if (k * 8 + t * 2 < a.dim) *reinterpret_cast<uint32_t *>(out + k * 8 + t * 2) = pair_of<T>(o[k][2 * r] * inv, o[k][2 * r + 1] * inv);
+                        for (int k = 0; k < 2 * kChunks; ++k) {
+                            if (k * 8 + t * 2 >= a.dim) continue;
+                            float2 v = make_float2(0.0f, 0.0f);
+                            if (w) v = *reinterpret_cast<const float2 *>(w + k * 8 + t * 2);
+                            *reinterpret_cast<uint32_t *>(out + k * 8 + t * 2) =
+                                pair_of<T>(fmaf(v.x, also, f.o[k][2 * r] * keep) * inv, fmaf(v.y, also, f.o[k][2 * r + 1] * keep) * inv);
+                        }
                         if (a.lse && t == 0)
-                            a.lse[(size_t)note.x * a.n_heads + first + h] = l[r] == 0.0f ? -CUDART_INF_F : (m[r] + log2f(l[r])) * 0.69314718055994531f;
+                            a.lse[(size_t)note.x * a.n_heads + first + h] = sum == 0.0f ? -CUDART_INF_F : (top + log2f(sum)) * 0.69314718055994531f;
                     } else {
-#pragma unroll
-                        for (int k = 0; k < 2 * kChunks; ++k)
-                            *reinterpret_cast<float2 *>(part + h * S::kDim + k * 8 + t * 2) = make_float2(o[k][2 * r], o[k][2 * r + 1]);
-                        if (t == 0) *reinterpret_cast<float2 *>(part + kHeadRows * S::kDim + 2 * h) = make_float2(m[r], l[r]);
+                        f.store(part + h * S::kDim, part + kHeadRows * S::kDim + 2 * h, r);
                     }
                 }
             }
@@ -429,7 +530,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
             join_parts<T, S::kDim>(a, u.row, u.unit, a.parts, w1 - w0 + 1, [=](uint32_t k) { return 2 * (w0 + k) + (k == 0); }, nullptr, lane, 32);
     }
     float *const block_parts = a.parts + (size_t)2 * gridDim.x * S::kWarps * S::kPartFloats;
-    // a unit that came in from the block before, and one that goes on into the next: at most one each, and they may be the same
+    // a unit that came in from the block before, and one that begins here and goes on into the next: at most one each
 #pragma unroll 1
     for (uint32_t side = 0; side < 2; ++side) {
         Cut u{};
@@ -457,6 +558,342 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
             join_parts<T, S::kDim>(a, u.row, u.unit, block_parts, b1 - b0 + 1, [=](uint32_t k) { return 2 * (b0 + k) + (k == 0); }, nullptr,
                                    threadIdx.x, S::kThreads);
         __syncthreads();
+    }
+}
+
+// ---- tokens that a group's rows have in common ----
+// The responses of a GRPO group begin with the same pages.  share_plan_kernel finds how many, share_kernel takes those tokens
+// once for all the group's heads over a key head (blocks of up to 128 of them), and attend_kernel takes the rest of
+// each row and adds what the common tokens gave.
+constexpr uint32_t kMaxGroup = 512;                           // rows; a larger group is taken as several
+constexpr uint32_t kShareHeads = 128;                         // heads of a block: 8 warps of 16
+constexpr uint32_t kShareThreads = 256;
+constexpr uint32_t kLeastShared = 64;                         // tokens; writing and reading what they give costs a row about 2 * ratio tokens' bytes
+
+// A block per group.
+__global__ void __launch_bounds__(kShareThreads) share_plan_kernel(CacheView c, AttendArgs a) {
+    __shared__ int32_t seqs[kMaxGroup];
+    __shared__ int32_t least, lead, whole, active;
+    __shared__ uint32_t equal;
+    griddep_launch_dependents();
+    griddep_wait();
+    const uint32_t first = blockIdx.x * a.group, rows = min(a.group, a.n_rows - first);
+    if (threadIdx.x == 0) {
+        least = 0x7fffffff;
+        lead = kMaxGroup;
+        whole = 1;
+        active = 0;
+    }
+    __syncthreads();
+    for (uint32_t r = threadIdx.x; r < rows; r += kShareThreads) {
+        const Span p = span_of<false>(c, a, first + r, false);
+        seqs[r] = p.n > 0 ? p.s : -1;
+        if (p.n > 0) {
+            atomicMin(&least, p.n);
+            atomicMin(&lead, (int32_t)r);
+            atomicAdd(&active, 1);
+            if (p.lo > 0) whole = 0;                          // a window that has left the first tokens: nothing is shared
+        }
+    }
+    __syncthreads();
+    uint32_t pages = 0;
+    if (active > 1 && whole) pages = fast_div((uint32_t)least, c.by_page);
+    if (threadIdx.x == 0) equal = pages;
+    __syncthreads();
+    if (pages) {
+        const int32_t leader = seqs[lead];
+        for (uint32_t j0 = 0; j0 < pages; j0 += kShareThreads) {
+            const uint32_t j = j0 + threadIdx.x;
+            if (j < pages) {
+                const int32_t id = c.table[(size_t)leader * c.max_pages + j];
+                bool same = true;
+#pragma unroll 4
+                for (uint32_t r = lead + 1; r < rows; ++r)
+                    if (seqs[r] >= 0 && c.table[(size_t)seqs[r] * c.max_pages + j] != id) same = false;
+                if (!same) atomicMin(&equal, j);
+            }
+            __syncthreads();
+            const bool over = equal < j0 + kShareThreads;
+            __syncthreads();
+            if (over) break;
+        }
+    }
+    if (threadIdx.x == 0) {
+        const uint32_t tokens = equal * c.page_size;
+        a.shared[blockIdx.x] = make_int2(tokens >= kLeastShared ? (int32_t)tokens : 0, pages ? seqs[lead] : 0);
+    }
+}
+
+template <int kChunks>
+struct ShareShape {
+    using S = AttendShape<kChunks>;
+    static constexpr uint32_t kTokens = kChunks <= 8 ? 64 : 32;          // of a tile
+    static constexpr uint32_t kSide = kTokens * S::kPitch;
+    static constexpr uint32_t kStage = 2 * kSide + kTokens;              // keys, values, which tokens count
+    // Few heads leave warps idle: those take a share of a tile's tokens, and a unit's results are joined through `merge`.
+    static constexpr uint32_t kSplits = kChunks <= 8 ? 4 : 1;
+    static constexpr uint32_t kMerge = kChunks <= 8 ? 96 * (S::kDim + 2) * 4 : 0;
+    static constexpr uint32_t kQuery = S::kQueryInRegisters ? 0 : kShareHeads * S::kPitch;
+    static constexpr uint32_t kFits = (220 * 1024 - kMerge - kQuery) / kStage;
+    static constexpr uint32_t kStages = kFits < 6 ? kFits : 6;
+    static constexpr uint32_t kBytes = kStages * kStage + kMerge + kQuery;
+    static constexpr uint32_t kPartFloats = kShareHeads * (S::kDim + 2);
+};
+
+// A place in the line of all groups' units (blocks of heads of a key head), as attend_kernel's, a block of threads to a piece.
+struct Walk {
+    unsigned long long place;
+    uint32_t group, unit, tiles;
+    int32_t tile, tokens, seq;
+    __device__ __forceinline__ void enter(const AttendArgs &a, uint32_t per_tile) {
+        while (group < a.n_groups && a.shared[group].x == 0) ++group;
+        const int2 p = group < a.n_groups ? a.shared[group] : make_int2(0, 0);
+        tokens = p.x;
+        seq = p.y;
+        tiles = ((uint32_t)tokens + per_tile - 1) / per_tile;
+    }
+    __device__ __forceinline__ bool here(unsigned long long end) {          // to a tile, if there is one
+        if (place < end && tile < 0) {
+            ++place;
+            tile = 0;
+        }
+        return place < end;
+    }
+    __device__ __forceinline__ void step(const AttendArgs &a, uint32_t units, uint32_t per_tile) {
+        ++place;
+        if (++tile < (int32_t)tiles) return;
+        tile = -1;
+        if (++unit < units) return;
+        unit = 0;
+        ++group;
+        enter(a, per_tile);
+    }
+};
+struct ShareCut {
+    unsigned long long place;
+    uint32_t group, unit, tiles, valid;
+};
+
+template <typename T, int kChunks>
+__global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, AttendArgs a) {
+    using S = AttendShape<kChunks>;
+    using H = ShareShape<kChunks>;
+    constexpr uint32_t kPer = S::kDim / 8, kCopies = H::kTokens * kPer / kShareThreads;
+    static_assert(H::kTokens * kPer % kShareThreads == 0, "copies of a tile are the same for all threads");
+    extern __shared__ __align__(16) uint8_t memory[];
+    __shared__ unsigned long long sums[kShareThreads];
+    __shared__ uint32_t last;
+    griddep_launch_dependents();
+    griddep_wait();
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, units = a.kv_heads * a.m_blocks;
+    const uint32_t per_thread = (a.n_groups + kShareThreads - 1) / kShareThreads;
+    auto places_of = [&](uint32_t g) {
+        const uint32_t tokens = (uint32_t)a.shared[g].x;
+        return tokens ? (unsigned long long)units * ((tokens + H::kTokens - 1) / H::kTokens + 1) : 0ull;
+    };
+    sum_places<kShareThreads>(sums, a.n_groups, per_thread, places_of);
+    Line line;
+    line.total = sums[kShareThreads - 1];
+    if (line.total == 0) return;
+    line.warps = (uint32_t)min((unsigned long long)gridDim.x, line.total / 2 + 1);          // blocks, here
+    line.warps = (uint32_t)min((unsigned long long)line.warps, line.total);
+    if (blockIdx.x >= line.warps) return;
+    const unsigned long long begin = line.begin(blockIdx.x), end = line.begin(blockIdx.x + 1);
+
+    const uint32_t ring = shared_address(memory);
+    float *const merge = reinterpret_cast<float *>(memory + H::kStages * H::kStage);
+    const uint32_t query = ring + H::kStages * H::kStage + H::kMerge + warp * (H::kQuery / 8);
+    if (a.dim != S::kDim)                                     // columns that no copy writes
+        for (uint32_t i = threadIdx.x; i < H::kStages * H::kStage / 16; i += kShareThreads) reinterpret_cast<uint4 *>(memory)[i] = make_uint4(0u, 0u, 0u, 0u);
+    __syncthreads();
+
+    Walk load;
+    {
+        const uint32_t lo = thread_of<kShareThreads>(sums, begin);
+        unsigned long long before = lo ? sums[lo - 1] : 0;
+        load.group = lo * per_thread;
+        for (;; ++load.group) {
+            const unsigned long long places = places_of(load.group);
+            if (before + places > begin) break;
+            before += places;
+        }
+        load.enter(a, H::kTokens);
+        load.place = begin;
+        load.unit = (uint32_t)((begin - before) / (load.tiles + 1));
+        load.tile = (int32_t)(begin - before - (unsigned long long)load.unit * (load.tiles + 1)) - 1;
+    }
+    Walk use = load;
+    int32_t ids[kCopies];                                     // pages of the tokens this thread copies next
+    bool more;
+    auto look = [&]() {
+        more = load.here(end);
+        if (!more) return;
+#pragma unroll
+        for (uint32_t k = 0; k < kCopies; ++k) {
+            const int32_t j = load.tile * (int32_t)H::kTokens + (int32_t)((threadIdx.x + k * kShareThreads) / kPer);
+            ids[k] = j < load.tokens ? c.table[(size_t)load.seq * c.max_pages + fast_div((uint32_t)j, c.by_page)] : -1;
+        }
+    };
+    auto bring = [&](uint32_t to) {
+        if (more) {
+            const uint32_t stage = ring + to * H::kStage, kv = load.unit % a.kv_heads;
+            const T *keys = static_cast<const T *>(a.keys) + kv * a.head, *values = static_cast<const T *>(a.values) + kv * a.head;
+            uint8_t *const counts = memory + to * H::kStage + 2 * H::kSide;
+#pragma unroll
+            for (uint32_t k = 0; k < kCopies; ++k) {
+                const uint32_t i = threadIdx.x + k * kShareThreads, r = i / kPer, v = i - r * kPer;
+                const int32_t j = load.tile * (int32_t)H::kTokens + (int32_t)r;
+                const bool on = (uint32_t)ids[k] < c.n_pages;
+                if (v == 0) {
+                    counts[r] = on;
+                    if (!on && j < load.tokens && load.unit == 0) cache_flag(c, TD_ERR_OOB_INDEX);
+                }
+                if (v * 8 < a.dim) {
+                    const int64_t at = on ? ids[k] * a.page + (j - (int64_t)fast_div((uint32_t)j, c.by_page) * c.page_size) * a.token + v * 8 : 0;
+                    copy_async_or_zero(stage + r * S::kPitch + v * 16, keys + at, on ? 16u : 0u);
+                    copy_async_or_zero(stage + H::kSide + r * S::kPitch + v * 16, values + at, on ? 16u : 0u);
+                }
+            }
+            load.step(a, units, H::kTokens);
+            look();
+        }
+        copy_commit();
+    };
+    look();
+#pragma unroll 1
+    for (uint32_t i = 0; i + 1 < H::kStages; ++i) bring(i);
+
+    Fold<T, kChunks> f;
+    ShareCut cut_in{}, cut_out{};
+    uint32_t stage = 0, put = H::kStages - 1, m_count = 0, m_tile = 0, split = 0, splits = 1, wide = 1;
+    bool active = false, head_whole = false;
+#pragma unroll 1
+    while (use.here(end)) {
+        copy_wait<H::kStages - 2>();
+        __syncthreads();                                      // the tile is here, and the stage of the last turn is free
+        bring(put);
+        put = put + 1 == H::kStages ? 0 : put + 1;
+        const uint32_t m_block = use.unit / a.kv_heads, kv = use.unit - m_block * a.kv_heads, m_first = m_block * a.m_rows;
+        // The row and head of the block's row i (ratio rows of heads per row of the group), or false.
+        auto at_row = [&](uint32_t i, uint32_t &row, uint32_t &head) {
+            const uint32_t rr = fast_div(m_first + i, a.by_ratio);
+            row = use.group * a.group + rr;
+            head = kv * a.ratio + m_first + i - rr * a.ratio;
+            return i < m_count && row < a.n_rows;
+        };
+        if (use.tile == 0 || use.place == begin) {            // a unit begins here
+            head_whole = use.tile == 0;
+            m_count = min(a.m_rows, a.group * a.ratio - m_first);
+            const uint32_t m_tiles = (m_count + kHeadRows - 1) / kHeadRows;
+            wide = m_tiles <= 1 ? 1 : m_tiles <= 2 ? 2 : m_tiles <= 4 ? 4 : 8;
+            splits = min(H::kSplits, 8 / wide);
+            m_tile = warp & (wide - 1);
+            split = warp / wide;
+            active = m_tile < m_tiles && split < splits;
+            if (active) {
+                f.begin();
+                f.query(static_cast<const T *>(a.q), query, a.dim, [&](uint32_t h) {
+                    uint32_t row, head;
+                    return at_row(m_tile * kHeadRows + h, row, head) ? row * a.q_row + head * a.q_head : (int64_t)-1;
+                });
+            }
+        }
+        if (active) {
+            const uint32_t at = ring + stage * H::kStage;
+            const uint8_t *const on = memory + stage * H::kStage + 2 * H::kSide;
+#pragma unroll 1
+            for (uint32_t sub = split; sub < H::kTokens / 16; sub += splits) {
+                const uint32_t counts = __ballot_sync(kFullMask, on[sub * 16 + (lane & 15u)] != 0) & 0xffffu;
+                if (counts) f.add(at + sub * 16 * S::kPitch, at + H::kSide + sub * 16 * S::kPitch, query, counts, a.scale2);
+            }
+        }
+        stage = stage + 1 == H::kStages ? 0 : stage + 1;
+        const bool final = use.tile + 1 == (int32_t)use.tiles;
+        if (final || use.place + 1 == end) {                  // the unit, or this block's part of it, ends here
+            const uint32_t g = lane >> 2;
+            if (active) f.end();
+            if (splits > 1) {
+                if (active && split > 0) {
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        float *to = merge + (size_t)(((split - 1) * wide + m_tile) * kHeadRows + g + r * 8) * (S::kDim + 2);
+                        f.store(to, to + S::kDim, r);
+                    }
+                }
+                __syncthreads();
+                if (active && split == 0) {
+#pragma unroll 1
+                    for (uint32_t k = 1; k < splits; ++k) {
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const float *from = merge + (size_t)(((k - 1) * wide + m_tile) * kHeadRows + g + r * 8) * (S::kDim + 2);
+                            f.join(from, from + S::kDim, r);
+                        }
+                    }
+                }
+            }
+            const bool whole = head_whole && final;
+            if (active && split == 0) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const uint32_t i = m_tile * kHeadRows + g + r * 8;
+                    uint32_t row, head;
+                    if (!at_row(i, row, head)) continue;
+                    if (whole) {
+                        float *to = a.common + ((size_t)row * a.n_heads + head) * (S::kDim + 2);
+                        f.store(to, to + S::kDim, r);
+                    } else {
+                        float *to = a.share_parts + ((size_t)2 * blockIdx.x + (head_whole ? 1 : 0)) * H::kPartFloats;
+                        f.store(to + i * S::kDim, to + kShareHeads * S::kDim + 2 * i, r);
+                    }
+                }
+            }
+            if (!whole) {
+                const ShareCut cut{use.place - (uint32_t)use.tile - 1, use.group, use.unit, use.tiles, 1u};
+                if (head_whole) cut_out = cut; else cut_in = cut;
+            }
+        }
+        use.step(a, units, H::kTokens);
+    }
+    copy_wait<0>();
+#pragma unroll 1
+    for (uint32_t side = 0; side < 2; ++side) {
+        const ShareCut u = side == 0 ? cut_in : cut_out;
+        if (!u.valid) continue;
+        const uint32_t b0 = line.warp_of(u.place + 1), b1 = line.warp_of(u.place + u.tiles);
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            last = atomicAdd(a.share_arrived + b0, 1u) == b1 - b0;
+            if (last) a.share_arrived[b0] = 0;
+            __threadfence();
+        }
+        __syncthreads();
+        const bool joins = last;
+        __syncthreads();
+        if (!joins) continue;
+        const uint32_t m_block = u.unit / a.kv_heads, kv = u.unit - m_block * a.kv_heads, first = m_block * a.m_rows, count = min(a.m_rows, a.group * a.ratio - first);
+        for (uint32_t i = threadIdx.x; i < count * (S::kDim / 2); i += kShareThreads) {
+            const uint32_t r = i / (S::kDim / 2), d = (i - r * (S::kDim / 2)) * 2, rr = fast_div(first + r, a.by_ratio), row = u.group * a.group + rr;
+            if (row >= a.n_rows || d >= a.dim) continue;
+            auto part = [&](uint32_t b) { return a.share_parts + ((size_t)2 * b + (b == b0)) * H::kPartFloats; };
+            float top = -CUDART_INF_F;
+            for (uint32_t b = b0; b <= b1; ++b) top = max_nan(top, __ldcg(part(b) + kShareHeads * S::kDim + 2 * r));
+            const float ref = top == -CUDART_INF_F ? 0.0f : top;
+            float sum = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll 4
+            for (uint32_t b = b0; b <= b1; ++b) {
+                const float2 ml = __ldcg(reinterpret_cast<const float2 *>(part(b) + kShareHeads * S::kDim + 2 * r));
+                const float2 v = __ldcg(reinterpret_cast<const float2 *>(part(b) + r * S::kDim + d));
+                const float e = exp2_approx(ml.x - ref);
+                sum = fmaf(ml.y, e, sum);
+                x = fmaf(v.x, e, x);
+                y = fmaf(v.y, e, y);
+            }
+            float *to = a.common + ((size_t)row * a.n_heads + kv * a.ratio + first + r - rr * a.ratio) * (S::kDim + 2);
+            *reinterpret_cast<float2 *>(to + d) = make_float2(x, y);
+            if (d == 0) *reinterpret_cast<float2 *>(to + S::kDim) = make_float2(top, sum);
+        }
     }
 }
 

@@ -153,19 +153,42 @@ cudaError_t run_write(const CacheView &v, const PoolView &p, WriteArgs k, cudaSt
 constexpr uint32_t kBlocks = 148;                             // one per SM
 template <int kChunks>
 constexpr size_t part_bytes() { return (size_t)(2 * AttendShape<kChunks>::kWarps + 2) * kBlocks * AttendShape<kChunks>::kPartFloats * 4; }
-size_t attend_bytes(uint32_t dim) {                           // never falls as dim grows
-    size_t n = part_bytes<4>();
-    if (dim > 64) n = std::max(n, part_bytes<6>());
-    if (dim > 96) n = std::max(n, part_bytes<8>());
-    if (dim > 128) n = std::max(n, part_bytes<12>());
-    if (dim > 192) n = std::max(n, part_bytes<16>());
-    return round_up(kBlocks * 4, 256) + n;
+template <int kChunks>
+constexpr size_t share_bytes() { return (size_t)2 * kBlocks * ShareShape<kChunks>::kPartFloats * 4; }
+struct AttendLayout {
+    size_t arrived, share_arrived, shared, common, parts, share_parts, total;
+};
+AttendLayout attend_layout(uint32_t n_rows, uint32_t n_heads, uint32_t dim) {          // no area shrinks as an argument grows
+    size_t parts = part_bytes<4>(), share = share_bytes<4>(), padded = 64;
+    auto at_least = [&](uint32_t d, size_t p, size_t s) { if (dim > padded) { parts = std::max(parts, p); share = std::max(share, s); padded = d; } };
+    at_least(96, part_bytes<6>(), share_bytes<6>());
+    at_least(128, part_bytes<8>(), share_bytes<8>());
+    at_least(192, part_bytes<12>(), share_bytes<12>());
+    at_least(256, part_bytes<16>(), share_bytes<16>());
+    AttendLayout L{};
+    size_t p = 0;
+    auto take = [&](size_t bytes) { const size_t at = p; p = round_up(p + bytes, 256); return at; };
+    L.arrived = take(kBlocks * 4);
+    L.share_arrived = take(kBlocks * 4);
+    L.shared = take((size_t)n_rows * 8);
+    L.parts = take(parts);
+    L.share_parts = take(share);
+    L.common = take((size_t)n_rows * n_heads * (padded + 2) * 4);
+    L.total = p;
+    return L;
 }
 template <typename T, int kChunks>
 cudaError_t run_attend(const CacheView &v, const AttendArgs &k, cudaStream_t st) {
     using S = AttendShape<kChunks>;
     const cudaError_t rc = cudaFuncSetAttribute(attend_kernel<T, kChunks>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes);
     if (rc != cudaSuccess) return rc;
+    if (k.group > 1) {
+        using H = ShareShape<kChunks>;
+        cudaError_t rs = cudaFuncSetAttribute(share_kernel<T, kChunks>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)H::kBytes);
+        if (rs == cudaSuccess) rs = launch(share_plan_kernel, k.n_groups, kShareThreads, st, 1u, v, k);
+        if (rs == cudaSuccess) rs = launch_smem(share_kernel<T, kChunks>, kBlocks, kShareThreads, H::kBytes, st, 1u, v, k);
+        if (rs != cudaSuccess) return rs;
+    }
     return launch_smem(attend_kernel<T, kChunks>, kBlocks, S::kThreads, S::kBytes, st, 1u, v, k);
 }
 template <typename T>
@@ -285,7 +308,7 @@ int td_cache_write(const td_cache_write_args *a, void *stream) {
 
 size_t td_cache_attention_workspace_bytes(uint32_t n_rows, uint32_t n_heads, uint32_t dim) {
     if (n_rows >= kMaxRows || n_heads >= (1u << 16) || dim > kMaxDim) return 0;
-    return attend_bytes(dim);
+    return attend_layout(n_rows, n_heads, dim).total;
 }
 
 int td_cache_attention(const td_cache_attention_args *a, void *stream) {
@@ -331,9 +354,21 @@ int td_cache_attention(const td_cache_attention_args *a, void *stream) {
     k.units = k.kv_heads * ((k.ratio + kHeadRows - 1) / kHeadRows);
     k.scale = a->scale;
     k.scale2 = (float)(1.4426950408889634 * (double)a->scale);
+    // rows that share, and their heads over one key head in blocks of like size
+    k.group = std::min({a->group, a->n_rows, kMaxGroup});
+    k.n_groups = (a->n_rows + k.group - 1) / k.group;
+    k.m_blocks = (k.group * k.ratio + kShareHeads - 1) / kShareHeads;
+    k.m_rows = (k.group * k.ratio + k.m_blocks - 1) / k.m_blocks;
+    k.by_group = make_fastdiv(k.group);
+    k.by_ratio = make_fastdiv(k.ratio);
+    const AttendLayout L = attend_layout(a->n_rows, a->n_heads, c->dim);
     uint8_t *ws = static_cast<uint8_t *>(a->workspace);
-    k.arrived = reinterpret_cast<uint32_t *>(ws);
-    k.parts = reinterpret_cast<float *>(ws + round_up(kBlocks * 4, 256));
+    k.arrived = reinterpret_cast<uint32_t *>(ws + L.arrived);
+    k.share_arrived = reinterpret_cast<uint32_t *>(ws + L.share_arrived);
+    k.shared = reinterpret_cast<int2 *>(ws + L.shared);
+    k.parts = reinterpret_cast<float *>(ws + L.parts);
+    k.share_parts = reinterpret_cast<float *>(ws + L.share_parts);
+    k.common = reinterpret_cast<float *>(ws + L.common);
     cudaStream_t st = (cudaStream_t)stream;
     const CacheView v = cache_view(c);
     return result(c->dtype == TD_F32 ? run_attend_float(v, k, st) : c->dtype == TD_BF16 ? run_attend<__nv_bfloat16>(v, k, st)

@@ -14,6 +14,10 @@ __device__ __forceinline__ void copy_async_or_zero(uint32_t to, const void *from
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
 
+__device__ __forceinline__ void store_shared(uint32_t to, const uint4 &v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
 // Four 8 x 8 matrices of 16-bit elements; lane l gives the address of row l % 8 of matrix l / 8.  Lane 4 g + t gets elements
 // 2t and 2t + 1 of row g of each (transposed: of column g).
 __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
