@@ -1,14 +1,17 @@
 // Attention of one new token per row over a paged cache.
 //
-// The work is one pass over the keys and values with a running maximum and sum per row and head.  A unit is a row's
-// heads over one key head (16 at most: the rows of a matrix instruction), its tokens come in tiles of kTile.  All
-// units' tiles, one unit after the other, are a line that is cut into equal pieces, a piece per warp, wherever the cuts
+// The work is one pass over the keys and values with a running reference and sum per row and head.  A unit is a row's
+// heads over one key head, 8 or 16 at most; its tokens come in tiles of kTile.  Both products have the cache on the matrix
+// instructions' long side: scores are (16 tokens) x (8 heads), results (16 columns of values) x (8 heads), so that few heads
+// waste nothing; a transposition of 8 x 8 matrices turns the one's output into the other's input.  All units'
+// tiles, one unit after the other, are a line that is cut into equal pieces, a piece per warp, wherever the cuts
 // fall: so one long sequence and a thousand short ones load the machine alike.  A warp has its tiles brought by its own ring of
-// asynchronous copies, several tiles ahead and across units; no warp waits for another.  Units that a cut
-// went through leave parts (maximum, sum, weighted values), joined in the order of the tokens: within a block after its
+// bulk copies (one per token and side), several tiles ahead and across units; no warp waits for another.  Units that a cut
+// went through leave parts (reference, sum, weighted values), joined in the order of the tokens: within a block after its
 // warps are done, between blocks by the last block to arrive.  The same call gives the same bits.
 #pragma once
 
+#include "td_async.cuh"
 #include "td_cache.cuh"
 #include "td_mma.cuh"
 
@@ -37,27 +40,36 @@ struct AttendArgs {
 };
 
 constexpr uint32_t kTile = 16;                                // tokens of a tile
-constexpr uint32_t kHeadRows = 16;                            // heads of a unit
+constexpr float kSlack = 8.0f;                                // how far (log2) a score may pass the reference before that moves
+constexpr uint32_t kBarBytes = 8;
 constexpr uint32_t kLeastTiles = 4;                           // of a warp, before another block is used
 
-// Shapes of a kernel for heads of up to 16 * kChunks elements.
-template <int kChunks>
+// Shapes of a kernel for heads of up to 16 * kChunks elements, 8 * kN of them side by side.
+template <int kChunks, int kN>
 struct AttendShape {
-    static constexpr uint32_t kDim = 16 * kChunks;
+    static constexpr uint32_t kDim = 16 * kChunks, kHeads = 8 * kN;
     static constexpr uint32_t kWarps = kChunks <= 8 ? 8 : 4;
     static constexpr uint32_t kThreads = 32 * kWarps;
     static constexpr uint32_t kPitch = kDim * 2 + 16;         // bytes of a row in shared memory: an odd number of 16s, so that 8 rows lie in different banks
     static constexpr uint32_t kSide = kTile * kPitch;         // keys, or values, of a tile
     static constexpr uint32_t kStage = 2 * kSide;
-    static constexpr bool kQueryInRegisters = kChunks <= 8;
-    static constexpr uint32_t kQuery = kQueryInRegisters ? 0 : kHeadRows * kPitch;
+    static constexpr bool kQueryInRegisters = kChunks * kN <= 16;
+    static constexpr uint32_t kQuery = kQueryInRegisters ? 0 : kHeads * kPitch;
     static constexpr uint32_t kRoom = 216 * 1024 / kWarps;    // bytes a warp may have
-    static constexpr uint32_t kFits = (kRoom - kQuery) / (kStage + 16);
+    static constexpr uint32_t kFits = (kRoom - kQuery) / (kStage + 16 + kBarBytes);
     static constexpr uint32_t kStages = kFits < 6 ? kFits : 6;
-    static constexpr uint32_t kWarpBytes = kStages * (kStage + 16) + kQuery;
+    static constexpr uint32_t kWarpBytes = (kStages * (kStage + 16 + kBarBytes) + kQuery + 15) / 16 * 16;
     static constexpr uint32_t kBytes = kWarps * kWarpBytes;
-    static constexpr uint32_t kPartFloats = kHeadRows * (kDim + 2);      // weighted values [16][kDim], then {maximum, sum} [16]
+    static constexpr uint32_t kPartFloats = kHeads * (kDim + 2);         // weighted values [kHeads][kDim], then {reference, sum} [kHeads]
 };
+
+// A warp's wait for a copy into one of its stages, bounded; false: it did not land in time.
+__device__ __forceinline__ bool wait_copy(uint32_t bar, uint32_t parity) {
+    constexpr uint32_t kPolls = 1u << 16;
+    for (uint32_t i = 0; i < kPolls; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
+    return false;
+}
 
 struct Span {                                                 // the tokens [lo, n) of sequence s
     int32_t s, lo, n;
@@ -130,10 +142,11 @@ struct Cut {
     uint32_t row, unit, tiles, valid;
 };
 
+template <uint32_t kHeads>
 __device__ __forceinline__ uint32_t heads_of(const AttendArgs &a, uint32_t unit, uint32_t &first) {          // heads of a unit, from `first` on
-    const uint32_t per_kv = a.units / a.kv_heads, kv = unit / per_kv, at = (unit - kv * per_kv) * kHeadRows;
+    const uint32_t per_kv = a.units / a.kv_heads, kv = unit / per_kv, at = (unit - kv * per_kv) * kHeads;
     first = kv * a.ratio + at;
-    return min(kHeadRows, a.ratio - at);
+    return min(kHeads, a.ratio - at);
 }
 
 // What a row's head has from the tokens its group has in common; nullptr: there are none.
@@ -146,25 +159,25 @@ __device__ __forceinline__ const float *common_of(const AttendArgs &a, uint32_t 
 constexpr uint32_t kNoTokens = 0xffffffffu;
 // Joins the parts k = 0 .. count - 1 of a unit (slot(k) of `parts`) into out and lse, or into another part; `me` of `all` threads.
 // A maximum of -inf means that a part has nothing; NaN stays.
-template <typename T, uint32_t kDim, typename Slot>
+template <typename T, uint32_t kDim, uint32_t kHeads, typename Slot>
 __device__ __forceinline__ void join_parts(const AttendArgs &a, uint32_t row, uint32_t unit, const float *parts, uint32_t count, Slot slot,
                                            float *to, uint32_t me, uint32_t all) {
-    constexpr uint32_t kFloats = kHeadRows * (kDim + 2);
+    constexpr uint32_t kFloats = kHeads * (kDim + 2);
     uint32_t first;
-    const uint32_t heads = heads_of(a, unit, first), pairs = kDim / 2;
+    const uint32_t heads = heads_of<kHeads>(a, unit, first), pairs = kDim / 2;
     const bool nothing = count == kNoTokens;                  // the row has no tokens, its group may
     if (nothing) count = 0;
     for (uint32_t i = me; i < heads * pairs; i += all) {
         const uint32_t h = i / pairs, d = (i - h * pairs) * 2;
         if (d >= a.dim) continue;
         float top = -CUDART_INF_F;
-        for (uint32_t k = 0; k < count; ++k) top = max_nan(__ldcg(parts + (size_t)slot(k) * kFloats + kHeadRows * kDim + 2 * h), top);
+        for (uint32_t k = 0; k < count; ++k) top = max_nan(__ldcg(parts + (size_t)slot(k) * kFloats + kHeads * kDim + 2 * h), top);
         const float ref = top == -CUDART_INF_F ? 0.0f : top;
         float sum = 0.0f, x = 0.0f, y = 0.0f;
 #pragma unroll 4
         for (uint32_t k = 0; k < count; ++k) {
             const float *p = parts + (size_t)slot(k) * kFloats;
-            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(p + kHeadRows * kDim + 2 * h)), v = __ldcg(reinterpret_cast<const float2 *>(p + h * kDim + d));
+            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(p + kHeads * kDim + 2 * h)), v = __ldcg(reinterpret_cast<const float2 *>(p + h * kDim + d));
             const float e = exp2_approx(ml.x - ref);
             sum = fmaf(ml.y, e, sum);
             x = fmaf(v.x, e, x);
@@ -182,7 +195,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs &a, uint32_t row, ui
         }
         if (to) {
             *reinterpret_cast<float2 *>(to + h * kDim + d) = make_float2(x, y);
-            if (d == 0) *reinterpret_cast<float2 *>(to + kHeadRows * kDim + 2 * h) = make_float2(top, sum);
+            if (d == 0) *reinterpret_cast<float2 *>(to + kHeads * kDim + 2 * h) = make_float2(top, sum);
             continue;
         }
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -191,36 +204,44 @@ __device__ __forceinline__ void join_parts(const AttendArgs &a, uint32_t row, ui
     }
 }
 
-// Sixteen rows' running maximum (in units of log2), sum and weighted values, in the layout of the matrix instructions: lane
-// 4 g + t has rows g and g + 8.
-template <typename T, int kChunks>
+// The running reference (in units of log2), sum and weighted values of 8 * kN heads, in the layout of the matrix instructions: lane
+// 4 g + t has heads 8 n + 2 t and 8 n + 2 t + 1, of every 16 columns of values those g and g + 8 places in, and of every 16
+// tokens the same.  The reference follows the scores' maximum only when one passes it by kSlack: weights stay below
+// 2^kSlack, and results hardly ever have to be brought to a new reference.
+template <typename T, int kChunks, int kN>
 struct Fold {
-    using S = AttendShape<kChunks>;
-    uint32_t qf[S::kQueryInRegisters ? kChunks : 1][4];
-    float o[2 * kChunks][4], m[2], l[2];
+    using S = AttendShape<kChunks, kN>;
+    uint32_t qf[S::kQueryInRegisters ? kChunks : 1][kN][2];
+    float o[kChunks][kN][4], m[kN][2], l[kN][2];
 
     __device__ __forceinline__ void begin() {
 #pragma unroll
-        for (int k = 0; k < 2 * kChunks; ++k) o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.0f;
-        m[0] = m[1] = -CUDART_INF_F;
-        l[0] = l[1] = 0.0f;
+        for (int n = 0; n < kN; ++n) {
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) o[c][n][0] = o[c][n][1] = o[c][n][2] = o[c][n][3] = 0.0f;
+            m[n][0] = m[n][1] = -CUDART_INF_F;
+            l[n][0] = l[n][1] = 0.0f;
+        }
     }
-    // The rows' queries, from q + offset(row) on (negative: zeros), into registers or, for long heads, into the warp's shared memory.
+    // The heads' queries, from q + offset(head) on (negative: zeros), into registers or, for many long ones, into the warp's shared memory.
     template <typename Offset>
     __device__ __forceinline__ void query(const T *q, uint32_t shared, uint32_t dim, Offset offset) {
         const uint32_t lane = threadIdx.x & 31u, g = lane >> 2, t = lane & 3u;
         if constexpr (S::kQueryInRegisters) {
-            const int64_t at[2] = {offset(g), offset(g + 8)};
 #pragma unroll
-            for (int k = 0; k < kChunks; ++k)
+            for (int n = 0; n < kN; ++n) {
+                const int64_t at = offset(n * 8 + g);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t d = k * 16 + t * 2 + (i >> 1) * 8;
-                    qf[k][i] = at[i & 1] >= 0 && d < dim ? *reinterpret_cast<const uint32_t *>(q + at[i & 1] + d) : 0u;
-                }
+                for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t d = c * 16 + i * 8 + t * 2;
+                        qf[c][n][i] = at >= 0 && d < dim ? *reinterpret_cast<const uint32_t *>(q + at + d) : 0u;
+                    }
+            }
         } else {
             __syncwarp();
-            for (uint32_t i = lane; i < kHeadRows * S::kDim / 8; i += 32) {
+            for (uint32_t i = lane; i < S::kHeads * S::kDim / 8; i += 32) {
                 const uint32_t h = i / (S::kDim / 8), v = i - h * (S::kDim / 8);
                 const int64_t at = offset(h);
                 uint4 x = make_uint4(0u, 0u, 0u, 0u);
@@ -230,110 +251,119 @@ struct Fold {
             __syncwarp();
         }
     }
-    // Sixteen more tokens: keys and values in shared memory, bit i of `counts`: token i counts.
+    // Sixteen more tokens: keys and values in shared memory, bit i of the 16 in `counts`: token i counts.
     __device__ __forceinline__ void add(uint32_t keys, uint32_t values, uint32_t shared, uint32_t counts, float scale2) {
-        const uint32_t lane = threadIdx.x & 31u, t = lane & 3u;
-        // scores of 16 heads and 16 tokens, two products of 8 tokens
-        float s[2][4] = {};
+        const uint32_t lane = threadIdx.x & 31u, g = lane >> 2, row = lane & 7u, upper = lane >> 3 & 1u, right = lane >> 4;
+        float s[kN][4] = {};
+        const uint32_t key = keys + (row + upper * 8) * S::kPitch + right * 16;
 #pragma unroll
-        for (int k = 0; k < kChunks; ++k) {
-            uint32_t b[4], qa[4];
-            load_matrices(b, keys + ((lane & 7u) + (lane >> 4) * 8) * S::kPitch + k * 32 + (lane >> 3 & 1u) * 16);
+        for (int c = 0; c < kChunks; ++c) {
+            uint32_t a[4];
+            load_matrices(a, key + c * 32);
             if constexpr (S::kQueryInRegisters) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) qa[i] = qf[k][i];
+                for (int n = 0; n < kN; ++n) multiply_add<T>(s[n], a, qf[c][n][0], qf[c][n][1]);
             } else {
-                load_matrices(qa, shared + (lane & 15u) * S::kPitch + k * 32 + (lane >> 4) * 16);
+                static_assert(S::kQueryInRegisters || kN == 2, "two columns of matrices, loaded together");
+                uint32_t b[4];
+                load_matrices(b, shared + (row + right * 8) * S::kPitch + c * 32 + upper * 16);
+                multiply_add<T>(s[0], a, b[0], b[1]);
+                multiply_add<T>(s[kN - 1], a, b[2], b[3]);
             }
-            multiply_add<T>(s[0], qa, b[0], b[1]);
-            multiply_add<T>(s[1], qa, b[2], b[3]);
         }
-        float top[2] = {m[0], m[1]};
+        bool past = false;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int n = 0; n < kN; ++n)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const bool on = counts >> (i * 8 + t * 2 + (k & 1)) & 1u;
-                s[i][k] = on ? s[i][k] * scale2 : -CUDART_INF_F;
-                top[k >> 1] = max_nan(top[k >> 1], s[i][k]);
+            for (int i = 0; i < 4; ++i) {
+                s[n][i] = counts >> (g + (i >> 1) * 8) & 1u ? s[n][i] * scale2 : -CUDART_INF_F;
+                past |= !(s[n][i] <= m[n][i & 1] + kSlack);
             }
+        if (__any_sync(kFullMask, past)) {                    // a new reference (also where a score is NaN, which stays)
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            top[r] = max_nan(top[r], __shfl_xor_sync(kFullMask, top[r], 1));
-            top[r] = max_nan(top[r], __shfl_xor_sync(kFullMask, top[r], 2));
-        }
-        // the sums so far are brought to the new maximum where it has moved (or is NaN), which is seldom
-        if (__any_sync(kFullMask, !(top[0] == m[0]) || !(top[1] == m[1]))) {
+            for (int n = 0; n < kN; ++n) {
+                float top[2], keep[2];
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const float keep = m[r] == -CUDART_INF_F ? 0.0f : exp2_approx(m[r] - top[r]);
-                l[r] *= keep;
+                for (int i = 0; i < 2; ++i) {
+                    top[i] = max_nan(max_nan(s[n][i], s[n][i + 2]), m[n][i]);
 #pragma unroll
-                for (int k = 0; k < 2 * kChunks; ++k) {
-                    o[k][2 * r] *= keep;
-                    o[k][2 * r + 1] *= keep;
+                    for (int d = 4; d < 32; d *= 2) top[i] = max_nan(top[i], __shfl_xor_sync(kFullMask, top[i], d));
+                    keep[i] = m[n][i] == -CUDART_INF_F ? 0.0f : exp2_approx(m[n][i] - top[i]);
+                    l[n][i] *= keep[i];
+                    m[n][i] = top[i];
                 }
-                m[r] = top[r];
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[c][n][i] *= keep[i & 1];
             }
         }
-        uint32_t p[4];
-        {
-            const float ref[2] = {m[0] == -CUDART_INF_F ? 0.0f : m[0], m[1] == -CUDART_INF_F ? 0.0f : m[1]};
+        uint32_t p[kN][2];
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[n][i] = exp2_approx(s[n][i] - (m[n][i & 1] == -CUDART_INF_F ? 0.0f : m[n][i & 1]));
+                l[n][i & 1] += s[n][i];
+            }
+            // Weights are rounded to the type of the values, as the matrix instruction takes them; their sum is not.
+            p[n][0] = transposed(pair_of<T>(s[n][0], s[n][1]));
+            p[n][1] = transposed(pair_of<T>(s[n][2], s[n][3]));
+        }
+        const uint32_t value = values + (row + right * 8) * S::kPitch + upper * 16;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            uint32_t a[4];
+            load_matrices_transposed(a, value + c * 32);
+#pragma unroll
+            for (int n = 0; n < kN; ++n) multiply_add<T>(o[c][n], a, p[n][0], p[n][1]);
+        }
+    }
+    // The sums over all tokens, in every lane.
+    __device__ __forceinline__ void end() {
+#pragma unroll
+        for (int n = 0; n < kN; ++n)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    s[i][k] = exp2_approx(s[i][k] - ref[k >> 1]);
-                    l[k >> 1] += s[i][k];
-                }
-            // Weights are rounded to the type of the values, as the matrix instruction takes them; their sum is not.
-            p[0] = pair_of<T>(s[0][0], s[0][1]);
-            p[1] = pair_of<T>(s[0][2], s[0][3]);
-            p[2] = pair_of<T>(s[1][0], s[1][1]);
-            p[3] = pair_of<T>(s[1][2], s[1][3]);
-        }
-#pragma unroll
-        for (int k = 0; k < kChunks; ++k) {
-            uint32_t b[4];
-            load_matrices_transposed(b, values + ((lane & 7u) + (lane >> 3 & 1u) * 8) * S::kPitch + k * 32 + (lane >> 4) * 16);
-            multiply_add<T>(o[2 * k], p, b[0], b[1]);
-            multiply_add<T>(o[2 * k + 1], p, b[2], b[3]);
-        }
+                for (int d = 4; d < 32; d *= 2) l[n][i] += __shfl_xor_sync(kFullMask, l[n][i], d);
     }
-    // The sums over a row, in all four of its lanes.
-    __device__ __forceinline__ void end() {
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            l[r] += __shfl_xor_sync(kFullMask, l[r], 1);
-            l[r] += __shfl_xor_sync(kFullMask, l[r], 2);
-        }
-    }
-    // Row g + 8 r joined with a part of it.
-    __device__ __forceinline__ void join(const float *from, const float *ml, int r) {
-        const uint32_t t = threadIdx.x & 3u;
+    // Head 8 n + 2 t + i joined with a part of it, and as a part: values and {reference, sum}.
+    __device__ __forceinline__ void join(const float *from, const float *ml, int n, int i) {
+        const uint32_t g = (threadIdx.x & 31u) >> 2;
         const float2 other = *reinterpret_cast<const float2 *>(ml);
-        const float top = max_nan(m[r], other.x), ref = top == -CUDART_INF_F ? 0.0f : top, e = exp2_approx(m[r] - ref), f = exp2_approx(other.x - ref);
+        const float top = max_nan(m[n][i], other.x), ref = top == -CUDART_INF_F ? 0.0f : top, e = exp2_approx(m[n][i] - ref), f = exp2_approx(other.x - ref);
 #pragma unroll
-        for (int k = 0; k < 2 * kChunks; ++k) {
-            const float2 v = *reinterpret_cast<const float2 *>(from + k * 8 + t * 2);
-            o[k][2 * r] = fmaf(v.x, f, o[k][2 * r] * e);
-            o[k][2 * r + 1] = fmaf(v.y, f, o[k][2 * r + 1] * e);
-        }
-        l[r] = fmaf(other.y, f, l[r] * e);
-        m[r] = top;
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) o[c][n][i + 2 * k] = fmaf(from[c * 16 + k * 8 + g], f, o[c][n][i + 2 * k] * e);
+        l[n][i] = fmaf(other.y, f, l[n][i] * e);
+        m[n][i] = top;
     }
-    // Row g + 8 r as a part: values to `to`, {maximum, sum} to `ml`.
-    __device__ __forceinline__ void store(float *to, float *ml, int r) const {
-        const uint32_t t = threadIdx.x & 3u;
+    __device__ __forceinline__ void store(float *to, float *ml, int n, int i) const {
+        const uint32_t g = (threadIdx.x & 31u) >> 2;
 #pragma unroll
-        for (int k = 0; k < 2 * kChunks; ++k) *reinterpret_cast<float2 *>(to + k * 8 + t * 2) = make_float2(o[k][2 * r], o[k][2 * r + 1]);
-        if (t == 0) *reinterpret_cast<float2 *>(ml) = make_float2(m[r], l[r]);
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) to[c * 16 + k * 8 + g] = o[c][n][i + 2 * k];
+        if (g == 0) *reinterpret_cast<float2 *>(ml) = make_float2(m[n][i], l[n][i]);
+    }
+    // The head's result.
+    __device__ __forceinline__ void finish(T *out, float *lse, uint32_t dim, int n, int i) const {
+        const uint32_t g = (threadIdx.x & 31u) >> 2;
+        const float inv = l[n][i] == 0.0f ? 0.0f : 1.0f / l[n][i];
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (c * 16 + k * 8 < dim) out[c * 16 + k * 8 + g] = Elem<T>::from(o[c][n][i + 2 * k] * inv);
+        if (lse && g == 0) *lse = l[n][i] == 0.0f ? -CUDART_INF_F : (m[n][i] + log2f(l[n][i])) * 0.69314718055994531f;
     }
 };
 
-template <typename T, int kChunks>
-__global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kernel(CacheView c, AttendArgs a) {
-    using S = AttendShape<kChunks>;
+template <typename T, int kChunks, int kN>
+__global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_kernel(CacheView c, AttendArgs a) {
+    using S = AttendShape<kChunks, kN>;
     extern __shared__ __align__(16) uint8_t memory[];
     __shared__ unsigned long long sums[S::kThreads];          // places of all rows up to and with those of each thread
     __shared__ Cut cut_in, cut_out[S::kWarps];                // the unit that warp 0 began in the middle of; those a warp began and left
@@ -357,10 +387,16 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
     const unsigned long long begin = line.begin(min(w_global, line.warps)), end = line.begin(min(w_global + 1, line.warps));
 
     uint8_t *const mem = memory + warp * S::kWarpBytes;
-    const uint32_t ring = shared_address(mem), query = ring + S::kStages * S::kStage;
+    const uint32_t ring = smem_u32(mem), query = ring + S::kStages * S::kStage;
     uint4 *const notes = reinterpret_cast<uint4 *>(mem + S::kStages * S::kStage + S::kQuery);          // per stage: row, unit, tokens that count and flags and heads, first head
+    const uint32_t bars = query + S::kQuery + S::kStages * 16;
     if (a.dim != S::kDim)                                     // columns that no copy writes
         for (uint32_t i = lane; i < S::kStages * S::kStage / 16; i += 32) reinterpret_cast<uint4 *>(mem)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (lane == 0) {
+        for (uint32_t i = 0; i < S::kStages; ++i) mbar_init(bars + i * kBarBytes, 1);
+        fence_mbar_init();
+    }
+    fence_proxy_async();
     __syncwarp();
 
     if (begin < end) {
@@ -383,7 +419,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
 
         uint32_t kv, first, heads;
         auto enter = [&]() {                                  // a unit's key head and its heads
-            heads = heads_of(a, unit, first);
+            heads = heads_of<S::kHeads>(a, unit, first);
             kv = first / a.ratio;
         };
         auto leave = [&]() {                                  // to the unit behind
@@ -398,86 +434,84 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
             enter();
         };
         enter();
-        // Brings the next tile into stage `to`; false: there is none.  An empty unit's result is written on the way.
-        auto bring = [&](uint32_t to) -> bool {
-            for (;;) {
-                if (place >= end) return false;
-                if (tile >= 0) break;
+        // To the next tile; an empty unit's result is written on the way.  Then lanes 0 .. 15 and 16 .. 31 fetch the numbers of its
+        // tokens' pages, which the next call of bring() needs.
+        bool more = true;
+        int32_t id = -1;
+        auto look = [&]() {
+            while (place < end && tile < 0) {
                 ++place;
-                if (tiles == 0) {
-                    // nothing of its own: zeros, or what its group has in common
-                    join_parts<T, S::kDim>(a, row, unit, nullptr, span.n > 0 ? 0u : kNoTokens, [](uint32_t) { return 0u; }, nullptr, lane, 32);
-                    leave();
-                } else {
+                if (tiles) {
                     tile = 0;
+                } else {
+                    join_parts<T, S::kDim, S::kHeads>(a, row, unit, nullptr, span.n > 0 ? 0u : kNoTokens, [](uint32_t) { return 0u; }, nullptr, lane, 32);
+                    leave();
                 }
             }
-            // lanes 0 .. 15: where each token lies
+            more = place < end;
             const int32_t j = span.lo + tile * (int32_t)kTile + (int32_t)(lane & 15u);
-            int64_t at = -1;
-            if (j < span.n) {
-                const uint32_t page = fast_div((uint32_t)j, c.by_page);
-                const int32_t id = c.table[(size_t)span.s * c.max_pages + page];
-                if ((uint32_t)id < c.n_pages) at = id * a.page + (j - (int64_t)page * c.page_size) * a.token;
-                else if (unit == 0 && lane < 16) cache_flag(c, TD_ERR_OOB_INDEX);
-            }
-            const uint32_t counts = __ballot_sync(kFullMask, at >= 0) & 0xffffu;
-            const T *keys = static_cast<const T *>(a.keys) + kv * a.head, *values = static_cast<const T *>(a.values) + kv * a.head;
-            const uint32_t stage = ring + to * S::kStage;
-            constexpr uint32_t kPer = S::kDim / 8;            // 16-byte vectors of a row
-#pragma unroll
-            for (uint32_t i0 = 0; i0 < kTile * kPer; i0 += 32) {
-                const uint32_t i = i0 + lane, r = i / kPer, v = i - r * kPer;
-                const int64_t from = __shfl_sync(kFullMask, at, r);
-                if (v * 8 < a.dim) {
-                    const int64_t o = from < 0 ? 0 : from + v * 8;
-                    copy_async_or_zero(stage + r * S::kPitch + v * 16, keys + o, from < 0 ? 0u : 16u);
-                    copy_async_or_zero(stage + S::kSide + r * S::kPitch + v * 16, values + o, from < 0 ? 0u : 16u);
+            id = more && j < span.n ? c.table[(size_t)span.s * c.max_pages + fast_div((uint32_t)j, c.by_page)] : -1;
+        };
+        // Brings the tile into stage `to`: a lane per token and side.
+        auto bring = [&](uint32_t to) {
+            const int32_t j = span.lo + tile * (int32_t)kTile + (int32_t)(lane & 15u);
+            const bool on = (uint32_t)id < c.n_pages;
+            const uint32_t counts = __ballot_sync(kFullMask, on) & 0xffffu, bar = bars + to * kBarBytes;
+            const uint32_t at = ring + to * S::kStage + (lane >> 4) * S::kSide + (lane & 15u) * S::kPitch;
+            const bool fresh = tile == 0 || place == begin, final = tile + 1 == (int32_t)tiles, over = final || place + 1 == end;
+            if (lane == 0) {
+                mbar_expect_tx(bar, __popc(counts) * a.dim * 4);
+                notes[to] = make_uint4(row, unit, counts | (fresh ? 1u << 16 : 0u) | (over ? 1u << 17 : 0u) | (tile == 0 ? 1u << 18 : 0u) |
+                                       (final ? 1u << 19 : 0u) | heads << 20, first);
+                if (over) {                                   // a cut unit, for the joins: noted before the block's barrier
+                    const Cut cut{place - (uint32_t)tile - 1, row, unit, tiles, 1u};
+                    if (place - (uint32_t)tile < begin) { if (warp == 0) cut_in = cut; }
+                    else if (!final) cut_out[warp] = cut;
                 }
             }
-            const bool fresh = tile == 0 || place == begin, final = tile + 1 == (int32_t)tiles, over = final || place + 1 == end;
-            if (lane == 0) notes[to] = make_uint4(row, unit, counts | (fresh ? 1u << 16 : 0u) | (over ? 1u << 17 : 0u) | (tile == 0 ? 1u << 18 : 0u) |
-                                                  (final ? 1u << 19 : 0u) | heads << 20, first);
-            // a cut unit, for the join: the note is complete before the block's barrier
-            if (lane == 0 && over) {
-                const bool whole_head = place - tile >= begin, whole_tail = final;
-                const Cut cut{place - (uint32_t)tile - 1, row, unit, tiles, 1u};
-                if (!whole_head) { if (warp == 0) cut_in = cut; }
-                else if (!whole_tail) cut_out[warp] = cut;
+            if (on) {
+                const int64_t from = id * a.page + (j - (int64_t)fast_div((uint32_t)j, c.by_page) * c.page_size) * a.token + kv * a.head;
+                bulk_global_to_shared(at, static_cast<const T *>(lane < 16 ? a.keys : a.values) + from, a.dim * 2, bar);
+            } else {                                          // behind the end, or not a page: zeros, so that nothing there is used
+                for (uint32_t i = 0; i < S::kDim / 8; ++i) store_shared(at + i * 16, make_uint4(0u, 0u, 0u, 0u));
+                fence_proxy_async();
+                if (j < span.n && unit == 0 && lane < 16) cache_flag(c, TD_ERR_OOB_INDEX);
             }
             ++place;
             if (++tile == (int32_t)tiles) leave();
-            return true;
+            look();
         };
 
-        uint32_t brought = 0;                                 // tiles on their way or here
-        bool more = true;
-#pragma unroll 1
-        for (uint32_t i = 0; i + 1 < S::kStages; ++i) {
-            if (more) more = bring(i);
-            if (more) ++brought;
-            copy_commit();
-        }
-        Fold<T, kChunks> f;
+        uint32_t brought = 0, put = 0, stage = 0, parity = 0, done = 0;          // tiles brought; stages of the next to bring and to use
+        look();
+        for (; more && brought + 1 < S::kStages; ++brought) bring(put++);
+        Fold<T, kChunks, kN> f;
         bool head_whole = false;
-        uint32_t stage = 0, put = S::kStages - 1;
 #pragma unroll 1
-        for (uint32_t done = 0; done < brought; ++done) {
-            copy_wait<S::kStages - 2>();
+        for (; done < brought; ++done) {
+            // never seen to run out; the rest is then left, what is on its way still waited for
+            if (!wait_copy(bars + stage * kBarBytes, parity)) {
+                if (lane == 0) cache_flag(c, TD_ERR_COPY_TIMEOUT);
+                more = false;
+            }
             __syncwarp();
-            if (more) more = bring(put);                      // into the stage that the last turn was done with
-            if (more) ++brought;
-            copy_commit();
-            put = put + 1 == S::kStages ? 0 : put + 1;
+            if (more) {                                       // into the stage that the last turn was done with
+                bring(put);
+                ++brought;
+                put = put + 1 == S::kStages ? 0 : put + 1;
+            }
             const uint4 note = notes[stage];
             const uint32_t at = ring + stage * S::kStage;
-            stage = stage + 1 == S::kStages ? 0 : stage + 1;
-            const uint32_t first = note.w, heads = note.z >> 20, g = lane >> 2, t = lane & 3u;
+            if (++stage == S::kStages) {
+                stage = 0;
+                parity ^= 1u;
+            }
+            const uint32_t first = note.w, heads = note.z >> 20, t = lane & 3u;
             if (note.z >> 16 & 1u) {                          // a unit begins here
                 head_whole = note.z >> 18 & 1u;
-                const T *q = static_cast<const T *>(a.q) + note.x * a.q_row + first * a.q_head;
                 f.begin();
-                f.query(q, query, a.dim, [&](uint32_t h) { return h < heads ? (int64_t)h * a.q_head : (int64_t)-1; });
+                f.query(static_cast<const T *>(a.q) + note.x * a.q_row + first * a.q_head, query, a.dim,
+                        [&](uint32_t h) { return h < heads ? (int64_t)h * a.q_head : (int64_t)-1; });
             }
             f.add(at, at + S::kSide, query, note.z, a.scale2);
             if (note.z >> 17 & 1u) {                          // the unit, or this warp's part of it, ends here
@@ -485,40 +519,22 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
                 const bool whole = head_whole && (note.z >> 19 & 1u);
                 float *part = a.parts + ((size_t)2 * w_global + (head_whole ? 1 : 0)) * S::kPartFloats;
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const uint32_t h = g + r * 8;
-                    if (h >= heads) continue;
-                    if (whole) {
-                        float keep = 1.0f, sum = f.l[r], top = f.m[r], also = 0.0f;
-                        const float *w = common_of<S::kDim>(a, note.x, first + h);
-                        if (w) {
-                            const float2 ml = *reinterpret_cast<const float2 *>(w + S::kDim);
-                            const float most = max_nan(top, ml.x), ref = most == -CUDART_INF_F ? 0.0f : most;
-                            keep = exp2_approx(top - ref);
-                            also = exp2_approx(ml.x - ref);
-                            sum = fmaf(ml.y, also, sum * keep);
-                            top = most;
-                        }
-                        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                        T *out = static_cast<T *>(a.out) + note.x * a.out_row + (first + h) * a.out_head;
+                for (int n = 0; n < kN; ++n)
 #pragma unroll
-                        for (int k = 0; k < 2 * kChunks; ++k) {
-                            if (k * 8 + t * 2 >= a.dim) continue;
-                            float2 v = make_float2(0.0f, 0.0f);
-                            if (w) v = *reinterpret_cast<const float2 *>(w + k * 8 + t * 2);
-                            *reinterpret_cast<uint32_t *>(out + k * 8 + t * 2) =
-                                pair_of<T>(fmaf(v.x, also, f.o[k][2 * r] * keep) * inv, fmaf(v.y, also, f.o[k][2 * r + 1] * keep) * inv);
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t h = n * 8 + t * 2 + i;
+                        if (h >= heads) continue;
+                        if (whole) {
+                            if (const float *w = common_of<S::kDim>(a, note.x, first + h)) f.join(w, w + S::kDim, n, i);
+                            f.finish(static_cast<T *>(a.out) + note.x * a.out_row + (first + h) * a.out_head,
+                                     a.lse ? a.lse + (size_t)note.x * a.n_heads + first + h : nullptr, a.dim, n, i);
+                        } else {
+                            f.store(part + h * S::kDim, part + S::kHeads * S::kDim + 2 * h, n, i);
                         }
-                        if (a.lse && t == 0)
-                            a.lse[(size_t)note.x * a.n_heads + first + h] = sum == 0.0f ? -CUDART_INF_F : (top + log2f(sum)) * 0.69314718055994531f;
-                    } else {
-                        f.store(part + h * S::kDim, part + kHeadRows * S::kDim + 2 * h, r);
                     }
-                }
             }
         }
     }
-    copy_wait<0>();
     __syncthreads();
 
     // ---- units that cuts went through ----
@@ -527,7 +543,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
         const Cut u = cut_out[warp];
         const uint32_t w0 = w_global, w1 = line.warp_of(u.place + u.tiles);
         if (w1 <= w_last)
-            join_parts<T, S::kDim>(a, u.row, u.unit, a.parts, w1 - w0 + 1, [=](uint32_t k) { return 2 * (w0 + k) + (k == 0); }, nullptr, lane, 32);
+            join_parts<T, S::kDim, S::kHeads>(a, u.row, u.unit, a.parts, w1 - w0 + 1, [=](uint32_t k) { return 2 * (w0 + k) + (k == 0); }, nullptr, lane, 32);
     }
     float *const block_parts = a.parts + (size_t)2 * gridDim.x * S::kWarps * S::kPartFloats;
     // a unit that came in from the block before, and one that begins here and goes on into the next: at most one each
@@ -544,7 +560,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
         if (!u.valid) continue;
         const uint32_t w0 = line.warp_of(u.place + 1), w1 = line.warp_of(u.place + u.tiles), from = max(w0, w_first), to = min(w1, w_last);
         const uint32_t b0 = w0 / S::kWarps, b1 = w1 / S::kWarps;
-        join_parts<T, S::kDim>(a, u.row, u.unit, a.parts, to - from + 1, [=](uint32_t k) { return 2 * (from + k) + (from + k == w0); },
+        join_parts<T, S::kDim, S::kHeads>(a, u.row, u.unit, a.parts, to - from + 1, [=](uint32_t k) { return 2 * (from + k) + (from + k == w0); },
                                block_parts + ((size_t)2 * blockIdx.x + (blockIdx.x == b0)) * S::kPartFloats, threadIdx.x, S::kThreads);
         __threadfence();
         __syncthreads();
@@ -555,7 +571,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks>::kThreads, 1) attend_kern
         }
         __syncthreads();
         if (last)
-            join_parts<T, S::kDim>(a, u.row, u.unit, block_parts, b1 - b0 + 1, [=](uint32_t k) { return 2 * (b0 + k) + (k == 0); }, nullptr,
+            join_parts<T, S::kDim, S::kHeads>(a, u.row, u.unit, block_parts, b1 - b0 + 1, [=](uint32_t k) { return 2 * (b0 + k) + (k == 0); }, nullptr,
                                    threadIdx.x, S::kThreads);
         __syncthreads();
     }
@@ -624,15 +640,16 @@ __global__ void __launch_bounds__(kShareThreads) share_plan_kernel(CacheView c, 
     }
 }
 
-template <int kChunks>
+template <int kChunks, int kN>
 struct ShareShape {
-    using S = AttendShape<kChunks>;
+    using S = AttendShape<kChunks, kN>;
     static constexpr uint32_t kTokens = kChunks <= 8 ? 64 : 32;          // of a tile
+    static constexpr uint32_t kBringers = 2 * kTokens / 32;              // warps that bring a tile: a lane per token and side
     static constexpr uint32_t kSide = kTokens * S::kPitch;
-    static constexpr uint32_t kStage = 2 * kSide + kTokens;              // keys, values, which tokens count
+    static constexpr uint32_t kStage = 2 * kSide + 16;                   // keys, values, which tokens count (a bit each), a barrier
     // Few heads leave warps idle: those take a share of a tile's tokens, and a unit's results are joined through `merge`.
     static constexpr uint32_t kSplits = kChunks <= 8 ? 4 : 1;
-    static constexpr uint32_t kMerge = kChunks <= 8 ? 96 * (S::kDim + 2) * 4 : 0;
+    static constexpr uint32_t kMerge = kChunks <= 8 ? 6 * S::kHeads * (S::kDim + 2) * 4 : 0;          // 2 x 3 or 4 x 1 or 1 x 3 warps' heads
     static constexpr uint32_t kQuery = S::kQueryInRegisters ? 0 : kShareHeads * S::kPitch;
     static constexpr uint32_t kFits = (220 * 1024 - kMerge - kQuery) / kStage;
     static constexpr uint32_t kStages = kFits < 6 ? kFits : 6;
@@ -674,12 +691,10 @@ struct ShareCut {
     uint32_t group, unit, tiles, valid;
 };
 
-template <typename T, int kChunks>
+template <typename T, int kChunks, int kN>
 __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, AttendArgs a) {
-    using S = AttendShape<kChunks>;
-    using H = ShareShape<kChunks>;
-    constexpr uint32_t kPer = S::kDim / 8, kCopies = H::kTokens * kPer / kShareThreads;
-    static_assert(H::kTokens * kPer % kShareThreads == 0, "copies of a tile are the same for all threads");
+    using S = AttendShape<kChunks, kN>;
+    using H = ShareShape<kChunks, kN>;
     extern __shared__ __align__(16) uint8_t memory[];
     __shared__ unsigned long long sums[kShareThreads];
     __shared__ uint32_t last;
@@ -700,11 +715,18 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
     if (blockIdx.x >= line.warps) return;
     const unsigned long long begin = line.begin(blockIdx.x), end = line.begin(blockIdx.x + 1);
 
-    const uint32_t ring = shared_address(memory);
+    // stages (keys and values), then {tokens that count, barrier} per stage
+    const uint32_t ring = smem_u32(memory), bars = ring + H::kStages * 2 * H::kSide + 8;
+    uint32_t *const counts = reinterpret_cast<uint32_t *>(memory + H::kStages * 2 * H::kSide);
     float *const merge = reinterpret_cast<float *>(memory + H::kStages * H::kStage);
     const uint32_t query = ring + H::kStages * H::kStage + H::kMerge + warp * (H::kQuery / 8);
     if (a.dim != S::kDim)                                     // columns that no copy writes
-        for (uint32_t i = threadIdx.x; i < H::kStages * H::kStage / 16; i += kShareThreads) reinterpret_cast<uint4 *>(memory)[i] = make_uint4(0u, 0u, 0u, 0u);
+        for (uint32_t i = threadIdx.x; i < H::kStages * 2 * H::kSide / 16; i += kShareThreads) reinterpret_cast<uint4 *>(memory)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (threadIdx.x == 0) {
+        for (uint32_t i = 0; i < H::kStages; ++i) mbar_init(bars + i * 16, H::kBringers);
+        fence_mbar_init();
+    }
+    fence_proxy_async();
     __syncthreads();
 
     Walk load;
@@ -723,56 +745,54 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
         load.tile = (int32_t)(begin - before - (unsigned long long)load.unit * (load.tiles + 1)) - 1;
     }
     Walk use = load;
-    int32_t ids[kCopies];                                     // pages of the tokens this thread copies next
-    bool more;
+    bool more = true;
+    int32_t id = -1;                                          // page of the token this thread copies next
+    const uint32_t token = threadIdx.x % H::kTokens, side = threadIdx.x / H::kTokens;          // side 0: keys, 1: values, above: none
     auto look = [&]() {
         more = load.here(end);
-        if (!more) return;
-#pragma unroll
-        for (uint32_t k = 0; k < kCopies; ++k) {
-            const int32_t j = load.tile * (int32_t)H::kTokens + (int32_t)((threadIdx.x + k * kShareThreads) / kPer);
-            ids[k] = j < load.tokens ? c.table[(size_t)load.seq * c.max_pages + fast_div((uint32_t)j, c.by_page)] : -1;
-        }
+        const int32_t j = load.tile * (int32_t)H::kTokens + (int32_t)token;
+        id = more && side < 2 && j < load.tokens ? c.table[(size_t)load.seq * c.max_pages + fast_div((uint32_t)j, c.by_page)] : -1;
     };
     auto bring = [&](uint32_t to) {
-        if (more) {
-            const uint32_t stage = ring + to * H::kStage, kv = load.unit % a.kv_heads;
-            const T *keys = static_cast<const T *>(a.keys) + kv * a.head, *values = static_cast<const T *>(a.values) + kv * a.head;
-            uint8_t *const counts = memory + to * H::kStage + 2 * H::kSide;
-#pragma unroll
-            for (uint32_t k = 0; k < kCopies; ++k) {
-                const uint32_t i = threadIdx.x + k * kShareThreads, r = i / kPer, v = i - r * kPer;
-                const int32_t j = load.tile * (int32_t)H::kTokens + (int32_t)r;
-                const bool on = (uint32_t)ids[k] < c.n_pages;
-                if (v == 0) {
-                    counts[r] = on;
-                    if (!on && j < load.tokens && load.unit == 0) cache_flag(c, TD_ERR_OOB_INDEX);
-                }
-                if (v * 8 < a.dim) {
-                    const int64_t at = on ? ids[k] * a.page + (j - (int64_t)fast_div((uint32_t)j, c.by_page) * c.page_size) * a.token + v * 8 : 0;
-                    copy_async_or_zero(stage + r * S::kPitch + v * 16, keys + at, on ? 16u : 0u);
-                    copy_async_or_zero(stage + H::kSide + r * S::kPitch + v * 16, values + at, on ? 16u : 0u);
-                }
+        if (warp < H::kBringers) {
+            const int32_t j = load.tile * (int32_t)H::kTokens + (int32_t)token;
+            const uint32_t at = ring + (to * 2 + side) * H::kSide + token * S::kPitch, bar = bars + to * 16;
+            const bool on = (uint32_t)id < c.n_pages;
+            const uint32_t which = __ballot_sync(kFullMask, on);
+            if (lane == 0) {
+                mbar_expect_tx(bar, __popc(which) * a.dim * 2);
+                if (side == 0) counts[to * 4 + warp] = which;
             }
-            load.step(a, units, H::kTokens);
-            look();
+            if (on) {
+                const int64_t from = id * a.page + (j - (int64_t)fast_div((uint32_t)j, c.by_page) * c.page_size) * a.token + (load.unit % a.kv_heads) * a.head;
+                bulk_global_to_shared(at, static_cast<const T *>(side ? a.values : a.keys) + from, a.dim * 2, bar);
+            } else {
+                for (uint32_t i = 0; i < S::kDim / 8; ++i) store_shared(at + i * 16, make_uint4(0u, 0u, 0u, 0u));
+                fence_proxy_async();
+                if (j < load.tokens && load.unit == 0 && side == 0) cache_flag(c, TD_ERR_OOB_INDEX);
+            }
         }
-        copy_commit();
+        load.step(a, units, H::kTokens);
+        look();
     };
+    uint32_t stage = 0, put = 0, parity = 0, m_count = 0, m_tile = 0, split = 0, splits = 1, wide = 1;
+    uint32_t flying = 0;                                      // tiles brought and not yet used
     look();
-#pragma unroll 1
-    for (uint32_t i = 0; i + 1 < H::kStages; ++i) bring(i);
-
-    Fold<T, kChunks> f;
+    for (; more && put + 1 < H::kStages; ++put, ++flying) bring(put);
+    Fold<T, kChunks, kN> f;
     ShareCut cut_in{}, cut_out{};
-    uint32_t stage = 0, put = H::kStages - 1, m_count = 0, m_tile = 0, split = 0, splits = 1, wide = 1;
     bool active = false, head_whole = false;
 #pragma unroll 1
     while (use.here(end)) {
-        copy_wait<H::kStages - 2>();
-        __syncthreads();                                      // the tile is here, and the stage of the last turn is free
-        bring(put);
-        put = put + 1 == H::kStages ? 0 : put + 1;
+        const bool landed = wait_copy(bars + stage * 16, parity);
+        if (!landed && lane == 0) cache_flag(c, TD_ERR_COPY_TIMEOUT);
+        if (__syncthreads_or(!landed)) break;                 // never seen: the rest is left; and the stage of the last turn is free
+        if (more) {
+            bring(put);
+            ++flying;
+            put = put + 1 == H::kStages ? 0 : put + 1;
+        }
+        --flying;
         const uint32_t m_block = use.unit / a.kv_heads, kv = use.unit - m_block * a.kv_heads, m_first = m_block * a.m_rows;
         // The row and head of the block's row i (ratio rows of heads per row of the group), or false.
         auto at_row = [&](uint32_t i, uint32_t &row, uint32_t &head) {
@@ -784,7 +804,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
         if (use.tile == 0 || use.place == begin) {            // a unit begins here
             head_whole = use.tile == 0;
             m_count = min(a.m_rows, a.group * a.ratio - m_first);
-            const uint32_t m_tiles = (m_count + kHeadRows - 1) / kHeadRows;
+            const uint32_t m_tiles = (m_count + S::kHeads - 1) / S::kHeads;
             wide = m_tiles <= 1 ? 1 : m_tiles <= 2 ? 2 : m_tiles <= 4 ? 4 : 8;
             splits = min(H::kSplits, 8 / wide);
             m_tile = warp & (wide - 1);
@@ -794,59 +814,62 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
                 f.begin();
                 f.query(static_cast<const T *>(a.q), query, a.dim, [&](uint32_t h) {
                     uint32_t row, head;
-                    return at_row(m_tile * kHeadRows + h, row, head) ? row * a.q_row + head * a.q_head : (int64_t)-1;
+                    return at_row(m_tile * S::kHeads + h, row, head) ? row * a.q_row + head * a.q_head : (int64_t)-1;
                 });
             }
         }
         if (active) {
-            const uint32_t at = ring + stage * H::kStage;
-            const uint8_t *const on = memory + stage * H::kStage + 2 * H::kSide;
+            const uint32_t at = ring + stage * 2 * H::kSide;
 #pragma unroll 1
             for (uint32_t sub = split; sub < H::kTokens / 16; sub += splits) {
-                const uint32_t counts = __ballot_sync(kFullMask, on[sub * 16 + (lane & 15u)] != 0) & 0xffffu;
-                if (counts) f.add(at + sub * 16 * S::kPitch, at + H::kSide + sub * 16 * S::kPitch, query, counts, a.scale2);
+                const uint32_t which = counts[stage * 4 + sub / 2] >> (sub & 1u) * 16 & 0xffffu;
+                if (which) f.add(at + sub * 16 * S::kPitch, at + H::kSide + sub * 16 * S::kPitch, query, which, a.scale2);
             }
         }
-        stage = stage + 1 == H::kStages ? 0 : stage + 1;
+        if (++stage == H::kStages) {
+            stage = 0;
+            parity ^= 1u;
+        }
         const bool final = use.tile + 1 == (int32_t)use.tiles;
         if (final || use.place + 1 == end) {                  // the unit, or this block's part of it, ends here
-            const uint32_t g = lane >> 2;
+            const uint32_t t = lane & 3u;
             if (active) f.end();
+            auto merged = [&](uint32_t k, int n, int i) { return merge + (size_t)(((k - 1) * wide + m_tile) * S::kHeads + n * 8 + t * 2 + i) * (S::kDim + 2); };
             if (splits > 1) {
                 if (active && split > 0) {
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        float *to = merge + (size_t)(((split - 1) * wide + m_tile) * kHeadRows + g + r * 8) * (S::kDim + 2);
-                        f.store(to, to + S::kDim, r);
-                    }
+                    for (int n = 0; n < kN; ++n)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) f.store(merged(split, n, i), merged(split, n, i) + S::kDim, n, i);
                 }
                 __syncthreads();
                 if (active && split == 0) {
 #pragma unroll 1
                     for (uint32_t k = 1; k < splits; ++k) {
 #pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            const float *from = merge + (size_t)(((k - 1) * wide + m_tile) * kHeadRows + g + r * 8) * (S::kDim + 2);
-                            f.join(from, from + S::kDim, r);
-                        }
+                        for (int n = 0; n < kN; ++n)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) f.join(merged(k, n, i), merged(k, n, i) + S::kDim, n, i);
                     }
                 }
             }
             const bool whole = head_whole && final;
             if (active && split == 0) {
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const uint32_t i = m_tile * kHeadRows + g + r * 8;
-                    uint32_t row, head;
-                    if (!at_row(i, row, head)) continue;
-                    if (whole) {
-                        float *to = a.common + ((size_t)row * a.n_heads + head) * (S::kDim + 2);
-                        f.store(to, to + S::kDim, r);
-                    } else {
-                        float *to = a.share_parts + ((size_t)2 * blockIdx.x + (head_whole ? 1 : 0)) * H::kPartFloats;
-                        f.store(to + i * S::kDim, to + kShareHeads * S::kDim + 2 * i, r);
+                for (int n = 0; n < kN; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t r = m_tile * S::kHeads + n * 8 + t * 2 + i;
+                        uint32_t row, head;
+                        if (!at_row(r, row, head)) continue;
+                        if (whole) {
+                            float *to = a.common + ((size_t)row * a.n_heads + head) * (S::kDim + 2);
+                            f.store(to, to + S::kDim, n, i);
+                        } else {
+                            float *to = a.share_parts + ((size_t)2 * blockIdx.x + (head_whole ? 1 : 0)) * H::kPartFloats;
+                            f.store(to + r * S::kDim, to + kShareHeads * S::kDim + 2 * r, n, i);
+                        }
                     }
-                }
             }
             if (!whole) {
                 const ShareCut cut{use.place - (uint32_t)use.tile - 1, use.group, use.unit, use.tiles, 1u};
@@ -855,7 +878,8 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
         }
         use.step(a, units, H::kTokens);
     }
-    copy_wait<0>();
+    if (use.place < end)                                      // after a wait that ran out: for what is still on its way, again with a limit
+        for (uint32_t i = 0; i < flying; ++i) wait_copy(bars + (stage + i) % H::kStages * 16, parity ^ (stage + i >= H::kStages ? 1u : 0u));
 #pragma unroll 1
     for (uint32_t side = 0; side < 2; ++side) {
         const ShareCut u = side == 0 ? cut_in : cut_out;

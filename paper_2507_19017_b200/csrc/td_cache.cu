@@ -152,9 +152,9 @@ cudaError_t run_write(const CacheView &v, const PoolView &p, WriteArgs k, cudaSt
 // ---- attention ----
 constexpr uint32_t kBlocks = 148;                             // one per SM
 template <int kChunks>
-constexpr size_t part_bytes() { return (size_t)(2 * AttendShape<kChunks>::kWarps + 2) * kBlocks * AttendShape<kChunks>::kPartFloats * 4; }
+constexpr size_t part_bytes() { return (size_t)(2 * AttendShape<kChunks, 2>::kWarps + 2) * kBlocks * AttendShape<kChunks, 2>::kPartFloats * 4; }
 template <int kChunks>
-constexpr size_t share_bytes() { return (size_t)2 * kBlocks * ShareShape<kChunks>::kPartFloats * 4; }
+constexpr size_t share_bytes() { return (size_t)2 * kBlocks * ShareShape<kChunks, 2>::kPartFloats * 4; }
 struct AttendLayout {
     size_t arrived, share_arrived, shared, common, parts, share_parts, total;
 };
@@ -177,19 +177,23 @@ AttendLayout attend_layout(uint32_t n_rows, uint32_t n_heads, uint32_t dim) {   
     L.total = p;
     return L;
 }
+template <typename T, int kChunks, int kN>
+cudaError_t run_attend(const CacheView &v, AttendArgs k, cudaStream_t st) {
+    using S = AttendShape<kChunks, kN>;
+    k.units = k.kv_heads * ((k.ratio + S::kHeads - 1) / S::kHeads);
+    cudaError_t rc = cudaFuncSetAttribute(attend_kernel<T, kChunks, kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes);
+    if (rc == cudaSuccess && k.group > 1) {
+        using H = ShareShape<kChunks, 2>;
+        rc = cudaFuncSetAttribute(share_kernel<T, kChunks, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)H::kBytes);
+        if (rc == cudaSuccess) rc = launch(share_plan_kernel, k.n_groups, kShareThreads, st, 1u, v, k);
+        if (rc == cudaSuccess) rc = launch_smem(share_kernel<T, kChunks, 2>, kBlocks, kShareThreads, H::kBytes, st, 1u, v, k);
+    }
+    if (rc == cudaSuccess) rc = launch_smem(attend_kernel<T, kChunks, kN>, kBlocks, S::kThreads, S::kBytes, st, 1u, v, k);
+    return rc;
+}
 template <typename T, int kChunks>
 cudaError_t run_attend(const CacheView &v, const AttendArgs &k, cudaStream_t st) {
-    using S = AttendShape<kChunks>;
-    const cudaError_t rc = cudaFuncSetAttribute(attend_kernel<T, kChunks>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes);
-    if (rc != cudaSuccess) return rc;
-    if (k.group > 1) {
-        using H = ShareShape<kChunks>;
-        cudaError_t rs = cudaFuncSetAttribute(share_kernel<T, kChunks>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)H::kBytes);
-        if (rs == cudaSuccess) rs = launch(share_plan_kernel, k.n_groups, kShareThreads, st, 1u, v, k);
-        if (rs == cudaSuccess) rs = launch_smem(share_kernel<T, kChunks>, kBlocks, kShareThreads, H::kBytes, st, 1u, v, k);
-        if (rs != cudaSuccess) return rs;
-    }
-    return launch_smem(attend_kernel<T, kChunks>, kBlocks, S::kThreads, S::kBytes, st, 1u, v, k);
+    return k.ratio <= 8 ? run_attend<T, kChunks, 1>(v, k, st) : run_attend<T, kChunks, 2>(v, k, st);
 }
 template <typename T>
 cudaError_t run_attend(const CacheView &v, const AttendArgs &k, cudaStream_t st) {
@@ -351,7 +355,6 @@ int td_cache_attention(const td_cache_attention_args *a, void *stream) {
     k.ratio = a->n_heads / c->n_heads;
     k.dim = c->dim;
     k.window = a->window;
-    k.units = k.kv_heads * ((k.ratio + kHeadRows - 1) / kHeadRows);
     k.scale = a->scale;
     k.scale2 = (float)(1.4426950408889634 * (double)a->scale);
     // rows that share, and their heads over one key head in blocks of like size

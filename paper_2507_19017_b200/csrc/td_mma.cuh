@@ -7,13 +7,6 @@
 
 namespace td {
 
-__device__ __forceinline__ uint32_t shared_address(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-// 16 bytes from global to shared memory, asynchronously; bytes = 0: zeros, and the source is not read.
-__device__ __forceinline__ void copy_async_or_zero(uint32_t to, const void *from, uint32_t bytes) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
-}
-
 __device__ __forceinline__ void store_shared(uint32_t to, const uint4 &v) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -25,6 +18,13 @@ __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
 }
 __device__ __forceinline__ void load_matrices_transposed(uint32_t (&r)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+
+// An 8 x 8 matrix of 16-bit elements in the same layout, transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
 }
 
 // c (16 x 8, float) += a (16 x 16) b (16 x 8).  Lane 4 g + t holds of c rows g (c[0], c[1]) and g + 8 (c[2], c[3]), columns 2t and
