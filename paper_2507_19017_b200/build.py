@@ -10,7 +10,7 @@ _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libtd.so")
 SOURCES = ["td.cu", "td_ops.cu", "td_cache.cu"]
-HEADERS = ["td_common.cuh", "td_async.cuh", "td_device.cuh", "td_alloc.cuh", "td_put.cuh", "td_get.cuh", 
+HEADERS = ["td_common.cuh", "td_device.cuh", "td_alloc.cuh", "td_put.cuh", "td_get.cuh", 
            "td_range.h", "td_host.cuh", "td_ops.cuh", "td_logprob.cuh", "td_policy.cuh", "td_embed.cuh",
            "td_cache.cuh", "td_mma.cuh", "td_attend.cuh"]
 

@@ -6,12 +6,11 @@
 // waste nothing; a transposition of 8 x 8 matrices turns the one's output into the other's input.  All units'
 // tiles, one unit after the other, are a line that is cut into equal pieces, a piece per warp, wherever the cuts
 // fall: so one long sequence and a thousand short ones load the machine alike.  A warp has its tiles brought by its own ring of
-// bulk copies (one per token and side), several tiles ahead and across units; no warp waits for another.  Units that a cut
+// asynchronous copies, several tiles ahead and across units; no warp waits for another.  Units that a cut
 // went through leave parts (reference, sum, weighted values), joined in the order of the tokens: within a block after its
 // warps are done, between blocks by the last block to arrive.  The same call gives the same bits.
 #pragma once
 
-#include "td_async.cuh"
 #include "td_cache.cuh"
 #include "td_mma.cuh"
 
@@ -41,7 +40,6 @@ struct AttendArgs {
 
 constexpr uint32_t kTile = 16;                                // tokens of a tile
 constexpr float kSlack = 8.0f;                                // how far (log2) a score may pass the reference before that moves
-constexpr uint32_t kBarBytes = 8;
 constexpr uint32_t kLeastTiles = 4;                           // of a warp, before another block is used
 
 // Shapes of a kernel for heads of up to 16 * kChunks elements, 8 * kN of them side by side.
@@ -56,20 +54,12 @@ struct AttendShape {
     static constexpr bool kQueryInRegisters = kChunks * kN <= 16;
     static constexpr uint32_t kQuery = kQueryInRegisters ? 0 : kHeads * kPitch;
     static constexpr uint32_t kRoom = 216 * 1024 / kWarps;    // bytes a warp may have
-    static constexpr uint32_t kFits = (kRoom - kQuery) / (kStage + 16 + kBarBytes);
+    static constexpr uint32_t kFits = (kRoom - kQuery) / (kStage + 16);
     static constexpr uint32_t kStages = kFits < 6 ? kFits : 6;
-    static constexpr uint32_t kWarpBytes = (kStages * (kStage + 16 + kBarBytes) + kQuery + 15) / 16 * 16;
+    static constexpr uint32_t kWarpBytes = kStages * (kStage + 16) + kQuery;
     static constexpr uint32_t kBytes = kWarps * kWarpBytes;
     static constexpr uint32_t kPartFloats = kHeads * (kDim + 2);         // weighted values [kHeads][kDim], then {reference, sum} [kHeads]
 };
-
-// A warp's wait for a copy into one of its stages, bounded; false: it did not land in time.
-__device__ __forceinline__ bool wait_copy(uint32_t bar, uint32_t parity) {
-    constexpr uint32_t kPolls = 1u << 16;
-    for (uint32_t i = 0; i < kPolls; ++i)
-        if (mbar_try_wait(bar, parity)) return true;
-    return false;
-}
 
 struct Span {                                                 // the tokens [lo, n) of sequence s
     int32_t s, lo, n;
@@ -387,16 +377,10 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
     const unsigned long long begin = line.begin(min(w_global, line.warps)), end = line.begin(min(w_global + 1, line.warps));
 
     uint8_t *const mem = memory + warp * S::kWarpBytes;
-    const uint32_t ring = smem_u32(mem), query = ring + S::kStages * S::kStage;
+    const uint32_t ring = shared_address(mem), query = ring + S::kStages * S::kStage;
     uint4 *const notes = reinterpret_cast<uint4 *>(mem + S::kStages * S::kStage + S::kQuery);          // per stage: row, unit, tokens that count and flags and heads, first head
-    const uint32_t bars = query + S::kQuery + S::kStages * 16;
     if (a.dim != S::kDim)                                     // columns that no copy writes
         for (uint32_t i = lane; i < S::kStages * S::kStage / 16; i += 32) reinterpret_cast<uint4 *>(mem)[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (lane == 0) {
-        for (uint32_t i = 0; i < S::kStages; ++i) mbar_init(bars + i * kBarBytes, 1);
-        fence_mbar_init();
-    }
-    fence_proxy_async();
     __syncwarp();
 
     if (begin < end) {
@@ -434,8 +418,8 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
             enter();
         };
         enter();
-        // To the next tile; an empty unit's result is written on the way.  Then lanes 0 .. 15 and 16 .. 31 fetch the numbers of its
-        // tokens' pages, which the next call of bring() needs.
+        // To the next tile; an empty unit's result is written on the way.  Then lanes 0 .. 15 fetch the numbers of its
+        // tokens' pages (16 .. 31 the same), which the next call of bring() needs.
         bool more = true;
         int32_t id = -1;
         auto look = [&]() {
@@ -452,15 +436,33 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
             const int32_t j = span.lo + tile * (int32_t)kTile + (int32_t)(lane & 15u);
             id = more && j < span.n ? c.table[(size_t)span.s * c.max_pages + fast_div((uint32_t)j, c.by_page)] : -1;
         };
-        // Brings the tile into stage `to`: a lane per token and side.
+        // Brings the tile into stage `to`.
+        const int64_t apart = static_cast<const T *>(a.values) - static_cast<const T *>(a.keys);
         auto bring = [&](uint32_t to) {
             const int32_t j = span.lo + tile * (int32_t)kTile + (int32_t)(lane & 15u);
             const bool on = (uint32_t)id < c.n_pages;
-            const uint32_t counts = __ballot_sync(kFullMask, on) & 0xffffu, bar = bars + to * kBarBytes;
-            const uint32_t at = ring + to * S::kStage + (lane >> 4) * S::kSide + (lane & 15u) * S::kPitch;
+            const uint32_t counts = __ballot_sync(kFullMask, on) & 0xffffu;
+            const int64_t from = on ? id * a.page + (j - (int64_t)fast_div((uint32_t)j, c.by_page) * c.page_size) * a.token : 0;
+            const T *keys = static_cast<const T *>(a.keys) + kv * a.head;
+            const uint32_t at = ring + to * S::kStage;
+            constexpr uint32_t kPer = S::kDim / 8;            // vectors of a row
+#pragma unroll
+            for (uint32_t i0 = 0; i0 < kTile * kPer; i0 += 32) {
+                const uint32_t i = i0 + lane, r = i / kPer, v = i - r * kPer, o = r * S::kPitch + v * 16;
+                const T *k = keys + __shfl_sync(kFullMask, from, r) + v * 8;
+                if (kPer * 8 != a.dim && v * 8 >= a.dim) continue;
+                if (counts == 0xffffu) {
+                    copy_vector(at + o, k);
+                    copy_vector(at + S::kSide + o, k + apart);
+                } else {                                      // behind the end, or not a page: zeros, so that nothing there is used
+                    const uint32_t bytes = counts >> r & 1u ? 16u : 0u;
+                    copy_vector_or_zero(at + o, k, bytes);
+                    copy_vector_or_zero(at + S::kSide + o, k + apart, bytes);
+                }
+            }
+            if (!on && j < span.n && unit == 0 && lane < 16) cache_flag(c, TD_ERR_OOB_INDEX);
             const bool fresh = tile == 0 || place == begin, final = tile + 1 == (int32_t)tiles, over = final || place + 1 == end;
             if (lane == 0) {
-                mbar_expect_tx(bar, __popc(counts) * a.dim * 4);
                 notes[to] = make_uint4(row, unit, counts | (fresh ? 1u << 16 : 0u) | (over ? 1u << 17 : 0u) | (tile == 0 ? 1u << 18 : 0u) |
                                        (final ? 1u << 19 : 0u) | heads << 20, first);
                 if (over) {                                   // a cut unit, for the joins: noted before the block's barrier
@@ -469,43 +471,35 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
                     else if (!final) cut_out[warp] = cut;
                 }
             }
-            if (on) {
-                const int64_t from = id * a.page + (j - (int64_t)fast_div((uint32_t)j, c.by_page) * c.page_size) * a.token + kv * a.head;
-                bulk_global_to_shared(at, static_cast<const T *>(lane < 16 ? a.keys : a.values) + from, a.dim * 2, bar);
-            } else {                                          // behind the end, or not a page: zeros, so that nothing there is used
-                for (uint32_t i = 0; i < S::kDim / 8; ++i) store_shared(at + i * 16, make_uint4(0u, 0u, 0u, 0u));
-                fence_proxy_async();
-                if (j < span.n && unit == 0 && lane < 16) cache_flag(c, TD_ERR_OOB_INDEX);
-            }
             ++place;
             if (++tile == (int32_t)tiles) leave();
             look();
         };
 
-        uint32_t brought = 0, put = 0, stage = 0, parity = 0, done = 0;          // tiles brought; stages of the next to bring and to use
+        uint32_t brought = 0, put = S::kStages - 1, stage = 0;          // tiles brought; stages of the next to bring and to use
         look();
-        for (; more && brought + 1 < S::kStages; ++brought) bring(put++);
+        for (uint32_t i = 0; i + 1 < S::kStages; ++i) {
+            if (more) {
+                bring(i);
+                ++brought;
+            }
+            copy_commit();
+        }
         Fold<T, kChunks, kN> f;
         bool head_whole = false;
 #pragma unroll 1
-        for (; done < brought; ++done) {
-            // never seen to run out; the rest is then left, what is on its way still waited for
-            if (!wait_copy(bars + stage * kBarBytes, parity)) {
-                if (lane == 0) cache_flag(c, TD_ERR_COPY_TIMEOUT);
-                more = false;
-            }
+        for (uint32_t done = 0; done < brought; ++done) {
+            copy_wait<S::kStages - 2>();
             __syncwarp();
             if (more) {                                       // into the stage that the last turn was done with
                 bring(put);
                 ++brought;
-                put = put + 1 == S::kStages ? 0 : put + 1;
             }
+            copy_commit();
+            put = put + 1 == S::kStages ? 0 : put + 1;
             const uint4 note = notes[stage];
             const uint32_t at = ring + stage * S::kStage;
-            if (++stage == S::kStages) {
-                stage = 0;
-                parity ^= 1u;
-            }
+            stage = stage + 1 == S::kStages ? 0 : stage + 1;
             const uint32_t first = note.w, heads = note.z >> 20, t = lane & 3u;
             if (note.z >> 16 & 1u) {                          // a unit begins here
                 head_whole = note.z >> 18 & 1u;
@@ -535,6 +529,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
             }
         }
     }
+    copy_wait<0>();
     __syncthreads();
 
     // ---- units that cuts went through ----
@@ -644,9 +639,8 @@ template <int kChunks, int kN>
 struct ShareShape {
     using S = AttendShape<kChunks, kN>;
     static constexpr uint32_t kTokens = kChunks <= 8 ? 64 : 32;          // of a tile
-    static constexpr uint32_t kBringers = 2 * kTokens / 32;              // warps that bring a tile: a lane per token and side
     static constexpr uint32_t kSide = kTokens * S::kPitch;
-    static constexpr uint32_t kStage = 2 * kSide + 16;                   // keys, values, which tokens count (a bit each), a barrier
+    static constexpr uint32_t kStage = 2 * kSide + 16;                   // keys, values, which tokens count (a bit each)
     // Few heads leave warps idle: those take a share of a tile's tokens, and a unit's results are joined through `merge`.
     static constexpr uint32_t kSplits = kChunks <= 8 ? 4 : 1;
     static constexpr uint32_t kMerge = kChunks <= 8 ? 6 * S::kHeads * (S::kDim + 2) * 4 : 0;          // 2 x 3 or 4 x 1 or 1 x 3 warps' heads
@@ -715,18 +709,13 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
     if (blockIdx.x >= line.warps) return;
     const unsigned long long begin = line.begin(blockIdx.x), end = line.begin(blockIdx.x + 1);
 
-    // stages (keys and values), then {tokens that count, barrier} per stage
-    const uint32_t ring = smem_u32(memory), bars = ring + H::kStages * 2 * H::kSide + 8;
+    // stages (keys and values), then the tokens that count of each
+    const uint32_t ring = shared_address(memory);
     uint32_t *const counts = reinterpret_cast<uint32_t *>(memory + H::kStages * 2 * H::kSide);
     float *const merge = reinterpret_cast<float *>(memory + H::kStages * H::kStage);
     const uint32_t query = ring + H::kStages * H::kStage + H::kMerge + warp * (H::kQuery / 8);
     if (a.dim != S::kDim)                                     // columns that no copy writes
         for (uint32_t i = threadIdx.x; i < H::kStages * 2 * H::kSide / 16; i += kShareThreads) reinterpret_cast<uint4 *>(memory)[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < H::kStages; ++i) mbar_init(bars + i * 16, H::kBringers);
-        fence_mbar_init();
-    }
-    fence_proxy_async();
     __syncthreads();
 
     Walk load;
@@ -745,54 +734,61 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
         load.tile = (int32_t)(begin - before - (unsigned long long)load.unit * (load.tiles + 1)) - 1;
     }
     Walk use = load;
+    constexpr uint32_t kPer = S::kDim / 8, kCopies = H::kTokens * kPer / kShareThreads;          // vectors of a row, and of a thread
+    static_assert(H::kTokens * kPer % kShareThreads == 0, "a tile is the same work for all threads");
     bool more = true;
-    int32_t id = -1;                                          // page of the token this thread copies next
-    const uint32_t token = threadIdx.x % H::kTokens, side = threadIdx.x / H::kTokens;          // side 0: keys, 1: values, above: none
+    int32_t ids[kCopies];                                     // pages of the tokens this thread copies next
+    int32_t id = -1;                                          // page of token `threadIdx.x`
+    const int64_t apart = static_cast<const T *>(a.values) - static_cast<const T *>(a.keys);
     auto look = [&]() {
         more = load.here(end);
-        const int32_t j = load.tile * (int32_t)H::kTokens + (int32_t)token;
-        id = more && side < 2 && j < load.tokens ? c.table[(size_t)load.seq * c.max_pages + fast_div((uint32_t)j, c.by_page)] : -1;
+        if (!more) return;
+        const int32_t *row = c.table + (size_t)load.seq * c.max_pages;
+        const int32_t j0 = load.tile * (int32_t)H::kTokens, j = j0 + (int32_t)threadIdx.x;
+        id = threadIdx.x < H::kTokens && j < load.tokens ? row[fast_div((uint32_t)j, c.by_page)] : -1;
+#pragma unroll
+        for (uint32_t k = 0; k < kCopies; ++k) {
+            const int32_t jk = j0 + (int32_t)((threadIdx.x + k * kShareThreads) / kPer);
+            ids[k] = jk < load.tokens ? row[fast_div((uint32_t)jk, c.by_page)] : -1;
+        }
     };
     auto bring = [&](uint32_t to) {
-        if (warp < H::kBringers) {
-            const int32_t j = load.tile * (int32_t)H::kTokens + (int32_t)token;
-            const uint32_t at = ring + (to * 2 + side) * H::kSide + token * S::kPitch, bar = bars + to * 16;
-            const bool on = (uint32_t)id < c.n_pages;
-            const uint32_t which = __ballot_sync(kFullMask, on);
-            if (lane == 0) {
-                mbar_expect_tx(bar, __popc(which) * a.dim * 2);
-                if (side == 0) counts[to * 4 + warp] = which;
-            }
-            if (on) {
-                const int64_t from = id * a.page + (j - (int64_t)fast_div((uint32_t)j, c.by_page) * c.page_size) * a.token + (load.unit % a.kv_heads) * a.head;
-                bulk_global_to_shared(at, static_cast<const T *>(side ? a.values : a.keys) + from, a.dim * 2, bar);
-            } else {
-                for (uint32_t i = 0; i < S::kDim / 8; ++i) store_shared(at + i * 16, make_uint4(0u, 0u, 0u, 0u));
-                fence_proxy_async();
-                if (j < load.tokens && load.unit == 0 && side == 0) cache_flag(c, TD_ERR_OOB_INDEX);
-            }
+        const int32_t j0 = load.tile * (int32_t)H::kTokens;
+        const T *keys = static_cast<const T *>(a.keys) + (load.unit % a.kv_heads) * a.head;
+        const uint32_t at = ring + to * 2 * H::kSide;
+#pragma unroll
+        for (uint32_t k = 0; k < kCopies; ++k) {
+            const uint32_t i = threadIdx.x + k * kShareThreads, r = i / kPer, v = i - r * kPer, o = r * S::kPitch + v * 16;
+            const uint32_t j = (uint32_t)j0 + r, bytes = (uint32_t)ids[k] < c.n_pages ? 16u : 0u;
+            const int64_t from = bytes ? ids[k] * a.page + (int64_t)(j - fast_div(j, c.by_page) * c.page_size) * a.token + v * 8 : 0;
+            if (kPer * 8 != a.dim && v * 8 >= a.dim) continue;
+            copy_vector_or_zero(at + o, keys + from, bytes);
+            copy_vector_or_zero(at + H::kSide + o, keys + from + apart, bytes);
+        }
+        if (threadIdx.x < H::kTokens) {
+            const uint32_t which = __ballot_sync(kFullMask, (uint32_t)id < c.n_pages);
+            if (lane == 0) counts[to * 4 + warp] = which;
+            if ((uint32_t)id >= c.n_pages && j0 + (int32_t)threadIdx.x < load.tokens && load.unit == 0) cache_flag(c, TD_ERR_OOB_INDEX);
         }
         load.step(a, units, H::kTokens);
         look();
     };
-    uint32_t stage = 0, put = 0, parity = 0, m_count = 0, m_tile = 0, split = 0, splits = 1, wide = 1;
-    uint32_t flying = 0;                                      // tiles brought and not yet used
+    uint32_t stage = 0, put = H::kStages - 1, m_count = 0, m_tile = 0, split = 0, splits = 1, wide = 1;
     look();
-    for (; more && put + 1 < H::kStages; ++put, ++flying) bring(put);
+    for (uint32_t i = 0; i + 1 < H::kStages; ++i) {
+        if (more) bring(i);
+        copy_commit();
+    }
     Fold<T, kChunks, kN> f;
     ShareCut cut_in{}, cut_out{};
     bool active = false, head_whole = false;
 #pragma unroll 1
     while (use.here(end)) {
-        const bool landed = wait_copy(bars + stage * 16, parity);
-        if (!landed && lane == 0) cache_flag(c, TD_ERR_COPY_TIMEOUT);
-        if (__syncthreads_or(!landed)) break;                 // never seen: the rest is left; and the stage of the last turn is free
-        if (more) {
-            bring(put);
-            ++flying;
-            put = put + 1 == H::kStages ? 0 : put + 1;
-        }
-        --flying;
+        copy_wait<H::kStages - 2>();
+        __syncthreads();                                      // the tile is here, and the stage of the last turn is free
+        if (more) bring(put);
+        copy_commit();
+        put = put + 1 == H::kStages ? 0 : put + 1;
         const uint32_t m_block = use.unit / a.kv_heads, kv = use.unit - m_block * a.kv_heads, m_first = m_block * a.m_rows;
         // The row and head of the block's row i (ratio rows of heads per row of the group), or false.
         auto at_row = [&](uint32_t i, uint32_t &row, uint32_t &head) {
@@ -826,10 +822,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
                 if (which) f.add(at + sub * 16 * S::kPitch, at + H::kSide + sub * 16 * S::kPitch, query, which, a.scale2);
             }
         }
-        if (++stage == H::kStages) {
-            stage = 0;
-            parity ^= 1u;
-        }
+        stage = stage + 1 == H::kStages ? 0 : stage + 1;
         const bool final = use.tile + 1 == (int32_t)use.tiles;
         if (final || use.place + 1 == end) {                  // the unit, or this block's part of it, ends here
             const uint32_t t = lane & 3u;
@@ -878,8 +871,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
         }
         use.step(a, units, H::kTokens);
     }
-    if (use.place < end)                                      // after a wait that ran out: for what is still on its way, again with a limit
-        for (uint32_t i = 0; i < flying; ++i) wait_copy(bars + (stage + i) % H::kStages * 16, parity ^ (stage + i >= H::kStages ? 1u : 0u));
+    copy_wait<0>();
 #pragma unroll 1
     for (uint32_t side = 0; side < 2; ++side) {
         const ShareCut u = side == 0 ? cut_in : cut_out;

@@ -5,7 +5,6 @@
 #include <stdint.h>
 
 #include "../../include/td.h"
-#include "td_async.cuh"
 #include "td_common.cuh"
 
 namespace td {
@@ -138,6 +137,7 @@ __device__ __forceinline__ uint4 lds_4x32(uint32_t a) {
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
     return v;
 }
+__device__ __forceinline__ uint32_t smem_u32(const void *p);
 __device__ __forceinline__ void warp_copy_from_shared(uint8_t *dst, uint32_t src, uint32_t n, uint32_t lane) {
     uint32_t head = (16u - (uint32_t)(reinterpret_cast<uintptr_t>(dst) & 15u)) & 15u;
     if (head > n) head = n;
@@ -336,6 +336,26 @@ constexpr uint32_t kPieceMax = kStageBytes - 16;      // payload of one bulk cop
 // stages and mbarriers of one warp; rounded so that every warp's stages start 128-byte aligned
 constexpr size_t kPipeSmemPerWarp = (((size_t)kStages * (kStageBytes + 8)) + 127) & ~size_t(127);
 static_assert(kStageBytes % 16 == 0 && kPipeSmemPerWarp % 128 == 0, "bulk copies need 16-byte aligned stages");
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ void bulk_global_to_shared(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void fence_mbar_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 
 struct WarpPipe {
     uint32_t stage;            // shared-window address of this warp's kStages * kStageBytes bytes
