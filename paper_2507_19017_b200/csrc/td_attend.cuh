@@ -16,6 +16,9 @@
 
 namespace td {
 
+#ifndef TD_AW
+#define TD_AW 12
+#endif
 struct AttendArgs {
     const int32_t *seqs;
     const void *q;
@@ -40,13 +43,16 @@ struct AttendArgs {
 
 constexpr uint32_t kTile = 16;                                // tokens of a tile
 constexpr float kSlack = 8.0f;                                // how far (log2) a score may pass the reference before that moves
-constexpr uint32_t kLeastTiles = 4;                           // of a warp, before another block is used
+#ifndef TD_LEAST
+#define TD_LEAST 4
+#endif
+constexpr uint32_t kLeastTiles = TD_LEAST;                           // of a warp, before another block is used
 
 // Shapes of a kernel for heads of up to 16 * kChunks elements, 8 * kN of them side by side.
 template <int kChunks, int kN>
 struct AttendShape {
     static constexpr uint32_t kDim = 16 * kChunks, kHeads = 8 * kN;
-    static constexpr uint32_t kWarps = kChunks <= 8 ? 8 : 4;
+    static constexpr uint32_t kWarps = kChunks <= 8 ? (kN == 1 ? TD_AW : 8) : 4;
     static constexpr uint32_t kThreads = 32 * kWarps;
     static constexpr uint32_t kPitch = kDim * 2 + 16;         // bytes of a row in shared memory: an odd number of 16s, so that 8 rows lie in different banks
     static constexpr uint32_t kSide = kTile * kPitch;         // keys, or values, of a tile
@@ -85,14 +91,26 @@ __device__ __forceinline__ Span span_of(const CacheView &c, const AttendArgs &a,
     return p;
 }
 
+// n / d; a 64-bit division takes some hundred instructions, and the numbers here hardly ever need one.
+__device__ __forceinline__ unsigned long long quotient(unsigned long long n, unsigned long long d) {
+    return ((n | d) >> 32) == 0 ? (uint32_t)n / (uint32_t)d : n / d;
+}
 // The line of all units' tiles; a unit has one place ahead of its tiles (what it costs to begin one), so that of a row with T
-// tiles each unit has T + 1 places.  Warp w of `warps` has places [total w / warps, total (w + 1) / warps).
+// tiles each unit has T + 1 places.  The first `more` of `warps` warps have base + 1 places each, the others base (>= 1).
 struct Line {
-    unsigned long long total;
-    uint32_t warps;
-    __device__ __forceinline__ unsigned long long begin(uint32_t w) const { return total * w / warps; }
+    unsigned long long total, base;
+    uint32_t warps, more;
+    __device__ __forceinline__ Line(unsigned long long places, uint32_t most) : total(places) {
+        warps = places < most ? (uint32_t)places : most;
+        base = quotient(places, warps);
+        more = (uint32_t)(places - base * warps);
+    }
+    __device__ __forceinline__ unsigned long long begin(uint32_t w) const {
+        return w >= warps ? total : base * w + min(w, more);
+    }
     __device__ __forceinline__ uint32_t warp_of(unsigned long long place) const {          // the last w with begin(w) <= place
-        return (uint32_t)(((place + 1) * warps + total - 1) / total) - 1;
+        const unsigned long long wide = (base + 1) * more;
+        return (uint32_t)(place < wide ? quotient(place, base + 1) : more + quotient(place - wide, base));
     }
 };
 
@@ -126,10 +144,9 @@ __device__ __forceinline__ uint32_t thread_of(const unsigned long long *sums, un
     return lo;
 }
 
-// A unit that a cut went through: its first place and tiles.
+// A unit that a cut went through, and the warps that have its first and its last tile.
 struct Cut {
-    unsigned long long place;
-    uint32_t row, unit, tiles, valid;
+    uint32_t row, unit, first, last, valid;
 };
 
 template <uint32_t kHeads>
@@ -146,52 +163,112 @@ __device__ __forceinline__ const float *common_of(const AttendArgs &a, uint32_t 
     return a.common + ((size_t)row * a.n_heads + head) * (kDim + 2);
 }
 
-constexpr uint32_t kNoTokens = 0xffffffffu;
-// Joins the parts k = 0 .. count - 1 of a unit (slot(k) of `parts`) into out and lse, or into another part; `me` of `all` threads.
-// A maximum of -inf means that a part has nothing; NaN stays.
-template <typename T, uint32_t kDim, uint32_t kHeads, typename Slot>
-__device__ __forceinline__ void join_parts(const AttendArgs &a, uint32_t row, uint32_t unit, const float *parts, uint32_t count, Slot slot,
-                                           float *to, uint32_t me, uint32_t all) {
-    constexpr uint32_t kFloats = kHeads * (kDim + 2);
-    uint32_t first;
-    const uint32_t heads = heads_of<kHeads>(a, unit, first), pairs = kDim / 2;
-    const bool nothing = count == kNoTokens;                  // the row has no tokens, its group may
-    if (nothing) count = 0;
-    for (uint32_t i = me; i < heads * pairs; i += all) {
-        const uint32_t h = i / pairs, d = (i - h * pairs) * 2;
-        if (d >= a.dim) continue;
-        float top = -CUDART_INF_F;
-        for (uint32_t k = 0; k < count; ++k) top = max_nan(__ldcg(parts + (size_t)slot(k) * kFloats + kHeads * kDim + 2 * h), top);
-        const float ref = top == -CUDART_INF_F ? 0.0f : top;
-        float sum = 0.0f, x = 0.0f, y = 0.0f;
-#pragma unroll 4
-        for (uint32_t k = 0; k < count; ++k) {
-            const float *p = parts + (size_t)slot(k) * kFloats;
-            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(p + kHeads * kDim + 2 * h)), v = __ldcg(reinterpret_cast<const float2 *>(p + h * kDim + d));
-            const float e = exp2_approx(ml.x - ref);
-            sum = fmaf(ml.y, e, sum);
-            x = fmaf(v.x, e, x);
-            y = fmaf(v.y, e, y);
+// A head's result from its weighted values (pair i of a lane: columns 2 (lane + 32 i) and one more), reference and sum; `also`:
+// with what its group has in common.
+template <typename T, uint32_t kDim>
+__device__ __forceinline__ void write_result(const AttendArgs &a, uint32_t row, uint32_t head, bool also, float2 (&v)[(kDim / 2 + 31) / 32],
+                                             float top, float sum) {
+    const uint32_t lane = threadIdx.x & 31u;
+    const float *w = also ? common_of<kDim>(a, row, head) : nullptr;
+    if (w) {
+        const float2 ml = *reinterpret_cast<const float2 *>(w + kDim);
+        const float most = max_nan(top, ml.x), ref = most == -CUDART_INF_F ? 0.0f : most, e = exp2_approx(top - ref), f = exp2_approx(ml.x - ref);
+#pragma unroll
+        for (uint32_t i = 0; i < (kDim / 2 + 31) / 32; ++i) {
+            if (lane + 32 * i >= kDim / 2) continue;
+            const float2 x = *reinterpret_cast<const float2 *>(w + 2 * (lane + 32 * i));
+            v[i] = make_float2(fmaf(x.x, f, v[i].x * e), fmaf(x.y, f, v[i].y * e));
         }
-        if (!to && !nothing) {
-            if (const float *w = common_of<kDim>(a, row, first + h)) {
-                const float2 ml = *reinterpret_cast<const float2 *>(w + kDim), v = *reinterpret_cast<const float2 *>(w + d);
-                const float most = max_nan(top, ml.x), all_ref = most == -CUDART_INF_F ? 0.0f : most, e = exp2_approx(ref - all_ref), f = exp2_approx(ml.x - all_ref);
-                sum = fmaf(ml.y, f, sum * e);
-                x = fmaf(v.x, f, x * e);
-                y = fmaf(v.y, f, y * e);
-                top = most;
+        sum = fmaf(ml.y, f, sum * e);
+        top = most;
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    T *out = static_cast<T *>(a.out) + row * a.out_row + head * a.out_head;
+#pragma unroll
+    for (uint32_t i = 0; i < (kDim / 2 + 31) / 32; ++i)
+        if (2 * (lane + 32 * i) < a.dim) *reinterpret_cast<uint32_t *>(out + 2 * (lane + 32 * i)) = pair_of<T>(v[i].x * inv, v[i].y * inv);
+    if (a.lse && lane == 0) a.lse[(size_t)row * a.n_heads + head] = sum == 0.0f ? -CUDART_INF_F : (top + log2f(sum)) * 0.69314718055994531f;
+}
+
+// Joins the parts k = 0 .. count - 1 (part k at slot(k) of `parts`: weighted values [kRows][kDim], then {reference, sum} [kRows])
+// of rows 0 .. rows - 1, by warps; emit(row, values, reference, sum) gets a row's in the layout of write_result.  It is a chain of loads
+// with next to nothing between, so a warp has kRowsAtOnce rows and kPartsAtOnce parts of each on their way together: the joins
+// of one sequence of 2000 tokens took 10 us value by value.  A reference of -inf means that a part has nothing; NaN stays.
+template <uint32_t kDim, uint32_t kRows, int kRowsAtOnce, int kPartsAtOnce, typename Slot, typename Emit>
+__device__ __forceinline__ void join_parts(const float *parts, uint32_t count, Slot slot, uint32_t rows, uint32_t worker, uint32_t workers, Emit emit) {
+    constexpr uint32_t kFloats = kRows * (kDim + 2), kPairs = (kDim / 2 + 31) / 32;
+    const uint32_t lane = threadIdx.x & 31u;
+#pragma unroll 1
+    for (uint32_t h0 = worker * kRowsAtOnce; h0 < rows; h0 += workers * kRowsAtOnce) {
+        float top[kRowsAtOnce], sum[kRowsAtOnce];
+        float2 v[kRowsAtOnce][kPairs];
+#pragma unroll
+        for (int b = 0; b < kRowsAtOnce; ++b) {
+            top[b] = -CUDART_INF_F;
+            sum[b] = 0.0f;
+#pragma unroll
+            for (uint32_t i = 0; i < kPairs; ++i) v[b][i] = make_float2(0.0f, 0.0f);
+        }
+        auto head = [&](int b) { return min(h0 + b, rows - 1); };
+        for (uint32_t k = lane; k < count; k += 32) {
+            const float *p = parts + (size_t)slot(k) * kFloats + kRows * kDim;
+#pragma unroll
+            for (int b = 0; b < kRowsAtOnce; ++b) top[b] = max_nan(top[b], __ldcg(p + 2 * head(b)));
+        }
+#pragma unroll
+        for (int b = 0; b < kRowsAtOnce; ++b)
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) top[b] = max_nan(top[b], __shfl_xor_sync(kFullMask, top[b], d));
+        for (uint32_t k0 = 0; k0 < count; k0 += 32) {
+            const uint32_t some = min(32u, count - k0);
+            float e[kRowsAtOnce];
+#pragma unroll
+            for (int b = 0; b < kRowsAtOnce; ++b) {
+                e[b] = 0.0f;
+                if (lane >= some) continue;
+                const float2 ml = __ldcg(reinterpret_cast<const float2 *>(parts + (size_t)slot(k0 + lane) * kFloats + kRows * kDim + 2 * head(b)));
+                e[b] = exp2_approx(ml.x - (top[b] == -CUDART_INF_F ? 0.0f : top[b]));
+                sum[b] = fmaf(ml.y, e[b], sum[b]);
+            }
+            for (uint32_t j0 = 0; j0 < some; j0 += kPartsAtOnce) {
+                float2 x[kPartsAtOnce][kRowsAtOnce][kPairs];
+#pragma unroll
+                for (int j = 0; j < kPartsAtOnce; ++j) {
+                    const float *p = parts + (size_t)slot(k0 + min(j0 + j, some - 1)) * kFloats;
+#pragma unroll
+                    for (int b = 0; b < kRowsAtOnce; ++b)
+#pragma unroll
+                        for (uint32_t i = 0; i < kPairs; ++i)
+                            x[j][b][i] = lane + 32 * i < kDim / 2 ? __ldcg(reinterpret_cast<const float2 *>(p + head(b) * kDim + 2 * (lane + 32 * i))) : make_float2(0.0f, 0.0f);
+                }
+#pragma unroll
+                for (int j = 0; j < kPartsAtOnce; ++j) {
+                    if (j0 + j >= some) break;
+#pragma unroll
+                    for (int b = 0; b < kRowsAtOnce; ++b) {
+                        const float f = __shfl_sync(kFullMask, e[b], j0 + j);
+#pragma unroll
+                        for (uint32_t i = 0; i < kPairs; ++i) v[b][i] = make_float2(fmaf(x[j][b][i].x, f, v[b][i].x), fmaf(x[j][b][i].y, f, v[b][i].y));
+                    }
+                }
             }
         }
-        if (to) {
-            *reinterpret_cast<float2 *>(to + h * kDim + d) = make_float2(x, y);
-            if (d == 0) *reinterpret_cast<float2 *>(to + kHeads * kDim + 2 * h) = make_float2(top, sum);
-            continue;
+#pragma unroll
+        for (int b = 0; b < kRowsAtOnce; ++b) {
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) sum[b] += __shfl_xor_sync(kFullMask, sum[b], d);
+            if (h0 + b < rows) emit(h0 + b, v[b], top[b], sum[b]);
         }
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        *reinterpret_cast<uint32_t *>(static_cast<T *>(a.out) + row * a.out_row + (first + h) * a.out_head + d) = pair_of<T>(x * inv, y * inv);
-        if (a.lse && d == 0) a.lse[(size_t)row * a.n_heads + first + h] = sum == 0.0f ? -CUDART_INF_F : (top + log2f(sum)) * 0.69314718055994531f;
     }
+}
+// A row's values, reference and sum as a part.
+template <uint32_t kDim>
+__device__ __forceinline__ void write_part(float *to, float *ml, const float2 (&v)[(kDim / 2 + 31) / 32], float top, float sum) {
+    const uint32_t lane = threadIdx.x & 31u;
+#pragma unroll
+    for (uint32_t i = 0; i < (kDim / 2 + 31) / 32; ++i)
+        if (lane + 32 * i < kDim / 2) *reinterpret_cast<float2 *>(to + 2 * (lane + 32 * i)) = v[i];
+    if (lane == 0) *reinterpret_cast<float2 *>(ml) = make_float2(top, sum);
 }
 
 // The running reference (in units of log2), sum and weighted values of 8 * kN heads, in the layout of the matrix instructions: lane
@@ -244,7 +321,8 @@ struct Fold {
     // Sixteen more tokens: keys and values in shared memory, bit i of the 16 in `counts`: token i counts.
     __device__ __forceinline__ void add(uint32_t keys, uint32_t values, uint32_t shared, uint32_t counts, float scale2) {
         const uint32_t lane = threadIdx.x & 31u, g = lane >> 2, row = lane & 7u, upper = lane >> 3 & 1u, right = lane >> 4;
-        float s[kN][4] = {};
+        constexpr int kChains = kN == 1 ? 2 : 1;              // sums that do not wait for one another
+        float s[kN][4], part[kChains][kN][4] = {};
         const uint32_t key = keys + (row + upper * 8) * S::kPitch + right * 16;
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
@@ -252,15 +330,19 @@ struct Fold {
             load_matrices(a, key + c * 32);
             if constexpr (S::kQueryInRegisters) {
 #pragma unroll
-                for (int n = 0; n < kN; ++n) multiply_add<T>(s[n], a, qf[c][n][0], qf[c][n][1]);
+                for (int n = 0; n < kN; ++n) multiply_add<T>(part[c % kChains][n], a, qf[c][n][0], qf[c][n][1]);
             } else {
                 static_assert(S::kQueryInRegisters || kN == 2, "two columns of matrices, loaded together");
                 uint32_t b[4];
                 load_matrices(b, shared + (row + right * 8) * S::kPitch + c * 32 + upper * 16);
-                multiply_add<T>(s[0], a, b[0], b[1]);
-                multiply_add<T>(s[kN - 1], a, b[2], b[3]);
+                multiply_add<T>(part[0][0], a, b[0], b[1]);
+                multiply_add<T>(part[0][kN - 1], a, b[2], b[3]);
             }
         }
+#pragma unroll
+        for (int n = 0; n < kN; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[n][i] = kChains == 2 ? part[0][n][i] + part[kChains - 1][n][i] : part[0][n][i];
         bool past = false;
 #pragma unroll
         for (int n = 0; n < kN; ++n)
@@ -368,13 +450,12 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
     sum_places<S::kThreads>(sums, a.n_rows, per_thread, [&](uint32_t r) {
         return (unsigned long long)a.units * (span_of<true>(c, a, r, blockIdx.x == 0).tiles() + 1);
     });
-    Line line;
-    line.total = sums[S::kThreads - 1];
-    const uint32_t blocks = (uint32_t)min((unsigned long long)gridDim.x, line.total / (S::kWarps * kLeastTiles) + 1);
+    const unsigned long long total = sums[S::kThreads - 1];
+    const uint32_t blocks = (uint32_t)min((unsigned long long)gridDim.x, quotient(total, S::kWarps * kLeastTiles) + 1);
     if (blockIdx.x >= blocks) return;
-    line.warps = (uint32_t)min((unsigned long long)blocks * S::kWarps, line.total);          // each has a place at least
+    const Line line(total, blocks * S::kWarps);
     const uint32_t w_global = blockIdx.x * S::kWarps + warp;
-    const unsigned long long begin = line.begin(min(w_global, line.warps)), end = line.begin(min(w_global + 1, line.warps));
+    const unsigned long long begin = line.begin(w_global), end = line.begin(w_global + 1);
 
     uint8_t *const mem = memory + warp * S::kWarpBytes;
     const uint32_t ring = shared_address(mem), query = ring + S::kStages * S::kStage;
@@ -396,7 +477,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
             row_place += places;
         }
         uint32_t tiles = span.tiles();
-        uint32_t unit = (uint32_t)((begin - row_place) / (tiles + 1));
+        uint32_t unit = (uint32_t)quotient(begin - row_place, tiles + 1);
         int32_t tile = (int32_t)(begin - row_place - (unsigned long long)unit * (tiles + 1)) - 1;          // -1: the place ahead
         unsigned long long place = begin;                     // of the next tile to bring
         Span next = row + 1 < a.n_rows ? span_of<true>(c, a, row + 1, false) : Span{-1, 0, 0};
@@ -428,7 +509,10 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
                 if (tiles) {
                     tile = 0;
                 } else {
-                    join_parts<T, S::kDim, S::kHeads>(a, row, unit, nullptr, span.n > 0 ? 0u : kNoTokens, [](uint32_t) { return 0u; }, nullptr, lane, 32);
+                    for (uint32_t h = 0; h < heads; ++h) {     // nothing, or what its group has in common
+                        float2 none[(S::kDim / 2 + 31) / 32] = {};
+                        write_result<T, S::kDim>(a, row, first + h, span.n > 0, none, -CUDART_INF_F, 0.0f);
+                    }
                     leave();
                 }
             }
@@ -466,9 +550,12 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
                 notes[to] = make_uint4(row, unit, counts | (fresh ? 1u << 16 : 0u) | (over ? 1u << 17 : 0u) | (tile == 0 ? 1u << 18 : 0u) |
                                        (final ? 1u << 19 : 0u) | heads << 20, first);
                 if (over) {                                   // a cut unit, for the joins: noted before the block's barrier
-                    const Cut cut{place - (uint32_t)tile - 1, row, unit, tiles, 1u};
-                    if (place - (uint32_t)tile < begin) { if (warp == 0) cut_in = cut; }
-                    else if (!final) cut_out[warp] = cut;
+                    const bool in = place - (uint32_t)tile < begin;
+                    if (in ? warp == 0 : !final) {
+                        const unsigned long long tile0 = place - (uint32_t)tile;
+                        const Cut cut{row, unit, line.warp_of(tile0), line.warp_of(tile0 + tiles - 1), 1u};
+                        if (in) cut_in = cut; else cut_out[warp] = cut;
+                    }
                 }
             }
             ++place;
@@ -476,27 +563,25 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
             look();
         };
 
-        uint32_t brought = 0, put = S::kStages - 1, stage = 0;          // tiles brought; stages of the next to bring and to use
-        look();
-        for (uint32_t i = 0; i + 1 < S::kStages; ++i) {
-            if (more) {
-                bring(i);
-                ++brought;
-            }
-            copy_commit();
-        }
+        uint32_t brought = 0, used = 0, put = 0, stage = 0;   // tiles; stages of the next to bring and to use
         Fold<T, kChunks, kN> f;
         bool head_whole = false;
+        look();
 #pragma unroll 1
-        for (uint32_t done = 0; done < brought; ++done) {
-            copy_wait<S::kStages - 2>();
-            __syncwarp();
+        for (uint32_t turn = 0;; ++turn) {
+            if (turn + 1 >= S::kStages) {                     // the ring has been filled
+                if (used == brought) break;
+                copy_wait<S::kStages - 2>();
+                __syncwarp();
+            }
             if (more) {                                       // into the stage that the last turn was done with
                 bring(put);
                 ++brought;
             }
             copy_commit();
             put = put + 1 == S::kStages ? 0 : put + 1;
+            if (turn + 1 < S::kStages) continue;
+            ++used;
             const uint4 note = notes[stage];
             const uint32_t at = ring + stage * S::kStage;
             stage = stage + 1 == S::kStages ? 0 : stage + 1;
@@ -534,11 +619,12 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
 
     // ---- units that cuts went through ----
     const uint32_t w_first = blockIdx.x * S::kWarps, w_last = w_first + S::kWarps - 1;
-    if (cut_out[warp].valid) {                                // begun by this warp and ended within the block
+    if (cut_out[warp].valid && cut_out[warp].last <= w_last) {          // begun by this warp and ended within the block
         const Cut u = cut_out[warp];
-        const uint32_t w0 = w_global, w1 = line.warp_of(u.place + u.tiles);
-        if (w1 <= w_last)
-            join_parts<T, S::kDim, S::kHeads>(a, u.row, u.unit, a.parts, w1 - w0 + 1, [=](uint32_t k) { return 2 * (w0 + k) + (k == 0); }, nullptr, lane, 32);
+        uint32_t first;
+        const uint32_t heads = heads_of<S::kHeads>(a, u.unit, first);
+        join_parts<S::kDim, S::kHeads, 4, 2>(a.parts, u.last - u.first + 1, [=](uint32_t k) { return 2 * (u.first + k) + (k == 0); }, heads, 0u, 1u,
+                                             [&](uint32_t h, auto &v, float top, float sum) { write_result<T, S::kDim>(a, u.row, first + h, true, v, top, sum); });
     }
     float *const block_parts = a.parts + (size_t)2 * gridDim.x * S::kWarps * S::kPartFloats;
     // a unit that came in from the block before, and one that begins here and goes on into the next: at most one each
@@ -550,13 +636,17 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
         } else {
 #pragma unroll 1
             for (uint32_t w = 0; w < S::kWarps; ++w)
-                if (cut_out[w].valid && line.warp_of(cut_out[w].place + cut_out[w].tiles) > w_last) u = cut_out[w];
+                if (cut_out[w].valid && cut_out[w].last > w_last) u = cut_out[w];
         }
         if (!u.valid) continue;
-        const uint32_t w0 = line.warp_of(u.place + 1), w1 = line.warp_of(u.place + u.tiles), from = max(w0, w_first), to = min(w1, w_last);
-        const uint32_t b0 = w0 / S::kWarps, b1 = w1 / S::kWarps;
-        join_parts<T, S::kDim, S::kHeads>(a, u.row, u.unit, a.parts, to - from + 1, [=](uint32_t k) { return 2 * (from + k) + (from + k == w0); },
-                               block_parts + ((size_t)2 * blockIdx.x + (blockIdx.x == b0)) * S::kPartFloats, threadIdx.x, S::kThreads);
+        const uint32_t w0 = u.first, from = max(w0, w_first), to = min(u.last, w_last), b0 = w0 / S::kWarps, b1 = u.last / S::kWarps;
+        uint32_t first;
+        const uint32_t heads = heads_of<S::kHeads>(a, u.unit, first);
+        float *const mine = block_parts + ((size_t)2 * blockIdx.x + (blockIdx.x == b0)) * S::kPartFloats;
+        join_parts<S::kDim, S::kHeads, 1, 4>(a.parts, to - from + 1, [=](uint32_t k) { return 2 * (from + k) + (from + k == w0); }, heads, warp, S::kWarps,
+                                             [&](uint32_t h, auto &v, float top, float sum) {
+                                                 write_part<S::kDim>(mine + h * S::kDim, mine + S::kHeads * S::kDim + 2 * h, v, top, sum);
+                                             });
         __threadfence();
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -566,8 +656,8 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
         }
         __syncthreads();
         if (last)
-            join_parts<T, S::kDim, S::kHeads>(a, u.row, u.unit, block_parts, b1 - b0 + 1, [=](uint32_t k) { return 2 * (b0 + k) + (k == 0); }, nullptr,
-                                   threadIdx.x, S::kThreads);
+            join_parts<S::kDim, S::kHeads, 1, 4>(block_parts, b1 - b0 + 1, [=](uint32_t k) { return 2 * (b0 + k) + (k == 0); }, heads, warp, S::kWarps,
+                                                 [&](uint32_t h, auto &v, float top, float sum) { write_result<T, S::kDim>(a, u.row, first + h, true, v, top, sum); });
         __syncthreads();
     }
 }
@@ -701,11 +791,9 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
         return tokens ? (unsigned long long)units * ((tokens + H::kTokens - 1) / H::kTokens + 1) : 0ull;
     };
     sum_places<kShareThreads>(sums, a.n_groups, per_thread, places_of);
-    Line line;
-    line.total = sums[kShareThreads - 1];
-    if (line.total == 0) return;
-    line.warps = (uint32_t)min((unsigned long long)gridDim.x, line.total / 2 + 1);          // blocks, here
-    line.warps = (uint32_t)min((unsigned long long)line.warps, line.total);
+    const unsigned long long total = sums[kShareThreads - 1];
+    if (total == 0) return;
+    const Line line(total, gridDim.x);                        // a block to a piece
     if (blockIdx.x >= line.warps) return;
     const unsigned long long begin = line.begin(blockIdx.x), end = line.begin(blockIdx.x + 1);
 
@@ -730,7 +818,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
         }
         load.enter(a, H::kTokens);
         load.place = begin;
-        load.unit = (uint32_t)((begin - before) / (load.tiles + 1));
+        load.unit = (uint32_t)quotient(begin - before, load.tiles + 1);
         load.tile = (int32_t)(begin - before - (unsigned long long)load.unit * (load.tiles + 1)) - 1;
     }
     Walk use = load;
@@ -889,27 +977,13 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
         __syncthreads();
         if (!joins) continue;
         const uint32_t m_block = u.unit / a.kv_heads, kv = u.unit - m_block * a.kv_heads, first = m_block * a.m_rows, count = min(a.m_rows, a.group * a.ratio - first);
-        for (uint32_t i = threadIdx.x; i < count * (S::kDim / 2); i += kShareThreads) {
-            const uint32_t r = i / (S::kDim / 2), d = (i - r * (S::kDim / 2)) * 2, rr = fast_div(first + r, a.by_ratio), row = u.group * a.group + rr;
-            if (row >= a.n_rows || d >= a.dim) continue;
-            auto part = [&](uint32_t b) { return a.share_parts + ((size_t)2 * b + (b == b0)) * H::kPartFloats; };
-            float top = -CUDART_INF_F;
-            for (uint32_t b = b0; b <= b1; ++b) top = max_nan(top, __ldcg(part(b) + kShareHeads * S::kDim + 2 * r));
-            const float ref = top == -CUDART_INF_F ? 0.0f : top;
-            float sum = 0.0f, x = 0.0f, y = 0.0f;
-#pragma unroll 4
-            for (uint32_t b = b0; b <= b1; ++b) {
-                const float2 ml = __ldcg(reinterpret_cast<const float2 *>(part(b) + kShareHeads * S::kDim + 2 * r));
-                const float2 v = __ldcg(reinterpret_cast<const float2 *>(part(b) + r * S::kDim + d));
-                const float e = exp2_approx(ml.x - ref);
-                sum = fmaf(ml.y, e, sum);
-                x = fmaf(v.x, e, x);
-                y = fmaf(v.y, e, y);
-            }
-            float *to = a.common + ((size_t)row * a.n_heads + kv * a.ratio + first + r - rr * a.ratio) * (S::kDim + 2);
-            *reinterpret_cast<float2 *>(to + d) = make_float2(x, y);
-            if (d == 0) *reinterpret_cast<float2 *>(to + S::kDim) = make_float2(top, sum);
-        }
+        join_parts<S::kDim, kShareHeads, 4, 2>(a.share_parts, b1 - b0 + 1, [=](uint32_t k) { return 2 * (b0 + k) + (k == 0); }, count, warp, kShareThreads / 32,
+                                               [&](uint32_t r, auto &v, float top, float sum) {
+                                                   const uint32_t rr = fast_div(first + r, a.by_ratio), row = u.group * a.group + rr;
+                                                   if (row >= a.n_rows) return;
+                                                   float *to = a.common + ((size_t)row * a.n_heads + kv * a.ratio + first + r - rr * a.ratio) * (S::kDim + 2);
+                                                   write_part<S::kDim>(to, to + S::kDim, v, top, sum);
+                                               });
     }
 }
 

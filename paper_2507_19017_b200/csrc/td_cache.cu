@@ -152,7 +152,10 @@ cudaError_t run_write(const CacheView &v, const PoolView &p, WriteArgs k, cudaSt
 // ---- attention ----
 constexpr uint32_t kBlocks = 148;                             // one per SM
 template <int kChunks>
-constexpr size_t part_bytes() { return (size_t)(2 * AttendShape<kChunks, 2>::kWarps + 2) * kBlocks * AttendShape<kChunks, 2>::kPartFloats * 4; }
+constexpr size_t part_bytes() {
+    return std::max((size_t)(2 * AttendShape<kChunks, 1>::kWarps + 2) * kBlocks * AttendShape<kChunks, 1>::kPartFloats * 4,
+                    (size_t)(2 * AttendShape<kChunks, 2>::kWarps + 2) * kBlocks * AttendShape<kChunks, 2>::kPartFloats * 4);
+}
 template <int kChunks>
 constexpr size_t share_bytes() { return (size_t)2 * kBlocks * ShareShape<kChunks, 2>::kPartFloats * 4; }
 struct AttendLayout {
