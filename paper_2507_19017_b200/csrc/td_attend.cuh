@@ -16,9 +16,6 @@
 
 namespace td {
 
-#ifndef TD_AW
-#define TD_AW 12
-#endif
 struct AttendArgs {
     const int32_t *seqs;
     const void *q;
@@ -28,7 +25,8 @@ struct AttendArgs {
     int64_t page, token, head;                                // element strides of the cache
     int64_t q_row, q_head, out_row, out_head;
     uint32_t n_rows, n_heads, kv_heads, ratio, dim, window;
-    uint32_t units;                                           // of a row: key heads times sixteens of heads of each
+    uint32_t units, per_kv;                                   // of a row: per_kv for each key head
+    FastDiv by_per_kv;
     float scale, scale2;                                      // scale2 = scale * log2(e)
     float *parts;                                             // [2 per warp, then 2 per block][part floats]
     uint32_t *arrived;                                        // [blocks], zero between calls
@@ -43,16 +41,13 @@ struct AttendArgs {
 
 constexpr uint32_t kTile = 16;                                // tokens of a tile
 constexpr float kSlack = 8.0f;                                // how far (log2) a score may pass the reference before that moves
-#ifndef TD_LEAST
-#define TD_LEAST 4
-#endif
-constexpr uint32_t kLeastTiles = TD_LEAST;                           // of a warp, before another block is used
+constexpr uint32_t kLeastTiles = 2;                           // of a warp, before another block is used
 
 // Shapes of a kernel for heads of up to 16 * kChunks elements, 8 * kN of them side by side.
 template <int kChunks, int kN>
 struct AttendShape {
     static constexpr uint32_t kDim = 16 * kChunks, kHeads = 8 * kN;
-    static constexpr uint32_t kWarps = kChunks <= 8 ? (kN == 1 ? TD_AW : 8) : 4;
+    static constexpr uint32_t kWarps = kChunks <= 8 ? (kN == 1 ? 12 : 8) : 4;
     static constexpr uint32_t kThreads = 32 * kWarps;
     static constexpr uint32_t kPitch = kDim * 2 + 16;         // bytes of a row in shared memory: an odd number of 16s, so that 8 rows lie in different banks
     static constexpr uint32_t kSide = kTile * kPitch;         // keys, or values, of a tile
@@ -150,8 +145,9 @@ struct Cut {
 };
 
 template <uint32_t kHeads>
-__device__ __forceinline__ uint32_t heads_of(const AttendArgs &a, uint32_t unit, uint32_t &first) {          // heads of a unit, from `first` on
-    const uint32_t per_kv = a.units / a.kv_heads, kv = unit / per_kv, at = (unit - kv * per_kv) * kHeads;
+__device__ __forceinline__ uint32_t heads_of(const AttendArgs &a, uint32_t unit, uint32_t &kv, uint32_t &first) {          // heads of a unit, from `first` on
+    kv = fast_div(unit, a.by_per_kv);
+    const uint32_t at = (unit - kv * a.per_kv) * kHeads;
     first = kv * a.ratio + at;
     return min(kHeads, a.ratio - at);
 }
@@ -438,15 +434,18 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
     using S = AttendShape<kChunks, kN>;
     extern __shared__ __align__(16) uint8_t memory[];
     __shared__ unsigned long long sums[S::kThreads];          // places of all rows up to and with those of each thread
-    __shared__ Cut cut_in, cut_out[S::kWarps];                // the unit that warp 0 began in the middle of; those a warp began and left
-    __shared__ uint32_t last;
+    // units that cuts went through: cut[0] came in from the block before, cut[1] goes on into the next, cut_out[w] were begun by warp w
+    // and ended within the block
+    __shared__ Cut cut[2], cut_out[S::kWarps];
+    __shared__ uint32_t last[2];
     griddep_launch_dependents();
     griddep_wait();
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
 
     // ---- this warp's share ----
     const uint32_t per_thread = (a.n_rows + S::kThreads - 1) / S::kThreads;
-    if (lane == 0) cut_in.valid = cut_out[warp].valid = 0;
+    if (lane == 0) cut_out[warp].valid = 0;
+    if (threadIdx.x < 2) cut[threadIdx.x].valid = last[threadIdx.x] = 0;
     sum_places<S::kThreads>(sums, a.n_rows, per_thread, [&](uint32_t r) {
         return (unsigned long long)a.units * (span_of<true>(c, a, r, blockIdx.x == 0).tiles() + 1);
     });
@@ -454,7 +453,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
     const uint32_t blocks = (uint32_t)min((unsigned long long)gridDim.x, quotient(total, S::kWarps * kLeastTiles) + 1);
     if (blockIdx.x >= blocks) return;
     const Line line(total, blocks * S::kWarps);
-    const uint32_t w_global = blockIdx.x * S::kWarps + warp;
+    const uint32_t w_first = blockIdx.x * S::kWarps, w_last = w_first + S::kWarps - 1, w_global = w_first + warp;
     const unsigned long long begin = line.begin(w_global), end = line.begin(w_global + 1);
 
     uint8_t *const mem = memory + warp * S::kWarpBytes;
@@ -484,8 +483,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
 
         uint32_t kv, first, heads;
         auto enter = [&]() {                                  // a unit's key head and its heads
-            heads = heads_of<S::kHeads>(a, unit, first);
-            kv = first / a.ratio;
+            heads = heads_of<S::kHeads>(a, unit, kv, first);
         };
         auto leave = [&]() {                                  // to the unit behind
             tile = -1;
@@ -553,8 +551,8 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
                     const bool in = place - (uint32_t)tile < begin;
                     if (in ? warp == 0 : !final) {
                         const unsigned long long tile0 = place - (uint32_t)tile;
-                        const Cut cut{row, unit, line.warp_of(tile0), line.warp_of(tile0 + tiles - 1), 1u};
-                        if (in) cut_in = cut; else cut_out[warp] = cut;
+                        const Cut u{row, unit, line.warp_of(tile0), line.warp_of(tile0 + tiles - 1), 1u};
+                        if (in) cut[0] = u; else if (u.last > w_last) cut[1] = u; else cut_out[warp] = u;
                     }
                 }
             }
@@ -565,8 +563,17 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
 
         uint32_t brought = 0, used = 0, put = 0, stage = 0;   // tiles; stages of the next to bring and to use
         Fold<T, kChunks, kN> f;
-        bool head_whole = false;
+        bool head_whole = false, asked = false;               // asked: the first unit's queries are on their way already
         look();
+        auto ask = [&](uint32_t of_row, uint32_t of_first, uint32_t of_heads) {
+            f.begin();
+            f.query(static_cast<const T *>(a.q) + of_row * a.q_row + of_first * a.q_head, query, a.dim,
+                    [&](uint32_t h) { return h < of_heads ? (int64_t)h * a.q_head : (int64_t)-1; });
+        };
+        if (more) {
+            ask(row, first, heads);
+            asked = true;
+        }
 #pragma unroll 1
         for (uint32_t turn = 0;; ++turn) {
             if (turn + 1 >= S::kStages) {                     // the ring has been filled
@@ -588,9 +595,8 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
             const uint32_t first = note.w, heads = note.z >> 20, t = lane & 3u;
             if (note.z >> 16 & 1u) {                          // a unit begins here
                 head_whole = note.z >> 18 & 1u;
-                f.begin();
-                f.query(static_cast<const T *>(a.q) + note.x * a.q_row + first * a.q_head, query, a.dim,
-                        [&](uint32_t h) { return h < heads ? (int64_t)h * a.q_head : (int64_t)-1; });
+                if (!asked) ask(note.x, first, heads);
+                asked = false;
             }
             f.add(at, at + S::kSide, query, note.z, a.scale2);
             if (note.z >> 17 & 1u) {                          // the unit, or this warp's part of it, ends here
@@ -618,48 +624,40 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
     __syncthreads();
 
     // ---- units that cuts went through ----
-    const uint32_t w_first = blockIdx.x * S::kWarps, w_last = w_first + S::kWarps - 1;
-    if (cut_out[warp].valid && cut_out[warp].last <= w_last) {          // begun by this warp and ended within the block
+    if (cut_out[warp].valid) {
         const Cut u = cut_out[warp];
-        uint32_t first;
-        const uint32_t heads = heads_of<S::kHeads>(a, u.unit, first);
+        uint32_t kv, first;
+        const uint32_t heads = heads_of<S::kHeads>(a, u.unit, kv, first);
         join_parts<S::kDim, S::kHeads, 4, 2>(a.parts, u.last - u.first + 1, [=](uint32_t k) { return 2 * (u.first + k) + (k == 0); }, heads, 0u, 1u,
                                              [&](uint32_t h, auto &v, float top, float sum) { write_result<T, S::kDim>(a, u.row, first + h, true, v, top, sum); });
     }
+    if (!cut[0].valid && !cut[1].valid) return;
+    // This block's share of the one and of the other, half of the warps each where there are both; then the last block of
+    // a unit joins the blocks' shares.
+    const bool both = cut[0].valid && cut[1].valid;
+    const uint32_t half = S::kWarps / 2, side = both ? warp / half : cut[1].valid, worker = both ? warp % half : warp, workers = both ? half : S::kWarps;
+    const Cut u = cut[side];
+    const uint32_t from = max(u.first, w_first), to = min(u.last, w_last), b0 = u.first / S::kWarps, b1 = u.last / S::kWarps;
     float *const block_parts = a.parts + (size_t)2 * gridDim.x * S::kWarps * S::kPartFloats;
-    // a unit that came in from the block before, and one that begins here and goes on into the next: at most one each
-#pragma unroll 1
-    for (uint32_t side = 0; side < 2; ++side) {
-        Cut u{};
-        if (side == 0) {
-            u = cut_in;
-        } else {
-#pragma unroll 1
-            for (uint32_t w = 0; w < S::kWarps; ++w)
-                if (cut_out[w].valid && cut_out[w].last > w_last) u = cut_out[w];
-        }
-        if (!u.valid) continue;
-        const uint32_t w0 = u.first, from = max(w0, w_first), to = min(u.last, w_last), b0 = w0 / S::kWarps, b1 = u.last / S::kWarps;
-        uint32_t first;
-        const uint32_t heads = heads_of<S::kHeads>(a, u.unit, first);
-        float *const mine = block_parts + ((size_t)2 * blockIdx.x + (blockIdx.x == b0)) * S::kPartFloats;
-        join_parts<S::kDim, S::kHeads, 1, 4>(a.parts, to - from + 1, [=](uint32_t k) { return 2 * (from + k) + (from + k == w0); }, heads, warp, S::kWarps,
-                                             [&](uint32_t h, auto &v, float top, float sum) {
-                                                 write_part<S::kDim>(mine + h * S::kDim, mine + S::kHeads * S::kDim + 2 * h, v, top, sum);
-                                             });
+    float *const mine = block_parts + ((size_t)2 * blockIdx.x + (blockIdx.x == b0)) * S::kPartFloats;
+    uint32_t kv, first;
+    const uint32_t heads = heads_of<S::kHeads>(a, u.unit, kv, first);
+    join_parts<S::kDim, S::kHeads, 2, 4>(a.parts, to - from + 1, [=](uint32_t k) { return 2 * (from + k) + (from + k == u.first); }, heads, worker, workers,
+                                         [&](uint32_t h, auto &v, float top, float sum) {
+                                             write_part<S::kDim>(mine + h * S::kDim, mine + S::kHeads * S::kDim + 2 * h, v, top, sum);
+                                         });
+    __threadfence();
+    __syncthreads();
+    if (worker == 0 && lane == 0) {
+        const uint32_t before = atomicAdd(a.arrived + b0, 1u);
+        last[side] = before == b1 - b0;
+        if (before == b1 - b0) a.arrived[b0] = 0;
         __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            last = atomicAdd(a.arrived + b0, 1u) == b1 - b0;
-            if (last) a.arrived[b0] = 0;
-            __threadfence();
-        }
-        __syncthreads();
-        if (last)
-            join_parts<S::kDim, S::kHeads, 1, 4>(block_parts, b1 - b0 + 1, [=](uint32_t k) { return 2 * (b0 + k) + (k == 0); }, heads, warp, S::kWarps,
-                                                 [&](uint32_t h, auto &v, float top, float sum) { write_result<T, S::kDim>(a, u.row, first + h, true, v, top, sum); });
-        __syncthreads();
     }
+    __syncthreads();
+    if (last[side])
+        join_parts<S::kDim, S::kHeads, 2, 4>(block_parts, b1 - b0 + 1, [=](uint32_t k) { return 2 * (b0 + k) + (k == 0); }, heads, worker, workers,
+                                             [&](uint32_t h, auto &v, float top, float sum) { write_result<T, S::kDim>(a, u.row, first + h, true, v, top, sum); });
 }
 
 // ---- tokens that a group's rows have in common ----

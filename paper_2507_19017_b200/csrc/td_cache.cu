@@ -183,7 +183,9 @@ AttendLayout attend_layout(uint32_t n_rows, uint32_t n_heads, uint32_t dim) {   
 template <typename T, int kChunks, int kN>
 cudaError_t run_attend(const CacheView &v, AttendArgs k, cudaStream_t st) {
     using S = AttendShape<kChunks, kN>;
-    k.units = k.kv_heads * ((k.ratio + S::kHeads - 1) / S::kHeads);
+    k.per_kv = (k.ratio + S::kHeads - 1) / S::kHeads;
+    k.units = k.kv_heads * k.per_kv;
+    k.by_per_kv = make_fastdiv(k.per_kv);
     cudaError_t rc = cudaFuncSetAttribute(attend_kernel<T, kChunks, kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes);
     if (rc == cudaSuccess && k.group > 1) {
         using H = ShareShape<kChunks, 2>;
