@@ -12,7 +12,7 @@ LIB_PATH = os.path.join(_HERE, "libtd.so")
 SOURCES = ["td.cu", "td_ops.cu", "td_cache.cu"]
 HEADERS = ["td_common.cuh", "td_device.cuh", "td_alloc.cuh", "td_put.cuh", "td_get.cuh", 
            "td_range.h", "td_host.cuh", "td_ops.cuh", "td_logprob.cuh", "td_policy.cuh", "td_embed.cuh",
-           "td_cache.cuh", "td_mma.cuh", "td_attend.cuh"]
+           "td_cache.cuh", "td_mma.cuh", "td_tensor.cuh", "td_attend.cuh"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

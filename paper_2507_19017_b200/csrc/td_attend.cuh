@@ -13,6 +13,7 @@
 
 #include "td_cache.cuh"
 #include "td_mma.cuh"
+#include "td_tensor.cuh"
 
 namespace td {
 
@@ -773,6 +774,37 @@ struct ShareCut {
     uint32_t group, unit, tiles, valid;
 };
 
+// Units that were cut: the last of their blocks to come joins the parts.
+template <uint32_t kDim>
+__device__ __forceinline__ void join_shares(const AttendArgs &a, const Line &line, const ShareCut &cut_in, const ShareCut &cut_out, uint32_t *last) {
+    const uint32_t warp = threadIdx.x >> 5;
+#pragma unroll 1
+    for (uint32_t side = 0; side < 2; ++side) {
+        const ShareCut u = side == 0 ? cut_in : cut_out;
+        if (!u.valid) continue;
+        const uint32_t b0 = line.warp_of(u.place + 1), b1 = line.warp_of(u.place + u.tiles);
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            *last = atomicAdd(a.share_arrived + b0, 1u) == b1 - b0;
+            if (*last) a.share_arrived[b0] = 0;
+            __threadfence();
+        }
+        __syncthreads();
+        const bool joins = *last;
+        __syncthreads();
+        if (!joins) continue;
+        const uint32_t m_block = u.unit / a.kv_heads, kv = u.unit - m_block * a.kv_heads, first = m_block * a.m_rows, count = min(a.m_rows, a.group * a.ratio - first);
+        join_parts<kDim, kShareHeads, 4, 2>(a.share_parts, b1 - b0 + 1, [=](uint32_t k) { return 2 * (b0 + k) + (k == 0); }, count, warp, kShareThreads / 32,
+                                               [&](uint32_t r, auto &v, float top, float sum) {
+                                                   const uint32_t rr = fast_div(first + r, a.by_ratio), row = u.group * a.group + rr;
+                                                   if (row >= a.n_rows) return;
+                                                   float *to = a.common + ((size_t)row * a.n_heads + kv * a.ratio + first + r - rr * a.ratio) * (kDim + 2);
+                                                   write_part<kDim>(to, to + kDim, v, top, sum);
+                                               });
+    }
+}
+
 template <typename T, int kChunks, int kN>
 __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, AttendArgs a) {
     using S = AttendShape<kChunks, kN>;
@@ -958,31 +990,346 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
         use.step(a, units, H::kTokens);
     }
     copy_wait<0>();
-#pragma unroll 1
-    for (uint32_t side = 0; side < 2; ++side) {
-        const ShareCut u = side == 0 ? cut_in : cut_out;
-        if (!u.valid) continue;
-        const uint32_t b0 = line.warp_of(u.place + 1), b1 = line.warp_of(u.place + u.tiles);
-        __threadfence();
+    join_shares<S::kDim>(a, line, cut_in, cut_out, &last);
+}
+
+// The same for heads of up to 128 elements, the products on the tensor memory: 128 heads by 128 tokens at a time, scores and weights
+// never in shared memory.  Two threads have a head's 64 scores each.  While the threads turn a tile's scores into weights, the
+// tensor cores take the last tile's values and the next tile's scores: per tile of 128 tokens there are
+//   scores i + 1 = queries keys   ->   (threads: weights i from scores i)   ->   results += weights i values i.
+// Keys come three tiles and values two tiles ahead through 16-byte copies that put each vector where the products expect it, so any
+// pages and strides will do.  The reference is moved as in Fold: the weights are first taken against the one there is, and
+// only where a score passed it is the tile taken again.
+template <int kChunks>
+struct WideShape {
+    static constexpr uint32_t kDim = 16 * kChunks, kHalves = (kChunks + 3) / 4, kColumns = 64 * kHalves;
+    static constexpr uint32_t kTokens = 128, kHalf = kTokens * 128, kSide = kHalves * kHalf;
+    static constexpr uint32_t kKeys = 3, kValues = 2;         // tiles of each in shared memory
+    static constexpr uint32_t kBytes = (kKeys + kValues + 1) * kSide + 1024;
+    static constexpr uint32_t kPartFloats = kShareHeads * (kDim + 2);
+    static constexpr uint32_t kScores = 0, kResults = 256, kWeights = 384, kTensor = 512;          // columns of tensor memory: 2 x 128, 128, 2 x 64
+};
+
+template <typename T, int kChunks>
+__global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView c, AttendArgs a) {
+    using W = WideShape<kChunks>;
+    extern __shared__ __align__(16) uint8_t memory[];
+    __shared__ unsigned long long sums[kShareThreads];
+    __shared__ int64_t offsets[4][W::kTokens];                // of a tile's tokens; -1: does not count
+    __shared__ uint32_t counts[8][W::kTokens / 32];
+    __shared__ float exchange[2][kShareHeads];
+    __shared__ __align__(8) unsigned long long bars[3];       // scores of even and odd tiles, results
+    __shared__ uint32_t tensor_at, failed, last;
+    griddep_launch_dependents();
+    griddep_wait();
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, units = a.kv_heads * a.m_blocks;
+    const uint32_t per_thread = (a.n_groups + kShareThreads - 1) / kShareThreads;
+    auto places_of = [&](uint32_t g) {
+        const uint32_t tokens = (uint32_t)a.shared[g].x;
+        return tokens ? (unsigned long long)units * ((tokens + W::kTokens - 1) / W::kTokens + 1) : 0ull;
+    };
+    sum_places<kShareThreads>(sums, a.n_groups, per_thread, places_of);
+    const unsigned long long total = sums[kShareThreads - 1];
+    if (total == 0) return;
+    const Line line(total, gridDim.x);                        // a block to a piece
+    if (blockIdx.x >= line.warps) return;
+    const unsigned long long begin = line.begin(blockIdx.x), end = line.begin(blockIdx.x + 1);
+
+    const uint32_t memory_at = shared_address(memory), pad = (1024u - memory_at % 1024u) % 1024u;
+    const uint32_t queries = memory_at + pad, keys = queries + W::kSide, values = keys + W::kKeys * W::kSide;
+    const uint32_t bar = shared_address(bars);
+    if (a.dim != W::kColumns)                                 // columns that no copy writes
+        for (uint32_t i = threadIdx.x; i < (W::kKeys + W::kValues + 1) * W::kSide / 16; i += kShareThreads)
+            reinterpret_cast<uint4 *>(memory + pad)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (threadIdx.x == 0) {
+        failed = 0;
+        for (uint32_t i = 0; i < 3; ++i) product_bar_init(bar + 8 * i);
+    }
+    __syncwarp();
+    if (warp == 0) tensor_alloc(shared_address(&tensor_at), W::kTensor);
+
+    Walk ahead;
+    {
+        const uint32_t lo = thread_of<kShareThreads>(sums, begin);
+        unsigned long long before = lo ? sums[lo - 1] : 0;
+        ahead.group = lo * per_thread;
+        for (;; ++ahead.group) {
+            const unsigned long long places = places_of(ahead.group);
+            if (before + places > begin) break;
+            before += places;
+        }
+        ahead.enter(a, W::kTokens);
+        ahead.place = begin;
+        ahead.unit = (uint32_t)quotient(begin - before, ahead.tiles + 1);
+        ahead.tile = (int32_t)(begin - before - (unsigned long long)ahead.unit * (ahead.tiles + 1)) - 1;
+    }
+    Walk use = ahead;
+    // Where the tokens of the tile that `ahead` is at lie: looked up by 128 threads, noted later as those of tile `number`.
+    int32_t id = -1, token = 0;
+    uint32_t ahead_unit = 0;
+    bool there = false;
+    auto look = [&]() {
+        there = ahead.here(end);
+        id = -1;
+        if (!there) return;
+        ahead_unit = ahead.unit;
+        token = ahead.tile * (int32_t)W::kTokens + (int32_t)threadIdx.x;
+        if (threadIdx.x < W::kTokens && token < ahead.tokens) {
+            id = c.table[(size_t)ahead.seq * c.max_pages + fast_div((uint32_t)token, c.by_page)];
+            if ((uint32_t)id >= c.n_pages && ahead_unit == 0) cache_flag(c, TD_ERR_OOB_INDEX);
+        }
+        ahead.step(a, units, W::kTokens);
+    };
+    auto note = [&](uint32_t number) {
+        if (threadIdx.x >= W::kTokens) return;
+        const bool on = (uint32_t)id < c.n_pages;
+        offsets[number & 3u][threadIdx.x] =
+            on ? id * a.page + (token - (int64_t)fast_div((uint32_t)token, c.by_page) * c.page_size) * a.token + (ahead_unit % a.kv_heads) * a.head : -1;
+        const uint32_t which = __ballot_sync(kFullMask, on);
+        if (lane == 0) counts[number & 7u][warp] = which;
+    };
+    // Vectors of tile `number` from `from` to `to`.
+    auto bring = [&](const void *from, uint32_t to, uint32_t number) {
+        constexpr uint32_t kPer = 8 * W::kHalves;
+#pragma unroll
+        for (uint32_t k = 0; k < W::kTokens * kPer / kShareThreads; ++k) {
+            const uint32_t i = threadIdx.x + k * kShareThreads, r = i / kPer, v = i - r * kPer;
+            const int64_t at = offsets[number & 3u][r];
+            if (v * 8 >= a.dim) continue;
+            copy_vector_or_zero(to + (v >> 3) * W::kHalf + r * 128 + ((v ^ r) & 7u) * 16, static_cast<const T *>(from) + (at < 0 ? 0 : at + v * 8), at < 0 ? 0u : 16u);
+        }
+    };
+    uint32_t tiles_noted = 0;
+    for (; tiles_noted < 4; ++tiles_noted) {
+        look();
+        note(tiles_noted);
+    }
+    tensor_before_sync();
+    __syncthreads();
+    tensor_after_sync();
+    const uint32_t tensor = tensor_at, mine = tensor + ((warp & 3u) * 32 << 16), half = warp >> 2, my_row = (warp & 3u) * 32 + lane;
+    // copies in groups: {keys 0}, {keys 1}, {keys 2, values 0}, then {keys i + 3, values i + 1} in turn i; tiles behind the last are zeros
+    bring(a.keys, keys, 0);
+    copy_commit();
+    bring(a.keys, keys + W::kSide, 1);
+    copy_commit();
+    bring(a.keys, keys + 2 * W::kSide, 2);
+    bring(a.values, values, 0);
+    copy_commit();
+
+    uint32_t m_count = 0;
+    auto heads_in = [&](const Walk &w, uint32_t &kv, uint32_t &first) {
+        const uint32_t m_block = w.unit / a.kv_heads;
+        kv = w.unit - m_block * a.kv_heads;
+        first = m_block * a.m_rows;
+        return min(a.m_rows, a.group * a.ratio - first);
+    };
+    // The queries of a unit into shared memory, zeros behind them.
+    auto ask = [&](const Walk &w) {
+        uint32_t kv, first;
+        const uint32_t n = heads_in(w, kv, first);
+        constexpr uint32_t kPer = 8 * W::kHalves;
+#pragma unroll 4
+        for (uint32_t k = 0; k < kShareHeads * kPer / kShareThreads; ++k) {
+            const uint32_t i = threadIdx.x + k * kShareThreads, r = i / kPer, v = i - r * kPer, rr = fast_div(first + r, a.by_ratio), row = w.group * a.group + rr;
+            uint4 x = make_uint4(0u, 0u, 0u, 0u);
+            if (r < n && row < a.n_rows && v * 8 < a.dim)
+                x = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + row * a.q_row + (kv * a.ratio + first + r - rr * a.ratio) * a.q_head + v * 8);
+            store_shared(queries + (v >> 3) * W::kHalf + r * 128 + ((v ^ r) & 7u) * 16, x);
+        }
+    };
+    auto score = [&](uint32_t number) {                       // scores of tile `number`, by one thread
+        const uint32_t at = keys + number % W::kKeys * W::kSide;
+#pragma unroll
+        for (uint32_t k = 0; k < 4 * W::kHalves; ++k)
+            product(tensor + W::kScores + (number & 1u) * 128, shared_matrix(queries + (k >> 2) * W::kHalf + (k & 3u) * 32, 1024, 16),
+                    shared_matrix(at + (k >> 2) * W::kHalf + (k & 3u) * 32, 1024, 16), product_kind<T>(128, false), k > 0);
+        product_commit(bar + 8 * (number & 1u));
+    };
+    bool fine = true;
+    uint32_t i = 0;                                           // the tile of this turn
+    ShareCut cut_in{}, cut_out{};
+    bool head_whole = false;
+    float m = -CUDART_INF_F, l = 0.0f;
+    use.here(end);
+    if (use.place < end) {
+        ask(use);
+        copy_wait<2>();
+        shared_for_products();
         __syncthreads();
         if (threadIdx.x == 0) {
-            last = atomicAdd(a.share_arrived + b0, 1u) == b1 - b0;
-            if (last) a.share_arrived[b0] = 0;
-            __threadfence();
+            tensor_after_sync();
+            score(0);
         }
-        __syncthreads();
-        const bool joins = last;
-        __syncthreads();
-        if (!joins) continue;
-        const uint32_t m_block = u.unit / a.kv_heads, kv = u.unit - m_block * a.kv_heads, first = m_block * a.m_rows, count = min(a.m_rows, a.group * a.ratio - first);
-        join_parts<S::kDim, kShareHeads, 4, 2>(a.share_parts, b1 - b0 + 1, [=](uint32_t k) { return 2 * (b0 + k) + (k == 0); }, count, warp, kShareThreads / 32,
-                                               [&](uint32_t r, auto &v, float top, float sum) {
-                                                   const uint32_t rr = fast_div(first + r, a.by_ratio), row = u.group * a.group + rr;
-                                                   if (row >= a.n_rows) return;
-                                                   float *to = a.common + ((size_t)row * a.n_heads + kv * a.ratio + first + r - rr * a.ratio) * (S::kDim + 2);
-                                                   write_part<S::kDim>(to, to + S::kDim, v, top, sum);
-                                               });
     }
+#pragma unroll 1
+    for (; use.here(end); ++i) {
+        Walk next = use;
+        next.step(a, units, W::kTokens);
+        const bool more = next.here(end), other = more && next.tile == 0;
+        copy_wait<1>();                                       // keys i + 1
+        if (other) {                                          // the next tile is another unit's: its queries, once the scores of this one are done
+            fine &= product_wait(bar + 8 * (i & 1u), i >> 1 & 1u);
+            ask(next);
+        }
+        shared_for_products();
+        __syncthreads();
+        if (more && threadIdx.x == 0) {
+            tensor_after_sync();
+            score(i + 1);
+        }
+        __syncwarp();
+        uint32_t kv, m_first;
+        m_count = heads_in(use, kv, m_first);
+        const bool fresh = use.tile == 0 || use.place == begin;
+        if (fresh) {
+            head_whole = use.tile == 0;
+            m = -CUDART_INF_F;
+            l = 0.0f;
+        }
+        look();
+        // scores to weights
+        fine &= product_wait(bar + 8 * (i & 1u), i >> 1 & 1u);
+        __syncwarp();
+        tensor_after_sync();
+        float x[64];
+        {
+            uint32_t r[4][16];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) tensor_load16(r[k], mine + W::kScores + (i & 1u) * 128 + half * 64 + 16 * k);
+            tensor_wait_loads();
+#pragma unroll
+            for (int k = 0; k < 64; ++k) x[k] = __uint_as_float(r[k >> 4][k & 15]);
+        }
+        const uint32_t which[2] = {counts[i & 7u][half * 2], counts[i & 7u][half * 2 + 1]};
+        if ((which[0] & which[1]) != ~0u) {
+#pragma unroll
+            for (int k = 0; k < 64; ++k) x[k] = which[k >> 5] >> (k & 31) & 1u ? x[k] * a.scale2 : -CUDART_INF_F;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 64; ++k) x[k] *= a.scale2;
+        }
+        auto weigh = [&](float ref, float &sum) {             // the largest of the weights, which go to tensor memory
+            float most = 0.0f;
+            float part[4] = {};
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                uint32_t p[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float u = exp2_approx(x[32 * k + 2 * j] - ref), w = exp2_approx(x[32 * k + 2 * j + 1] - ref);
+                    part[j & 3] += u + w;
+                    most = max_nan(most, max_nan(u, w));
+                    p[j] = pair_of<T>(u, w);                  // rounded as in Fold
+                }
+                tensor_store16(mine + W::kWeights + (i & 1u) * 64 + half * 32 + 16 * k, p);
+            }
+            sum = (part[0] + part[1]) + (part[2] + part[3]);
+            return most;
+        };
+        float sum = 0.0f;
+        bool past = fresh;                                    // a unit's first tile sets the reference
+        if (!fresh) {
+            past = !(weigh(m == -CUDART_INF_F ? 0.0f : m, sum) <= 256.0f);          // 2^kSlack
+            if (m == -CUDART_INF_F) {                         // nothing counted so far
+#pragma unroll
+                for (int k = 0; k < 64; ++k) past |= !(x[k] == -CUDART_INF_F);
+            }
+        }
+        if (i > 0) fine &= product_wait(bar + 16, (i - 1) & 1u);          // results of the last tile: its values' place is free
+        bring(a.keys, keys + i % W::kKeys * W::kSide, i + 3);
+        bring(a.values, values + (i + 1) % W::kValues * W::kSide, i + 1);
+        copy_commit();
+        copy_wait<1>();                                       // values i
+        shared_for_products();
+        if (!fine) failed = 1;
+        __syncwarp();
+        tensor_wait_stores();
+        tensor_before_sync();
+        const bool again = __syncthreads_or(past || !fine);
+        if (again && failed) break;                           // never seen
+        note(i + 4);
+        if (again) {
+            float top = x[0];
+#pragma unroll
+            for (int k = 1; k < 64; ++k) top = max_nan(top, x[k]);
+            exchange[half][my_row] = top;
+            __syncthreads();
+            top = max_nan(max_nan(exchange[0][my_row], exchange[1][my_row]), m);
+            const float keep = m == -CUDART_INF_F ? 0.0f : exp2_approx(m - top);
+            if (!fresh) {
+                tensor_after_sync();
+#pragma unroll
+                for (uint32_t k = 0; k < W::kColumns / 32; ++k) {
+                    uint32_t r[16];
+                    const uint32_t at = mine + W::kResults + half * (W::kColumns / 2) + 16 * k;
+                    tensor_load16(r, at);
+                    tensor_wait_loads();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * keep);
+                    tensor_store16(at, r);
+                }
+            }
+            m = top;
+            l *= keep;
+            weigh(m == -CUDART_INF_F ? 0.0f : m, sum);
+            tensor_wait_stores();
+            tensor_before_sync();
+            __syncthreads();
+        }
+        l += sum;
+        if (threadIdx.x == 0) {
+            tensor_after_sync();
+            const uint32_t at = values + i % W::kValues * W::kSide;
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k)
+                product_from_tensor(tensor + W::kResults, tensor + W::kWeights + (i & 1u) * 64 + 8 * k, shared_matrix(at + k * 2048, 1024, W::kHalf),
+                                    product_kind<T>(W::kColumns, true), !fresh || k > 0);
+            product_commit(bar + 16);
+        }
+        __syncwarp();
+        const bool final = use.tile + 1 == (int32_t)use.tiles;
+        if (final || use.place + 1 == end) {                  // the unit, or this block's part of it, ends here
+            exchange[half][my_row] = l;
+            fine &= product_wait(bar + 16, i & 1u);
+            __syncthreads();
+            tensor_after_sync();
+            const uint32_t rr = fast_div(m_first + my_row, a.by_ratio), row = use.group * a.group + rr, head = kv * a.ratio + m_first + my_row - rr * a.ratio;
+            const bool whole = head_whole && final;
+            float *const part = a.share_parts + ((size_t)2 * blockIdx.x + (head_whole ? 1 : 0)) * W::kPartFloats;
+            float *const to = whole ? a.common + ((size_t)row * a.n_heads + head) * (W::kDim + 2) : part + my_row * W::kDim;
+            float *const ml = whole ? to + W::kDim : part + kShareHeads * W::kDim + 2 * my_row;
+            const bool writes = my_row < m_count && row < a.n_rows;
+#pragma unroll
+            for (uint32_t k = 0; k < W::kColumns / 32; ++k) {
+                uint32_t r[16];
+                const uint32_t column = half * (W::kColumns / 2) + 16 * k;
+                tensor_load16(r, mine + W::kResults + column);
+                tensor_wait_loads();
+                if (writes && column < W::kDim)
+#pragma unroll
+                    for (int j = 0; j < 16; j += 2) *reinterpret_cast<float2 *>(to + column + j) = make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
+            }
+            if (writes && half == 0) *reinterpret_cast<float2 *>(ml) = make_float2(m, exchange[0][my_row] + exchange[1][my_row]);
+            tensor_before_sync();                             // read before the next unit's results are begun
+            if (!whole) {
+                const ShareCut cut{use.place - (uint32_t)use.tile - 1, use.group, use.unit, use.tiles, 1u};
+                if (head_whole) cut_out = cut; else cut_in = cut;
+            }
+        }
+        use.step(a, units, W::kTokens);
+    }
+    copy_wait<0>();
+    if (!fine) {                                              // never seen; what is still being computed is waited for, again with a limit
+        cache_flag(c, TD_ERR_COPY_TIMEOUT);
+        product_wait(bar + 8 * ((i + 1) & 1u), (i + 1) >> 1 & 1u);
+        product_wait(bar + 16, (i + 1) & 1u);
+    }
+    tensor_before_sync();
+    __syncthreads();
+    if (warp == 0) tensor_free(tensor, W::kTensor);
+    if (failed) return;
+    join_shares<W::kDim>(a, line, cut_in, cut_out, &last);
 }
 
 constexpr uint32_t kFloatThreads = 256;

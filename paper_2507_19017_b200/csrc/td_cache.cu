@@ -180,6 +180,22 @@ AttendLayout attend_layout(uint32_t n_rows, uint32_t n_heads, uint32_t dim) {   
     L.total = p;
     return L;
 }
+#ifndef TD_WIDE
+#define TD_WIDE 17
+#endif
+template <typename T, int kChunks>
+cudaError_t run_share(const CacheView &v, const AttendArgs &k, cudaStream_t st) {
+    if constexpr (kChunks <= 8) {
+        if (k.m_rows >= TD_WIDE) {
+            using W = WideShape<kChunks>;
+            const cudaError_t rc = cudaFuncSetAttribute(share_wide_kernel<T, kChunks>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)W::kBytes);
+            return rc != cudaSuccess ? rc : launch_smem(share_wide_kernel<T, kChunks>, kBlocks, kShareThreads, W::kBytes, st, 1u, v, k);
+        }
+    }
+    using H = ShareShape<kChunks, 2>;
+    const cudaError_t rc = cudaFuncSetAttribute(share_kernel<T, kChunks, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)H::kBytes);
+    return rc != cudaSuccess ? rc : launch_smem(share_kernel<T, kChunks, 2>, kBlocks, kShareThreads, H::kBytes, st, 1u, v, k);
+}
 template <typename T, int kChunks, int kN>
 cudaError_t run_attend(const CacheView &v, AttendArgs k, cudaStream_t st) {
     using S = AttendShape<kChunks, kN>;
@@ -188,10 +204,8 @@ cudaError_t run_attend(const CacheView &v, AttendArgs k, cudaStream_t st) {
     k.by_per_kv = make_fastdiv(k.per_kv);
     cudaError_t rc = cudaFuncSetAttribute(attend_kernel<T, kChunks, kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes);
     if (rc == cudaSuccess && k.group > 1) {
-        using H = ShareShape<kChunks, 2>;
-        rc = cudaFuncSetAttribute(share_kernel<T, kChunks, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)H::kBytes);
-        if (rc == cudaSuccess) rc = launch(share_plan_kernel, k.n_groups, kShareThreads, st, 1u, v, k);
-        if (rc == cudaSuccess) rc = launch_smem(share_kernel<T, kChunks, 2>, kBlocks, kShareThreads, H::kBytes, st, 1u, v, k);
+        rc = launch(share_plan_kernel, k.n_groups, kShareThreads, st, 1u, v, k);
+        if (rc == cudaSuccess) rc = run_share<T, kChunks>(v, k, st);
     }
     if (rc == cudaSuccess) rc = launch_smem(attend_kernel<T, kChunks, kN>, kBlocks, S::kThreads, S::kBytes, st, 1u, v, k);
     return rc;
