@@ -998,36 +998,48 @@ class Cache:
         return cls(keys, values, table, length, holders)
 
 
-def _cache_call(name: str, cache: Cache, stream, *addresses):
-    rc = getattr(lib(), name)(cache.address, *addresses, _op_stream(stream, cache.device))
-    if rc != 0:
-        raise TdError(name, rc)
+class _CacheCall:
+    """A call (cache, addresses, stream), its function looked up once."""
+
+    def __init__(self, name: str, extra: int):
+        self.name, self.extra, self.func = name, extra, None
+
+    def __call__(self, cache: Cache, stream, *addresses):
+        if self.func is None:
+            self.func = C.CFUNCTYPE(C.c_int, *[C.c_void_p] * (self.extra + 2))((self.name, lib()))
+        rc = self.func(cache.address, *addresses, _op_stream(stream, cache.device))
+        if rc != 0:
+            raise TdError(self.name, rc)
+
+
+_CACHE_EXTEND, _CACHE_FORK = _CacheCall("td_cache_extend", 2), _CacheCall("td_cache_fork", 1)
+_CACHE_FREE, _CACHE_COMPACT = _CacheCall("td_cache_free", 1), _CacheCall("td_cache_compact", 2)
 
 
 def cache_extend(cache: Cache, add=None, cu=None, stream=None):
     """Room for add[s] more tokens (int32 [max_seqs]; None: one for every sequence that has any): lengths grow, and the
     pages that takes are the lowest free ones, in order of sequence.  cu (int32 [max_seqs + 1]): written with the
     running sum of the tokens, as cache_write takes it."""
-    _cache_call("td_cache_extend", cache, stream, _vector(add, cache.max_seqs, "add", "i32", cache.device) or None,
-                _vector(cu, cache.max_seqs + 1, "cu", "i32", cache.device) or None)
+    _CACHE_EXTEND(cache, stream, _vector(add, cache.max_seqs, "add", "i32", cache.device) or None,
+                  _vector(cu, cache.max_seqs + 1, "cu", "i32", cache.device) or None)
 
 
 def cache_fork(cache: Cache, parent, stream=None):
     """Empty sequences s with parent[s] >= 0 (int32 [max_seqs]) become copies of parent[s]: full pages shared, a partly
     filled last page copied in every layer."""
-    _cache_call("td_cache_fork", cache, stream, _vector(parent, cache.max_seqs, "parent", "i32", cache.device) or None)
+    _CACHE_FORK(cache, stream, _vector(parent, cache.max_seqs, "parent", "i32", cache.device) or None)
 
 
 def cache_free(cache: Cache, release=None, stream=None):
     """Sequences with release[s] (bool or uint8 [max_seqs]; None: all) give back their pages and become empty."""
-    _cache_call("td_cache_free", cache, stream, _vector(release, cache.max_seqs, "release", "mask", cache.device) or None)
+    _CACHE_FREE(cache, stream, _vector(release, cache.max_seqs, "release", "mask", cache.device) or None)
 
 
 def cache_compact(cache: Cache, used=None, moved=None, stream=None):
     """Held pages move to the lowest numbers, tables and holders follow.  used (int32 [1]): how many they are;
     moved (int32 [pages]): every page's new number, -1 for a free one."""
-    _cache_call("td_cache_compact", cache, stream, _vector(used, 1, "used", "i32", cache.device) or None,
-                _vector(moved, cache.n_pages, "moved", "i32", cache.device) or None)
+    _CACHE_COMPACT(cache, stream, _vector(used, 1, "used", "i32", cache.device) or None,
+                   _vector(moved, cache.n_pages, "moved", "i32", cache.device) or None)
 
 
 def _rows_of_heads(t, what: str, cache: Cache, heads: Optional[int] = None):

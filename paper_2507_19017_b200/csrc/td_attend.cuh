@@ -701,19 +701,20 @@ __global__ void __launch_bounds__(kShareThreads) share_plan_kernel(CacheView c, 
     if (threadIdx.x == 0) equal = pages;
     __syncthreads();
     if (pages) {
-        const int32_t leader = seqs[lead];
-        for (uint32_t j0 = 0; j0 < pages; j0 += kShareThreads) {
-            const uint32_t j = j0 + threadIdx.x;
-            if (j < pages) {
-                const int32_t id = c.table[(size_t)leader * c.max_pages + j];
-                bool same = true;
+        // every row's pages against the leader's, some pages at a time, all rows side by side
+        const int32_t *first_row = c.table + (size_t)seqs[lead] * c.max_pages;
+        constexpr uint32_t kSome = 256;
+        for (uint32_t j0 = 0; j0 < pages; j0 += kSome) {
+            const uint32_t some = min(kSome, pages - j0), rest = rows - lead - 1;
+            const FastDiv by_some = make_fastdiv_dev(some);
 #pragma unroll 4
-                for (uint32_t r = lead + 1; r < rows; ++r)
-                    if (seqs[r] >= 0 && c.table[(size_t)seqs[r] * c.max_pages + j] != id) same = false;
-                if (!same) atomicMin(&equal, j);
+            for (uint32_t i = threadIdx.x; i < rest * some; i += kShareThreads) {
+                const uint32_t r = fast_div(i, by_some), j = j0 + i - r * some;
+                const int32_t s = seqs[lead + 1 + r];
+                if (s >= 0 && c.table[(size_t)s * c.max_pages + j] != first_row[j]) atomicMin(&equal, j);
             }
             __syncthreads();
-            const bool over = equal < j0 + kShareThreads;
+            const bool over = equal < j0 + some;
             __syncthreads();
             if (over) break;
         }
@@ -1067,17 +1068,16 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
     // Where the tokens of the tile that `ahead` is at lie: looked up by 128 threads, noted later as those of tile `number`.
     int32_t id = -1, token = 0;
     uint32_t ahead_unit = 0;
-    bool there = false;
+    bool there = false, counted = false;
     auto look = [&]() {
         there = ahead.here(end);
         id = -1;
+        counted = false;
         if (!there) return;
         ahead_unit = ahead.unit;
         token = ahead.tile * (int32_t)W::kTokens + (int32_t)threadIdx.x;
-        if (threadIdx.x < W::kTokens && token < ahead.tokens) {
-            id = c.table[(size_t)ahead.seq * c.max_pages + fast_div((uint32_t)token, c.by_page)];
-            if ((uint32_t)id >= c.n_pages && ahead_unit == 0) cache_flag(c, TD_ERR_OOB_INDEX);
-        }
+        counted = threadIdx.x < W::kTokens && token < ahead.tokens;
+        if (counted) id = c.table[(size_t)ahead.seq * c.max_pages + fast_div((uint32_t)token, c.by_page)];
         ahead.step(a, units, W::kTokens);
     };
     auto note = [&](uint32_t number) {
@@ -1085,6 +1085,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
         const bool on = (uint32_t)id < c.n_pages;
         offsets[number & 3u][threadIdx.x] =
             on ? id * a.page + (token - (int64_t)fast_div((uint32_t)token, c.by_page) * c.page_size) * a.token + (ahead_unit % a.kv_heads) * a.head : -1;
+        if (counted && !on && ahead_unit == 0) cache_flag(c, TD_ERR_OOB_INDEX);
         const uint32_t which = __ballot_sync(kFullMask, on);
         if (lane == 0) counts[number & 7u][warp] = which;
     };

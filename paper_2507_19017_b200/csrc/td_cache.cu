@@ -26,7 +26,7 @@ CacheLayout cache_layout(uint32_t n_pages, uint32_t max_seqs) {
     L.tile_pages = take(kMaxTiles * 4);
     L.tile_need = take(kMaxTiles * 8);
     L.tile_add = take(kMaxTiles * 8);
-    L.moves = take(4);
+    L.moves = take(8);
     L.need_before = take((size_t)max_seqs * 8);
     L.add_before = take((size_t)max_seqs * 4);
     L.first = take((size_t)max_seqs * 4);

@@ -43,7 +43,7 @@ struct CacheScratch {
     int32_t *given;                                           // [sequences] the page a fork is given, -1: none
     uint32_t *from, *to;                                      // [pages] compaction: source by rank, free number by rank
     uint32_t *rank;                                           // [pages] rank of a source among the held pages
-    uint32_t *moves;                                          // how many pages move
+    uint32_t *moves;                                          // how many pages move, how many are held
     uint32_t page_steps, seq_steps;                           // steps of kPageStep pages (kSeqStep sequences) per tile
     uint32_t page_tiles, seq_tiles;
 };
@@ -183,63 +183,92 @@ __global__ void __launch_bounds__(kCacheThreads) cache_count_kernel(CacheView c,
     }
 }
 
-// The sums of the tiles before `mine` and of all, by the whole block.
+// The sums of the tiles before `mine` and of all.
+struct TileSum {
+    unsigned long long before, all;
+};
 template <typename T>
-__device__ __forceinline__ unsigned long long tiles_before(const T *sums, uint32_t n, uint32_t mine, unsigned long long *room,
-                                                           unsigned long long &total) {
-    unsigned long long part = 0, all = 0, before;
+__device__ __forceinline__ TileSum tile_part(const T *sums, uint32_t n, uint32_t mine) {          // a thread's share
+    TileSum t{0, 0};
     for (uint32_t i = threadIdx.x; i < n; i += kCacheThreads) {
         const unsigned long long v = sums[i];
-        all += v;
-        part += i < mine ? v : 0;
+        t.all += v;
+        t.before += i < mine ? v : 0;
     }
-    block_before(part, room, before);
-    block_before(all, room, total);
-    return before;
+    return t;
+}
+template <int kSums>
+__device__ __forceinline__ void tile_sums(TileSum (&t)[kSums], unsigned long long (*room)[2 * kSums]) {          // the block's, one row of room per warp
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+#pragma unroll
+        for (int d = 16; d; d /= 2) {
+            t[k].before += __shfl_xor_sync(kFullMask, t[k].before, d);
+            t[k].all += __shfl_xor_sync(kFullMask, t[k].all, d);
+        }
+        if (lane == 0) {
+            room[warp][2 * k] = t[k].before;
+            room[warp][2 * k + 1] = t[k].all;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+        t[k] = TileSum{0, 0};
+#pragma unroll
+        for (uint32_t w = 0; w < kCacheThreads / 32; ++w) {
+            t[k].before += room[w][2 * k];
+            t[k].all += room[w][2 * k + 1];
+        }
+    }
 }
 
 // Blocks of page tiles hand out their free pages; blocks of sequence tiles set lengths and cu; fork: further blocks, a warp per
 // sequence, share the full pages.
 template <Give kGive>
 __global__ void __launch_bounds__(kCacheThreads) cache_assign_kernel(CacheView c, CacheScratch w, const int32_t *ask, int32_t *cu) {
-    __shared__ unsigned long long room[kCacheThreads / 32];
+    __shared__ unsigned long long room[kCacheThreads / 32], sums[kCacheThreads / 32][6];
     __shared__ unsigned long long tile_need[kMaxTiles];       // pages needed ahead of each sequence tile
+    __shared__ uint32_t given[kPageStep];                     // free pages of a step, in order
     griddep_launch_dependents();
     griddep_wait();
-    unsigned long long need_total, add_total, page_total;
     const uint32_t seq_block = blockIdx.x - w.page_tiles;     // for blocks behind the page tiles
     const bool page_block = blockIdx.x < w.page_tiles;
-    const unsigned long long add_base = tiles_before(w.tile_add, w.seq_tiles, page_block ? 0u : seq_block, room, add_total);
-    const unsigned long long page_base = tiles_before(w.tile_pages, w.page_tiles, page_block ? blockIdx.x : 0u, room, page_total);
-    tiles_before(w.tile_need, w.seq_tiles, 0u, room, need_total);
+    TileSum t[3] = {tile_part(w.tile_need, w.seq_tiles, 0u), tile_part(w.tile_add, w.seq_tiles, page_block ? 0u : seq_block),
+                    tile_part(w.tile_pages, w.page_tiles, page_block ? blockIdx.x : 0u)};
+    tile_sums<3>(t, sums);
+    const unsigned long long need_total = t[0].all, add_total = t[1].all, add_base = t[1].before, page_total = t[2].all;
     const bool enough = need_total <= page_total && add_total < (1ull << 31);
     if (page_block) {
-        if (!enough || page_base >= need_total) return;
+        unsigned long long base = t[2].before;
+        if (!enough || base >= need_total) return;
         unsigned long long before = 0;
         for (uint32_t t0 = 0; t0 < w.seq_tiles; t0 += kCacheThreads) {
-            const uint32_t t = t0 + threadIdx.x;
+            const uint32_t i = t0 + threadIdx.x;
             unsigned long long step;
-            const unsigned long long b = block_before(t < w.seq_tiles ? w.tile_need[t] : 0ull, room, step);
-            if (t < w.seq_tiles) tile_need[t] = before + b;
+            const unsigned long long b = block_before(i < w.seq_tiles ? w.tile_need[i] : 0ull, room, step);
+            if (i < w.seq_tiles) tile_need[i] = before + b;
             before += step;
         }
-        __syncthreads();
-        unsigned long long base = page_base;
         for (uint32_t k = 0; k < w.page_steps && base < need_total; ++k) {
             const unsigned long long page = ((unsigned long long)blockIdx.x * w.page_steps + k) * kPageStep + threadIdx.x * kPagesPerThread;
             uint32_t bits = page < c.n_pages ? page_bits<false>(c, (uint32_t)page) : 0u;
-            unsigned long long step;
-            unsigned long long r = base + block_before((unsigned long long)__popc(bits), room, step);
-            base += step;
-            for (; bits && r < need_total; bits &= bits - 1, ++r) {
-                const uint32_t p = (uint32_t)page + (uint32_t)__ffs(bits) - 1;
+            uint32_t step;
+            uint32_t at = block_before((uint32_t)__popc(bits), reinterpret_cast<uint32_t *>(room), step);
+            for (; bits; bits &= bits - 1) given[at++] = (uint32_t)page + (uint32_t)__ffs(bits) - 1;
+            __syncthreads();
+            // a thread per page that is handed out: whose it is takes a search, so they go side by side
+            const uint32_t some = (uint32_t)min((unsigned long long)step, need_total - base);
+            for (uint32_t i = threadIdx.x; i < some; i += kCacheThreads) {
+                const unsigned long long r = base + i;
                 uint32_t lo = 0, hi = w.seq_tiles;            // the last tile with no more than r ahead of it
                 while (hi - lo > 1) {
                     const uint32_t mid = (lo + hi) / 2;
                     if (tile_need[mid] <= r) lo = mid; else hi = mid;
                 }
                 const unsigned long long local = r - tile_need[lo];
-                const uint32_t per_tile = w.seq_steps * kSeqStep;
+                const uint32_t per_tile = w.seq_steps * kSeqStep, p = given[i];
                 uint32_t s = lo * per_tile, end = min(c.max_seqs - s, per_tile) + s;
                 while (end - s > 1) {                         // and the last sequence of it
                     const uint32_t mid = s + (end - s) / 2;
@@ -250,6 +279,7 @@ __global__ void __launch_bounds__(kCacheThreads) cache_assign_kernel(CacheView c
                 c.holders[p] = 1;
                 if (kGive == Give::kFork) w.given[s] = (int32_t)p;
             }
+            base += step;
         }
         return;
     }
@@ -327,12 +357,15 @@ __global__ void __launch_bounds__(kCacheThreads) cache_rank_kernel(CacheView c, 
     __shared__ unsigned long long room[kCacheThreads / 32];
     griddep_launch_dependents();
     griddep_wait();
-    unsigned long long total;
-    unsigned long long base = tiles_before(w.tile_pages, w.page_tiles, blockIdx.x, room, total);
-    const uint32_t U = (uint32_t)total;
+    __shared__ unsigned long long sums[kCacheThreads / 32][2];
+    TileSum t[1] = {tile_part(w.tile_pages, w.page_tiles, blockIdx.x)};
+    tile_sums<1>(t, sums);
+    unsigned long long base = t[0].before;
+    const uint32_t U = (uint32_t)t[0].all;
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         if (used) *used = U;
-        if (U == c.n_pages) *w.moves = 0;
+        w.moves[1] = U;
+        if (U == c.n_pages) w.moves[0] = 0;
     }
     for (uint32_t k = 0; k < w.page_steps; ++k) {
         const unsigned long long page = ((unsigned long long)blockIdx.x * w.page_steps + k) * kPageStep + threadIdx.x * kPagesPerThread;
@@ -342,7 +375,7 @@ __global__ void __launch_bounds__(kCacheThreads) cache_rank_kernel(CacheView c, 
         base += step;
         for (uint32_t i = 0; i < kPagesPerThread && page + i < c.n_pages; ++i) {
             const uint32_t p = (uint32_t)page + i;
-            if (p == U) *w.moves = U - b;
+            if (p == U) w.moves[0] = U - b;
             if (bits >> i & 1u) {
                 if (p >= U) {
                     w.from[b] = p;
@@ -425,12 +458,9 @@ __global__ void __launch_bounds__(kCacheThreads) cache_move_kernel(CacheView c, 
                                                                    uint32_t page_blocks) {
     griddep_launch_dependents();
     griddep_wait();
-    const uint32_t M = *w.moves;
+    const uint32_t M = w.moves[0];
     if (M == 0) return;
-    unsigned long long total;
-    __shared__ unsigned long long room[kCacheThreads / 32];
-    tiles_before(w.tile_pages, w.page_tiles, 0u, room, total);
-    const uint32_t U = (uint32_t)total, kept = U - M;
+    const uint32_t U = w.moves[1], kept = U - M;
     if (blockIdx.x < seq_blocks) {
         const uint32_t s = blockIdx.x * (kCacheThreads / 32) + threadIdx.x / 32, lane = threadIdx.x & 31u;
         if (s >= c.max_seqs) return;
