@@ -1189,8 +1189,15 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
             l = 0.0f;
         }
         look();
+        // Half of the warps copy before they weigh and half behind it, so that the one's copies go with the other's arithmetic.
+        if (i > 0) fine &= product_wait(bar + 16, (i - 1) & 1u);          // results of the last tile: its values' place is free
+        fine &= product_wait(bar + 8 * (i & 1u), i >> 1 & 1u);            // scores of this tile: its keys' place is free
+        auto copies = [&]() {
+            bring(a.keys, keys + i % W::kKeys * W::kSide, i + 3);
+            bring(a.values, values + (i + 1) % W::kValues * W::kSide, i + 1);
+        };
+        if (half == 0) copies();
         // scores to weights
-        fine &= product_wait(bar + 8 * (i & 1u), i >> 1 & 1u);
         __syncwarp();
         tensor_after_sync();
         float x[64];
@@ -1237,9 +1244,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
                 for (int k = 0; k < 64; ++k) past |= !(x[k] == -CUDART_INF_F);
             }
         }
-        if (i > 0) fine &= product_wait(bar + 16, (i - 1) & 1u);          // results of the last tile: its values' place is free
-        bring(a.keys, keys + i % W::kKeys * W::kSide, i + 3);
-        bring(a.values, values + (i + 1) % W::kValues * W::kSide, i + 1);
+        if (half == 1) copies();
         copy_commit();
         copy_wait<1>();                                       // values i
         shared_for_products();

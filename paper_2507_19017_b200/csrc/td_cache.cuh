@@ -313,6 +313,10 @@ __global__ void __launch_bounds__(kCacheThreads) cache_assign_kernel(CacheView c
     }
 }
 
+constexpr uint32_t kClusterBlocks = 8;                        // of a compaction of few pages
+__device__ __forceinline__ void cluster_sync() {              // what the blocks wrote before it they all see behind it
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 // A warp per sequence.
 __global__ void __launch_bounds__(kCacheThreads) cache_free_kernel(CacheView c, const uint8_t *release) {
     griddep_launch_dependents();
@@ -338,37 +342,33 @@ __global__ void __launch_bounds__(kCacheThreads) cache_free_kernel(CacheView c, 
 }
 
 // ---- compaction ----
-__global__ void __launch_bounds__(kCacheThreads) cache_held_kernel(CacheView c, CacheScratch w) {
+__device__ __forceinline__ void held_block(const CacheView &c, const CacheScratch &w, uint32_t block) {
     __shared__ unsigned long long room[kCacheThreads / 32];
-    griddep_launch_dependents();
-    griddep_wait();
     unsigned long long count = 0, total;
     for (uint32_t k = 0; k < w.page_steps; ++k) {
-        const unsigned long long page = ((unsigned long long)blockIdx.x * w.page_steps + k) * kPageStep + threadIdx.x * kPagesPerThread;
+        const unsigned long long page = ((unsigned long long)block * w.page_steps + k) * kPageStep + threadIdx.x * kPagesPerThread;
         if (page < c.n_pages) count += __popc(page_bits<true>(c, (uint32_t)page));
     }
     block_before(count, room, total);
-    if (threadIdx.x == 0) w.tile_pages[blockIdx.x] = (uint32_t)total;
+    if (threadIdx.x == 0) w.tile_pages[block] = (uint32_t)total;
 }
 
 // With U pages held and b(p) of them before page p: the held pages from U on are those of ranks U - M .. U - 1 among the held, where
 // M = U - b(U) is how many free numbers lie below U; free number f has rank f - b(f) among the free.
-__global__ void __launch_bounds__(kCacheThreads) cache_rank_kernel(CacheView c, CacheScratch w, uint32_t *used, int32_t *moved) {
+__device__ __forceinline__ void rank_block(const CacheView &c, const CacheScratch &w, uint32_t *used, int32_t *moved, uint32_t block) {
     __shared__ unsigned long long room[kCacheThreads / 32];
-    griddep_launch_dependents();
-    griddep_wait();
     __shared__ unsigned long long sums[kCacheThreads / 32][2];
-    TileSum t[1] = {tile_part(w.tile_pages, w.page_tiles, blockIdx.x)};
+    TileSum t[1] = {tile_part(w.tile_pages, w.page_tiles, block)};
     tile_sums<1>(t, sums);
     unsigned long long base = t[0].before;
     const uint32_t U = (uint32_t)t[0].all;
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (block == 0 && threadIdx.x == 0) {
         if (used) *used = U;
         w.moves[1] = U;
         if (U == c.n_pages) w.moves[0] = 0;
     }
     for (uint32_t k = 0; k < w.page_steps; ++k) {
-        const unsigned long long page = ((unsigned long long)blockIdx.x * w.page_steps + k) * kPageStep + threadIdx.x * kPagesPerThread;
+        const unsigned long long page = ((unsigned long long)block * w.page_steps + k) * kPageStep + threadIdx.x * kPagesPerThread;
         const uint32_t bits = page < c.n_pages ? page_bits<true>(c, (uint32_t)page) : 0u;
         unsigned long long step;
         uint32_t b = (uint32_t)(base + block_before((unsigned long long)__popc(bits), room, step));
@@ -390,6 +390,24 @@ __global__ void __launch_bounds__(kCacheThreads) cache_rank_kernel(CacheView c, 
             }
         }
     }
+}
+
+__global__ void __launch_bounds__(kCacheThreads) cache_held_kernel(CacheView c, CacheScratch w) {
+    griddep_launch_dependents();
+    griddep_wait();
+    held_block(c, w, blockIdx.x);
+}
+__global__ void __launch_bounds__(kCacheThreads) cache_rank_kernel(CacheView c, CacheScratch w, uint32_t *used, int32_t *moved) {
+    griddep_launch_dependents();
+    griddep_wait();
+    rank_block(c, w, used, moved, blockIdx.x);
+}
+__global__ void __launch_bounds__(kCacheThreads) cache_held_rank_kernel(CacheView c, CacheScratch w, uint32_t *used, int32_t *moved) {          // one cluster
+    griddep_launch_dependents();
+    griddep_wait();
+    for (uint32_t b = blockIdx.x; b < w.page_tiles; b += gridDim.x, __syncthreads()) held_block(c, w, b);
+    cluster_sync();
+    for (uint32_t b = blockIdx.x; b < w.page_tiles; b += gridDim.x, __syncthreads()) rank_block(c, w, used, moved, b);
 }
 
 // ---- contents ----
