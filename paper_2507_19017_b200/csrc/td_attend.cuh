@@ -1338,62 +1338,95 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
     join_shares<W::kDim>(a, line, cut_in, cut_out, &last);
 }
 
-constexpr uint32_t kFloatThreads = 256;
-
-// A warp per row and head; a token at a time.
-template <typename T>
+// ---- a cache of float ----
+// Float keys and values would lose 13 bits to the matrix instructions, so they are multiplied as they are: a block per row and 8 heads
+// of a key head, a token at a time per warp (a lane has every 32nd column), the warps' results joined at the end.
+constexpr uint32_t kFloatThreads = 256, kFloatHeads = 8, kFloatColumns = 8;          // columns of a lane: dim <= 256
 __global__ void __launch_bounds__(kFloatThreads) attend_float_kernel(CacheView c, AttendArgs a) {
+    constexpr uint32_t kWarps = kFloatThreads / 32;
+    __shared__ float values[kWarps][32 * kFloatColumns], ml[kWarps][2];
     griddep_launch_dependents();
     griddep_wait();
-    const uint32_t lane = threadIdx.x & 31u;
-    const unsigned long long unit = (unsigned long long)blockIdx.x * (kFloatThreads / 32) + threadIdx.x / 32;
-    if (unit >= (unsigned long long)a.n_rows * a.n_heads) return;
-    const uint32_t row = (uint32_t)(unit / a.n_heads), h = (uint32_t)(unit - (unsigned long long)row * a.n_heads), kv = h / a.ratio;
-    const int32_t s = a.seqs ? a.seqs[row] : (int32_t)row;
-    int32_t n = 0;
-    if (s >= 0) {
-        if ((uint32_t)s < c.max_seqs) {
-            n = c.length[s];
-            if (!length_ok(c, n)) { n = 0; if (lane == 0) cache_flag(c, TD_ERR_BAD_LENGTH); }
-        } else if (lane == 0) {
-            cache_flag(c, TD_ERR_OOB_INDEX);
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t row = (uint32_t)(blockIdx.x / a.units), unit = blockIdx.x - row * a.units;
+    uint32_t kv, first;
+    const uint32_t heads = heads_of<kFloatHeads>(a, unit, kv, first);
+    const Span span = span_of<false>(c, a, row, unit == 0 && threadIdx.x == 0);
+    const float *q = static_cast<const float *>(a.q) + row * a.q_row + first * a.q_head;
+    float qv[kFloatHeads][kFloatColumns], o[kFloatHeads][kFloatColumns], m[kFloatHeads], l[kFloatHeads];
+#pragma unroll
+    for (uint32_t h = 0; h < kFloatHeads; ++h) {
+        m[h] = -CUDART_INF_F;
+        l[h] = 0.0f;
+#pragma unroll
+        for (uint32_t i = 0; i < kFloatColumns; ++i) {
+            o[h][i] = 0.0f;
+            qv[h][i] = h < heads && lane + 32 * i < a.dim ? q[h * a.q_head + lane + 32 * i] * a.scale2 : 0.0f;
         }
     }
-    const T *q = static_cast<const T *>(a.q) + row * a.q_row + h * a.q_head;
-    float qv[8], o[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t d = lane + 32 * i;
-        qv[i] = d < a.dim ? Elem<T>::load(q + d) * a.scale : 0.0f;
-        o[i] = 0.0f;
-    }
-    float m = -CUDART_INF_F, sum = 0.0f;
-    for (int32_t j = a.window && (uint32_t)n > a.window ? n - (int32_t)a.window : 0; j < n; ++j) {
+    for (int32_t j = span.lo + (int32_t)warp; j < span.n; j += kWarps) {
         const uint32_t page = fast_div((uint32_t)j, c.by_page);
-        const int32_t id = c.table[(size_t)s * c.max_pages + page];
-        if ((uint32_t)id >= c.n_pages) { if (lane == 0) cache_flag(c, TD_ERR_OOB_INDEX); continue; }
+        const int32_t id = c.table[(size_t)span.s * c.max_pages + page];
+        if ((uint32_t)id >= c.n_pages) {
+            if (unit == 0 && lane == 0) cache_flag(c, TD_ERR_OOB_INDEX);
+            continue;
+        }
         const int64_t at = id * a.page + (j - (int64_t)page * c.page_size) * a.token + kv * a.head;
-        const T *k = static_cast<const T *>(a.keys) + at, *v = static_cast<const T *>(a.values) + at;
-        float x = 0.0f;
+        float k[kFloatColumns], v[kFloatColumns], x[kFloatHeads];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (lane + 32 * i < a.dim) x = fmaf(qv[i], Elem<T>::load(k + lane + 32 * i), x);
+        for (uint32_t i = 0; i < kFloatColumns; ++i) {
+            const bool on = lane + 32 * i < a.dim;
+            k[i] = on ? static_cast<const float *>(a.keys)[at + lane + 32 * i] : 0.0f;
+            v[i] = on ? static_cast<const float *>(a.values)[at + lane + 32 * i] : 0.0f;
+        }
 #pragma unroll
-        for (int d = 16; d; d /= 2) x += __shfl_xor_sync(kFullMask, x, d);
-        if (x == -CUDART_INF_F) continue;
-        const float top = max_nan(x, m), keep = expf(m - top), p = expf(x - top);
-        sum = sum * keep + p;
-        m = top;
+        for (uint32_t h = 0; h < kFloatHeads; ++h) {
+            x[h] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (lane + 32 * i < a.dim) o[i] = fmaf(p, Elem<T>::load(v + lane + 32 * i), o[i] * keep);
+            for (uint32_t i = 0; i < kFloatColumns; ++i) x[h] = fmaf(qv[h][i], k[i], x[h]);
+        }
+#pragma unroll
+        for (int d = 16; d; d /= 2)
+#pragma unroll
+            for (uint32_t h = 0; h < kFloatHeads; ++h) x[h] += __shfl_xor_sync(kFullMask, x[h], d);
+#pragma unroll
+        for (uint32_t h = 0; h < kFloatHeads; ++h) {
+            if (x[h] == -CUDART_INF_F) continue;
+            if (!(x[h] <= m[h])) {                            // a new maximum, or NaN, which stays
+                const float top = max_nan(x[h], m[h]), keep = exp2f(m[h] - top);
+                l[h] *= keep;
+                m[h] = top;
+#pragma unroll
+                for (uint32_t i = 0; i < kFloatColumns; ++i) o[h][i] *= keep;
+            }
+            const float p = exp2f(x[h] - m[h]);
+            l[h] += p;
+#pragma unroll
+            for (uint32_t i = 0; i < kFloatColumns; ++i) o[h][i] = fmaf(p, v[i], o[h][i]);
+        }
     }
-    T *out = static_cast<T *>(a.out) + row * a.out_row + h * a.out_head;
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (lane + 32 * i < a.dim) out[lane + 32 * i] = Elem<T>::from(o[i] * inv);
-    if (a.lse && lane == 0) a.lse[(size_t)row * a.n_heads + h] = sum == 0.0f ? -CUDART_INF_F : m + logf(sum);
+    for (uint32_t h = 0; h < kFloatHeads; ++h) {
+        if (h >= heads) break;
+#pragma unroll
+        for (uint32_t i = 0; i < kFloatColumns; ++i) values[warp][lane + 32 * i] = o[h][i];
+        if (lane == 0) {
+            ml[warp][0] = m[h];
+            ml[warp][1] = l[h];
+        }
+        __syncthreads();
+        float top = -CUDART_INF_F, sum = 0.0f, x = 0.0f;
+        for (uint32_t w = 0; w < kWarps; ++w) top = max_nan(top, ml[w][0]);
+        for (uint32_t w = 0; w < kWarps; ++w) {
+            const float e = exp2f(ml[w][0] - (top == -CUDART_INF_F ? 0.0f : top));
+            sum = fmaf(ml[w][1], e, sum);
+            x = fmaf(values[w][threadIdx.x], e, x);
+        }
+        if (threadIdx.x < a.dim) static_cast<float *>(a.out)[row * a.out_row + (first + h) * a.out_head + threadIdx.x] = sum == 0.0f ? 0.0f : x / sum;
+        if (a.lse && threadIdx.x == 0)
+            a.lse[(size_t)row * a.n_heads + first + h] = sum == 0.0f ? -CUDART_INF_F : (top + log2f(sum)) * 0.69314718055994531f;
+        __syncthreads();
+    }
 }
 
 }  // namespace td

@@ -127,7 +127,7 @@ bool apart(uint32_t rows, int64_t row, uint32_t heads, int64_t head, int64_t dim
 constexpr uint32_t kWarps = kCacheThreads / 32;
 uint32_t warp_blocks(uint32_t n) { return (n + kWarps - 1) / kWarps; }
 
-int result(cudaError_t rc) { return rc == cudaSuccess ? TD_OK : TD_ECUDA; }
+int result(cudaError_t rc) { return rc == cudaSuccess ? TD_OK : rc == cudaErrorInvalidValue ? TD_EINVAL : TD_ECUDA; }
 
 template <Give kGive>
 cudaError_t run_give(const CacheView &v, const CacheScratch &w, const int32_t *ask, int32_t *cu, uint32_t sharing, cudaStream_t st) {
@@ -228,9 +228,12 @@ cudaError_t run_attend(const CacheView &v, const AttendArgs &k, cudaStream_t st)
     if (k.dim <= 192) return run_attend<T, 12>(v, k, st);
     return run_attend<T, 16>(v, k, st);
 }
-cudaError_t run_attend_float(const CacheView &v, const AttendArgs &k, cudaStream_t st) {
-    const uint64_t units = (uint64_t)k.n_rows * k.n_heads, blocks = (units + kFloatThreads / 32 - 1) / (kFloatThreads / 32);
-    return launch(attend_float_kernel<float>, blocks, kFloatThreads, st, 1u, v, k);
+cudaError_t run_attend_float(const CacheView &v, AttendArgs k, cudaStream_t st) {
+    k.per_kv = (k.ratio + kFloatHeads - 1) / kFloatHeads;
+    k.units = k.kv_heads * k.per_kv;
+    k.by_per_kv = make_fastdiv(k.per_kv);
+    const uint64_t blocks = (uint64_t)k.n_rows * k.units;
+    return blocks > kMaxGrid ? cudaErrorInvalidValue : launch(attend_float_kernel, blocks, kFloatThreads, st, 1u, v, k);
 }
 
 }  // namespace

@@ -648,3 +648,135 @@ def test_two_attentions_at_once():
             td.cache_attention(b, cache, q, window=w, stream=s)
     torch.cuda.synchronize()
     assert all(torch.equal(b.out, w) for b, w in zip(both, want))
+
+
+SHARED = [(4, 2, 64, 4, "bf16"), (32, 2, 128, 4, "bf16"), (20, 4, 96, 8, "f16"), (48, 3, 64, 5, "f16"), (32, 4, 256, 4, "bf16")]
+
+
+@pytest.mark.parametrize("heads,kv,dim,group,dtype", SHARED)
+def test_extreme_scores_among_common_tokens(heads, kv, dim, group, dtype):
+    """Infinities, NaN and scores of thousands in the tokens that a group has in common: as without groups, where every row takes
+    them for itself (each within its bounds)."""
+    page, rows = 16, 2 * group
+    shared = [400] * group + [144] * group
+    lengths = np.array(shared) + np.arange(rows) * 7 + 1
+    for change in ("none", "large", "minus", "all minus", "nan", "plus"):
+        cache, q = attention_case(lengths, heads, kv, dim, page, dtype, group=group, shared=shared, seed=heads, q_scale=300.0 if change == "large" else 1.0)
+        q[..., 5] = -1.0
+        k0, first = cache.keys[0], cache.table[0].long()
+        if change == "minus":                                         # every third common token has weight 0
+            at = torch.arange(0, 400, 3, device="cuda")
+            k0[first[at // page], at % page, :, 5] = math.inf
+        elif change == "all minus":                                   # all of the first group's
+            at = torch.arange(400, device="cuda")
+            k0[first[at // page], at % page, :, 5] = math.inf
+        elif change == "nan":
+            k0[first[9], 3, kv - 1, 2] = math.nan
+        elif change == "plus":
+            k0[first[20], 0, 0, 5] = -math.inf
+        got = []
+        for g in (1, group):
+            out = td.AttentionBuffers(rows, heads, dim, q.dtype, lse=True)
+            td.cache_attention(out, cache, q, group=g)
+            got.append((out.out.double(), out.lse.double()))
+        (a, la), (b, lb) = got
+        assert torch.equal(a.isnan(), b.isnan()) and torch.equal(la.isnan(), lb.isnan())
+        assert a.isnan().any() == (change in ("nan", "plus"))
+        if change in ("none", "large"):
+            o, lse, bound, lse_bound = exact_attention(cache, q)
+            assert ((b - o).abs() <= bound).all() and ((lb - lse).abs() <= lse_bound).all()
+        fine = ~a.isnan()
+        half = HALF[dtype]
+        assert ((a - b)[fine].abs() <= (4 * half + 1e-3) * 5.0).all()          # values are normal numbers: |v| <= 5 for nearly all, |o| less
+        assert ((la - lb)[~la.isnan()].abs() <= 1e-3 + 1e-4 * la[~la.isnan()].abs()).all()
+
+
+@pytest.mark.parametrize("heads,kv,dim,group,dtype", SHARED)
+def test_common_pages_that_are_not_pages(heads, kv, dim, group, dtype):
+    """A number outside the pool in the common part of the tables: its tokens are passed over by all rows, and noted."""
+    page, rows = 16, group
+    lengths = 160 + np.arange(rows)
+    cache, q = attention_case(lengths, heads, kv, dim, page, dtype, group=group, shared=[160] * rows, poison=False)
+    cache.table[:, 3], cache.table[:, 7] = -1, cache.n_pages
+    out = td.AttentionBuffers(rows, heads, dim, q.dtype)
+    td.cache_attention(out, cache, q, group=group)
+    assert cache.status.item() == td.ERR_OOB_INDEX
+    keep = torch.tensor([j for j in range(160 + rows) if j // page not in (3, 7)], device="cuda")
+    for r in range(rows):
+        at = keep[keep < lengths[r]]
+        k, v = (t[0][cache.table[r].long()[at // page], at % page].double().transpose(0, 1) for t in (cache.keys, cache.values))
+        p = torch.softmax(q[r].double().view(kv, heads // kv, dim) @ k.transpose(1, 2) * dim ** -0.5, 2)
+        assert ((out.out[r].double() - (p @ v).reshape(heads, dim)).abs() <= (4 * HALF[dtype] + 1e-4) * (p @ v.abs()).reshape(heads, dim)).all()
+
+
+@pytest.mark.parametrize("heads,kv,dim,page,group,dtype", [(8, 2, 64, 16, 4, "bf16"), (28, 4, 128, 8, 8, "bf16"), (5, 1, 80, 24, 3, "f16"), (4, 4, 16, 16, 4, "f32")])
+def test_a_rollout_of_groups(heads, kv, dim, page, group, dtype):
+    """Generation as a state would run it: prompts come in and are written, their responses forked, every step makes room, writes
+    and attends; responses end at different lengths and are freed, new prompts take their place, the pool is compacted now and then.
+    Attention is compared with every sequence's own keys and values, kept apart from the cache."""
+    prompts, n = 3, 3 * group
+    g = np.random.default_rng(heads)
+    t = DTYPES[dtype]
+    cache = td.Cache.empty(1, n * (260 // page + 2), page, kv, dim, n, 260 // page + 2, t, heads_first=page != 24)
+    cu = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    used = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = td.AttentionBuffers(n, heads, dim, t, lse=True)
+    gen = torch.Generator(device="cuda").manual_seed(heads)
+    kept = [None] * n                                                 # each sequence's keys and values, [tokens, kv, dim]
+    left = [0] * n
+
+    def rows(count):
+        return tuple(torch.randn(count, kv, dim, generator=gen, device="cuda").to(t) for _ in range(2))
+
+    def admit(which):
+        add = np.zeros(n, int)
+        for p in which:
+            add[p * group] = g.integers(1, 200)
+        td.cache_extend(cache, ints(add), cu)
+        k, v = rows(int(add.sum()))
+        td.cache_write(cache, k, v, cu)
+        parent, at = np.full(n, -1), 0
+        for p in which:
+            m = int(add[p * group])
+            for s in range(p * group, (p + 1) * group):
+                kept[s] = (k[at:at + m], v[at:at + m])
+                left[s] = int(g.integers(1, 25))
+                if s != p * group:
+                    parent[s] = p * group
+            at += m
+        td.cache_fork(cache, ints(parent))
+
+    admit(range(prompts))
+    for step in range(40):
+        add = ints([1 if x is not None else 0 for x in kept])
+        td.cache_extend(cache, add, cu)
+        live = [s for s in range(n) if kept[s] is not None]
+        k, v = rows(len(live))
+        td.cache_write(cache, k, v, cu)
+        for i, s in enumerate(live):
+            kept[s] = tuple(torch.cat([old, new[i:i + 1]]) for old, new in zip(kept[s], (k, v)))
+        q = torch.randn(n, heads, dim, generator=gen, device="cuda").to(t)
+        seqs = ints([s if kept[s] is not None else -1 for s in range(n)])
+        td.cache_attention(out, cache, q, seqs, group=group)
+        for s in range(n):
+            if kept[s] is None:
+                assert not out.out[s].any()
+                continue
+            ks, vs = (x.double().transpose(0, 1) for x in kept[s])
+            p = torch.softmax(q[s].double().view(kv, heads // kv, dim) @ ks.transpose(1, 2) * dim ** -0.5, 2)
+            bound = (4 * HALF[dtype] + 1e-4) * (p @ vs.abs()).reshape(heads, dim)
+            assert ((out.out[s].double() - (p @ vs).reshape(heads, dim)).abs() <= bound).all()
+        release = np.zeros(n, bool)
+        for s in live:
+            left[s] -= 1
+            if left[s] == 0:
+                release[s], kept[s] = True, None
+        td.cache_free(cache, ints(release, torch.bool))
+        gone = [p for p in range(prompts) if all(kept[s] is None for s in range(p * group, (p + 1) * group))]
+        if gone and step < 30:
+            admit(gone)
+        if step % 7 == 6:
+            td.cache_compact(cache, used)
+            assert used.item() == int((cache.holders > 0).sum()) and not (cache.holders[used.item():] != 0).any()
+    td.cache_free(cache)
+    assert cache.status.item() == 0 and not cache.holders.any() and not cache.length.any()
