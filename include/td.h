@@ -689,8 +689,8 @@ int td_cache_write(const td_cache_write_args *args, void *stream);
 /* Attention of one new token per row over the cache: with kv = h / (n_heads / cache->n_heads),
  *   x_j = scale * q[r][h] . K[j][kv],  lse = ln sum_j e^(x_j),  out[r][h] = sum_j e^(x_j - lse) V[j][kv]
  * over the tokens j of sequence seqs[r] (seqs == NULL: r), with window > 0 its last `window` ones only.
- * Scores, their maximum and both sums are float; the weights e^(x_j - max) are rounded to the cache's
- * type for the product with V (bfloat16, half).  A row without a token (seqs[r] < 0, length 0, or every score -inf)
+ * Scores, their maximum and both sums are float; the weights e^(x_j - reference) are rounded to the cache's
+ * type for the product with V (bfloat16, half), the reference being the maximum or up to 2^8 times less.  A row without a token (seqs[r] < 0, length 0, or every score -inf)
  * has out 0 and lse -inf; seqs[r] >= max_seqs is the same with TD_ERR_OOB_INDEX.  A score of -inf has weight 0; NaN or +inf
  * among a row's scores makes that row's head NaN.  What lies in a page behind a sequence's last token is never used.
  * group > 1: rows i * group .. i * group + group - 1 are likely to share leading pages, as the
