@@ -658,17 +658,17 @@ def test_extreme_scores_among_common_tokens(heads, kv, dim, group, dtype):
     """Infinities, NaN and scores of thousands in the tokens that a group has in common: as without groups, where every row takes
     them for itself (each within its bounds)."""
     page, rows = 16, 2 * group
-    shared = [400] * group + [144] * group
+    shared = [1200] * group + [720] * group                           # enough for the kernels that take common tokens once
     lengths = np.array(shared) + np.arange(rows) * 7 + 1
     for change in ("none", "large", "minus", "all minus", "nan", "plus"):
         cache, q = attention_case(lengths, heads, kv, dim, page, dtype, group=group, shared=shared, seed=heads, q_scale=300.0 if change == "large" else 1.0)
         q[..., 5] = -1.0
         k0, first = cache.keys[0], cache.table[0].long()
         if change == "minus":                                         # every third common token has weight 0
-            at = torch.arange(0, 400, 3, device="cuda")
+            at = torch.arange(0, 1200, 3, device="cuda")
             k0[first[at // page], at % page, :, 5] = math.inf
         elif change == "all minus":                                   # all of the first group's
-            at = torch.arange(400, device="cuda")
+            at = torch.arange(1200, device="cuda")
             k0[first[at // page], at % page, :, 5] = math.inf
         elif change == "nan":
             k0[first[9], 3, kv - 1, 2] = math.nan
@@ -695,13 +695,13 @@ def test_extreme_scores_among_common_tokens(heads, kv, dim, group, dtype):
 def test_common_pages_that_are_not_pages(heads, kv, dim, group, dtype):
     """A number outside the pool in the common part of the tables: its tokens are passed over by all rows, and noted."""
     page, rows = 16, group
-    lengths = 160 + np.arange(rows)
-    cache, q = attention_case(lengths, heads, kv, dim, page, dtype, group=group, shared=[160] * rows, poison=False)
+    lengths = 800 + np.arange(rows)
+    cache, q = attention_case(lengths, heads, kv, dim, page, dtype, group=group, shared=[800] * rows, poison=False)
     cache.table[:, 3], cache.table[:, 7] = -1, cache.n_pages
     out = td.AttentionBuffers(rows, heads, dim, q.dtype)
     td.cache_attention(out, cache, q, group=group)
     assert cache.status.item() == td.ERR_OOB_INDEX
-    keep = torch.tensor([j for j in range(160 + rows) if j // page not in (3, 7)], device="cuda")
+    keep = torch.tensor([j for j in range(800 + rows) if j // page not in (3, 7)], device="cuda")
     for r in range(rows):
         at = keep[keep < lengths[r]]
         k, v = (t[0][cache.table[r].long()[at // page], at % page].double().transpose(0, 1) for t in (cache.keys, cache.values))
@@ -717,7 +717,7 @@ def test_a_rollout_of_groups(heads, kv, dim, page, group, dtype):
     prompts, n = 3, 3 * group
     g = np.random.default_rng(heads)
     t = DTYPES[dtype]
-    cache = td.Cache.empty(1, n * (260 // page + 2), page, kv, dim, n, 260 // page + 2, t, heads_first=page != 24)
+    cache = td.Cache.empty(1, n * (680 // page + 2), page, kv, dim, n, 680 // page + 2, t, heads_first=page != 24)
     cu = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
     used = torch.zeros(1, dtype=torch.int32, device="cuda")
     out = td.AttentionBuffers(n, heads, dim, t, lse=True)
@@ -731,7 +731,7 @@ def test_a_rollout_of_groups(heads, kv, dim, page, group, dtype):
     def admit(which):
         add = np.zeros(n, int)
         for p in which:
-            add[p * group] = g.integers(1, 200)
+            add[p * group] = g.integers(1, 640)
         td.cache_extend(cache, ints(add), cu)
         k, v = rows(int(add.sum()))
         td.cache_write(cache, k, v, cu)
