@@ -63,9 +63,11 @@ struct AttendShape {
     static constexpr uint32_t kPartFloats = kHeads * (kDim + 2);         // weighted values [kHeads][kDim], then {reference, sum} [kHeads]
 };
 
+// Lengths reach 2^31 - 1, so positions, which run to a tile's end, are unsigned.
 struct Span {                                                 // the tokens [lo, n) of sequence s
     int32_t s, lo, n;
-    __device__ __forceinline__ uint32_t tiles() const { return (uint32_t)(n - lo + (int32_t)kTile - 1) / kTile; }
+    __device__ __forceinline__ uint32_t tiles() const { return ((uint32_t)(n - lo) + kTile - 1) / kTile; }
+    __device__ __forceinline__ uint32_t at(int32_t tile, uint32_t i) const { return (uint32_t)lo + (uint32_t)tile * kTile + i; }          // position of token i of a tile
 };
 // kOwn: without the tokens that the row's group has in common.
 template <bool kOwn>
@@ -516,16 +518,16 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
                 }
             }
             more = place < end;
-            const int32_t j = span.lo + tile * (int32_t)kTile + (int32_t)(lane & 15u);
-            id = more && j < span.n ? c.table[(size_t)span.s * c.max_pages + fast_div((uint32_t)j, c.by_page)] : -1;
+            const uint32_t j = span.at(tile, lane & 15u);
+            id = more && j < (uint32_t)span.n ? c.table[(size_t)span.s * c.max_pages + fast_div(j, c.by_page)] : -1;
         };
         // Brings the tile into stage `to`.
         const int64_t apart = static_cast<const T *>(a.values) - static_cast<const T *>(a.keys);
         auto bring = [&](uint32_t to) {
-            const int32_t j = span.lo + tile * (int32_t)kTile + (int32_t)(lane & 15u);
+            const uint32_t j = span.at(tile, lane & 15u);
             const bool on = (uint32_t)id < c.n_pages;
             const uint32_t counts = __ballot_sync(kFullMask, on) & 0xffffu;
-            const int64_t from = on ? id * a.page + (j - (int64_t)fast_div((uint32_t)j, c.by_page) * c.page_size) * a.token : 0;
+            const int64_t from = on ? id * a.page + (int64_t)(j - fast_div(j, c.by_page) * c.page_size) * a.token : 0;
             const T *keys = static_cast<const T *>(a.keys) + kv * a.head;
             const uint32_t at = ring + to * S::kStage;
             constexpr uint32_t kPer = S::kDim / 8;            // vectors of a row
@@ -543,7 +545,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
                     copy_vector_or_zero(at + S::kSide + o, k + apart, bytes);
                 }
             }
-            if (!on && j < span.n && unit == 0 && lane < 16) cache_flag(c, TD_ERR_OOB_INDEX);
+            if (!on && j < (uint32_t)span.n && unit == 0 && lane < 16) cache_flag(c, TD_ERR_OOB_INDEX);
             const bool fresh = tile == 0 || place == begin, final = tile + 1 == (int32_t)tiles, over = final || place + 1 == end;
             if (lane == 0) {
                 notes[to] = make_uint4(row, unit, counts | (fresh ? 1u << 16 : 0u) | (over ? 1u << 17 : 0u) | (tile == 0 ? 1u << 18 : 0u) |
@@ -867,22 +869,22 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
         more = load.here(end);
         if (!more) return;
         const int32_t *row = c.table + (size_t)load.seq * c.max_pages;
-        const int32_t j0 = load.tile * (int32_t)H::kTokens, j = j0 + (int32_t)threadIdx.x;
-        id = threadIdx.x < H::kTokens && j < load.tokens ? row[fast_div((uint32_t)j, c.by_page)] : -1;
+        const uint32_t j0 = (uint32_t)load.tile * H::kTokens, j = j0 + threadIdx.x, tokens = (uint32_t)load.tokens;
+        id = threadIdx.x < H::kTokens && j < tokens ? row[fast_div(j, c.by_page)] : -1;
 #pragma unroll
         for (uint32_t k = 0; k < kCopies; ++k) {
-            const int32_t jk = j0 + (int32_t)((threadIdx.x + k * kShareThreads) / kPer);
-            ids[k] = jk < load.tokens ? row[fast_div((uint32_t)jk, c.by_page)] : -1;
+            const uint32_t jk = j0 + (threadIdx.x + k * kShareThreads) / kPer;
+            ids[k] = jk < tokens ? row[fast_div(jk, c.by_page)] : -1;
         }
     };
     auto bring = [&](uint32_t to) {
-        const int32_t j0 = load.tile * (int32_t)H::kTokens;
+        const uint32_t j0 = (uint32_t)load.tile * H::kTokens;
         const T *keys = static_cast<const T *>(a.keys) + (load.unit % a.kv_heads) * a.head;
         const uint32_t at = ring + to * 2 * H::kSide;
 #pragma unroll
         for (uint32_t k = 0; k < kCopies; ++k) {
             const uint32_t i = threadIdx.x + k * kShareThreads, r = i / kPer, v = i - r * kPer, o = r * S::kPitch + v * 16;
-            const uint32_t j = (uint32_t)j0 + r, bytes = (uint32_t)ids[k] < c.n_pages ? 16u : 0u;
+            const uint32_t j = j0 + r, bytes = (uint32_t)ids[k] < c.n_pages ? 16u : 0u;
             const int64_t from = bytes ? ids[k] * a.page + (int64_t)(j - fast_div(j, c.by_page) * c.page_size) * a.token + v * 8 : 0;
             if (kPer * 8 != a.dim && v * 8 >= a.dim) continue;
             copy_vector_or_zero(at + o, keys + from, bytes);
@@ -891,7 +893,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
         if (threadIdx.x < H::kTokens) {
             const uint32_t which = __ballot_sync(kFullMask, (uint32_t)id < c.n_pages);
             if (lane == 0) counts[to * 4 + warp] = which;
-            if ((uint32_t)id >= c.n_pages && j0 + (int32_t)threadIdx.x < load.tokens && load.unit == 0) cache_flag(c, TD_ERR_OOB_INDEX);
+            if ((uint32_t)id >= c.n_pages && j0 + threadIdx.x < (uint32_t)load.tokens && load.unit == 0) cache_flag(c, TD_ERR_OOB_INDEX);
         }
         load.step(a, units, H::kTokens);
         look();
@@ -1070,8 +1072,8 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
     }
     Walk use = ahead;
     // Where the tokens of the tile that `ahead` is at lie: looked up by 128 threads, noted later as those of tile `number`.
-    int32_t id = -1, token = 0;
-    uint32_t ahead_unit = 0;
+    int32_t id = -1;
+    uint32_t token = 0, ahead_unit = 0;
     bool there = false, counted = false;
     auto look = [&]() {
         there = ahead.here(end);
@@ -1079,16 +1081,16 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
         counted = false;
         if (!there) return;
         ahead_unit = ahead.unit;
-        token = ahead.tile * (int32_t)W::kTokens + (int32_t)threadIdx.x;
-        counted = threadIdx.x < W::kTokens && token < ahead.tokens;
-        if (counted) id = c.table[(size_t)ahead.seq * c.max_pages + fast_div((uint32_t)token, c.by_page)];
+        token = (uint32_t)ahead.tile * W::kTokens + threadIdx.x;
+        counted = threadIdx.x < W::kTokens && token < (uint32_t)ahead.tokens;
+        if (counted) id = c.table[(size_t)ahead.seq * c.max_pages + fast_div(token, c.by_page)];
         ahead.step(a, units, W::kTokens);
     };
     auto note = [&](uint32_t number) {
         if (threadIdx.x >= W::kTokens) return;
         const bool on = (uint32_t)id < c.n_pages;
         offsets[number & 3u][threadIdx.x] =
-            on ? id * a.page + (token - (int64_t)fast_div((uint32_t)token, c.by_page) * c.page_size) * a.token + (ahead_unit % a.kv_heads) * a.head : -1;
+            on ? id * a.page + (int64_t)(token - fast_div(token, c.by_page) * c.page_size) * a.token + (ahead_unit % a.kv_heads) * a.head : -1;
         if (counted && !on && ahead_unit == 0) cache_flag(c, TD_ERR_OOB_INDEX);
         const uint32_t which = __ballot_sync(kFullMask, on);
         if (lane == 0) counts[number & 7u][warp] = which;
@@ -1368,14 +1370,14 @@ __global__ void __launch_bounds__(kFloatThreads) attend_float_kernel(CacheView c
             qv[h][i] = h < heads && lane + 32 * i < a.dim ? q[h * a.q_head + lane + 32 * i] * a.scale2 : 0.0f;
         }
     }
-    for (int32_t j = span.lo + (int32_t)warp; j < span.n; j += kWarps) {
-        const uint32_t page = fast_div((uint32_t)j, c.by_page);
+    for (uint32_t j = span.at(0, warp); j < (uint32_t)span.n; j += kWarps) {
+        const uint32_t page = fast_div(j, c.by_page);
         const int32_t id = c.table[(size_t)span.s * c.max_pages + page];
         if ((uint32_t)id >= c.n_pages) {
             if (unit == 0 && lane == 0) cache_flag(c, TD_ERR_OOB_INDEX);
             continue;
         }
-        const int64_t at = id * a.page + (j - (int64_t)page * c.page_size) * a.token + kv * a.head;
+        const int64_t at = id * a.page + (int64_t)(j - page * c.page_size) * a.token + kv * a.head;
         float k[kFloatColumns], v[kFloatColumns], x[kFloatHeads];
 #pragma unroll
         for (uint32_t i = 0; i < kFloatColumns; ++i) {
