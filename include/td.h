@@ -67,7 +67,8 @@ enum {
     TD_ERR_LOOKBACK_TIMEOUT = 1u << 5,  /* get: a scan tile gave up waiting; nothing is served,
                                            nothing stays claimed, the groups remain available   */
     TD_ERR_BAD_LENGTH       = 1u << 6,  /* put: cu not monotone or beyond data_elems            */
-    TD_ERR_COPY_TIMEOUT     = 1u << 7   /* a staged copy did not land in time; plain loads used  */
+    TD_ERR_COPY_TIMEOUT     = 1u << 7   /* a staged copy did not land in time; plain loads used.
+                                           td_cache_attention: products did not come in time, see there */
 };
 
 typedef struct {
@@ -695,7 +696,10 @@ int td_cache_write(const td_cache_write_args *args, void *stream);
  * among a row's scores makes that row's head NaN.  What lies in a page behind a sequence's last token is never used.
  * group > 1: rows i * group .. i * group + group - 1 are likely to share leading pages, as the
  * responses of a GRPO group do; full pages that all of a group's rows (with a token) have in common are
- * then read once for all.  Only time depends on it. */
+ * then read once for all.  Only time depends on it.
+ * Should the products that a group's common tokens are taken with not come in time, the wait for them ends all the same:
+ * TD_ERR_COPY_TIMEOUT is raised, out and lse of the heads that needed them are NaN, everything else is right, and the
+ * workspace may be used again as it is. */
 typedef struct {
     const td_cache *cache;
     uint32_t layer, n_rows, n_heads;       /* n_heads: a multiple of cache->n_heads; n_rows < 2^24 */
@@ -716,6 +720,10 @@ typedef struct {
 /* Never falls as an argument grows. 0 where an argument is out of range. */
 size_t td_cache_attention_workspace_bytes(uint32_t n_rows, uint32_t n_heads, uint32_t dim);
 int td_cache_attention(const td_cache_attention_args *args, void *stream);
+
+/* Test hook for that wait: in calls enqueued after it, block number `block` of the kernel takes the wait for its tile-th tile
+ * (of 128 common tokens) as run out.  UINT32_MAX: none.  For the whole process. */
+int td_debug_cache_wait(uint32_t block, uint32_t tile);
 
 const char *td_strerror(int code);
 

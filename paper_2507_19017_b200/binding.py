@@ -47,7 +47,7 @@ EXPORTS = ["td_query_workspace", "td_create", "td_destroy", "td_put", "td_get",
            "td_token_logprob", "td_token_logprob_grad", "td_policy_loss_workspace_bytes", "td_policy_loss",
            "td_embed", "td_embed_grad_workspace_bytes", "td_embed_grad",
            "td_cache_workspace_bytes", "td_cache_extend", "td_cache_fork", "td_cache_free", "td_cache_compact", "td_cache_write",
-           "td_cache_attention_workspace_bytes", "td_cache_attention"]
+           "td_cache_attention_workspace_bytes", "td_cache_attention", "td_debug_cache_wait"]
 
 
 class TdModel(C.Structure):
@@ -289,6 +289,8 @@ def lib():
         for name, extra in (("td_cache_extend", 2), ("td_cache_fork", 1), ("td_cache_free", 1), ("td_cache_compact", 2)):
             getattr(L, name).restype = C.c_int
             getattr(L, name).argtypes = [vp] * (extra + 2)
+        L.td_debug_cache_wait.restype = C.c_int
+        L.td_debug_cache_wait.argtypes = [u32, u32]
         L.td_cache_workspace_bytes.restype = C.c_size_t
         L.td_cache_workspace_bytes.argtypes = [u32, u32]
         L.td_cache_attention_workspace_bytes.restype = C.c_size_t
@@ -1097,3 +1099,9 @@ def cache_attention(out: AttentionBuffers, cache: Cache, q, seqs=None, layer: in
                      cache.dim ** -0.5 if scale is None else scale, 0, _vector(seqs, n, "seqs", "i32", cache.device), address, row, head,
                      *out._addresses)
     return out
+
+
+def debug_cache_wait(block: int = 0xFFFFFFFF, tile: int = 0xFFFFFFFF):
+    """Test hook: a block's wait for the products over a tile of common tokens counts as run out in later calls of
+    cache_attention, whose heads that needed them are then NaN (ERR_COPY_TIMEOUT).  Without arguments: off again."""
+    lib().td_debug_cache_wait(block, tile)

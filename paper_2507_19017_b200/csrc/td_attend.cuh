@@ -38,6 +38,7 @@ struct AttendArgs {
     float *common;                                            // [rows * heads][dim, then maximum, sum] what the common tokens give
     float *share_parts;                                       // [2 per block]
     uint32_t *share_arrived;                                  // [blocks], zero between calls
+    uint32_t lost_block, lost_tile;                           // a wait of share_wide_kernel that is taken as run out, for tests; ~0: none
 };
 
 constexpr uint32_t kTile = 16;                                // tokens of a tile
@@ -1025,7 +1026,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
     __shared__ int64_t offsets[4][W::kTokens];                // of a tile's tokens; -1: does not count
     __shared__ uint32_t counts[8][W::kTokens / 32];
     __shared__ float exchange[2][kShareHeads];
-    __shared__ __align__(8) unsigned long long bars[3];       // scores of even and odd tiles, results
+    __shared__ __align__(8) unsigned long long bars[4];       // scores of even and odd tiles, results, all products where a wait ran out
     __shared__ uint32_t tensor_at, failed, last;
     griddep_launch_dependents();
     griddep_wait();
@@ -1050,7 +1051,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
             reinterpret_cast<uint4 *>(memory + pad)[i] = make_uint4(0u, 0u, 0u, 0u);
     if (threadIdx.x == 0) {
         failed = 0;
-        for (uint32_t i = 0; i < 3; ++i) product_bar_init(bar + 8 * i);
+        for (uint32_t i = 0; i < 4; ++i) product_bar_init(bar + 8 * i);
     }
     __syncwarp();
     if (warp == 0) tensor_alloc(shared_address(&tensor_at), W::kTensor);
@@ -1124,7 +1125,6 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
     bring(a.values, values, 0);
     copy_commit();
 
-    uint32_t m_count = 0;
     auto heads_in = [&](const Walk &w, uint32_t &kv, uint32_t &first) {
         const uint32_t m_block = w.unit / a.kv_heads;
         kv = w.unit - m_block * a.kv_heads;
@@ -1158,6 +1158,19 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
     ShareCut cut_in{}, cut_out{};
     bool head_whole = false;
     float m = -CUDART_INF_F, l = 0.0f;
+    // Where what a unit gives this thread's row goes: its values, and its reference and sum.  False: nowhere.
+    auto place_of = [&](const Walk &w, bool whole, float *&to, float *&ml) {
+        uint32_t kv, first;
+        const uint32_t n = heads_in(w, kv, first), rr = fast_div(first + my_row, a.by_ratio), row = w.group * a.group + rr, head = kv * a.ratio + first + my_row - rr * a.ratio;
+        float *const part = a.share_parts + ((size_t)2 * blockIdx.x + (head_whole ? 1 : 0)) * W::kPartFloats;
+        to = whole ? a.common + ((size_t)row * a.n_heads + head) * (W::kDim + 2) : part + my_row * W::kDim;
+        ml = whole ? to + W::kDim : part + kShareHeads * W::kDim + 2 * my_row;
+        return my_row < n && row < a.n_rows;
+    };
+    auto cut_of = [&](const Walk &w) {
+        const ShareCut cut{w.place - (uint32_t)w.tile - 1, w.group, w.unit, w.tiles, 1u};
+        if (head_whole) cut_out = cut; else cut_in = cut;
+    };
     use.here(end);
     if (use.place < end) {
         ask(use);
@@ -1186,8 +1199,6 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
             score(i + 1);
         }
         __syncwarp();
-        uint32_t kv, m_first;
-        m_count = heads_in(use, kv, m_first);
         const bool fresh = use.tile == 0 || use.place == begin;
         if (fresh) {
             head_whole = use.tile == 0;
@@ -1198,6 +1209,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
         // Half of the warps copy before they weigh and half behind it, so that the one's copies go with the other's arithmetic.
         if (i > 0) fine &= product_wait(bar + 16, (i - 1) & 1u);          // results of the last tile: its values' place is free
         fine &= product_wait(bar + 8 * (i & 1u), i >> 1 & 1u);            // scores of this tile: its keys' place is free
+        fine &= blockIdx.x != a.lost_block || i != a.lost_tile;
         auto copies = [&]() {
             bring(a.keys, keys + i % W::kKeys * W::kSide, i + 3);
             bring(a.values, values + (i + 1) % W::kValues * W::kSide, i + 1);
@@ -1259,7 +1271,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
         tensor_wait_stores();
         tensor_before_sync();
         const bool again = __syncthreads_or(past || !fine);
-        if (again && failed) break;                           // never seen
+        if (again && failed) break;                           // a wait ran out: never seen
         note(i + 4);
         if (again) {
             float top = x[0];
@@ -1304,14 +1316,12 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
         if (final || use.place + 1 == end) {                  // the unit, or this block's part of it, ends here
             exchange[half][my_row] = l;
             fine &= product_wait(bar + 16, i & 1u);
+            if (!fine) failed = 1;
             __syncthreads();
             tensor_after_sync();
-            const uint32_t rr = fast_div(m_first + my_row, a.by_ratio), row = use.group * a.group + rr, head = kv * a.ratio + m_first + my_row - rr * a.ratio;
             const bool whole = head_whole && final;
-            float *const part = a.share_parts + ((size_t)2 * blockIdx.x + (head_whole ? 1 : 0)) * W::kPartFloats;
-            float *const to = whole ? a.common + ((size_t)row * a.n_heads + head) * (W::kDim + 2) : part + my_row * W::kDim;
-            float *const ml = whole ? to + W::kDim : part + kShareHeads * W::kDim + 2 * my_row;
-            const bool writes = my_row < m_count && row < a.n_rows;
+            float *to, *ml;
+            const bool writes = place_of(use, whole, to, ml);
 #pragma unroll
             for (uint32_t k = 0; k < W::kColumns / 32; ++k) {
                 uint32_t r[16];
@@ -1322,25 +1332,34 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
 #pragma unroll
                     for (int j = 0; j < 16; j += 2) *reinterpret_cast<float2 *>(to + column + j) = make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
             }
-            if (writes && half == 0) *reinterpret_cast<float2 *>(ml) = make_float2(m, exchange[0][my_row] + exchange[1][my_row]);
+            if (writes && half == 0) *reinterpret_cast<float2 *>(ml) = failed ? make_float2(CUDART_NAN_F, CUDART_NAN_F) : make_float2(m, exchange[0][my_row] + exchange[1][my_row]);
             tensor_before_sync();                             // read before the next unit's results are begun
-            if (!whole) {
-                const ShareCut cut{use.place - (uint32_t)use.tile - 1, use.group, use.unit, use.tiles, 1u};
-                if (head_whole) cut_out = cut; else cut_in = cut;
-            }
+            if (!whole) cut_of(use);
         }
         use.step(a, units, W::kTokens);
     }
     copy_wait<0>();
-    if (!fine) {                                              // never seen; what is still being computed is waited for, again with a limit
-        cache_flag(c, TD_ERR_COPY_TIMEOUT);
-        product_wait(bar + 8 * ((i + 1) & 1u), (i + 1) >> 1 & 1u);
-        product_wait(bar + 16, (i + 1) & 1u);
+    // A wait ran out (never seen): the block's units that are not done get NaN, so that their heads' results are NaN and nothing of an
+    // earlier call is taken for theirs, and the block arrives where it is counted on.  What is still being computed is waited for, again with
+    // a limit, before the tensor memory is given back.
+    if (failed) {
+        if (threadIdx.x == 0) {
+            cache_flag(c, TD_ERR_COPY_TIMEOUT);
+            product_commit(bar + 24);
+            product_wait(bar + 24, 0u);
+        }
+        for (; use.here(end); use.step(a, units, W::kTokens)) {
+            if (use.tile == 0 || use.place == begin) head_whole = use.tile == 0;
+            const bool final = use.tile + 1 == (int32_t)use.tiles, whole = head_whole && final;
+            if (!final && use.place + 1 != end) continue;
+            float *to, *ml;
+            if (place_of(use, whole, to, ml) && half == 0) *reinterpret_cast<float2 *>(ml) = make_float2(CUDART_NAN_F, CUDART_NAN_F);
+            if (!whole) cut_of(use);
+        }
     }
     tensor_before_sync();
     __syncthreads();
     if (warp == 0) tensor_free(tensor, W::kTensor);
-    if (failed) return;
     join_shares<W::kDim>(a, line, cut_in, cut_out, &last);
 }
 

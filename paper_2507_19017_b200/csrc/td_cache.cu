@@ -1,6 +1,7 @@
 // Host side of the paged key-value cache (include/td.h): argument checks and launches.
 // Nothing is allocated and nothing synchronises.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "td_attend.cuh"
@@ -156,6 +157,7 @@ cudaError_t run_write(const CacheView &v, const PoolView &p, WriteArgs k, cudaSt
 }
 
 // ---- attention ----
+std::atomic<uint32_t> g_lost_block{~0u}, g_lost_tile{~0u};    // td_debug_cache_wait
 constexpr uint32_t kBlocks = 148;                             // one per SM
 template <int kChunks>
 constexpr size_t part_bytes() {
@@ -340,6 +342,12 @@ int td_cache_write(const td_cache_write_args *a, void *stream) {
     return result(vec == 16 ? run_write<uint4>(v, p, k, st) : vec == 4 ? run_write<uint32_t>(v, p, k, st) : run_write<uint16_t>(v, p, k, st));
 }
 
+int td_debug_cache_wait(uint32_t block, uint32_t tile) {
+    g_lost_block.store(block, std::memory_order_relaxed);
+    g_lost_tile.store(tile, std::memory_order_relaxed);
+    return TD_OK;
+}
+
 size_t td_cache_attention_workspace_bytes(uint32_t n_rows, uint32_t n_heads, uint32_t dim) {
     if (n_rows >= kMaxRows || n_heads >= (1u << 16) || dim > kMaxDim) return 0;
     return attend_layout(n_rows, n_heads, dim).total;
@@ -402,6 +410,8 @@ int td_cache_attention(const td_cache_attention_args *a, void *stream) {
     k.parts = reinterpret_cast<float *>(ws + L.parts);
     k.share_parts = reinterpret_cast<float *>(ws + L.share_parts);
     k.common = reinterpret_cast<float *>(ws + L.common);
+    k.lost_block = g_lost_block.load(std::memory_order_relaxed);
+    k.lost_tile = g_lost_tile.load(std::memory_order_relaxed);
     cudaStream_t st = (cudaStream_t)stream;
     const CacheView v = cache_view(c);
     return result(c->dtype == TD_F32 ? run_attend_float(v, k, st) : c->dtype == TD_BF16 ? run_attend<__nv_bfloat16>(v, k, st)

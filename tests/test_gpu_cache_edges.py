@@ -9,7 +9,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2507_19017_b200 import binding as td
-from tests.test_gpu_cache import DTYPES, HALF, U, built, ints  # noqa: F401
+from tests.test_gpu_cache import DTYPES, HALF, attention_case, built, ints  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +41,60 @@ def test_a_sequence_of_the_most_tokens_there_can_be(dtype):
         assert ((out.out[0].double() - o).abs() <= (2 * HALF[dtype] + 2.0 ** -14) * 4).all()
         assert ((out.lse[0].double() - lse).abs() <= 2.0 ** -14 * 8).all()
     assert cache.status.item() == 0
+
+
+# ------------------------------------------------------------------ groups
+def spared(shared, group):
+    """How many reads of common tokens a group's rows spare: from 2000 on, and from 64 tokens on, they are taken once."""
+    return shared * (group - 1)
+
+
+def common_case(groups, group, shared, own, heads, kv, dim, page, dtype, seed=0, **kw):
+    """Groups whose rows have `shared` tokens in common (whole pages of them, shuffled over the pool) and up to `own` more."""
+    assert shared % page == 0 and shared >= 64 and spared(shared, group) >= 2000
+    g = np.random.default_rng(seed)
+    lengths = shared + g.integers(0, own + 1, groups * group)
+    return attention_case(lengths, heads, kv, dim, page, dtype, group=group, shared=[shared] * len(lengths), seed=seed, poison=False, **kw)
+
+
+def tiles_of_block(block, groups, group, shared, heads, kv, blocks=148):
+    """How many tiles of 128 common tokens a block takes: all units' tiles, and a place ahead of each unit's, in equal pieces."""
+    tiles = -(-shared // 128)
+    places = groups * kv * -(-group * (heads // kv) // 128) * (tiles + 1)
+    pieces = min(blocks, places)
+    begin = [b * (places // pieces) + min(b, places % pieces) for b in (block, block + 1)]
+    return sum(p % (tiles + 1) > 0 for p in range(begin[0], min(begin[1], places)))
+
+
+@pytest.mark.parametrize("shape", [(1, 32, 6400, 300, 32, 4, 128, 16, "bf16"), (60, 8, 400, 40, 16, 2, 64, 8, "f16"),
+                                   (2, 16, 12800, 100, 8, 1, 96, 16, "f16")], ids=str)
+@pytest.mark.parametrize("block,tile", [(0, 0), (2, 1), (1, 3), (4, 2)])
+def test_a_wait_that_runs_out_gives_nan_and_no_more(shape, block, tile):
+    """The heads whose common tokens were lost are NaN, and it is said; all others have the bits of a call that was not; and the next
+    call with the same buffers is as if nothing had been."""
+    groups, group, shared, own, heads, kv, dim, page, dtype = shape
+    cache, q = common_case(*shape)
+    out = td.AttentionBuffers(q.shape[0], heads, dim, q.dtype, lse=True)
+    td.cache_attention(out, cache, q, group=group)
+    want = out.out.clone(), out.lse.clone()
+    assert cache.status.item() == 0 and want[0].isfinite().all() and want[1].isfinite().all()
+    # what an earlier call left in the buffers is not taken for this one's
+    other = torch.randn(q.shape, device=q.device).to(q.dtype)
+    td.cache_attention(out, cache, other, group=group)
+    try:
+        td.debug_cache_wait(block, tile)
+        for _ in range(2):
+            td.cache_attention(out, cache, q, group=group)
+            lost = out.lse.isnan()
+            if tile < tiles_of_block(block, groups, group, shared, heads, kv):
+                assert cache.status.item() == td.ERR_COPY_TIMEOUT and lost.any() and not lost.all()
+            else:                                                     # the block has no such tile
+                assert cache.status.item() == 0 and not lost.any()
+            assert torch.equal(out.out.isnan().all(2), lost) and torch.equal(out.out.isnan().any(2), lost)
+            assert torch.equal(out.out[~lost], want[0][~lost]) and torch.equal(out.lse[~lost], want[1][~lost])
+            cache.status.zero_()
+    finally:
+        td.debug_cache_wait()
+    for _ in range(2):
+        td.cache_attention(out, cache, q, group=group)
+        assert cache.status.item() == 0 and torch.equal(out.out, want[0]) and torch.equal(out.lse, want[1])
