@@ -349,7 +349,7 @@ struct Fold {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 s[n][i] = counts >> (g + (i >> 1) * 8) & 1u ? s[n][i] * scale2 : -CUDART_INF_F;
-                past |= !(s[n][i] <= m[n][i & 1] + kSlack);
+                past |= !(s[n][i] - m[n][i & 1] <= kSlack);          // the difference: from 2^27 on the sum would round up by as much again
             }
         if (__any_sync(kFullMask, past)) {                    // a new reference (also where a score is NaN, which stays)
 #pragma unroll

@@ -98,3 +98,29 @@ def test_a_wait_that_runs_out_gives_nan_and_no_more(shape, block, tile):
     for _ in range(2):
         td.cache_attention(out, cache, q, group=group)
         assert cache.status.item() == 0 and torch.equal(out.out, want[0]) and torch.equal(out.lse, want[1])
+
+
+# ------------------------------------------------------------------ numbers
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("heads,kv,group", [(1, 1, 1), (10, 1, 1), (2, 1, 4), (8, 1, 8)])
+def test_scores_so_large_that_a_step_passes_the_slack(dtype, heads, kv, group):
+    """Scores of 2^27 (in bits), where floats are 16 apart: one that is a step above the others has all the weight, and no weight is infinite."""
+    dim, page, n, scale = 64, 16, 2048, 0.6931471824645996           # scale log2(e) is 1 in float
+    tokens = torch.zeros(n, dim, dtype=torch.float64)
+    tokens[:, 0], tokens[:, 1] = 4096.0, 1.0                          # 2^27 + 16
+    for j in (700, 1333):
+        tokens[j, 1] = 2.0                                            # 2^27 + 32
+    cache, q = attention_case([n] * group, heads, kv, dim, page, dtype, group=group, shared=[n] * group, seed=5, poison=False)
+    at = torch.arange(n, device="cuda")
+    place = cache.table[0].long()[at // page], at % page
+    cache.keys[0][place] = tokens.to(cache.keys).view(n, 1, dim)
+    q.zero_()
+    q[..., 0], q[..., 1] = 32768.0, 16.0
+    out = td.AttentionBuffers(group, heads, dim, q.dtype, lse=True)
+    td.cache_attention(out, cache, q, group=group, scale=scale)
+    o, lse = formula(cache.keys[0][place], cache.values[0][place], q[0], scale)
+    # weights of 2^-16 and 1, products and sums as in test_gpu_cache.py; scores are exact, the scale's rounding is 2^-24 of 16
+    v = cache.values[0][place].double().abs()
+    bound = 2 * HALF[dtype] * v.amax() + (n + 40) * 2.0 ** -24 * v.amax() + n * 2.0 ** -16 * 2.0 ** -8
+    assert ((out.out.double() - o).abs() <= bound).all()
+    assert ((out.lse.double() - lse).abs() <= 8 * 2.0 ** -24 * lse.abs()).all()
