@@ -42,7 +42,11 @@ struct AttendArgs {
 };
 
 constexpr uint32_t kTile = 16;                                // tokens of a tile
-constexpr float kSlack = 8.0f;                                // how far (log2) a score may pass the reference before that moves
+constexpr float kSlack = 8.0f;                                // how far (log2) a score may pass the reference's place before that moves
+// The reference is set this far (log2) below the maximum.  Weights are rounded to T, and half has no normal numbers below 2^-14 and none below
+// 2^-24: from weights of up to 2^(7 + 8) on, it keeps what lies 2^32 below the largest, so that a long row of small weights behind a large one counts.
+template <typename T> constexpr float kLift = 0.0f;
+template <> constexpr float kLift<__half> = 7.0f;
 constexpr uint32_t kLeastTiles = 2;                           // of a warp, before another block is used
 
 // Shapes of a kernel for heads of up to 16 * kChunks elements, 8 * kN of them side by side.
@@ -273,8 +277,8 @@ __device__ __forceinline__ void write_part(float *to, float *ml, const float2 (&
 
 // The running reference (in units of log2), sum and weighted values of 8 * kN heads, in the layout of the matrix instructions: lane
 // 4 g + t has heads 8 n + 2 t and 8 n + 2 t + 1, of every 16 columns of values those g and g + 8 places in, and of every 16
-// tokens the same.  The reference follows the scores' maximum only when one passes it by kSlack: weights stay below
-// 2^kSlack, and results hardly ever have to be brought to a new reference.
+// tokens the same.  The reference follows the scores' maximum (kLift below it) only when one passes it by kSlack more: weights stay
+// below 2^(kSlack + kLift), and results hardly ever have to be brought to a new reference.
 template <typename T, int kChunks, int kN>
 struct Fold {
     using S = AttendShape<kChunks, kN>;
@@ -349,7 +353,7 @@ struct Fold {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 s[n][i] = counts >> (g + (i >> 1) * 8) & 1u ? s[n][i] * scale2 : -CUDART_INF_F;
-                past |= !(s[n][i] - m[n][i & 1] <= kSlack);          // the difference: from 2^27 on the sum would round up by as much again
+                past |= !(s[n][i] - m[n][i & 1] <= kSlack + kLift<T>);          // the difference: from 2^27 on the sum would round up by as much again
             }
         if (__any_sync(kFullMask, past)) {                    // a new reference (also where a score is NaN, which stays)
 #pragma unroll
@@ -357,7 +361,7 @@ struct Fold {
                 float top[2], keep[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    top[i] = max_nan(max_nan(s[n][i], s[n][i + 2]), m[n][i]);
+                    top[i] = max_nan(max_nan(s[n][i], s[n][i + 2]) - kLift<T>, m[n][i]);
 #pragma unroll
                     for (int d = 4; d < 32; d *= 2) top[i] = max_nan(top[i], __shfl_xor_sync(kFullMask, top[i], d));
                     keep[i] = m[n][i] == -CUDART_INF_F ? 0.0f : exp2_approx(m[n][i] - top[i]);
@@ -1256,7 +1260,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
         float sum = 0.0f;
         bool past = fresh;                                    // a unit's first tile sets the reference
         if (!fresh) {
-            past = !(weigh(m == -CUDART_INF_F ? 0.0f : m, sum) <= 256.0f);          // 2^kSlack
+            past = !(weigh(m == -CUDART_INF_F ? 0.0f : m, sum) <= (kLift<T> == 7.0f ? 32768.0f : 256.0f));          // 2^(kSlack + kLift)
             if (m == -CUDART_INF_F) {                         // nothing counted so far
 #pragma unroll
                 for (int k = 0; k < 64; ++k) past |= !(x[k] == -CUDART_INF_F);
@@ -1279,7 +1283,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
             for (int k = 1; k < 64; ++k) top = max_nan(top, x[k]);
             exchange[half][my_row] = top;
             __syncthreads();
-            top = max_nan(max_nan(exchange[0][my_row], exchange[1][my_row]), m);
+            top = max_nan(max_nan(exchange[0][my_row], exchange[1][my_row]) - kLift<T>, m);
             const float keep = m == -CUDART_INF_F ? 0.0f : exp2_approx(m - top);
             if (!fresh) {
                 tensor_after_sync();

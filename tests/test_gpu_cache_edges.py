@@ -124,3 +124,28 @@ def test_scores_so_large_that_a_step_passes_the_slack(dtype, heads, kv, group):
     bound = 2 * HALF[dtype] * v.amax() + (n + 40) * 2.0 ** -24 * v.amax() + n * 2.0 ** -16 * 2.0 ** -8
     assert ((out.out.double() - o).abs() <= bound).all()
     assert ((out.lse.double() - lse).abs() <= 8 * 2.0 ** -24 * lse.abs()).all()
+
+
+@pytest.mark.parametrize("heads,kv,group,rows", [(1, 1, 1, 2000), (10, 1, 1, 1000), (2, 1, 4, 1200), (8, 1, 8, 1200)])
+def test_many_small_weights_behind_a_large_one_count_in_half(heads, kv, group, rows, n=100_000):
+    """One token with nearly all of the weight and a value of 0, the others with 2^-26.5 each and a value of 1: together they
+    are the result.  Rows enough that each is taken as one piece, all of one sequence."""
+    dim, page = 8, 16
+    cache, q = attention_case([n], heads, kv, dim, page, "f16", seed=6, poison=False, seqs=[0] * rows)
+    at = torch.arange(n, device="cuda")
+    place = cache.table[0].long()[at // page], at % page
+    for t, first, others in ((cache.keys[0], 0.0, -26.5), (cache.values[0], 0.0, 1.0)):
+        t.zero_()
+        t[..., 0] = others
+        t[place[0][3], 3, :, 0] = first
+    q.zero_()
+    q[..., 0] = 1.0
+    scale = 0.6931471824645996
+    out = td.AttentionBuffers(rows, heads, dim, q.dtype, lse=True)
+    td.cache_attention(out, cache, q, ints([0] * rows), group=group, scale=scale)
+    o, lse = formula(cache.keys[0][place], cache.values[0][place], q[0], scale)
+    # |V| <= 1: the weights' rounding in half below its normal range, 2^-25 of a largest weight of 2^7 at least; the others as in test_gpu_cache.py
+    bound = o * (2 * 2.0 ** -11 + 2.0 ** -20 + (n + 40) * 2.0 ** -24) + n * 2.0 ** -32 + 2.0 ** -25
+    assert o[0, 0] > 0.9 * n * 2.0 ** -26.5
+    assert ((out.out.double() - o).abs() <= bound).all()
+    assert ((out.lse.double() - lse).abs() <= 2.0 ** -20 + (n + 40) * 2.0 ** -24).all()
