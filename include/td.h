@@ -693,8 +693,9 @@ int td_cache_write(const td_cache_write_args *args, void *stream);
  * Scores, their maximum and both sums are float; the weights e^(x_j - reference) are rounded to the cache's
  * type for the product with V (bfloat16, half), where the largest weight of the tokens taken together lies in [1, 2^8]
  * (bfloat16) or [2^7, 2^15] (half): weights 2^33 below it are lost to half, and sums of 2^8 |V| have to stay within
- * float's range, which only bfloat16 values above 10^36 over the number of tokens pass.  A row without a token (seqs[r] < 0, length 0, or every score -inf)
- * has out 0 and lse -inf; seqs[r] >= max_seqs is the same with TD_ERR_OOB_INDEX.  A score of -inf has weight 0; NaN or +inf
+ * float's range, which only bfloat16 values above 10^36 over the number of tokens pass.  A row without a token (seqs[r] < 0, length 0,
+ * or every score -inf) has out 0 and lse -inf; seqs[r] >= max_seqs is the same with TD_ERR_OOB_INDEX.  Otherwise the value
+ * of a token with a score of -inf is multiplied by 0, so that one that is not finite gives NaN in its column; NaN or +inf
  * among a row's scores makes that row's head NaN.  What lies in a page behind a sequence's last token is never used.
  * group > 1: rows i * group .. i * group + group - 1 are likely to share leading pages, as the
  * responses of a GRPO group do; full pages that all of a group's rows (with a token) have in common are

@@ -186,11 +186,12 @@ __device__ __forceinline__ void write_result(const AttendArgs &a, uint32_t row, 
         sum = fmaf(ml.y, f, sum * e);
         top = most;
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float inv = 1.0f / sum;
     T *out = static_cast<T *>(a.out) + row * a.out_row + head * a.out_head;
 #pragma unroll
     for (uint32_t i = 0; i < (kDim / 2 + 31) / 32; ++i)
-        if (2 * (lane + 32 * i) < a.dim) *reinterpret_cast<uint32_t *>(out + 2 * (lane + 32 * i)) = pair_of<T>(v[i].x * inv, v[i].y * inv);
+        if (2 * (lane + 32 * i) < a.dim)
+            *reinterpret_cast<uint32_t *>(out + 2 * (lane + 32 * i)) = sum == 0.0f ? 0u : pair_of<T>(v[i].x * inv, v[i].y * inv);          // 0, also where the values are not finite
     if (a.lse && lane == 0) a.lse[(size_t)row * a.n_heads + head] = sum == 0.0f ? -CUDART_INF_F : (top + log2f(sum)) * 0.69314718055994531f;
 }
 
@@ -427,12 +428,12 @@ struct Fold {
     // The head's result.
     __device__ __forceinline__ void finish(T *out, float *lse, uint32_t dim, int n, int i) const {
         const uint32_t g = (threadIdx.x & 31u) >> 2;
-        const float inv = l[n][i] == 0.0f ? 0.0f : 1.0f / l[n][i];
+        const float inv = 1.0f / l[n][i];
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
 #pragma unroll
             for (int k = 0; k < 2; ++k)
-                if (c * 16 + k * 8 < dim) out[c * 16 + k * 8 + g] = Elem<T>::from(o[c][n][i + 2 * k] * inv);
+                if (c * 16 + k * 8 < dim) out[c * 16 + k * 8 + g] = Elem<T>::from(l[n][i] == 0.0f ? 0.0f : o[c][n][i + 2 * k] * inv);
         if (lse && g == 0) *lse = l[n][i] == 0.0f ? -CUDART_INF_F : (m[n][i] + log2f(l[n][i])) * 0.69314718055994531f;
     }
 };
@@ -1400,7 +1401,7 @@ __global__ void __launch_bounds__(kFloatThreads) attend_float_kernel(CacheView c
             if (unit == 0 && lane == 0) cache_flag(c, TD_ERR_OOB_INDEX);
             continue;
         }
-        const int64_t at = id * a.page + (int64_t)(j - page * c.page_size) * a.token + kv * a.head;
+        const int64_t at = id * a.page + ((int64_t)j - (int64_t)page * c.page_size) * a.token + kv * a.head;
         float k[kFloatColumns], v[kFloatColumns], x[kFloatHeads];
 #pragma unroll
         for (uint32_t i = 0; i < kFloatColumns; ++i) {
@@ -1420,7 +1421,6 @@ __global__ void __launch_bounds__(kFloatThreads) attend_float_kernel(CacheView c
             for (uint32_t h = 0; h < kFloatHeads; ++h) x[h] += __shfl_xor_sync(kFullMask, x[h], d);
 #pragma unroll
         for (uint32_t h = 0; h < kFloatHeads; ++h) {
-            if (x[h] == -CUDART_INF_F) continue;
             if (!(x[h] <= m[h])) {                            // a new maximum, or NaN, which stays
                 const float top = max_nan(x[h], m[h]), keep = exp2f(m[h] - top);
                 l[h] *= keep;
@@ -1428,7 +1428,7 @@ __global__ void __launch_bounds__(kFloatThreads) attend_float_kernel(CacheView c
 #pragma unroll
                 for (uint32_t i = 0; i < kFloatColumns; ++i) o[h][i] *= keep;
             }
-            const float p = exp2f(x[h] - m[h]);
+            const float p = m[h] == -CUDART_INF_F ? 0.0f : exp2f(x[h] - m[h]);
             l[h] += p;
 #pragma unroll
             for (uint32_t i = 0; i < kFloatColumns; ++i) o[h][i] = fmaf(p, v[i], o[h][i]);

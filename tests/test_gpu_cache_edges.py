@@ -149,3 +149,34 @@ def test_many_small_weights_behind_a_large_one_count_in_half(heads, kv, group, r
     assert o[0, 0] > 0.9 * n * 2.0 ** -26.5
     assert ((out.out.double() - o).abs() <= bound).all()
     assert ((out.lse.double() - lse).abs() <= 2.0 ** -20 + (n + 40) * 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("heads,kv,dim,group", [(4, 2, 64, 1), (24, 2, 128, 1), (4, 2, 64, 4), (32, 2, 64, 4), (6, 2, 192, 4)])
+def test_values_that_are_not_finite_where_the_score_is_minus_infinity(dtype, heads, kv, dim, group):
+    """By the formula: 0 times such a value is NaN, in its column and in every type, where another token counts; where none does the row
+    has nothing."""
+    page, rows, shared = 16, 2 * max(group, 2), 800
+    lengths = np.full(rows, shared) + np.arange(rows)
+    cache, q = attention_case(lengths, heads, kv, dim, page, dtype, group=group, shared=[shared] * rows, seed=8, poison=False)
+    q[..., 5] = -1.0
+    clean = cache.values[0].clone(), cache.keys[0].clone()
+    first = cache.table[0].long()
+    out = td.AttentionBuffers(rows, heads, dim, q.dtype, lse=True)
+    cache.keys[0][first[20], 3, :, 5] = math.inf                      # token 323 of the first row (of the group, where there is one)
+    cache.values[0][first[20], 3, :, 2], cache.values[0][first[20], 3, :, 7] = math.inf, math.nan
+    td.cache_attention(out, cache, q, group=group)
+    gone = torch.zeros(rows, heads, dim, dtype=torch.bool, device="cuda")
+    gone[:group, :, 2] = gone[:group, :, 7] = True
+    assert torch.equal(out.out.isnan(), gone) and out.out[~gone].isfinite().all() and out.lse.isfinite().all()
+    # no token of the first rows counts
+    cache.values[0].copy_(clean[0])
+    cache.keys[0].copy_(clean[1])
+    for r in range(group):
+        at = torch.arange(lengths[r], device="cuda")
+        place = cache.table[r].long()[at // page], at % page
+        cache.keys[0][place[0], place[1], :, 5] = math.inf
+        cache.values[0][place[0], place[1], :, 2], cache.values[0][place[0], place[1], :, 7] = math.inf, math.nan
+    td.cache_attention(out, cache, q, group=group)
+    assert not out.out[:group].any() and (out.lse[:group] == -math.inf).all()
+    assert out.out[group:].isfinite().all() and out.lse[group:].isfinite().all()
