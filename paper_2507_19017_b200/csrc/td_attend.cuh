@@ -31,9 +31,10 @@ struct AttendArgs {
     float scale, scale2;                                      // scale2 = scale * log2(e)
     float *parts;                                             // [2 per warp, then 2 per block][part floats]
     uint32_t *arrived;                                        // [blocks], zero between calls
-    // groups of rows with common pages; group == 1: none
+    // groups of rows with common pages; group == 1: none.  Those of more than kMaxGroup rows are taken as `pieces` groups of like size each.
     uint32_t group, n_groups, m_blocks, m_rows;               // a group's heads over one key head in m_blocks blocks of m_rows (128 at most)
-    FastDiv by_group, by_ratio;
+    uint32_t whole, pieces;                                   // rows of a group as the caller has them
+    FastDiv by_group, by_whole, by_ratio;
     int2 *shared;                                             // [n_groups] common tokens, and a sequence that has them
     float *common;                                            // [rows * heads][dim, then maximum, sum] what the common tokens give
     float *share_parts;                                       // [2 per block]
@@ -74,6 +75,16 @@ struct Span {                                                 // the tokens [lo,
     __device__ __forceinline__ uint32_t tiles() const { return ((uint32_t)(n - lo) + kTile - 1) / kTile; }
     __device__ __forceinline__ uint32_t at(int32_t tile, uint32_t i) const { return (uint32_t)lo + (uint32_t)tile * kTile + i; }          // position of token i of a tile
 };
+// The group of a row; the rows of a group.
+__device__ __forceinline__ uint32_t group_of(const AttendArgs &a, uint32_t row) {
+    const uint32_t g = fast_div(row, a.by_whole);
+    return a.pieces == 1 ? g : g * a.pieces + fast_div(row - g * a.whole, a.by_group);
+}
+__device__ __forceinline__ uint32_t rows_of(const AttendArgs &a, uint32_t group, uint32_t &first) {
+    const uint32_t g = a.pieces == 1 ? group : group / a.pieces, at = (group - g * a.pieces) * a.group;
+    first = g * a.whole + at;
+    return first < a.n_rows ? min(min(a.group, a.whole - at), a.n_rows - first) : 0u;
+}
 // kOwn: without the tokens that the row's group has in common.
 template <bool kOwn>
 __device__ __forceinline__ Span span_of(const CacheView &c, const AttendArgs &a, uint32_t row, bool flag) {
@@ -90,7 +101,7 @@ __device__ __forceinline__ Span span_of(const CacheView &c, const AttendArgs &a,
     }
     p.n = n;
     p.lo = a.window && (uint32_t)n > a.window ? n - (int32_t)a.window : 0;
-    if (kOwn && a.group > 1 && n > 0) p.lo = max(p.lo, a.shared[fast_div(row, a.by_group)].x);          // never both: see share_plan_kernel
+    if (kOwn && a.group > 1 && n > 0) p.lo = max(p.lo, a.shared[group_of(a, row)].x);          // never both: see share_plan_kernel
     return p;
 }
 
@@ -163,7 +174,7 @@ __device__ __forceinline__ uint32_t heads_of(const AttendArgs &a, uint32_t unit,
 // What a row's head has from the tokens its group has in common; nullptr: there are none.
 template <uint32_t kDim>
 __device__ __forceinline__ const float *common_of(const AttendArgs &a, uint32_t row, uint32_t head) {
-    if (a.group <= 1 || a.shared[fast_div(row, a.by_group)].x == 0) return nullptr;
+    if (a.group <= 1 || a.shared[group_of(a, row)].x == 0) return nullptr;
     return a.common + ((size_t)row * a.n_heads + head) * (kDim + 2);
 }
 
@@ -673,7 +684,7 @@ __global__ void __launch_bounds__(AttendShape<kChunks, kN>::kThreads, 1) attend_
 // The responses of a GRPO group begin with the same pages.  share_plan_kernel finds how many, share_kernel takes those tokens
 // once for all the group's heads over a key head (blocks of up to 128 of them), and attend_kernel takes the rest of
 // each row and adds what the common tokens gave.
-constexpr uint32_t kMaxGroup = 512;                           // rows; a larger group is taken as several
+constexpr uint32_t kMaxGroup = 512;                           // rows
 constexpr uint32_t kShareHeads = 128;                         // heads of a block: 8 warps of 16
 constexpr uint32_t kShareThreads = 256;
 constexpr uint32_t kLeastShared = 64;                         // common tokens
@@ -688,7 +699,8 @@ __global__ void __launch_bounds__(kShareThreads) share_plan_kernel(CacheView c, 
     __shared__ uint32_t equal;
     griddep_launch_dependents();
     griddep_wait();
-    const uint32_t first = blockIdx.x * a.group, rows = min(a.group, a.n_rows - first);
+    uint32_t first;
+    const uint32_t rows = rows_of(a, blockIdx.x, first);
     if (threadIdx.x == 0) {
         least = 0x7fffffff;
         lead = kMaxGroup;
@@ -808,11 +820,13 @@ __device__ __forceinline__ void join_shares(const AttendArgs &a, const Line &lin
         __syncthreads();
         if (!joins) continue;
         const uint32_t m_block = u.unit / a.kv_heads, kv = u.unit - m_block * a.kv_heads, first = m_block * a.m_rows, count = min(a.m_rows, a.group * a.ratio - first);
+        uint32_t first_row;
+        const uint32_t rows = rows_of(a, u.group, first_row);
         join_parts<kDim, kShareHeads, 4, 2>(a.share_parts, b1 - b0 + 1, [=](uint32_t k) { return 2 * (b0 + k) + (k == 0); }, count, warp, kShareThreads / 32,
                                                [&](uint32_t r, auto &v, float top, float sum) {
-                                                   const uint32_t rr = fast_div(first + r, a.by_ratio), row = u.group * a.group + rr;
-                                                   if (row >= a.n_rows) return;
-                                                   float *to = a.common + ((size_t)row * a.n_heads + kv * a.ratio + first + r - rr * a.ratio) * (kDim + 2);
+                                                   const uint32_t rr = fast_div(first + r, a.by_ratio);
+                                                   if (rr >= rows) return;
+                                                   float *to = a.common + ((size_t)(first_row + rr) * a.n_heads + kv * a.ratio + first + r - rr * a.ratio) * (kDim + 2);
                                                    write_part<kDim>(to, to + kDim, v, top, sum);
                                                });
     }
@@ -924,9 +938,10 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
         // The row and head of the block's row i (ratio rows of heads per row of the group), or false.
         auto at_row = [&](uint32_t i, uint32_t &row, uint32_t &head) {
             const uint32_t rr = fast_div(m_first + i, a.by_ratio);
-            row = use.group * a.group + rr;
+            const bool there = rr < rows_of(a, use.group, row);
+            row += rr;
             head = kv * a.ratio + m_first + i - rr * a.ratio;
-            return i < m_count && row < a.n_rows;
+            return i < m_count && there;
         };
         if (use.tile == 0 || use.place == begin) {            // a unit begins here
             head_whole = use.tile == 0;
@@ -1138,15 +1153,15 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
     };
     // The queries of a unit into shared memory, zeros behind them.
     auto ask = [&](const Walk &w) {
-        uint32_t kv, first;
-        const uint32_t n = heads_in(w, kv, first);
+        uint32_t kv, first, first_row;
+        const uint32_t n = heads_in(w, kv, first), rows = rows_of(a, w.group, first_row);
         constexpr uint32_t kPer = 8 * W::kHalves;
 #pragma unroll 4
         for (uint32_t k = 0; k < kShareHeads * kPer / kShareThreads; ++k) {
-            const uint32_t i = threadIdx.x + k * kShareThreads, r = i / kPer, v = i - r * kPer, rr = fast_div(first + r, a.by_ratio), row = w.group * a.group + rr;
+            const uint32_t i = threadIdx.x + k * kShareThreads, r = i / kPer, v = i - r * kPer, rr = fast_div(first + r, a.by_ratio);
             uint4 x = make_uint4(0u, 0u, 0u, 0u);
-            if (r < n && row < a.n_rows && v * 8 < a.dim)
-                x = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + row * a.q_row + (kv * a.ratio + first + r - rr * a.ratio) * a.q_head + v * 8);
+            if (r < n && rr < rows && v * 8 < a.dim)
+                x = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + (first_row + rr) * a.q_row + (kv * a.ratio + first + r - rr * a.ratio) * a.q_head + v * 8);
             store_shared(queries + (v >> 3) * W::kHalf + r * 128 + ((v ^ r) & 7u) * 16, x);
         }
     };
@@ -1165,12 +1180,14 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_wide_kernel(CacheView 
     float m = -CUDART_INF_F, l = 0.0f;
     // Where what a unit gives this thread's row goes: its values, and its reference and sum.  False: nowhere.
     auto place_of = [&](const Walk &w, bool whole, float *&to, float *&ml) {
-        uint32_t kv, first;
-        const uint32_t n = heads_in(w, kv, first), rr = fast_div(first + my_row, a.by_ratio), row = w.group * a.group + rr, head = kv * a.ratio + first + my_row - rr * a.ratio;
+        uint32_t kv, first, row;
+        const uint32_t n = heads_in(w, kv, first), rr = fast_div(first + my_row, a.by_ratio), head = kv * a.ratio + first + my_row - rr * a.ratio;
+        const bool there = rr < rows_of(a, w.group, row);
+        row += rr;
         float *const part = a.share_parts + ((size_t)2 * blockIdx.x + (head_whole ? 1 : 0)) * W::kPartFloats;
         to = whole ? a.common + ((size_t)row * a.n_heads + head) * (W::kDim + 2) : part + my_row * W::kDim;
         ml = whole ? to + W::kDim : part + kShareHeads * W::kDim + 2 * my_row;
-        return my_row < n && row < a.n_rows;
+        return my_row < n && there;
     };
     auto cut_of = [&](const Walk &w) {
         const ShareCut cut{w.place - (uint32_t)w.tile - 1, w.group, w.unit, w.tiles, 1u};

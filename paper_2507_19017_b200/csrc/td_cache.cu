@@ -396,11 +396,14 @@ int td_cache_attention(const td_cache_attention_args *a, void *stream) {
     k.scale = a->scale;
     k.scale2 = (float)(1.4426950408889634 * (double)a->scale);
     // rows that share, and their heads over one key head in blocks of like size
-    k.group = std::min({a->group, a->n_rows, kMaxGroup});
-    k.n_groups = (a->n_rows + k.group - 1) / k.group;
+    k.whole = std::min(a->group, a->n_rows);
+    k.pieces = (k.whole + kMaxGroup - 1) / kMaxGroup;
+    k.group = (k.whole + k.pieces - 1) / k.pieces;
+    k.n_groups = (a->n_rows + k.whole - 1) / k.whole * k.pieces;
     k.m_blocks = (k.group * k.ratio + kShareHeads - 1) / kShareHeads;
     k.m_rows = (k.group * k.ratio + k.m_blocks - 1) / k.m_blocks;
     k.by_group = make_fastdiv(k.group);
+    k.by_whole = make_fastdiv(k.whole);
     k.by_ratio = make_fastdiv(k.ratio);
     const AttendLayout L = attend_layout(a->n_rows, a->n_heads, c->dim);
     uint8_t *ws = static_cast<uint8_t *>(a->workspace);

@@ -9,7 +9,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2507_19017_b200 import binding as td
-from tests.test_gpu_cache import DTYPES, HALF, attention_case, built, ints  # noqa: F401
+from tests.test_gpu_cache import DTYPES, HALF, attention_case, built, exact_attention, ints  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -180,3 +180,34 @@ def test_values_that_are_not_finite_where_the_score_is_minus_infinity(dtype, hea
     td.cache_attention(out, cache, q, group=group)
     assert not out.out[:group].any() and (out.lse[:group] == -math.inf).all()
     assert out.out[group:].isfinite().all() and out.lse[group:].isfinite().all()
+
+
+@pytest.mark.parametrize("heads,kv", [(1, 1), (2, 1)])
+def test_a_group_of_more_than_512_rows_is_taken_in_like_pieces(heads, kv):
+    """Pieces do not reach over a group's end: two groups of 600 rows have the bits of four of 300."""
+    group, shared, dim, page = 600, 320, 64, 16
+    cache, q = common_case(2, group, shared, 3, heads, kv, dim, page, "bf16")
+    got = []
+    for g in (group, group // 2):
+        out = td.AttentionBuffers(2 * group, heads, dim, q.dtype, lse=True)
+        td.cache_attention(out, cache, q, group=g)
+        got.append((out.out, out.lse))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("rows,group", [(1100, 1025), (1100, 2000), (2051, 1025), (513, 513), (1400, 700)])
+@pytest.mark.parametrize("heads,kv,dim", [(4, 1, 64), (4, 2, 96), (16, 1, 192)])
+def test_large_groups_that_do_not_divide(rows, group, heads, kv, dim):
+    """Groups cut into pieces of unlike size, and a last one that is cut short."""
+    page, shared = 16, 160
+    groups = -(-rows // min(group, rows))
+    cache, q = common_case(groups, min(group, rows), shared, 40, heads, kv, dim, page, "bf16", seed=rows)
+    seqs = list(range(rows))
+    for r in (3, 511, 512, rows - 1):
+        seqs[r] = -1
+    out = td.AttentionBuffers(rows, heads, dim, q.dtype, lse=True)
+    td.cache_attention(out, cache, q[:rows], ints(seqs), group=group)
+    o, lse, bound, lse_bound = exact_attention(cache, q[:rows], seqs)
+    assert cache.status.item() == 0 and ((out.out.double() - o).abs() <= bound).all()
+    gone = lse == -math.inf
+    assert torch.equal(out.lse == -math.inf, gone) and ((out.lse.double() - lse)[~gone].abs() <= lse_bound[~gone]).all()
