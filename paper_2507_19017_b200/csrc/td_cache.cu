@@ -342,12 +342,6 @@ int td_cache_write(const td_cache_write_args *a, void *stream) {
     return result(vec == 16 ? run_write<uint4>(v, p, k, st) : vec == 4 ? run_write<uint32_t>(v, p, k, st) : run_write<uint16_t>(v, p, k, st));
 }
 
-int td_debug_cache_wait(uint32_t block, uint32_t tile) {
-    g_lost_block.store(block, std::memory_order_relaxed);
-    g_lost_tile.store(tile, std::memory_order_relaxed);
-    return TD_OK;
-}
-
 size_t td_cache_attention_workspace_bytes(uint32_t n_rows, uint32_t n_heads, uint32_t dim) {
     if (n_rows >= kMaxRows || n_heads >= (1u << 16) || dim > kMaxDim) return 0;
     return attend_layout(n_rows, n_heads, dim).total;
@@ -419,6 +413,12 @@ int td_cache_attention(const td_cache_attention_args *a, void *stream) {
     const CacheView v = cache_view(c);
     return result(c->dtype == TD_F32 ? run_attend_float(v, k, st) : c->dtype == TD_BF16 ? run_attend<__nv_bfloat16>(v, k, st)
                                                                                           : run_attend<__half>(v, k, st));
+}
+
+int td_debug_cache_wait(uint32_t block, uint32_t tile) {
+    g_lost_block.store(block, std::memory_order_relaxed);
+    g_lost_tile.store(tile, std::memory_order_relaxed);
+    return TD_OK;
 }
 
 }  // extern "C"

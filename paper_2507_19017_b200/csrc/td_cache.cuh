@@ -107,7 +107,7 @@ __device__ __forceinline__ uint32_t pages_needed(const CacheView &c, const int32
     first = add = 0;
     const int32_t n = c.length[s];
     if constexpr (kGive == Give::kExtend) {
-        const int32_t want = ask ? ask[s] : (n > 0 ? 1 : 0);
+        const int32_t want = ask ? ask[s] : (n != 0 ? 1 : 0);          // a negative length is looked at, and noted
         if (want == 0) return 0;
         if (want < 0 || !length_ok(c, n) || (unsigned long long)n + want > (unsigned long long)c.max_pages * c.page_size) {
             cache_flag(c, TD_ERR_BAD_LENGTH);

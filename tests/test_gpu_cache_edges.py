@@ -211,3 +211,23 @@ def test_large_groups_that_do_not_divide(rows, group, heads, kv, dim):
     assert cache.status.item() == 0 and ((out.out.double() - o).abs() <= bound).all()
     gone = lse == -math.inf
     assert torch.equal(out.lse == -math.inf, gone) and ((out.lse.double() - lse)[~gone].abs() <= lse_bound[~gone]).all()
+
+
+# ------------------------------------------------------------------ pages
+def tables_only(lengths, page, max_pages, n_pages, held=0):
+    holders = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    holders[:held] = 1
+    table = torch.arange(len(lengths) * max_pages, dtype=torch.int32, device="cuda").view(len(lengths), max_pages)
+    return td.Cache(None, None, table, ints(lengths), holders, page_size=page)
+
+
+def test_one_more_token_notes_a_negative_length():
+    cache = tables_only([3, -1, 0, 4], 4, 3, 12, held=3)
+    cu = torch.full((5,), 9, dtype=torch.int32, device="cuda")
+    td.cache_extend(cache, None, cu)
+    assert cache.status.item() == td.ERR_BAD_LENGTH
+    assert cache.length.tolist() == [4, -1, 0, 5] and cu.tolist() == [0, 1, 1, 1, 2]
+    cache.status.zero_()
+    cache.length.copy_(ints([12, 1, 0, 2]))                           # the first has no room for another
+    td.cache_extend(cache, None, cu)
+    assert cache.status.item() == td.ERR_BAD_LENGTH and cache.length.tolist() == [12, 2, 0, 3] and cu.tolist() == [0, 0, 1, 1, 2]
