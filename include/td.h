@@ -652,7 +652,7 @@ size_t td_cache_workspace_bytes(uint32_t n_pages, uint32_t max_seqs);
  * [max_seqs + 1] or NULL: written with the running sum of the tokens given, as td_cache_write takes it.
  * Negative entries and sequences that would pass max_pages get nothing (TD_ERR_BAD_LENGTH).  Where
  * the free pages do not suffice for the whole call nothing is changed, cu is zeros, and
- * TD_ERR_ARENA_FULL is raised.  The last page of a sequence must be its own unless it is full (a fork leaves
+ * TD_ERR_ARENA_FULL is raised; the same with TD_ERR_BAD_LENGTH where cu is given and the call's tokens are 2^31 or more in all.  The last page of a sequence must be its own unless it is full (a fork leaves
  * it so). */
 int td_cache_extend(const td_cache *cache, const int32_t *add, int32_t *cu, void *stream);
 

@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kCacheThreads) cache_assign_kernel(CacheView c
                     tile_part(w.tile_pages, w.page_tiles, page_block ? blockIdx.x : 0u)};
     tile_sums<3>(t, sums);
     const unsigned long long need_total = t[0].all, add_total = t[1].all, add_base = t[1].before, page_total = t[2].all;
-    const bool enough = need_total <= page_total && add_total < (1ull << 31);
+    const bool enough = need_total <= page_total && (!cu || add_total < (1ull << 31));          // cu's words are 32 bits wide
     if (page_block) {
         unsigned long long base = t[2].before;
         if (!enough || base >= need_total) return;

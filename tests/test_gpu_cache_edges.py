@@ -231,3 +231,22 @@ def test_one_more_token_notes_a_negative_length():
     cache.length.copy_(ints([12, 1, 0, 2]))                           # the first has no room for another
     td.cache_extend(cache, None, cu)
     assert cache.status.item() == td.ERR_BAD_LENGTH and cache.length.tolist() == [12, 2, 0, 3] and cu.tolist() == [0, 0, 1, 1, 2]
+
+
+def test_tokens_past_32_bits_in_one_call():
+    """2^31 new tokens in all: refused where they are to be numbered (cu), given where they are not."""
+    page, n = 65535, 2 ** 30
+    cache = tables_only([0, 0, 0], page, 16400, 40000)
+    cu = torch.full((4,), 9, dtype=torch.int32, device="cuda")
+    before = cache.table.clone()
+    td.cache_extend(cache, ints([n, 0, n]), cu)
+    assert cache.status.item() == td.ERR_BAD_LENGTH and not cu.any()
+    assert not cache.length.any() and not cache.holders.any() and torch.equal(cache.table, before)
+    cache.status.zero_()
+    td.cache_extend(cache, ints([n, 0, n]))
+    need = -(-n // page)
+    assert cache.status.item() == 0 and cache.length.tolist() == [n, 0, n]
+    assert cache.table[0, :need].tolist() == list(range(need)) and cache.table[2, :need].tolist() == list(range(need, 2 * need))
+    assert int(cache.holders.sum()) == 2 * need and cache.holders[:2 * need].all()
+    td.cache_extend(cache, ints([5, 7, 0]), cu)
+    assert cache.status.item() == 0 and cu.tolist() == [0, 5, 12, 12]
