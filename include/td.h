@@ -631,7 +631,8 @@ typedef struct {
     int32_t  dtype;                        /* TD_F32 | TD_BF16 | TD_F16 */
     uint32_t n_pages, page_size;           /* page_size < 2^16; n_pages * page_size < 2^40 */
     uint32_t n_layers, n_heads, dim;       /* of keys and values, >= 1; n_layers, n_heads < 2^16, dim < 2^16 */
-    int64_t  layer_stride, page_stride, token_stride, head_stride;   /* elements, >= 0, the same for both; dim is contiguous */
+    int64_t  layer_stride, page_stride, token_stride, head_stride;   /* elements, >= 0, the same for both; dim is contiguous.
+                                              td_cache_attention takes fewer dims and strides */
     void *keys, *values;                   /* device, layer 0; both NULL: tables only (extend, free) */
     uint32_t max_seqs, max_pages;          /* table rows < 2^24, and entries of a row; max_pages * page_size < 2^31 */
     int32_t *table;                        /* device [max_seqs][max_pages] */
@@ -692,14 +693,20 @@ int td_cache_write(const td_cache_write_args *args, void *stream);
  * over the tokens j of sequence seqs[r] (seqs == NULL: r), with window > 0 its last `window` ones only.
  * Scores, their maximum and both sums are float; the weights e^(x_j - reference) are rounded to the cache's
  * type for the product with V (bfloat16, half), where the largest weight of the tokens taken together lies in [1, 2^8]
- * (bfloat16) or [2^7, 2^15] (half): weights 2^33 below it are lost to half, and sums of 2^8 |V| have to stay within
- * float's range, which only bfloat16 values above 10^36 over the number of tokens pass.  A row without a token (seqs[r] < 0, length 0,
- * or every score -inf) has out 0 and lse -inf; seqs[r] >= max_seqs is the same with TD_ERR_OOB_INDEX.  Otherwise the value
- * of a token with a score of -inf is multiplied by 0, so that one that is not finite gives NaN in its column; NaN or +inf
- * among a row's scores makes that row's head NaN.  What lies in a page behind a sequence's last token is never used.
+ * (bfloat16) or [2^7, 2^15] (half): half loses weights below 2^-32 of it, and the sums of 2^8 |V| have to stay within
+ * float's range, which bfloat16 values above 10^36 over the number of tokens may pass.
+ * A row without a token (seqs[r] < 0, length 0, or every score -inf) has out 0 and lse -inf; seqs[r] >= max_seqs is the
+ * same with TD_ERR_OOB_INDEX.  Otherwise the value of a token with a score of -inf is multiplied by 0, so that one
+ * that is not finite gives NaN in its column; NaN or +inf among a row's scores makes that row's head NaN.  What lies in a
+ * page behind a sequence's last token is never used.
+ * Narrower than the other calls on a cache: dim is a multiple of 8 and 256 at most, and keys, values, q and out, and
+ * every stride of theirs, are multiples of 16 bytes, else TD_EINVAL.  A cache that is to be attended over is made so.  Float
+ * caches: n_rows * cache->n_heads * ceil(n_heads / cache->n_heads / 8) < 2^31.
  * group > 1: rows i * group .. i * group + group - 1 are likely to share leading pages, as the
- * responses of a GRPO group do; full pages that all of a group's rows (with a token) have in common are
- * then read once for all.  Only time depends on it.
+ * responses of a GRPO group do; the full pages that all of a group's rows (with a token) begin with are then read once
+ * for all, in bfloat16 and half, where they hold 64 tokens and spare 2000 reads (tokens times rows less one), no row's
+ * window has left the first token, and for every 512 rows (or a like part) of a larger group.  Only time, and the order
+ * of sums and so the last bits, depend on it.
  * Should the products that a group's common tokens are taken with not come in time, the wait for them ends all the same:
  * TD_ERR_COPY_TIMEOUT is raised, out and lse of the heads that needed them are NaN, everything else is right, and the
  * workspace may be used again as it is. */
@@ -711,16 +718,17 @@ typedef struct {
     float    scale;                        /* finite */
     uint32_t reserved2;
     const int32_t *seqs;                   /* device [n_rows] */
-    const void *q;                         /* device [n_rows][n_heads][dim] of the cache's dtype */
-    int64_t  q_row_stride, q_head_stride;  /* elements, >= 0 */
-    void    *out;                          /* device, the same shape and type; rows and heads must not overlap */
+    const void *q;                         /* device [n_rows][n_heads][dim] of the cache's dtype, 16-byte aligned */
+    int64_t  q_row_stride, q_head_stride;  /* elements, >= 0, multiples of 16 bytes */
+    void    *out;                          /* device, the same shape, type and alignment; rows and heads must not overlap */
     int64_t  out_row_stride, out_head_stride;
     float   *lse;                          /* device [n_rows][n_heads], or NULL */
     void    *workspace;                    /* device, 256-byte aligned, zero-filled once after allocation, private
                                               to this call while it is in flight */
     uint64_t workspace_bytes;              /* >= td_cache_attention_workspace_bytes(n_rows, n_heads, dim) */
 } td_cache_attention_args;
-/* Never falls as an argument grows. 0 where an argument is out of range. */
+/* Never falls as an argument grows. 0 where an argument is out of range.  Room for every form of the call: some 36 MB at
+ * dim 128, and (dim + 2) floats per row and head. */
 size_t td_cache_attention_workspace_bytes(uint32_t n_rows, uint32_t n_heads, uint32_t dim);
 int td_cache_attention(const td_cache_attention_args *args, void *stream);
 

@@ -1068,11 +1068,14 @@ def cache_write(cache: Cache, keys, values, cu, layer: int = 0, stream=None):
 
 
 class AttentionBuffers:
-    """Outputs and workspace of cache_attention for up to n_rows rows of n_heads heads: out [n_rows, n_heads, dim]
-    (a tensor of the caller's, or allocated), lse (lse=True: float32 [n_rows, n_heads])."""
+    """Outputs and workspace of cache_attention for up to n_rows rows of n_heads heads of dim elements, a multiple of 8 and 256 at
+    most: out [n_rows, n_heads, dim] (a tensor of the caller's, with rows and heads on 16-byte boundaries, or allocated), lse
+    (lse=True: float32 [n_rows, n_heads]).  The workspace has room for every form of the call, some 36 MB at 128 elements."""
 
     def __init__(self, n_rows: int, n_heads: int, dim: int, dtype, lse: bool = False, device: int = 0, out=None):
         import torch
+        if dim % 8 or dim > 256:
+            raise ValueError(f"dim: attention takes heads of a multiple of 8 elements, 256 at most, got {dim}")
         dev = torch.device("cuda", device)
         self.n_rows, self.n_heads, self.dim, self.device = n_rows, n_heads, dim, device
         self.out = out if out is not None else torch.zeros(n_rows, n_heads, dim, dtype=dtype, device=dev)
@@ -1090,14 +1093,22 @@ def cache_attention(out: AttentionBuffers, cache: Cache, q, seqs=None, layer: in
                     scale: Optional[float] = None, stream=None) -> AttentionBuffers:
     """Attention of one new token per row over a layer of the cache: q [rows, heads, dim] against the tokens of sequence
     seqs[row] (int32; None: the row's number; negative: none), the last `window` of them if it is not 0.  scale:
-    1 / sqrt(dim) unless given.  group > 1: rows come in groups that share leading pages, which are read once."""
+    1 / sqrt(dim) unless given.  group > 1: rows come in groups that share leading pages, which are read once where that spares
+    enough.  The cache's and q's heads lie on 16-byte boundaries."""
     address, row, head, n, heads = _rows_of_heads(q, "q", cache)
     if n > out.n_rows or heads != out.n_heads or cache.dim != out.dim or out.device != cache.device or out.out.dtype != q.dtype:
         raise ValueError(f"q: {n} rows of {heads} x {cache.dim} {q.dtype}, the buffers hold {out.n_rows} of {out.n_heads} x {out.dim} "
                          f"{out.out.dtype} on cuda:{out.device}")
-    _CACHE_ATTENTION(_op_stream(stream, cache.device), cache.address, layer, n, heads, group, window, 0,
-                     cache.dim ** -0.5 if scale is None else scale, 0, _vector(seqs, n, "seqs", "i32", cache.device), address, row, head,
-                     *out._addresses)
+    try:
+        _CACHE_ATTENTION(_op_stream(stream, cache.device), cache.address, layer, n, heads, group, window, 0,
+                         cache.dim ** -0.5 if scale is None else scale, 0, _vector(seqs, n, "seqs", "i32", cache.device), address, row, head,
+                         *out._addresses)
+    except TdError as error:
+        if error.code == EINVAL and (address | out._addresses[0] | cache.struct.keys | cache.struct.values) % 16 + sum(
+                x * q.element_size() % 16 for x in (row, head, *out._addresses[1:3], cache.struct.layer_stride, cache.struct.page_stride,
+                                                    cache.struct.token_stride, cache.struct.head_stride)):
+            error.args = (f"{error}: keys, values, q and out, and all of their strides, have to be multiples of 16 bytes",)
+        raise
     return out
 
 
