@@ -48,6 +48,12 @@ constexpr float kSlack = 8.0f;                                // how far (log2) 
 // 2^-24: from weights of up to 2^(7 + 8) on, it keeps what lies 2^32 below the largest, so that a long row of small weights behind a large one counts.
 template <typename T> constexpr float kLift = 0.0f;
 template <> constexpr float kLift<__half> = 7.0f;
+// A result lies among the values, but weights are rounded and their sum is not: near half's largest value, which an ordinary value may well be,
+// the quotient can be a half step too large and would round to infinity.
+template <typename T> __device__ __forceinline__ float fitted(float x) { return x; }
+template <> __device__ __forceinline__ float fitted<__half>(float x) {
+    return fabsf(x) < CUDART_INF_F ? fminf(fmaxf(x, -65504.0f), 65504.0f) : x;
+}
 constexpr uint32_t kLeastTiles = 2;                           // of a warp, before another block is used
 
 // Shapes of a kernel for heads of up to 16 * kChunks elements, 8 * kN of them side by side.
@@ -202,7 +208,7 @@ __device__ __forceinline__ void write_result(const AttendArgs &a, uint32_t row, 
 #pragma unroll
     for (uint32_t i = 0; i < (kDim / 2 + 31) / 32; ++i)
         if (2 * (lane + 32 * i) < a.dim)
-            *reinterpret_cast<uint32_t *>(out + 2 * (lane + 32 * i)) = sum == 0.0f ? 0u : pair_of<T>(v[i].x * inv, v[i].y * inv);          // 0, also where the values are not finite
+            *reinterpret_cast<uint32_t *>(out + 2 * (lane + 32 * i)) = sum == 0.0f ? 0u : pair_of<T>(fitted<T>(v[i].x * inv), fitted<T>(v[i].y * inv));          // 0, also where the values are not finite
     if (a.lse && lane == 0) a.lse[(size_t)row * a.n_heads + head] = sum == 0.0f ? -CUDART_INF_F : (top + log2f(sum)) * 0.69314718055994531f;
 }
 
@@ -444,7 +450,7 @@ struct Fold {
         for (int c = 0; c < kChunks; ++c)
 #pragma unroll
             for (int k = 0; k < 2; ++k)
-                if (c * 16 + k * 8 < dim) out[c * 16 + k * 8 + g] = Elem<T>::from(l[n][i] == 0.0f ? 0.0f : o[c][n][i + 2 * k] * inv);
+                if (c * 16 + k * 8 < dim) out[c * 16 + k * 8 + g] = Elem<T>::from(l[n][i] == 0.0f ? 0.0f : fitted<T>(o[c][n][i + 2 * k] * inv));
         if (lse && g == 0) *lse = l[n][i] == 0.0f ? -CUDART_INF_F : (m[n][i] + log2f(l[n][i])) * 0.69314718055994531f;
     }
 };

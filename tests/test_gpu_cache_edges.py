@@ -151,6 +151,33 @@ def test_many_small_weights_behind_a_large_one_count_in_half(heads, kv, group, r
     assert ((out.lse.double() - lse).abs() <= 2.0 ** -20 + (n + 40) * 2.0 ** -24).all()
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("heads,kv,group", [(1, 1, 1), (10, 1, 1), (2, 1, 4), (8, 1, 8)])
+def test_values_of_the_largest_size(dtype, heads, kv, group):
+    """Values that are all half's largest number (bfloat16 and float: 2^100) give that number, whatever the weights' rounding: most of the
+    tokens have a weight that rounds up by nearly half a step."""
+    dim, page, n, scale = 64, 16, 2048, 0.6931471824645996           # scale log2(e) is 1 in float
+    large = 65504.0 if dtype == "f16" else 2.0 ** 100
+    cache, q = attention_case([n] * group, heads, kv, dim, page, dtype, group=group, shared=[n] * group, seed=9, poison=False)
+    cache.keys[0].zero_()
+    # the others' weights lie just above the middle between two numbers of the type
+    step = {"f16": 2.0 ** -10, "bf16": 2.0 ** -7, "f32": 2.0 ** -23}[dtype]
+    exponent = math.log2(1 + 0.55 * step)
+    cache.keys[0][..., 0], cache.keys[0][..., 1], cache.keys[0][..., 2] = -1.0, 1.0, 1.0
+    cache.keys[0][:, 0, :, :3] = 0.0                                  # the first token of each page has score 0, the others -1 + exponent
+    cache.values[0].fill_(large)
+    q.zero_()
+    q[..., 0], q[..., 1] = 1.0, exponent
+    q[..., 2] = exponent - q[..., 1].double()
+    out = td.AttentionBuffers(group, heads, dim, q.dtype, lse=True)
+    td.cache_attention(out, cache, q, group=group, scale=scale)
+    assert ((out.out.double() - large).abs() <= 2 * HALF[dtype] * large).all()
+    cache.values[0][:, :, :, 5] = -large
+    cache.values[0][int(cache.table[0, 3]), 2, :, 9] = math.inf       # an infinite value stays one
+    td.cache_attention(out, cache, q, group=group, scale=scale)
+    assert ((out.out[..., 5].double() + large).abs() <= 2 * HALF[dtype] * large).all() and (out.out[..., 9] == math.inf).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("heads,kv,dim,group", [(4, 2, 64, 1), (24, 2, 128, 1), (4, 2, 64, 4), (32, 2, 64, 4), (6, 2, 192, 4)])
 def test_values_that_are_not_finite_where_the_score_is_minus_infinity(dtype, heads, kv, dim, group):
