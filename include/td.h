@@ -691,7 +691,7 @@ int td_cache_write(const td_cache_write_args *args, void *stream);
 /* Attention of one new token per row over the cache: with kv = h / (n_heads / cache->n_heads),
  *   x_j = scale * q[r][h] . K[j][kv],  lse = ln sum_j e^(x_j),  out[r][h] = sum_j e^(x_j - lse) V[j][kv]
  * over the tokens j of sequence seqs[r] (seqs == NULL: r), with window > 0 its last `window` ones only.
- * Scores, their maximum and both sums are float; the weights e^(x_j - reference) are rounded to the cache's
+ * Scores, in units of ln 2, their maximum and both sums are float; the weights e^(x_j - reference) are rounded to the cache's
  * type for the product with V (bfloat16, half), where the largest weight of the tokens taken together lies in [1, 2^8]
  * (bfloat16) or [2^7, 2^15] (half): half loses weights below 2^-32 of it, and the sums of 2^8 |V| have to stay within
  * float's range, which bfloat16 values above 10^36 over the number of tokens may pass.
@@ -715,7 +715,7 @@ typedef struct {
     uint32_t layer, n_rows, n_heads;       /* n_heads: a multiple of cache->n_heads; n_rows < 2^24 */
     uint32_t group;                        /* >= 1 */
     uint32_t window, reserved;
-    float    scale;                        /* finite */
+    float    scale;                        /* scale * log2(e) is finite */
     uint32_t reserved2;
     const int32_t *seqs;                   /* device [n_rows] */
     const void *q;                         /* device [n_rows][n_heads][dim] of the cache's dtype, 16-byte aligned */

@@ -28,7 +28,7 @@ struct AttendArgs {
     uint32_t n_rows, n_heads, kv_heads, ratio, dim, window;
     uint32_t units, per_kv;                                   // of a row: per_kv for each key head
     FastDiv by_per_kv;
-    float scale, scale2;                                      // scale2 = scale * log2(e)
+    float scale2;                                             // scale * log2(e)
     float *parts;                                             // [2 per warp, then 2 per block][part floats]
     uint32_t *arrived;                                        // [blocks], zero between calls
     // groups of rows with common pages; group == 1: none.  Those of more than kMaxGroup rows are taken as `pieces` groups of like size each.

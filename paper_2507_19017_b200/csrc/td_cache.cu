@@ -353,7 +353,8 @@ int td_cache_attention(const td_cache_attention_args *a, void *stream) {
     const td_cache *c = a->cache;
     const int chk = check_cache(c, true);
     if (chk != TD_OK) return chk;
-    if (a->n_rows >= kMaxRows || a->n_heads >= (1u << 16) || a->group == 0 || !std::isfinite(a->scale)) return TD_EINVAL;
+    const float scale2 = (float)(1.4426950408889634 * (double)a->scale);
+    if (a->n_rows >= kMaxRows || a->n_heads >= (1u << 16) || a->group == 0 || !std::isfinite(scale2)) return TD_EINVAL;
     if (a->q_row_stride < 0 || a->q_head_stride < 0) return TD_EINVAL;
     if (!c->keys || a->layer >= c->n_layers || c->dim > kMaxDim || c->dim % 8 || a->n_heads == 0 || a->n_heads % c->n_heads) return TD_EINVAL;
     if (a->n_rows == 0) return TD_OK;
@@ -387,8 +388,7 @@ int td_cache_attention(const td_cache_attention_args *a, void *stream) {
     k.ratio = a->n_heads / c->n_heads;
     k.dim = c->dim;
     k.window = a->window;
-    k.scale = a->scale;
-    k.scale2 = (float)(1.4426950408889634 * (double)a->scale);
+    k.scale2 = scale2;
     // rows that share, and their heads over one key head in blocks of like size
     k.whole = std::min(a->group, a->n_rows);
     k.pieces = (k.whole + kMaxGroup - 1) / kMaxGroup;

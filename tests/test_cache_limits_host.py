@@ -1,7 +1,7 @@
 """What attention over a cache takes less of than the other calls on it is said where it is refused (no device is touched)."""
 import pytest
 
-from tests.test_cache_host import OnDevice, some_cache, td  # noqa: F401
+from tests.test_cache_host import OnDevice, attend, some_cache, td  # noqa: F401
 
 
 class Sized(OnDevice):
@@ -33,3 +33,11 @@ def test_strides_that_attention_does_not_take(td, monkeypatch, which):
         td.cache_attention(fine, some_cache(td, monkeypatch, keys=Sized(bf16, 2, 20, 16, 4, 64), values=Sized(bf16, 2, 20, 16, 4, 64)),
                            Sized(bf16, 3, 8, 64), layer=2, stream=0)
     assert "16 bytes" not in str(refused.value)
+
+
+def test_scales_that_pass_floats_range_in_units_of_ln_2(td):
+    import torch
+    for scale in (2.4e38, -2.4e38, 3.4e38):
+        assert attend(td, scale=scale) == td.EINVAL
+    if not torch.cuda.is_available():
+        assert attend(td, scale=2.3e38) == attend(td, scale=-2.3e38) == td.ECUDA
