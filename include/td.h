@@ -625,8 +625,8 @@ int td_embed_grad(const td_embed_grad_args *args, void *stream);
  * table may hold anything.  Which sequences a call is about is said by one entry per sequence, so
  * that none is named twice.  A table entry outside [0, n_pages) never causes an access outside the cache: the
  * token or page is passed over and TD_ERR_OOB_INDEX is OR-ed into *status (device, may be NULL,
- * never cleared here).  A sequence whose length lies outside [0, max_pages * page_size] is passed over with
- * TD_ERR_BAD_LENGTH. */
+ * never cleared here).  A sequence whose length lies outside [0, max_pages * page_size] is passed over by a call that
+ * has something to do to it, with TD_ERR_BAD_LENGTH. */
 typedef struct {
     int32_t  dtype;                        /* TD_F32 | TD_BF16 | TD_F16 */
     uint32_t n_pages, page_size;           /* page_size < 2^16; n_pages * page_size < 2^40 */
@@ -653,8 +653,8 @@ size_t td_cache_workspace_bytes(uint32_t n_pages, uint32_t max_seqs);
  * [max_seqs + 1] or NULL: written with the running sum of the tokens given, as td_cache_write takes it.
  * Negative entries and sequences that would pass max_pages get nothing (TD_ERR_BAD_LENGTH).  Where
  * the free pages do not suffice for the whole call nothing is changed, cu is zeros, and
- * TD_ERR_ARENA_FULL is raised; the same with TD_ERR_BAD_LENGTH where cu is given and the call's tokens are 2^31 or more in all.  The last page of a sequence must be its own unless it is full (a fork leaves
- * it so). */
+ * TD_ERR_ARENA_FULL is raised; the same with TD_ERR_BAD_LENGTH where cu is given and the call's tokens are
+ * 2^31 or more in all.  The last page of a sequence must be its own unless it is full (a fork leaves it so). */
 int td_cache_extend(const td_cache *cache, const int32_t *add, int32_t *cu, void *stream);
 
 /* Sequence s becomes a copy of sequence parent[s] (device [max_seqs], negative: none): it holds the parent's
@@ -706,7 +706,8 @@ int td_cache_write(const td_cache_write_args *args, void *stream);
  * responses of a GRPO group do; the full pages that all of a group's rows (with a token) begin with are then read once
  * for all, in bfloat16 and half, where they hold 64 tokens and spare 2000 reads (tokens times rows less one), no row's
  * window has left the first token, and for every 512 rows (or a like part) of a larger group.  Only time, and the order
- * of sums and so the last bits, depend on it.
+ * of sums and so the last bits, depend on it.  Some hundred groups of 8 rows with 600 common tokens, or of 4 with 2000, are
+ * faster with it; groups of two rows, and a few groups of 4, are faster with group = 1.
  * Should the products that a group's common tokens are taken with not come in time, the wait for them ends all the same:
  * TD_ERR_COPY_TIMEOUT is raised, out and lse of the heads that needed them are NaN, everything else is right, and the
  * workspace may be used again as it is. */

@@ -695,7 +695,10 @@ constexpr uint32_t kShareHeads = 128;                         // heads of a bloc
 constexpr uint32_t kShareThreads = 256;
 constexpr uint32_t kLeastShared = 64;                         // common tokens
 // Common tokens times the rows that need not read them: below it two more kernels cost more than they spare.  256 groups of 8, 28 heads over 4
-// of 128, prompts of 150 and 300 tokens on average: 213 us without and 254 with, 288 and 289.
+// of 128, prompts of 150 and 300 tokens on average: 213 us without and 254 with, 288 and 289.  Above it they do not always pay: they win
+// with many rows and tokens (us without and with, prompts of 2000, 32 heads over 4 of 128: 128 groups of 8 603 and 303, 256 of 4
+// 692 and 455, 170 of 3 349 and 319) and lose with few (256 groups of 2 364 and 412, 24 of 4 64 and 95; prompts of 600, 170 of 3 121 and 164).  The
+// caller says whether rows are to share at all.
 constexpr uint32_t kLeastSpared = 2000;
 
 // A block per group.
@@ -1031,7 +1034,7 @@ __global__ void __launch_bounds__(kShareThreads, 1) share_kernel(CacheView c, At
 // never in shared memory.  Two threads have a head's 64 scores each.  While the threads turn a tile's scores into weights, the
 // tensor cores take the last tile's values and the next tile's scores: per tile of 128 tokens there are
 //   scores i + 1 = queries keys   ->   (threads: weights i from scores i)   ->   results += weights i values i.
-// Keys come three tiles and values two tiles ahead through 16-byte copies that put each vector where the products expect it, so any
+// Keys come three tiles and values one tile ahead through 16-byte copies that put each vector where the products expect it, so any
 // pages and strides will do.  The reference is moved as in Fold: the weights are first taken against the one there is, and
 // only where a score passed it is the tile taken again.
 template <int kChunks>
