@@ -1074,7 +1074,7 @@ class AttentionBuffers:
 
     def __init__(self, n_rows: int, n_heads: int, dim: int, dtype, lse: bool = False, device: int = 0, out=None):
         import torch
-        if dim % 8 or dim > 256:
+        if dim % 8 or not 0 < dim <= 256:
             raise ValueError(f"dim: attention takes heads of a multiple of 8 elements, 256 at most, got {dim}")
         dev = torch.device("cuda", device)
         self.n_rows, self.n_heads, self.dim, self.device = n_rows, n_heads, dim, device
@@ -1105,7 +1105,7 @@ def cache_attention(out: AttentionBuffers, cache: Cache, q, seqs=None, layer: in
                          cache.dim ** -0.5 if scale is None else scale, 0, _vector(seqs, n, "seqs", "i32", cache.device), address, row, head,
                          *out._addresses)
     except TdError as error:
-        if error.code == EINVAL and (address | out._addresses[0] | cache.struct.keys | cache.struct.values) % 16 + sum(
+        if error.code == EINVAL and (address | out._addresses[0] | (cache.struct.keys or 0) | (cache.struct.values or 0)) % 16 + sum(
                 x * q.element_size() % 16 for x in (row, head, *out._addresses[1:3], cache.struct.layer_stride, cache.struct.page_stride,
                                                     cache.struct.token_stride, cache.struct.head_stride)):
             error.args = (f"{error}: keys, values, q and out, and all of their strides, have to be multiples of 16 bytes",)

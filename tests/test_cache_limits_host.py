@@ -9,7 +9,7 @@ class Sized(OnDevice):
         return 2
 
 
-@pytest.mark.parametrize("dim", [4, 12, 60, 250, 264, 576])
+@pytest.mark.parametrize("dim", [0, 4, 12, 60, 250, 264, 576])
 def test_buffers_of_a_head_size_that_attention_does_not_take(td, dim):
     import torch
     with pytest.raises(ValueError, match="multiple of 8 elements, 256 at most"):
@@ -41,3 +41,14 @@ def test_scales_that_pass_floats_range_in_units_of_ln_2(td):
         assert attend(td, scale=scale) == td.EINVAL
     if not torch.cuda.is_available():
         assert attend(td, scale=2.3e38) == attend(td, scale=-2.3e38) == td.ECUDA
+
+
+def test_a_cache_without_contents_is_refused_as_such(td, monkeypatch):
+    """Tables only: the refusal is the call's own, and has no word of strides."""
+    import torch
+    tables = some_cache(td, monkeypatch, keys=None, values=None, page_size=16)
+    tables.dim, tables.tag = 64, td.BF16
+    out = td.AttentionBuffers(3, 8, 64, torch.bfloat16, out=Sized(torch.bfloat16, 3, 8, 64))
+    with pytest.raises(td.TdError) as refused:
+        td.cache_attention(out, tables, Sized(torch.bfloat16, 3, 8, 64), stream=0)
+    assert refused.value.code == td.EINVAL and "16 bytes" not in str(refused.value)
